@@ -1,4 +1,4 @@
-"""ctypes binding over the C ABI declared in include/gf.h.
+"""ctypes binding over the C ABI declared in include/gf.h and include/gf_train.h.
 
 Argument marshalling only: every step of the method runs in the CUDA kernels
 of libgf_b200.so.  torch is used for device memory and streams.  There is no
@@ -29,6 +29,7 @@ EXPORTS = (
     "gf_kernel_name", "gf_kernel_id_count", "gf_backward_static_scratch", "gf_set_dense_path",
     "gf_snr_terms", "gf_filter_snr_terms", "gf_dcac_ratio", "gf_act_stash_forward",
     "gf_backward_int8", "gf_backward_int8_workspace_bytes", "gf_selftest_bounded_wait",
+    "gf_layer_norm_forward", "gf_layer_norm_backward_workspace_bytes", "gf_layer_norm_backward",
 )
 
 
@@ -36,6 +37,10 @@ class gf_conv_desc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in
                 ("N", "C_in", "C_out", "H", "W", "KH", "KW", "stride", "pad_h", "pad_w",
                  "groups", "r", "dtype", "layout")]
+
+
+class gf_norm_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("N", "C", "H", "W", "dtype", "param_dtype", "layout")] + [("eps", ctypes.c_float)]
 
 
 class gf_kernel_time(ctypes.Structure):
@@ -104,6 +109,12 @@ def lib() -> ctypes.CDLL:
         L.gf_filter_snr_terms.argtypes = [vp, i64, i32, i32, i32, i32, vp, vp]
         L.gf_dcac_ratio.argtypes = [vp, i32, i32, i32, i32, i32, i32, i32, vp, vp]
         for name in ("gf_snr_terms", "gf_filter_snr_terms", "gf_dcac_ratio"):
+            getattr(L, name).restype = ctypes.c_int
+        nd = ctypes.POINTER(gf_norm_desc)
+        L.gf_layer_norm_forward.argtypes = [nd, vp, vp, vp, vp, vp, vp, vp]
+        L.gf_layer_norm_backward_workspace_bytes.argtypes = [nd, ctypes.POINTER(sz)]
+        L.gf_layer_norm_backward.argtypes = [nd, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        for name in ("gf_layer_norm_forward", "gf_layer_norm_backward_workspace_bytes", "gf_layer_norm_backward"):
             getattr(L, name).restype = ctypes.c_int
         L.gf_selftest_bounded_wait.argtypes = [vp, ctypes.c_int64, vp]
         L.gf_selftest_bounded_wait.restype = ctypes.c_int
@@ -275,6 +286,51 @@ def gf_dcac_ratio(W: torch.Tensor, ratio: torch.Tensor, dft: tuple[int, int] = (
     assert ratio.dtype == torch.float32 and ratio.numel() == C_out * C_ig
     _check(lib().gf_dcac_ratio(_ptr(W), C_out, C_ig, KH, KW, int(dft[0]), int(dft[1]), _gf_dtype(W), _ptr(ratio),
                                _stream(stream)), "gf_dcac_ratio")
+
+
+# ---- operators of a fine-tuning step (gf_train.h) --------------------------------------------
+
+def _dt(dtype) -> int:
+    """gf_dtype of a torch dtype (an int is passed through)."""
+    if isinstance(dtype, torch.dtype):
+        try:
+            return {torch.float32: GF_F32, torch.bfloat16: GF_BF16}[dtype]
+        except KeyError:
+            raise TypeError(f"float32 or bfloat16 expected, got {dtype}") from None
+    return int(dtype)
+
+
+def make_norm_desc(N, C, H=1, W=1, *, dtype=GF_F32, param_dtype=GF_F32, layout=GF_NHWC, eps=1e-5) -> gf_norm_desc:
+    return gf_norm_desc(N, C, H, W, _dt(dtype), _dt(param_dtype), layout, eps)
+
+
+def _size(fn, desc, where: str) -> int:
+    out = ctypes.c_size_t(0)
+    _check(fn(ctypes.byref(desc), ctypes.byref(out)), where)
+    return int(out.value)
+
+
+def _nbytes(workspace) -> int:
+    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def gf_layer_norm_forward(desc: gf_norm_desc, x, gamma, beta, y, mean=None, rstd=None, stream=None) -> None:
+    """y <- (x - mean) rstd gamma + beta over the channels; mean and rstd (fp32, one per pixel) for the backward pass."""
+    _check(lib().gf_layer_norm_forward(ctypes.byref(desc), _ptr(x), _ptr(gamma), _ptr(beta), _ptr(y), _ptr(mean), _ptr(rstd),
+                                       _stream(stream)), "gf_layer_norm_forward")
+
+
+def gf_layer_norm_backward_workspace_bytes(desc: gf_norm_desc) -> int:
+    return _size(lib().gf_layer_norm_backward_workspace_bytes, desc, "gf_layer_norm_backward_workspace_bytes")
+
+
+def gf_layer_norm_backward(desc: gf_norm_desc, g_y, x, gamma, mean, rstd, g_x, g_gamma, g_beta, workspace,
+                           workspace_bytes=None, stream=None) -> None:
+    if workspace_bytes is None:
+        workspace_bytes = _nbytes(workspace)
+    _check(lib().gf_layer_norm_backward(ctypes.byref(desc), _ptr(g_y), _ptr(x), _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(g_x),
+                                        _ptr(g_gamma), _ptr(g_beta), _ptr(workspace), workspace_bytes, _stream(stream)),
+           "gf_layer_norm_backward")
 
 
 def gf_selftest_bounded_wait(workspace, limit_cycles: int, stream=None) -> None:
