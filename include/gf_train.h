@@ -1,6 +1,7 @@
 /*
  * gf_train.h -- operators of a fine-tuning step around the filtered convolution (gf.h): layer
- * normalisation over channels, forward and backward.
+ * normalisation over channels, forward and backward, and the Muon update of the weights with its
+ * Newton-Schulz orthogonalisation.
  *
  * The conventions of gf.h hold: device pointers 16-byte aligned and dense, inputs read-only,
  * outputs overwritten, work enqueued on `stream` without synchronising, errors that the host can
@@ -49,6 +50,73 @@ gf_status gf_layer_norm_backward(const gf_norm_desc* desc, const void* g_y, cons
                                  const void* gamma, const float* mean, const float* rstd, void* g_x,
                                  float* g_gamma, float* g_beta, void* workspace,
                                  size_t workspace_bytes, void* stream);
+
+/* ---- Newton-Schulz orthogonalisation ---------------------------------------------------------
+ * For every matrix G [rows, cols] of a batch: X = G / (||G||_F + eps); then for each step k, with
+ * its coefficients (a, b, c),
+ *     X <- a X + (b A + c A A) X,   A = X X^T
+ * (A = X^T X from the other side when rows > cols: the same result from the smaller products);
+ * O = X.  A step maps every singular value s to a s + b s^3 + c s^5 and keeps the singular
+ * vectors; with the default coefficients five steps bring the singular values near 1.
+ *   precision GF_NS_F16: the products' operands are rounded to fp16 under a fixed scale (11
+ *     significant bits), sums are fp32 -- for updates that are applied in 16 bits or that are
+ *     small beside the weights.
+ *   precision GF_NS_F32: operands are carried as pairs of fp16 (22 significant bits), three
+ *     products each -- results as from fp32 arithmetic.
+ * The coefficients have to keep the entries of X, A and b A + c A A below 32 in magnitude (the
+ * defaults keep the singular values below 1.3); beyond that the fp16 range ends and the result
+ * is not finite.  A matrix of zeros gives zeros; one with a non-finite entry or whose squares
+ * overflow fp32 gives non-finite values or zeros, other matrices of the batch are not affected. */
+typedef enum gf_ns_precision { GF_NS_F16 = 0, GF_NS_F32 = 1 } gf_ns_precision;
+#define GF_NS_MAX_STEPS 16
+
+typedef struct gf_ns_desc {
+    int32_t batch;          /* >= 0; matrices lie one behind the other */
+    int32_t rows, cols;     /* 1 .. 16384 */
+    int32_t in_dtype;       /* gf_dtype of G */
+    int32_t out_dtype;      /* gf_dtype of O */
+    int32_t precision;      /* gf_ns_precision */
+    int32_t steps;          /* 1 .. GF_NS_MAX_STEPS */
+    float eps;              /* >= 0 */
+} gf_ns_desc;
+
+/* h_coeffs: HOST array of 3 * steps floats (a, b, c of each step; read before the call returns),
+ * or NULL for (3.4445, -4.7750, 2.0315) at every step.  O must not be G. */
+gf_status gf_newton_schulz_workspace_bytes(const gf_ns_desc* desc, size_t* bytes);
+gf_status gf_newton_schulz(const gf_ns_desc* desc, const void* G, void* O, void* workspace,
+                           size_t workspace_bytes, const float* h_coeffs, void* stream);
+
+/* ---- Muon step -----------------------------------------------------------------------------------
+ * For `count` layers of one shape, each with a weight W and a gradient g of [rows, cols, taps]
+ * and a momentum M of [rows, cols] (fp32):
+ *     M' = momentum M + (1 - momentum) g,
+ *     u  = nesterov ? (1 - momentum) g + momentum M' : M',
+ *     W' = (1 - lr weight_decay) W - lr scale NS(u)
+ * with NS the Newton-Schulz map above of the flattened [rows, cols taps] matrix.
+ * taps > 1 is for gradients that have ONE value for all taps of a [rows, cols] pair, as g_W of
+ * gf_backward has with r >= 2: g is then read at its first tap, M holds one value per pair, and
+ * since the flattened matrix is u (x) (1 .. 1), NS of it is NS(u) / sqrt(taps) at every tap --
+ * the products are those of [rows, cols] alone.  Any other convolution weight is given with its
+ * taps flattened into cols and taps = 1.
+ * h_grad, h_momentum, ... are HOST arrays of `count` DEVICE pointers (read before the call
+ * returns); these pointers need only the alignment of their elements (parameters and gradients are
+ * often slices of one flat buffer).  The outputs may be the inputs (in place) or other buffers;
+ * buffers of different layers must not overlap. */
+typedef struct gf_muon_desc {
+    int32_t count;          /* >= 0 */
+    int32_t rows, cols;     /* 1 .. 16384 */
+    int32_t taps;           /* 1 .. 4096 */
+    int32_t grad_dtype, weight_dtype;   /* gf_dtype */
+    int32_t precision, steps;           /* as gf_ns_desc */
+    int32_t nesterov;       /* 0 or 1 */
+    float eps, momentum, lr, weight_decay, scale;
+} gf_muon_desc;
+
+gf_status gf_muon_workspace_bytes(const gf_muon_desc* desc, size_t* bytes);
+gf_status gf_muon_step(const gf_muon_desc* desc, const void* const* h_grad,
+                       const float* const* h_momentum, const void* const* h_weight,
+                       float* const* h_momentum_out, void* const* h_weight_out, void* workspace,
+                       size_t workspace_bytes, const float* h_coeffs, void* stream);
 
 #ifdef __cplusplus
 }

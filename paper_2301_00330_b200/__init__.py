@@ -8,4 +8,5 @@ from . import workloads  # noqa: F401
 from .binding import *  # noqa: F401,F403
 from .binding import build_library, lib, library_path  # noqa: F401
 from .norm import LayerNorm, layer_norm  # noqa: F401
+from .muon import Muon, newton_schulz  # noqa: F401
 from .autograd import FilteredConv2d, filtered_conv2d  # noqa: F401

@@ -86,6 +86,7 @@ class FilteredConv2d(torch.nn.Module):
         self.r, self.groups, self.stride = r, groups, stride
         self.weight = torch.nn.Parameter(torch.empty(out_channels, in_channels // groups, kernel_size, kernel_size,
                                                      device=device, dtype=dtype))
+        self.weight.filtered_taps = r >= 2          # gradients have one value for all taps of a kernel
         torch.nn.init.kaiming_normal_(self.weight)
         self.bias = torch.nn.Parameter(torch.zeros(out_channels, device=device, dtype=dtype)) if bias else None
 

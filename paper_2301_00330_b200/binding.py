@@ -21,6 +21,8 @@ GF_F32, GF_BF16 = 0, 1
 GF_NCHW, GF_NHWC = 0, 1
 GF_PATH_AUTO, GF_PATH_FUSED, GF_PATH_SPLIT = 0, 1, 2
 GF_ACT_NONE, GF_ACT_RELU, GF_ACT_RELU6 = 0, 1, 2
+GF_NS_F16, GF_NS_F32 = 0, 1
+GF_NS_MAX_STEPS = 16
 
 EXPORTS = (
     "gf_stash_dims", "gf_stash_bytes", "gf_backward_workspace_bytes", "gf_stash_forward",
@@ -30,6 +32,7 @@ EXPORTS = (
     "gf_snr_terms", "gf_filter_snr_terms", "gf_dcac_ratio", "gf_act_stash_forward",
     "gf_backward_int8", "gf_backward_int8_workspace_bytes", "gf_selftest_bounded_wait",
     "gf_layer_norm_forward", "gf_layer_norm_backward_workspace_bytes", "gf_layer_norm_backward",
+    "gf_newton_schulz_workspace_bytes", "gf_newton_schulz", "gf_muon_workspace_bytes", "gf_muon_step",
 )
 
 
@@ -41,6 +44,17 @@ class gf_conv_desc(ctypes.Structure):
 
 class gf_norm_desc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("N", "C", "H", "W", "dtype", "param_dtype", "layout")] + [("eps", ctypes.c_float)]
+
+
+class gf_ns_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in
+                ("batch", "rows", "cols", "in_dtype", "out_dtype", "precision", "steps")] + [("eps", ctypes.c_float)]
+
+
+class gf_muon_desc(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("count", "rows", "cols", "taps", "grad_dtype", "weight_dtype", "precision",
+                                               "steps", "nesterov")]
+                + [(n, ctypes.c_float) for n in ("eps", "momentum", "lr", "weight_decay", "scale")])
 
 
 class gf_kernel_time(ctypes.Structure):
@@ -110,11 +124,16 @@ def lib() -> ctypes.CDLL:
         L.gf_dcac_ratio.argtypes = [vp, i32, i32, i32, i32, i32, i32, i32, vp, vp]
         for name in ("gf_snr_terms", "gf_filter_snr_terms", "gf_dcac_ratio"):
             getattr(L, name).restype = ctypes.c_int
-        nd = ctypes.POINTER(gf_norm_desc)
+        nd, sd, md = ctypes.POINTER(gf_norm_desc), ctypes.POINTER(gf_ns_desc), ctypes.POINTER(gf_muon_desc)
         L.gf_layer_norm_forward.argtypes = [nd, vp, vp, vp, vp, vp, vp, vp]
         L.gf_layer_norm_backward_workspace_bytes.argtypes = [nd, ctypes.POINTER(sz)]
         L.gf_layer_norm_backward.argtypes = [nd, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
-        for name in ("gf_layer_norm_forward", "gf_layer_norm_backward_workspace_bytes", "gf_layer_norm_backward"):
+        L.gf_newton_schulz_workspace_bytes.argtypes = [sd, ctypes.POINTER(sz)]
+        L.gf_newton_schulz.argtypes = [sd, vp, vp, vp, sz, vp, vp]
+        L.gf_muon_workspace_bytes.argtypes = [md, ctypes.POINTER(sz)]
+        L.gf_muon_step.argtypes = [md, vp, vp, vp, vp, vp, vp, sz, vp, vp]
+        for name in ("gf_layer_norm_forward", "gf_layer_norm_backward_workspace_bytes", "gf_layer_norm_backward",
+                     "gf_newton_schulz_workspace_bytes", "gf_newton_schulz", "gf_muon_workspace_bytes", "gf_muon_step"):
             getattr(L, name).restype = ctypes.c_int
         L.gf_selftest_bounded_wait.argtypes = [vp, ctypes.c_int64, vp]
         L.gf_selftest_bounded_wait.restype = ctypes.c_int
@@ -304,6 +323,16 @@ def make_norm_desc(N, C, H=1, W=1, *, dtype=GF_F32, param_dtype=GF_F32, layout=G
     return gf_norm_desc(N, C, H, W, _dt(dtype), _dt(param_dtype), layout, eps)
 
 
+def make_ns_desc(batch, rows, cols, *, in_dtype=GF_F32, out_dtype=GF_F32, precision=GF_NS_F32, steps=5, eps=1e-7) -> gf_ns_desc:
+    return gf_ns_desc(batch, rows, cols, _dt(in_dtype), _dt(out_dtype), precision, steps, eps)
+
+
+def make_muon_desc(count, rows, cols, taps=1, *, grad_dtype=GF_F32, weight_dtype=GF_F32, precision=GF_NS_F32, steps=5,
+                   nesterov=True, eps=1e-7, momentum=0.95, lr=1e-3, weight_decay=0.0, scale=1.0) -> gf_muon_desc:
+    return gf_muon_desc(count, rows, cols, taps, _dt(grad_dtype), _dt(weight_dtype), precision, steps, int(nesterov), eps,
+                        momentum, lr, weight_decay, scale)
+
+
 def _size(fn, desc, where: str) -> int:
     out = ctypes.c_size_t(0)
     _check(fn(ctypes.byref(desc), ctypes.byref(out)), where)
@@ -331,6 +360,49 @@ def gf_layer_norm_backward(desc: gf_norm_desc, g_y, x, gamma, mean, rstd, g_x, g
     _check(lib().gf_layer_norm_backward(ctypes.byref(desc), _ptr(g_y), _ptr(x), _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(g_x),
                                         _ptr(g_gamma), _ptr(g_beta), _ptr(workspace), workspace_bytes, _stream(stream)),
            "gf_layer_norm_backward")
+
+
+def _coeffs(coeffs, steps: int):
+    """(a, b, c) per step as a host array, or NULL for the default ones."""
+    if coeffs is None:
+        return None
+    flat = [float(v) for abc in coeffs for v in abc]
+    if len(flat) != 3 * steps:
+        raise ValueError(f"{steps} triples of coefficients expected, got {len(flat)} values")
+    return (ctypes.c_float * len(flat))(*flat)
+
+
+def gf_newton_schulz_workspace_bytes(desc: gf_ns_desc) -> int:
+    return _size(lib().gf_newton_schulz_workspace_bytes, desc, "gf_newton_schulz_workspace_bytes")
+
+
+def gf_newton_schulz(desc: gf_ns_desc, G, O, workspace, workspace_bytes=None, coeffs=None, stream=None) -> None:
+    """O <- the Newton-Schulz iterates of the matrices G [batch, rows, cols]; coeffs: (a, b, c) for each step."""
+    if workspace_bytes is None:
+        workspace_bytes = _nbytes(workspace)
+    _check(lib().gf_newton_schulz(ctypes.byref(desc), _ptr(G), _ptr(O), _ptr(workspace), workspace_bytes,
+                                  _coeffs(coeffs, desc.steps), _stream(stream)), "gf_newton_schulz")
+
+
+def gf_muon_workspace_bytes(desc: gf_muon_desc) -> int:
+    return _size(lib().gf_muon_workspace_bytes, desc, "gf_muon_workspace_bytes")
+
+
+def _ptrs(tensors, count: int):
+    if len(tensors) != count:
+        raise ValueError(f"{count} tensors expected, got {len(tensors)}")
+    return (ctypes.c_void_p * count)(*[_ptr(t).value for t in tensors])
+
+
+def gf_muon_step(desc: gf_muon_desc, grads, momenta, weights, momenta_out, weights_out, workspace, workspace_bytes=None,
+                 coeffs=None, stream=None) -> None:
+    """One Muon update of `count` layers of one shape (lists of tensors); the outputs may be the inputs."""
+    if workspace_bytes is None:
+        workspace_bytes = _nbytes(workspace)
+    n = desc.count
+    _check(lib().gf_muon_step(ctypes.byref(desc), _ptrs(grads, n), _ptrs(momenta, n), _ptrs(weights, n), _ptrs(momenta_out, n),
+                              _ptrs(weights_out, n), _ptr(workspace), workspace_bytes, _coeffs(coeffs, desc.steps),
+                              _stream(stream)), "gf_muon_step")
 
 
 def gf_selftest_bounded_wait(workspace, limit_cycles: int, stream=None) -> None:

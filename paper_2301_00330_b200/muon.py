@@ -1,0 +1,113 @@
+"""Orthogonalised updates on the library's kernels (include/gf_train.h): `newton_schulz` for a matrix or a
+batch of them, and `Muon`, the optimiser built on it.
+
+Only marshalling happens here: grouping parameters of one shape into one library call, descriptors
+and workspaces.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+from . import binding as B
+from .norm import _dense
+
+_PRECISION = {"f16": B.GF_NS_F16, "f32": B.GF_NS_F32}
+
+
+def newton_schulz(G: torch.Tensor, steps: int = 5, eps: float = 1e-7, precision: str | None = None, coeffs=None,
+                  out_dtype: torch.dtype | None = None) -> torch.Tensor:
+    """Newton-Schulz iterates of G [..., rows, cols] (float32 or bfloat16), of G's dtype or `out_dtype`.
+
+    precision: "f16" (products of fp16 operands, fp32 sums) or "f32" (operands as pairs); by default
+    "f32" for float32 results and "f16" for bfloat16 ones.  coeffs: (a, b, c) for each step."""
+    if not G.is_cuda:
+        raise RuntimeError("newton_schulz needs a CUDA tensor: there is no CPU path")
+    if G.dim() < 2:
+        raise ValueError("newton_schulz needs a matrix or a batch of matrices")
+    out_dtype = G.dtype if out_dtype is None else out_dtype
+    if precision is None:
+        precision = "f32" if out_dtype == torch.float32 else "f16"
+    rows, cols = G.shape[-2:]
+    G = _dense(G.detach())
+    O = torch.empty(G.shape, dtype=out_dtype, device=G.device)
+    batch = math.prod(G.shape[:-2])
+    desc = B.make_ns_desc(batch, rows, cols, in_dtype=G.dtype, out_dtype=out_dtype, precision=_PRECISION[precision], steps=steps, eps=eps)
+    with torch.cuda.device(G.device):
+        ws = torch.empty(B.gf_newton_schulz_workspace_bytes(desc), dtype=torch.uint8, device=G.device)
+        B.gf_newton_schulz(desc, G, O, ws, None, coeffs, torch.cuda.current_stream(G.device))
+    return O
+
+
+class Muon(torch.optim.Optimizer):
+    """Muon for matrices and convolution kernels [C_out, C_in / groups, KH, KW] (flattened to
+    [C_out, C_in / groups * KH * KW]); vectors belong to another optimiser.
+
+    The momentum is M <- momentum M + (1 - momentum) g, the update NS(u) with u the Nesterov
+    combination or M, times lr * 0.2 * sqrt(max(rows, cols)), so that its entries have the size of
+    an Adam update and learning rates carry over; weight_decay is decoupled.
+
+    A parameter whose attribute `filtered_taps` is true has gradients with one value for all taps of a
+    kernel -- the weights of FilteredConv2d with r >= 2 -- and its update then costs the products of
+    [C_out, C_in / groups] alone; the result is the same.  Parameters of one shape and kind go through
+    one call of the library."""
+
+    def __init__(self, params, lr: float = 1e-3, momentum: float = 0.95, nesterov: bool = True, weight_decay: float = 0.0,
+                 steps: int = 5, eps: float = 1e-7, precision: str | None = None):
+        if lr < 0 or not 0 <= momentum < 1 or weight_decay < 0:
+            raise ValueError("lr >= 0, 0 <= momentum < 1 and weight_decay >= 0 expected")
+        if precision is not None and precision not in _PRECISION:
+            raise ValueError("precision is 'f16', 'f32' or None")
+        super().__init__(params, dict(lr=lr, momentum=momentum, nesterov=nesterov, weight_decay=weight_decay, steps=steps, eps=eps,
+                                      precision=precision))
+        for group in self.param_groups:
+            for p in group["params"]:
+                if p.dim() not in (2, 4):
+                    raise ValueError(f"Muon takes matrices and convolution kernels, got a parameter of shape {tuple(p.shape)}")
+        self._workspaces = {}
+
+    def _workspace(self, device, nbytes: int) -> torch.Tensor:
+        # one per device and stream: calls on one stream follow one another
+        key = device, torch.cuda.current_stream(device).cuda_stream
+        ws = self._workspaces.get(key)
+        if ws is None or ws.numel() < nbytes:
+            ws = self._workspaces[key] = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        return ws
+
+    @torch.no_grad()
+    def step(self, closure=None):
+        loss = None
+        if closure is not None:
+            with torch.enable_grad():
+                loss = closure()
+        for group in self.param_groups:
+            alike = {}
+            for p in group["params"]:
+                if p.grad is None:
+                    continue
+                if not p.is_cuda:
+                    raise RuntimeError("Muon needs CUDA parameters: there is no CPU path")
+                if not p.is_contiguous():
+                    raise ValueError("Muon updates parameters in place: they have to be contiguous")
+                rows, taps = p.shape[0], math.prod(p.shape[2:])
+                uniform = taps if getattr(p, "filtered_taps", False) else 1
+                cols = p.numel() // rows // uniform
+                alike.setdefault((p.device, rows, cols, uniform, p.grad.dtype, p.dtype), []).append(p)
+            for (device, rows, cols, taps, gdt, wdt), ps in alike.items():
+                momenta = []
+                for p in ps:
+                    state = self.state[p]
+                    if "momentum" not in state:
+                        state["momentum"] = torch.zeros((rows, cols), dtype=torch.float32, device=device)
+                    momenta.append(state["momentum"])
+                precision = group["precision"] or ("f32" if wdt == torch.float32 else "f16")
+                desc = B.make_muon_desc(len(ps), rows, cols, taps, grad_dtype=gdt, weight_dtype=wdt, precision=_PRECISION[precision],
+                                        steps=group["steps"], nesterov=group["nesterov"], eps=group["eps"],
+                                        momentum=group["momentum"], lr=group["lr"], weight_decay=group["weight_decay"],
+                                        scale=0.2 * math.sqrt(max(rows, cols * taps)))
+                with torch.cuda.device(device):
+                    grads = [p.grad.contiguous() for p in ps]
+                    B.gf_muon_step(desc, grads, momenta, ps, momenta, ps, self._workspace(device, B.gf_muon_workspace_bytes(desc)),
+                                   None, None, torch.cuda.current_stream(device))
+        return loss
