@@ -6,6 +6,14 @@
 // GF_NS_F32 each operand is a pair hi + lo of fp16 and a product is hi hi + hi lo + lo hi (2^-22
 // relative is dropped).  X is carried as a pair in either case: a X is added to the product in fp32.
 // Accumulators are fp32 in tensor memory.
+//
+// Layout of X, A = X X^T and B = b A + c A A in the workspace: [part][matrix][column / 8][row][column % 8], 16
+// bytes per (row, 8 columns).  A piece of 8 columns is the same thing to the tensor core whether its
+// columns are the contracted index (K-major, X X^T) or the free one (MN-major, B X): core matrices of
+// 8 rows of 16 bytes, unswizzled.  So one layout serves all products, the copy engine moves whole 1 or 2 KB lines of
+// it, and a warp that holds 32 rows of a result (a row per lane) writes 512 consecutive bytes per
+// instruction.  (Row-major operands in 128-byte-swizzled tiles measured 365 us per step of a 4096 x 4096 matrix:
+// boxes of 8 KB fed 44 bytes per clock and SM, and results written row by row took 10 us a tile.)
 #include <cuda_fp16.h>
 
 #include "gf_common.cuh"
@@ -81,12 +89,13 @@ template <bool MUON> __global__ void __launch_bounds__(kNormThreads) ns_norm_ker
     }
 }
 
-// X[b][i][j] = kScale u / (norm + eps) as pairs of fp16, rows of `ld` elements; transposed when the
-// matrix is tall.  A 64 x 64 tile per block, 16 elements per thread.
+// X = kScale u / (norm + eps) as pairs of fp16 in the blocked layout; transposed when the matrix is tall.  A 64 x 64 tile per
+// block through shared memory: read along the given rows, written 16 bytes (8 columns of a row) per thread.
+// Columns past n in the last piece are zeros: they are contracted over.
 constexpr int kCast = 64;
 template <bool MUON>
 __global__ void __launch_bounds__(256) ns_cast_kernel(const __grid_constant__ Source s, const double* part, int parts, float eps, __half* X,
-                                                      int m, int n, int ld, long long lo_off, int transposed) {
+                                                      int m, int n, int pieces, long long lo_off, int transposed) {
     __shared__ float tile[kCast][kCast + 1];
     __shared__ float scale_sh;
     pdl_launch_dependents();
@@ -115,25 +124,103 @@ __global__ void __launch_bounds__(256) ns_cast_kernel(const __grid_constant__ So
         const float scale = kScale / ((float)sqrt(q) + eps);
         if (threadIdx.x == 0) scale_sh = isinf(scale) ? 0.f : scale;
     }
+#pragma unroll
+    for (int k = 0; k < 16; ++k) tile[ty + 4 * k][tx] = u[k];
     __syncthreads();
     const float scale = scale_sh;
-    if (transposed) {
-#pragma unroll
-        for (int k = 0; k < 16; ++k) tile[ty + 4 * k][tx] = u[k];
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < 16; ++k) u[k] = tile[tx][ty + 4 * k];
-    }
     const int x0 = transposed ? i0 : j0, y0 = transposed ? j0 : i0;
 #pragma unroll
-    for (int k = 0; k < 16; ++k) {
-        const int i = y0 + ty + 4 * k, j = x0 + tx;
-        if (i < m && j < n) {
-            const float v = u[k] * scale;
-            const __half hi = __float2half_rn(v);
-            __half* dst = X + ((size_t)b * m + i) * ld + j;
-            dst[0] = hi;
-            dst[lo_off] = __float2half_rn(v - __half2float(hi));
+    for (int k = 0; k < 2; ++k) {
+        const int row = tx, piece = ty + 4 * k;
+        const int i = y0 + row, j = x0 + piece * 8;
+        if (i >= m || j >= n) continue;
+        uint32_t h[4], l[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            float v[2];
+#pragma unroll
+            for (int d = 0; d < 2; ++d) {
+                const int c = piece * 8 + 2 * e + d;
+                v[d] = j + 2 * e + d < n ? (transposed ? tile[c][row] : tile[row][c]) * scale : 0.f;
+            }
+            const __half2 hv = __floats2half2_rn(v[0], v[1]);
+            const float2 back = __half22float2(hv);
+            const __half2 lv = __floats2half2_rn(v[0] - back.x, v[1] - back.y);
+            h[e] = *reinterpret_cast<const uint32_t*>(&hv);
+            l[e] = *reinterpret_cast<const uint32_t*>(&lv);
+        }
+        __half* dst = X + (((long long)b * pieces + (j >> 3)) * m + i) * 8;
+        *reinterpret_cast<uint4*>(dst) = make_uint4(h[0], h[1], h[2], h[3]);
+        *reinterpret_cast<uint4*>(dst + lo_off) = make_uint4(l[0], l[1], l[2], l[3]);
+    }
+}
+
+// The last iterate to where it is wanted: O (row-major, transposed back), or the weights of a Muon step,
+// W' = keep W - f O with one value for all taps.
+struct FinishArgs {
+    const void* w[kMaxLayers];     // Muon: weights before and after
+    void* w_out[kMaxLayers];
+    void* out;                     // O of the whole batch
+    const __half* x;
+    int m, n, pieces, transposed, cols, rows;
+    long long lo;
+    int bf16, taps;
+    float keep, f;
+    FastDiv div_taps;
+};
+template <bool MUON> __global__ void __launch_bounds__(256) ns_finish_kernel(const __grid_constant__ FinishArgs a) {
+    __shared__ float tile[kCast][kCast + 1];       // [row][column] of the result as it is wanted
+    pdl_launch_dependents();
+    pdl_wait();
+    const int b = blockIdx.z, tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
+    const int c0 = blockIdx.x * kCast, r0 = blockIdx.y * kCast;
+    const int x0 = a.transposed ? r0 : c0, y0 = a.transposed ? c0 : r0;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int row = tx, piece = ty + 4 * k;
+        const int i = y0 + row, j = x0 + piece * 8;
+        if (i >= a.m || j >= a.n) continue;
+        const __half* src = a.x + (((long long)b * a.pieces + (j >> 3)) * a.m + i) * 8;
+        const uint4 hv = *reinterpret_cast<const uint4*>(src), lv = *reinterpret_cast<const uint4*>(src + a.lo);
+        const uint32_t h[4] = {hv.x, hv.y, hv.z, hv.w}, l[4] = {lv.x, lv.y, lv.z, lv.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&h[e])), q = __half22float2(*reinterpret_cast<const __half2*>(&l[e]));
+            const float v[2] = {(p.x + q.x) * kInvScale, (p.y + q.y) * kInvScale};
+#pragma unroll
+            for (int d = 0; d < 2; ++d) {
+                const int c = piece * 8 + 2 * e + d;
+                if (a.transposed) tile[c][row] = v[d];
+                else tile[row][c] = v[d];
+            }
+        }
+    }
+    __syncthreads();
+    const int nr = min(kCast, a.rows - r0), nc = min(kCast, a.cols - c0);
+    if constexpr (!MUON) {
+        const long long base = (long long)b * a.rows * a.cols;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            const int r = ty + 4 * k;
+            if (r < nr && tx < nc) {
+                const long long o = base + (long long)(r0 + r) * a.cols + c0 + tx;
+                if (a.bf16) static_cast<__nv_bfloat16*>(a.out)[o] = __float2bfloat16_rn(tile[r][tx]);
+                else static_cast<float*>(a.out)[o] = tile[r][tx];
+            }
+        }
+    } else {
+        // a row of the tile is nc * taps consecutive weights; a warp takes rows in turn
+        const int span = nc * a.taps, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+        for (int r = warp; r < nr; r += 8) {
+            const long long o = ((long long)(r0 + r) * a.cols + c0) * a.taps;
+#pragma unroll 4
+            for (int e = lane; e < span; e += 32) {
+                const float x = tile[r][a.div_taps.div((uint32_t)e)];
+                if (a.bf16)
+                    static_cast<__nv_bfloat16*>(a.w_out[b])[o + e] =
+                        __float2bfloat16_rn(a.keep * __bfloat162float(static_cast<const __nv_bfloat16*>(a.w[b])[o + e]) - a.f * x);
+                else static_cast<float*>(a.w_out[b])[o + e] = a.keep * static_cast<const float*>(a.w[b])[o + e] - a.f * x;
+            }
         }
     }
 }
@@ -141,25 +228,26 @@ __global__ void __launch_bounds__(256) ns_cast_kernel(const __grid_constant__ So
 // ---- products ------------------------------------------------------------------------------------------
 enum Phase { PH_GRAM = 0, PH_POLY, PH_APPLY };
 
+// One CTA works on 128 rows of a tile; a pair of CTAs (two SMs, one product of the tensor cores) on 256, each with half of the
+// tile's columns as its share of the second operand.
 struct PhaseShape {
-    int bn;                        // columns of a tile (128 rows)
-    int stages, stage_bytes;       // operand ring
+    int bn;                        // columns of a tile
+    int stages, stage_bytes;       // operand ring of a CTA
     int tiles, tiles_n;            // tiles per matrix; per row of tiles (not symmetric)
 };
 struct IterateArgs {
-    CUtensorMap tm_x[2], tm_a, tm_b;      // boxes of 64 x 64; third dimension: part * batch + matrix
+    CUtensorMap tm_a[4];           // first operands, 128 rows x 64 k: X[0], X[1], A, B
+    CUtensorMap tm_g[3];           // second operands of the symmetric products, rows x 64 k: X[0], X[1], A
+    CUtensorMap tm_n[2];           // second operand of B X, 64 k x columns: X[0], X[1]
     PhaseShape shape[3];
     float coeff[GF_NS_MAX_STEPS][3];
     int batch, m, n, steps;
     __half *x[2], *a, *b;
-    int ldx, lda;
+    int x_pieces, a_pieces;        // of 8 columns
     long long x_lo, a_lo;          // elements from the high to the low parts
-    void* out;
-    int out_bf16, transposed;
     uint32_t *err_word, *barrier;
 };
 
-constexpr int kBox = 8192;                 // bytes of a 64 x 64 box
 constexpr int kMaxStages = 8;
 constexpr int kRing = 196608;              // bytes of the operand ring
 constexpr int kThreads = 320;              // copies, products, eight warps of results
@@ -168,44 +256,36 @@ constexpr int kThreads = 320;              // copies, products, eight warps of r
 // of the result); 2 chunks are 24 additions, the rest are fp32 additions in registers.
 constexpr int kSegment = 2;
 
-// Row and column of tile t of the lower triangle (128-row tiles that reach the diagonal).
-__device__ __forceinline__ void lower_tile(int t, int bn, int& ti, int& tj) {
-    if (bn == 128) {
+// Tile t of the lower triangle: `rows` x bn tiles that reach the diagonal, rows = bn or 2 bn.
+__device__ __forceinline__ void lower_tile(int t, bool square, int& ti, int& tj) {
+    if (square) {
         int r = (int)((sqrtf(8.f * (float)t + 1.f) - 1.f) * 0.5f);
         while (r * (r + 1) / 2 > t) --r;
         while ((r + 1) * (r + 2) / 2 <= t) ++r;
         ti = r; tj = t - r * (r + 1) / 2;
-    } else {
-        // bn = 256: rows 2g and 2g + 1 have g + 1 tiles; bn = 64: row g has 2 (g + 1) tiles
+    } else {                       // row g has 2 (g + 1) tiles
         int g = (int)((sqrtf(4.f * (float)t + 1.f) - 1.f) * 0.5f);
         while (g * (g + 1) > t) --g;
         while ((g + 1) * (g + 2) <= t) ++g;
-        const int r = t - g * (g + 1);
-        if (bn == 256) { ti = 2 * g + r / (g + 1); tj = r % (g + 1); }
-        else { ti = g; tj = r; }
+        ti = g; tj = t - g * (g + 1);
     }
 }
-int lower_tiles(int M, int bn) {
+int lower_tiles(int M, int rows, int bn) {
     int n = 0;
-    for (int ti = 0; ti * 128 < M; ++ti) {
-        const int reach = ti * 128 + 127 < M - 1 ? ti * 128 + 127 : M - 1;
-        n += reach / bn + 1;
-    }
+    for (int i = 0; i < M; i += rows) n += (i + rows < M ? i + rows - 1 : M - 1) / bn + 1;
     return n;
 }
-__device__ __forceinline__ void tile_at(const PhaseShape& ps, bool symmetric, int tt, int& ti, int& tj) {
-    if (symmetric) lower_tile(tt, ps.bn, ti, tj);
-    else { ti = tt / ps.tiles_n; tj = tt - ti * ps.tiles_n; }
-}
 
-// 32 consecutive fp16 values, high and low parts.
+// 32 consecutive columns (4 pieces) of one row in the blocked layout, high and low parts; `piece` elements lie
+// between pieces.  Pieces from `live` on do not exist.
 struct Pairs { uint4 h[4], l[4]; };
-__device__ __forceinline__ void fetch_pairs(const __half* p, long long lo, bool has_lo, Pairs& r) {
+__device__ __forceinline__ void fetch_pairs(const __half* p, long long piece, long long lo, bool has_lo, int live, Pairs& r) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        r.h[q] = *reinterpret_cast<const uint4*>(p + q * 8);
-        if (has_lo) r.l[q] = *reinterpret_cast<const uint4*>(p + lo + q * 8);
-    }
+    for (int q = 0; q < 4; ++q)
+        if (q < live) {
+            r.h[q] = *reinterpret_cast<const uint4*>(p + q * piece);
+            if (has_lo) r.l[q] = *reinterpret_cast<const uint4*>(p + q * piece + lo);
+        }
 }
 __device__ __forceinline__ void add_pairs(const Pairs& r, bool has_lo, float scale, float v_scale, float (&v)[32]) {
 #pragma unroll
@@ -224,7 +304,7 @@ __device__ __forceinline__ void add_pairs(const Pairs& r, bool has_lo, float sca
         }
     }
 }
-__device__ __forceinline__ void store_pairs(__half* p, long long lo, bool has_lo, const float (&f)[32]) {
+__device__ __forceinline__ void store_pairs(__half* p, long long piece, long long lo, bool has_lo, int live, const float (&f)[32]) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         uint32_t h[4], l[4];
@@ -237,109 +317,121 @@ __device__ __forceinline__ void store_pairs(__half* p, long long lo, bool has_lo
             h[e] = *reinterpret_cast<const uint32_t*>(&hv);
             l[e] = *reinterpret_cast<const uint32_t*>(&lv);
         }
-        *reinterpret_cast<uint4*>(p + q * 8) = make_uint4(h[0], h[1], h[2], h[3]);
-        if (has_lo) *reinterpret_cast<uint4*>(p + lo + q * 8) = make_uint4(l[0], l[1], l[2], l[3]);
+        if (q < live) {
+            *reinterpret_cast<uint4*>(p + q * piece) = make_uint4(h[0], h[1], h[2], h[3]);
+            if (has_lo) *reinterpret_cast<uint4*>(p + q * piece + lo) = make_uint4(l[0], l[1], l[2], l[3]);
+        }
     }
 }
 
 // The values that the results of a block of 32 x 32 need besides the sums: A for the polynomial, X for the
-// last product of a step.  Row i, columns j0 ... (within the padded rows; row i < m).
+// last product of a step.  Row i, columns j0 ...
 template <int SPLIT>
 __device__ __forceinline__ void fetch(const IterateArgs& p, int phase, int step, int b, int i, int j0, Pairs& r) {
     if (i >= p.m) return;
-    if (phase == PH_POLY) fetch_pairs(p.a + ((long long)b * p.m + i) * p.lda + j0, p.a_lo, SPLIT == 2, r);
-    else if (phase == PH_APPLY) fetch_pairs(p.x[step & 1] + ((long long)b * p.m + i) * p.ldx + j0, p.x_lo, true, r);
+    if (phase == PH_POLY)
+        fetch_pairs(p.a + (((long long)b * p.a_pieces + (j0 >> 3)) * p.m + i) * 8, 8LL * p.m, p.a_lo, SPLIT == 2, p.a_pieces - (j0 >> 3), r);
+    else if (phase == PH_APPLY)
+        fetch_pairs(p.x[step & 1] + (((long long)b * p.x_pieces + (j0 >> 3)) * p.m + i) * 8, 8LL * p.m, p.x_lo, true, p.x_pieces - (j0 >> 3), r);
 }
 
-// What becomes of 32 columns of a row of the product: row i (of the warp's 32 from i0), columns j0 ..; `v` are the raw sums.
+// What becomes of 32 columns of a row of the product: row i (of the warp's 32), columns j0 ..; `v` are the raw sums.
 // Symmetric products: blocks of 32 x 32 below the diagonal are written twice (once mirrored), blocks on it once,
-// blocks above it not at all; a block is a warp's, so that nothing here diverges.
+// blocks above it not at all; a block is a warp's, so that nothing here diverges.  Columns past the matrix hold
+// zeros: their sums are of zeros.
 template <int SPLIT>
 __device__ __forceinline__ void emit(const IterateArgs& p, int phase, int step, int b, int i, int j0, const Pairs& r, float (&v)[32]) {
-    if (i >= p.m) return;
-    if (phase != PH_APPLY) {
-        if (phase == PH_POLY) add_pairs(r, SPLIT == 2, p.coeff[step][1], p.coeff[step][2] * kInvScale, v);
-        else {
-#pragma unroll
-            for (int k = 0; k < 32; ++k) v[k] *= kInvScale;
-        }
-        __half* out = phase == PH_GRAM ? p.a : p.b;
-        store_pairs(out + ((long long)b * p.m + i) * p.lda + j0, p.a_lo, SPLIT == 2, v);
-        if (j0 < (i & ~31)) {                              // j0 + 31 < m
-            __half* col = out + ((long long)b * p.m + j0) * p.lda + i;
-#pragma unroll
-            for (int k = 0; k < 32; ++k) {
-                const __half h = __float2half_rn(v[k]);
-                col[(long long)k * p.lda] = h;
-                if constexpr (SPLIT == 2) col[(long long)k * p.lda + p.a_lo] = __float2half_rn(v[k] - __half2float(h));
-            }
-        }
+    if (phase == PH_APPLY) {
+        if (i >= p.m) return;
+        // a X is added in fp32 from the pair, so that only the smaller part of the step sees rounded operands
+        add_pairs(r, true, p.coeff[step][0], kInvScale, v);
+        store_pairs(p.x[(step + 1) & 1] + (((long long)b * p.x_pieces + (j0 >> 3)) * p.m + i) * 8, 8LL * p.m, p.x_lo, true,
+                    p.x_pieces - (j0 >> 3), v);
         return;
     }
-    // a X is added in fp32 from the pair, so that only the smaller part of the step sees rounded operands
-    add_pairs(r, true, p.coeff[step][0], kInvScale, v);
-    if (step + 1 < p.steps) {
-        store_pairs(p.x[(step + 1) & 1] + ((long long)b * p.m + i) * p.ldx + j0, p.x_lo, true, v);
-        return;
+    if (i >= 8 * p.a_pieces) return;
+    if (phase == PH_POLY) add_pairs(r, SPLIT == 2, p.coeff[step][1], p.coeff[step][2] * kInvScale, v);
+    else {
+#pragma unroll
+        for (int k = 0; k < 32; ++k) v[k] *= kInvScale;
     }
-    const int live = min(32, p.n - j0);
-    const long long base = (long long)b * p.m * p.n;
+    __half* out = (phase == PH_GRAM ? p.a : p.b) + (long long)b * p.a_pieces * p.m * 8;
+    if (i < p.m) store_pairs(out + ((long long)(j0 >> 3) * p.m + i) * 8, 8LL * p.m, p.a_lo, SPLIT == 2, p.a_pieces - (j0 >> 3), v);
+    else {
 #pragma unroll
-    for (int k = 0; k < 32; ++k) v[k] *= kInvScale;
-    if (p.transposed) {
-#pragma unroll
-        for (int k = 0; k < 32; ++k)
-            if (k < live) {
-                const long long o = base + (long long)(j0 + k) * p.m + i;
-                if (p.out_bf16) static_cast<__nv_bfloat16*>(p.out)[o] = __float2bfloat16_rn(v[k]);
-                else static_cast<float*>(p.out)[o] = v[k];
-            }
-        return;
+        for (int k = 0; k < 32; ++k) v[k] = 0.f;       // the columns that fill up the last piece
     }
-    const long long o = base + (long long)i * p.n + j0;
-    if (p.out_bf16) {
-        __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(p.out) + o;
-        if (live == 32 && (p.n & 7) == 0) {
+    if (j0 < (i & ~31)) {                              // j0 + 31 < m
+        __half* col = out + ((long long)(i >> 3) * p.m + j0) * 8 + (i & 7);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                uint32_t w[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const __nv_bfloat162 h = __floats2bfloat162_rn(v[q * 8 + 2 * e], v[q * 8 + 2 * e + 1]);
-                    w[e] = *reinterpret_cast<const uint32_t*>(&h);
-                }
-                *reinterpret_cast<uint4*>(dst + q * 8) = make_uint4(w[0], w[1], w[2], w[3]);
-            }
-        } else {
-#pragma unroll
-            for (int k = 0; k < 32; ++k) if (k < live) dst[k] = __float2bfloat16_rn(v[k]);
-        }
-    } else {
-        float* dst = static_cast<float*>(p.out) + o;
-        if (live == 32 && (p.n & 3) == 0) {
-#pragma unroll
-            for (int q = 0; q < 8; ++q)
-                *reinterpret_cast<float4*>(dst + q * 4) = make_float4(v[q * 4], v[q * 4 + 1], v[q * 4 + 2], v[q * 4 + 3]);
-        } else {
-#pragma unroll
-            for (int k = 0; k < 32; ++k) if (k < live) dst[k] = v[k];
+        for (int k = 0; k < 32; ++k) {
+            const __half h = __float2half_rn(v[k]);
+            col[k * 8] = h;
+            if constexpr (SPLIT == 2) col[k * 8 + p.a_lo] = __float2half_rn(v[k] - __half2float(h));
         }
     }
 }
 
-// Orders generic-proxy accesses to global memory with the copy engine's.
-__device__ __forceinline__ void fence_proxy_async_all() { asm volatile("fence.proxy.async;" ::: "memory"); }
+// Unswizzled operand tile: core matrices of 8 rows x 16 bytes.  lbo / sbo: bytes between core matrices along k / along the free
+// index for a K-major tile, the other way round for an MN-major one.
+__device__ __forceinline__ uint64_t plain_smem_desc(uint32_t saddr, uint32_t lbo_bytes, uint32_t sbo_bytes) {
+    return (uint64_t)((saddr >> 4) & 0x3FFFu) | ((uint64_t)((lbo_bytes >> 4) & 0x3FFFu) << 16) |
+           ((uint64_t)((sbo_bytes >> 4) & 0x3FFFu) << 32) | ((uint64_t)1 << 46);
+}
 
-// All blocks of a cooperative launch meet.  `ok` false in any thread ends the kernel of every block: the error
-// word tells the others.  The wait is bounded like every other.
+// ---- pairs of CTAs ------------------------------------------------------------------------------------------
+constexpr uint32_t kLeaderMask = 0xFEFFFFFFu;      // a shared address of either CTA -> the same place in the first one
+template <bool PAIR> __device__ __forceinline__ void load_box(void* dst, const CUtensorMap* m, int x, int y, int z, uint64_t* bar) {
+    if constexpr (!PAIR) tma_load_3d(dst, m, x, y, z, bar);
+    else        // the bytes land here, their arrival is counted on the first CTA's barrier
+        asm volatile(
+            "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+                smem_u32(dst)),
+            "l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar) & kLeaderMask)
+            : "memory");
+}
+template <bool PAIR> __device__ __forceinline__ void mma_f16(uint32_t d, uint64_t ad, uint64_t bd, uint32_t idesc, uint32_t accumulate) {
+    if constexpr (!PAIR) umma_bf16(d, ad, bd, idesc, accumulate);      // kind::f16: the descriptor says fp16
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "setp.ne.b32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+            "l"(ad), "l"(bd), "r"(idesc), "r"(accumulate)
+            : "memory");
+}
+template <bool PAIR> __device__ __forceinline__ void commit(uint64_t* bar) {
+    if constexpr (!PAIR) umma_commit(bar);
+    else asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+                          smem_u32(bar)),
+                      "h"((uint16_t)3)
+                      : "memory");
+}
+__device__ __forceinline__ void arrive_leader(uint64_t* bar) {
+    asm volatile(
+        "{\n\t.reg .b32 a;\n\t"
+        "mapa.shared::cluster.u32 a, %0, 0;\n\t"
+        "mbarrier.arrive.release.cluster.shared::cluster.b64 _, [a];\n\t}" ::"r"(smem_u32(bar))
+        : "memory");
+}
+__device__ __forceinline__ void cluster_meet() {
+    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+
+// All blocks of a cooperative launch meet: the writes before it are visible to all after it.  `ok` false in any thread ends the
+// kernel of every block: the error word tells the others.  The wait is bounded like every other.
 __device__ __forceinline__ bool grid_meet(const IterateArgs& p, uint32_t target, bool ok, int* flag) {
-    __threadfence();
-    fence_proxy_async_all();
     const int bad = __syncthreads_or(!ok);
     if (threadIdx.x == 0) {
         int go = !bad;
         if (bad) atomicOr(p.err_word, 4096u);
         else {
+            __threadfence();
             atomicAdd(p.barrier, 1u);
             const long long t0 = clock64();
             for (int spins = 0;; ++spins) {
@@ -355,33 +447,42 @@ __device__ __forceinline__ bool grid_meet(const IterateArgs& p, uint32_t target,
             }
         }
         *flag = go;
-        __threadfence();
+        // what the other blocks wrote through the generic proxy is read by this thread's copies through the asynchronous one
+        asm volatile("fence.proxy.async;" ::: "memory");
     }
     __syncthreads();
-    fence_proxy_async_all();
     return *flag != 0;
 }
 
-// The whole iteration in one launch: every phase deals its tiles (128 x bn, of all matrices) to the blocks in turn, and
-// the blocks meet between phases.
-template <int SPLIT> __global__ void __launch_bounds__(kThreads, 1) ns_iterate_kernel(const __grid_constant__ IterateArgs p) {
+// The whole iteration in one launch: every phase deals its tiles (of all matrices) to the CTAs or pairs in turn, and
+// all meet between phases.
+template <int SPLIT, bool PAIR> __global__ void __launch_bounds__(kThreads, 1) ns_iterate_kernel(const __grid_constant__ IterateArgs p) {
     extern __shared__ unsigned char dyn_raw[];
     unsigned char* dyn = align1024(dyn_raw);
     __shared__ uint64_t full[kMaxStages], empty[kMaxStages], done[2], drained[2];
     __shared__ uint32_t tmem_base;
     __shared__ int flag;
+    constexpr int kRows = PAIR ? 256 : 128;                 // of a tile
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = PAIR ? cluster_rank() : 0u;
+    const int unit = PAIR ? blockIdx.x >> 1 : blockIdx.x, units = PAIR ? gridDim.x >> 1 : gridDim.x;
     if (threadIdx.x == 0) {
         for (int s = 0; s < kMaxStages; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
-        for (int s = 0; s < 2; ++s) { mbar_init(&done[s], 1); mbar_init(&drained[s], 8); }
+        for (int s = 0; s < 2; ++s) { mbar_init(&done[s], 1); mbar_init(&drained[s], PAIR ? 16 : 8); }
         mbar_fence_init();
     }
-    if (warp == 1) { tmem_alloc(&tmem_base, 512); tmem_relinquish(); }
+    if (warp == 1) {
+        if constexpr (PAIR) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base)), "r"(512) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else { tmem_alloc(&tmem_base, 512); tmem_relinquish(); }
+    }
     tc_fence_before_sync();
     __syncthreads();
+    if constexpr (PAIR) cluster_meet();                     // the other CTA's barriers are ready
     tc_fence_after_sync();
     const uint32_t tmem = tmem_base;
-    fence_proxy_async_all();
+    asm volatile("fence.proxy.async;" ::: "memory");
     bool ok = true;
     uint32_t ring = 0;                 // one bit per stage: the parity of its next use
     uint32_t use = 0;                  // accumulators taken so far (products), emptied so far (results)
@@ -394,32 +495,35 @@ template <int SPLIT> __global__ void __launch_bounds__(kThreads, 1) ns_iterate_k
         const int chunks = (K + 63) / 64;
         const int segment = SPLIT == 2 ? kSegment : chunks;
         const int total = ps.tiles * p.batch;
+        const int share = PAIR ? ps.bn / 2 : ps.bn;         // columns of the second operand held here
+        const uint32_t a_bytes = 128 * 128, b_bytes = (uint32_t)share * 128;
+        auto tile_at = [&](int t, int& b, int& ti, int& tj) {
+            b = t / ps.tiles;
+            const int tt = t - b * ps.tiles;
+            if (symmetric) lower_tile(tt, ps.bn == kRows, ti, tj);
+            else { ti = tt / ps.tiles_n; tj = tt - ti * ps.tiles_n; }
+        };
         if (warp == 0) {
             if (lane == 0) {
-                const CUtensorMap* ta = phase == PH_GRAM ? &p.tm_x[step & 1] : phase == PH_POLY ? &p.tm_a : &p.tm_b;
-                const CUtensorMap* tb = phase == PH_POLY ? &p.tm_a : &p.tm_x[step & 1];
-                const int a_bytes = 2 * kBox, b_bytes = ps.bn / 64 * kBox;
+                const CUtensorMap* ta = phase == PH_GRAM ? &p.tm_a[step & 1] : phase == PH_POLY ? &p.tm_a[2] : &p.tm_a[3];
+                const CUtensorMap* tb = phase == PH_GRAM ? &p.tm_g[step & 1] : phase == PH_POLY ? &p.tm_g[2] : &p.tm_n[step & 1];
                 int s = 0;
-                for (int t = blockIdx.x; t < total && ok; t += gridDim.x) {
-                    const int b = t / ps.tiles;
-                    int ti, tj;
-                    tile_at(ps, symmetric, t - b * ps.tiles, ti, tj);
+                for (int t = unit; t < total && ok; t += units) {
+                    int b, ti, tj;
+                    tile_at(t, b, ti, tj);
+                    const int row = ti * kRows + (int)rank * 128, col = tj * ps.bn + (int)rank * share;
                     for (int q = 0; q < chunks; ++q) {
                         ok = mbar_wait_bounded(&empty[s], ((ring >> s) & 1u) ^ 1u);
                         if (!ok) break;
                         unsigned char* st = dyn + (size_t)s * ps.stage_bytes;
-                        mbar_expect_tx(&full[s], (uint32_t)ps.stage_bytes);
+                        if (rank == 0) mbar_expect_tx(&full[s], (uint32_t)ps.stage_bytes * (PAIR ? 2u : 1u));
 #pragma unroll
                         for (int h = 0; h < SPLIT; ++h) {
                             const int z = h * p.batch + b;
-                            unsigned char* sa = st + h * a_bytes;
                             unsigned char* sb = st + SPLIT * a_bytes + h * b_bytes;
-                            tma_load_3d(sa, ta, q * 64, ti * 128, z, &full[s]);
-                            tma_load_3d(sa + kBox, ta, q * 64, ti * 128 + 64, z, &full[s]);
-                            for (int c = 0; c * 64 < ps.bn; ++c) {
-                                if (symmetric) tma_load_3d(sb + c * kBox, tb, q * 64, tj * ps.bn + c * 64, z, &full[s]);
-                                else tma_load_3d(sb + c * kBox, tb, tj * ps.bn + c * 64, q * 64, z, &full[s]);
-                            }
+                            load_box<PAIR>(st + h * a_bytes, ta, row * 2, q * 8, z, &full[s]);
+                            if (symmetric) load_box<PAIR>(sb, tb, col * 2, q * 8, z, &full[s]);
+                            else load_box<PAIR>(sb, tb, q * 128, col / 8, z, &full[s]);
                         }
                         ring ^= 1u << s;
                         if (++s == ps.stages) s = 0;
@@ -427,13 +531,13 @@ template <int SPLIT> __global__ void __launch_bounds__(kThreads, 1) ns_iterate_k
                 }
             }
         } else if (warp == 1) {
-            if (lane == 0) {
+            if (lane == 0 && rank == 0) {
                 // fp16 x fp16 -> fp32; B is K-major in the symmetric products, MN-major otherwise
-                const uint32_t idesc = (1u << 4) | ((symmetric ? 0u : 1u) << 16) | ((uint32_t)(ps.bn >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
-                const uint32_t b_step = symmetric ? 32u : 2048u, b_lbo = symmetric ? 16u : 8192u;
-                const uint32_t a_bytes = 2 * kBox, b_bytes = (uint32_t)(ps.bn / 64 * kBox);
+                const uint32_t idesc = (1u << 4) | ((symmetric ? 0u : 1u) << 16) | ((uint32_t)(ps.bn >> 3) << 17) | ((uint32_t)(kRows >> 4) << 24);
+                const uint32_t b_step = symmetric ? (uint32_t)share * 32u : 256u;      // 16 k further
+                const uint32_t b_lbo = symmetric ? (uint32_t)share * 16u : 128u, b_sbo = symmetric ? 128u : 1024u;
                 int s = 0;
-                for (int t = blockIdx.x; t < total && ok; t += gridDim.x) {
+                for (int t = unit; t < total && ok; t += units) {
                     for (int q = 0; q < chunks; ++q) {
                         const int buf = (int)(use & 1u);
                         const bool first = q % segment == 0, last = q % segment == segment - 1 || q == chunks - 1;
@@ -446,83 +550,79 @@ template <int SPLIT> __global__ void __launch_bounds__(kThreads, 1) ns_iterate_k
                         const uint32_t b_hi = a_hi + SPLIT * a_bytes, b_lo = b_hi + b_bytes;
 #pragma unroll
                         for (int ks = 0; ks < 4; ++ks) {
-                            const uint64_t ad = umma_smem_desc(a_hi + ks * 32, 16, 1024), bd = umma_smem_desc(b_hi + ks * b_step, b_lbo, 1024);
-                            umma_bf16(d, ad, bd, idesc, !(first && ks == 0));
+                            const uint64_t ad = plain_smem_desc(a_hi + ks * 4096, 2048, 128), bd = plain_smem_desc(b_hi + ks * b_step, b_lbo, b_sbo);
+                            mma_f16<PAIR>(d, ad, bd, idesc, !(first && ks == 0));
                             if constexpr (SPLIT == 2) {
-                                umma_bf16(d, ad, umma_smem_desc(b_lo + ks * b_step, b_lbo, 1024), idesc, 1u);
-                                umma_bf16(d, umma_smem_desc(a_lo + ks * 32, 16, 1024), bd, idesc, 1u);
+                                mma_f16<PAIR>(d, ad, plain_smem_desc(b_lo + ks * b_step, b_lbo, b_sbo), idesc, 1u);
+                                mma_f16<PAIR>(d, plain_smem_desc(a_lo + ks * 4096, 2048, 128), bd, idesc, 1u);
                             }
                         }
-                        umma_commit(&empty[s]);
+                        commit<PAIR>(&empty[s]);
                         ring ^= 1u << s;
                         if (++s == ps.stages) s = 0;
-                        if (last) { umma_commit(&done[buf]); ++use; }
+                        if (last) { commit<PAIR>(&done[buf]); ++use; }
                     }
                 }
             }
         } else {
             const int quarter = warp & 3, half = (warp - 2) >> 2;
             const int cols = ps.bn / 2;                       // of this warp
-            for (int t = blockIdx.x; t < total && ok; t += gridDim.x) {
-                const int b = t / ps.tiles;
-                int ti, tj;
-                tile_at(ps, symmetric, t - b * ps.tiles, ti, tj);
-                const int i = ti * 128 + quarter * 32 + lane;
+            constexpr int kChunks = PAIR ? 4 : 2;             // of 32 columns, at most
+            const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * cols);
+            for (int t = unit; t < total && ok; t += units) {
+                int b, ti, tj;
+                tile_at(t, b, ti, tj);
+                const int i0 = ti * kRows + (int)rank * 128 + quarter * 32, i = i0 + lane;
                 const int j0 = tj * ps.bn + half * cols;
                 // columns past the matrix, or past the diagonal of the warp's rows, are not read (the same for the whole warp)
-                const int reach = symmetric ? min(p.m, ti * 128 + quarter * 32 + 32) : p.n;
+                const int reach = i0 >= p.m ? 0 : symmetric ? min(p.m, i0 + 32) : p.n;
                 Pairs pr;
                 if (j0 < reach) fetch<SPLIT>(p, phase, step, b, i, j0, pr);        // on its way while the product runs
-                if constexpr (SPLIT == 1) {
+                float acc[SPLIT == 2 ? kChunks : 1][32];
+                if constexpr (SPLIT == 2) {
+#pragma unroll
+                    for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) acc[c][k] = 0.f;
+                }
+                for (int q = 0; q < chunks; q += segment) {
                     const int buf = (int)(use & 1u);
                     ok = mbar_wait_bounded(&done[buf], (use >> 1) & 1u);
                     ++use;
                     if (!ok) break;
                     tc_fence_after_sync();
-                    for (int c = 0; c < cols && j0 + c < reach; c += 32) {
-                        uint32_t raw[32];
-                        tmem_ld32(tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * 256 + half * cols + c), raw);
-                        const Pairs now = pr;
-                        if (c + 32 < cols && j0 + c + 32 < reach) fetch<SPLIT>(p, phase, step, b, i, j0 + c + 32, pr);
-                        tmem_ld_wait();
-                        float v[32];
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) v[k] = __uint_as_float(raw[k]);
-                        emit<SPLIT>(p, phase, step, b, i, j0 + c, now, v);
-                        __syncwarp();                         // the next read of tensor memory is the whole warp's
-                    }
-                    tc_fence_before_sync();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&drained[buf]);
-                } else {
-                    float acc[4][32];
+                    for (int c = 0; c < kChunks; ++c) {
+                        const int j = j0 + c * 32;
+                        if (c * 32 < cols && j < reach) {
+                            uint32_t raw[32];
+                            tmem_ld32(lanes + (uint32_t)(buf * 256 + c * 32), raw);
+                            if constexpr (SPLIT == 1) {
+                                const Pairs now = pr;
+                                if (c + 1 < kChunks && (c + 1) * 32 < cols && j + 32 < reach) fetch<SPLIT>(p, phase, step, b, i, j + 32, pr);
+                                tmem_ld_wait();
 #pragma unroll
-                    for (int c = 0; c < 4; ++c)
-#pragma unroll
-                        for (int k = 0; k < 32; ++k) acc[c][k] = 0.f;
-                    for (int q = 0; q < chunks; q += kSegment) {
-                        const int buf = (int)(use & 1u);
-                        ok = mbar_wait_bounded(&done[buf], (use >> 1) & 1u);
-                        ++use;
-                        if (!ok) break;
-                        tc_fence_after_sync();
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            if (c * 32 < cols && j0 + c * 32 < reach) {
-                                uint32_t raw[32];
-                                tmem_ld32(tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * 256 + half * cols + c * 32), raw);
+                                for (int k = 0; k < 32; ++k) acc[0][k] = __uint_as_float(raw[k]);
+                                emit<SPLIT>(p, phase, step, b, i, j, now, acc[0]);
+                                __syncwarp();                 // the next read of tensor memory is the whole warp's
+                            } else {
                                 tmem_ld_wait();
 #pragma unroll
                                 for (int k = 0; k < 32; ++k) acc[c][k] += __uint_as_float(raw[k]);
                             }
                         }
-                        tc_fence_before_sync();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(&drained[buf]);
                     }
-                    if (!ok) break;
+                    tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) {
+                        if constexpr (PAIR) arrive_leader(&drained[buf]);
+                        else mbar_arrive(&drained[buf]);
+                    }
+                }
+                if (!ok) break;
+                if constexpr (SPLIT == 2) {
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
+                    for (int c = 0; c < kChunks; ++c) {
                         if (c * 32 < cols && j0 + c * 32 < reach) {
                             if (c > 0) fetch<SPLIT>(p, phase, step, b, i, j0 + c * 32, pr);
                             emit<SPLIT>(p, phase, step, b, i, j0 + c * 32, pr, acc[c]);
@@ -544,109 +644,116 @@ template <int SPLIT> __global__ void __launch_bounds__(kThreads, 1) ns_iterate_k
     }
     tc_fence_before_sync();
     __syncthreads();
+    if constexpr (PAIR) cluster_meet();           // nothing of the other CTA refers to this one any more
     tc_fence_after_sync();
-    if (warp == 1) tmem_dealloc(tmem, 512);
-}
-
-// W' = (1 - lr wd) W - f O for the layers of a launch; O [rows, cols] fp32, one value for all taps.
-struct UpdateArgs {
-    const void* w[kMaxLayers];
-    void* w_out[kMaxLayers];
-    const float* O;
-    long long n;                   // rows * cols
-    int taps, bf16;
-    float keep, f;
-    FastDiv div_taps;
-};
-__global__ void __launch_bounds__(256) muon_update_kernel(const __grid_constant__ UpdateArgs a) {
-    pdl_launch_dependents();
-    pdl_wait();
-    const int b = blockIdx.y;
-    const float* O = a.O + (size_t)b * a.n;
-    const long long total = a.n * a.taps;
-    for (long long e = (long long)blockIdx.x * blockDim.x + threadIdx.x; e < total; e += (long long)gridDim.x * blockDim.x) {
-        const float o = O[a.taps == 1 ? e : e / a.taps];
-        if (a.bf16)
-            static_cast<__nv_bfloat16*>(a.w_out[b])[e] =
-                __float2bfloat16_rn(a.keep * __bfloat162float(static_cast<const __nv_bfloat16*>(a.w[b])[e]) - a.f * o);
-        else
-            static_cast<float*>(a.w_out[b])[e] = a.keep * static_cast<const float*>(a.w[b])[e] - a.f * o;
+    if (warp == 1) {
+        if constexpr (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+        else tmem_dealloc(tmem, 512);
     }
 }
 
 // ---- host side --------------------------------------------------------------------------------------------
 struct NsPlan {
-    int batch, rows, cols, m, n, ldx, lda, split, transposed;
+    int batch, rows, cols, m, n, x_pieces, a_pieces, split, transposed;
     int norm_blocks;
-    size_t off_part, off_x[2], off_a, off_b, off_o, total;
+    size_t off_part, off_x[2], off_a, off_b, total;
     long long x_lo, a_lo;          // elements from the high to the low parts
 };
 
-NsPlan ns_plan(int batch, int rows, int cols, int precision, bool muon) {
+NsPlan ns_plan(int batch, int rows, int cols, int precision) {
     NsPlan p = {};
     p.batch = batch; p.rows = rows; p.cols = cols;
     p.transposed = rows > cols;
     p.m = rows < cols ? rows : cols;
     p.n = rows < cols ? cols : rows;
     p.split = precision == GF_NS_F32 ? 2 : 1;
-    p.ldx = (p.n + 31) / 32 * 32;            // results are written 32 columns at a time
-    p.lda = (p.m + 31) / 32 * 32;
+    p.x_pieces = (p.n + 7) / 8;
+    p.a_pieces = (p.m + 7) / 8;
     const long long per = ((long long)rows * cols + 8 * kNormThreads - 1) / (8 * kNormThreads);
     p.norm_blocks = (int)(per < kNormBlocks ? per : kNormBlocks);
-    p.x_lo = (long long)batch * p.m * p.ldx;
-    p.a_lo = (long long)batch * p.m * p.lda;
+    p.x_lo = 8LL * batch * p.m * p.x_pieces;
+    p.a_lo = 8LL * batch * p.m * p.a_pieces;
     size_t off = 256;
     p.off_part = off; off += up((size_t)batch * p.norm_blocks * 8, 256);
     for (int k = 0; k < 2; ++k) { p.off_x[k] = off; off += up((size_t)p.x_lo * 4, 256); }
     p.off_a = off; off += up((size_t)p.a_lo * 2 * p.split, 256);
     p.off_b = off; off += up((size_t)p.a_lo * 2 * p.split, 256);
-    p.off_o = off;
-    if (muon) off += up((size_t)batch * rows * cols * 4, 256);
     p.total = off;
     return p;
 }
 
 const float kDefaultCoeffs[3] = {3.4445f, -4.7750f, 2.0315f};
 
-// The tile width with the least estimated time: rounds of tiles over the SMs, times the width plus what a tile
-// costs whatever its width (its 128 rows of A).
-PhaseShape phase_shape(const NsPlan& p, bool symmetric) {
+// Pairs of CTAs where every pair gets a tile of the largest product.
+bool use_pairs(const NsPlan& p, int pairs) {
+    return (long long)((p.m + 255) / 256) * ((p.n + 127) / 128) * p.batch >= pairs;
+}
+
+// The tile width with the least estimated time: rounds of tiles over the CTAs (pairs), times the width plus what a tile
+// costs whatever its width (its rows of the first operand).
+PhaseShape phase_shape(const NsPlan& p, bool symmetric, bool pair, int units) {
     PhaseShape best = {};
     double least = 0;
-    for (int bn = 256; bn >= 64; bn >>= 1) {
+    const int rows = pair ? 256 : 128;
+    for (int bn = rows; bn >= rows / 2; bn >>= 1) {
         PhaseShape s;
         s.bn = bn;
-        s.stage_bytes = p.split * (2 + bn / 64) * kBox;
+        s.stage_bytes = p.split * (128 + (pair ? bn / 2 : bn)) * 128;
         s.stages = kRing / s.stage_bytes < kMaxStages ? kRing / s.stage_bytes : kMaxStages;
         s.tiles_n = ((symmetric ? p.m : p.n) + bn - 1) / bn;
-        s.tiles = symmetric ? lower_tiles(p.m, bn) : (p.m + 127) / 128 * s.tiles_n;
-        const double cost = (double)cdiv64((long long)s.tiles * p.batch, sm_count()) * (bn + 64);
+        s.tiles = symmetric ? lower_tiles(p.m, rows, bn) : (p.m + rows - 1) / rows * s.tiles_n;
+        const double cost = (double)cdiv64((long long)s.tiles * p.batch, units) * (bn + 64);
         if (least == 0 || cost < least) { least = cost; best = s; }
     }
     return best;
 }
 
-template <int SPLIT> gf_status launch_iterate(const IterateArgs& a, cudaStream_t s) {
+template <int SPLIT, bool PAIR> gf_status launch_iterate(const IterateArgs& a, int units, cudaStream_t s) {
     constexpr size_t smem = (size_t)kRing + 1024;
     static size_t configured[kMaxDevices] = {};
-    if (gf_status st = ensure_dyn_smem(ns_iterate_kernel<SPLIT>, smem, configured); st != GF_OK) return st;
+    if (gf_status st = ensure_dyn_smem(ns_iterate_kernel<SPLIT, PAIR>, smem, configured); st != GF_OK) return st;
     long long most = 1;
     for (const PhaseShape& ps : a.shape) most = (long long)ps.tiles * a.batch > most ? (long long)ps.tiles * a.batch : most;
-    const int grid = most < sm_count() ? (int)most : sm_count();
+    const int used = most < units ? (int)most : units;
     ProfScope prof(K_NS_PRODUCT, s);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = smem; cfg.stream = s;
-    cudaLaunchAttribute attr[1];
+    cfg.gridDim = dim3(PAIR ? 2 * used : used); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = smem; cfg.stream = s;
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeCooperative;          // the blocks wait for one another between phases
     attr[0].val.cooperative = 1;
-    cfg.attrs = attr; cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, ns_iterate_kernel<SPLIT>, a);
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = PAIR ? 2 : 1; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = PAIR ? 2 : 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, ns_iterate_kernel<SPLIT, PAIR>, a);
     count_launch();
     return e == cudaSuccess ? GF_OK : GF_ERR_CUDA;
 }
 
-// The iteration from X in the workspace (written by ns_cast_kernel) to O.
-gf_status ns_iterate(const NsPlan& p, char* base, int steps, const float* coeffs, void* O, int out_bf16, cudaStream_t s) {
+// Pairs of CTAs that are resident at once (0: none).
+template <int SPLIT> int resident_pairs() {
+    static int cached[kMaxDevices] = {};                  // pairs + 1
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return 0;
+    if (cached[dev] == 0) {
+        constexpr size_t smem = (size_t)kRing + 1024;
+        static size_t configured[kMaxDevices] = {};
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(2); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = smem;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr; cfg.numAttrs = 1;
+        int n = 0;
+        if (ensure_dyn_smem(ns_iterate_kernel<SPLIT, true>, smem, configured) != GF_OK ||
+            cudaOccupancyMaxActiveClusters(&n, ns_iterate_kernel<SPLIT, true>, &cfg) != cudaSuccess)
+            n = 0;
+        cached[dev] = n + 1;
+    }
+    return cached[dev] - 1;
+}
+
+// The iteration from X in the workspace (written by ns_cast_kernel); the result is X[steps & 1].
+gf_status ns_iterate(const NsPlan& p, char* base, int steps, const float* coeffs, cudaStream_t s) {
     IterateArgs a = {};
     a.batch = p.batch; a.m = p.m; a.n = p.n; a.steps = steps;
     for (int k = 0; k < steps; ++k)
@@ -655,20 +762,39 @@ gf_status ns_iterate(const NsPlan& p, char* base, int steps, const float* coeffs
     a.x[1] = reinterpret_cast<__half*>(base + p.off_x[1]);
     a.a = reinterpret_cast<__half*>(base + p.off_a);
     a.b = reinterpret_cast<__half*>(base + p.off_b);
-    a.ldx = p.ldx; a.lda = p.lda; a.x_lo = p.x_lo; a.a_lo = p.a_lo;
-    a.out = O; a.out_bf16 = out_bf16; a.transposed = p.transposed;
+    a.x_pieces = p.x_pieces; a.a_pieces = p.a_pieces; a.x_lo = p.x_lo; a.a_lo = p.a_lo;
     a.err_word = reinterpret_cast<uint32_t*>(base);
     a.barrier = reinterpret_cast<uint32_t*>(base + 128);
-    a.shape[PH_GRAM] = a.shape[PH_POLY] = phase_shape(p, true);
-    a.shape[PH_APPLY] = phase_shape(p, false);
+    const int pairs = p.split == 2 ? resident_pairs<2>() : resident_pairs<1>();
+    const bool pair = pairs > 0 && use_pairs(p, pairs);
+    const int units = pair ? pairs : sm_count();
+    a.shape[PH_GRAM] = a.shape[PH_POLY] = phase_shape(p, true, pair, units);
+    a.shape[PH_APPLY] = phase_shape(p, false, pair, units);
     for (const PhaseShape& ps : a.shape)
         if ((long long)ps.tiles * p.batch > 0x3fffffffLL) return GF_ERR_UNSUPPORTED;
-    const uint64_t m = (uint64_t)p.m, n = (uint64_t)p.n, lx = (uint64_t)p.ldx, la = (uint64_t)p.lda, b = (uint64_t)p.batch;
-    // the maps move 16-bit elements; zeros beyond the matrices are the same in fp16
-    if (!make_tmap_bf16(&a.tm_x[0], a.x[0], 3, n, m, 2 * b, lx, m * lx, 64) || !make_tmap_bf16(&a.tm_x[1], a.x[1], 3, n, m, 2 * b, lx, m * lx, 64) ||
-        !make_tmap_bf16(&a.tm_a, a.a, 3, m, m, b * p.split, la, m * la, 64) || !make_tmap_bf16(&a.tm_b, a.b, 3, m, m, b * p.split, la, m * la, 64))
-        return GF_ERR_CUDA;
-    return p.split == 2 ? launch_iterate<2>(a, s) : launch_iterate<1>(a, s);
+    const uint64_t m = (uint64_t)p.m, b = (uint64_t)p.batch, xp = (uint64_t)p.x_pieces, ap = (uint64_t)p.a_pieces;
+    const uint32_t g_rows = (uint32_t)(pair ? a.shape[PH_GRAM].bn / 2 : a.shape[PH_GRAM].bn);
+    const uint32_t n_cols = (uint32_t)(pair ? a.shape[PH_APPLY].bn / 2 : a.shape[PH_APPLY].bn);
+    // two 8-byte units are the 8 columns of a row
+    auto map = [&](CUtensorMap* out, const __half* src, uint64_t pieces, uint64_t planes, uint32_t rows, uint32_t columns) {
+        return make_tmap_u64(out, src, 2 * m, pieces, planes, 2 * m, 2 * m * pieces, 2 * rows, columns / 8);
+    };
+    bool good = map(&a.tm_a[2], a.a, ap, b * p.split, 128, 64) && map(&a.tm_a[3], a.b, ap, b * p.split, 128, 64) &&
+                map(&a.tm_g[2], a.a, ap, b * p.split, g_rows, 64);
+    for (int k = 0; k < 2 && good; ++k)
+        good = map(&a.tm_a[k], a.x[k], xp, 2 * b, 128, 64) && map(&a.tm_g[k], a.x[k], xp, 2 * b, g_rows, 64) &&
+               map(&a.tm_n[k], a.x[k], xp, 2 * b, 64, n_cols);
+    if (!good) return GF_ERR_CUDA;
+    if (pair) return p.split == 2 ? launch_iterate<2, true>(a, units, s) : launch_iterate<1, true>(a, units, s);
+    return p.split == 2 ? launch_iterate<2, false>(a, units, s) : launch_iterate<1, false>(a, units, s);
+}
+
+dim3 finish_grid(const NsPlan& p, int count) { return dim3((p.cols + kCast - 1) / kCast, (p.rows + kCast - 1) / kCast, count); }
+FinishArgs finish_args(const NsPlan& p, char* base, int steps, int first) {
+    FinishArgs f = {};
+    f.x = reinterpret_cast<const __half*>(base + p.off_x[steps & 1]) + 8LL * first * p.x_pieces * p.m;
+    f.m = p.m; f.n = p.n; f.pieces = p.x_pieces; f.lo = p.x_lo; f.transposed = p.transposed; f.rows = p.rows; f.cols = p.cols; f.taps = 1;
+    return f;
 }
 
 template <bool MUON> gf_status launch_prepare(const NsPlan& p, const Source& src, int first, int count, char* base, float eps, cudaStream_t s) {
@@ -677,9 +803,9 @@ template <bool MUON> gf_status launch_prepare(const NsPlan& p, const Source& src
     gf_status st = launch_pdl(ns_norm_kernel<MUON>, dim3(p.norm_blocks, count), dim3(kNormThreads), 0, s, src, part,
                               first == 0 ? reinterpret_cast<uint32_t*>(base) : nullptr);
     if (st != GF_OK) return st;
-    __half* X = reinterpret_cast<__half*>(base + p.off_x[0]) + (size_t)first * p.m * p.ldx;
+    __half* X = reinterpret_cast<__half*>(base + p.off_x[0]) + 8LL * first * p.m * p.x_pieces;
     const dim3 grid((p.cols + kCast - 1) / kCast, (p.rows + kCast - 1) / kCast, count), block(256);
-    return launch_pdl(ns_cast_kernel<MUON>, grid, block, 0, s, src, (const double*)part, p.norm_blocks, eps, X, p.m, p.n, p.ldx, p.x_lo, p.transposed);
+    return launch_pdl(ns_cast_kernel<MUON>, grid, block, 0, s, src, (const double*)part, p.norm_blocks, eps, X, p.m, p.n, p.x_pieces, p.x_lo, p.transposed);
 }
 
 bool off16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
@@ -703,7 +829,7 @@ gf_status gf_newton_schulz_workspace_bytes(const gf_ns_desc* d, size_t* bytes) {
     if (!d || !bytes) return GF_ERR_NULL;
     if (gf_status st = check_shape(d->batch, d->rows, d->cols, d->precision, d->steps, d->eps); st != GF_OK) return st;
     if (bad_dtype(d->in_dtype) || bad_dtype(d->out_dtype)) return GF_ERR_BAD_DESC;
-    *bytes = ns_plan(d->batch, d->rows, d->cols, d->precision, false).total;
+    *bytes = ns_plan(d->batch, d->rows, d->cols, d->precision).total;
     return GF_OK;
 }
 
@@ -715,13 +841,16 @@ gf_status gf_newton_schulz(const gf_ns_desc* d, const void* G, void* O, void* wo
     if (!G || !O || !workspace) return GF_ERR_NULL;
     if (off16(G) || off16(O) || off16(workspace)) return GF_ERR_ALIGN;
     if (workspace_bytes < need) return GF_ERR_WORKSPACE;
-    const NsPlan p = ns_plan(d->batch, d->rows, d->cols, d->precision, false);
+    const NsPlan p = ns_plan(d->batch, d->rows, d->cols, d->precision);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     char* base = static_cast<char*>(workspace);
     Source src = {};
     src.g[0] = G; src.batched = 1; src.bf16 = d->in_dtype == GF_BF16; src.taps = 1; src.rows = d->rows; src.cols = d->cols;
     if (gf_status st = launch_prepare<false>(p, src, 0, d->batch, base, d->eps, s); st != GF_OK) return st;
-    return ns_iterate(p, base, d->steps, h_coeffs, O, d->out_dtype == GF_BF16, s);
+    if (gf_status st = ns_iterate(p, base, d->steps, h_coeffs, s); st != GF_OK) return st;
+    FinishArgs f = finish_args(p, base, d->steps, 0);
+    f.out = O; f.bf16 = d->out_dtype == GF_BF16;
+    return launch_pdl(ns_finish_kernel<false>, finish_grid(p, d->batch), dim3(256), 0, s, f);
 }
 
 gf_status gf_muon_workspace_bytes(const gf_muon_desc* d, size_t* bytes) {
@@ -729,7 +858,7 @@ gf_status gf_muon_workspace_bytes(const gf_muon_desc* d, size_t* bytes) {
     if (gf_status st = check_shape(d->count, d->rows, d->cols, d->precision, d->steps, d->eps); st != GF_OK) return st;
     if (bad_dtype(d->grad_dtype) || bad_dtype(d->weight_dtype) || d->taps < 1 || (d->nesterov != 0 && d->nesterov != 1)) return GF_ERR_BAD_DESC;
     if (d->taps > 4096) return GF_ERR_UNSUPPORTED;
-    *bytes = ns_plan(d->count, d->rows, d->cols, d->precision, true).total;
+    *bytes = ns_plan(d->count, d->rows, d->cols, d->precision).total;
     return GF_OK;
 }
 
@@ -750,7 +879,7 @@ gf_status gf_muon_step(const gf_muon_desc* d, const void* const* h_grad, const f
         }
     }
     if (workspace_bytes < need) return GF_ERR_WORKSPACE;
-    const NsPlan p = ns_plan(d->count, d->rows, d->cols, d->precision, true);
+    const NsPlan p = ns_plan(d->count, d->rows, d->cols, d->precision);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     char* base = static_cast<char*>(workspace);
     const float root = sqrtf((float)d->taps);
@@ -767,20 +896,15 @@ gf_status gf_muon_step(const gf_muon_desc* d, const void* const* h_grad, const f
         // the flattened matrix is u (x) (1 .. 1): its norm is sqrt(taps) times that of u
         if (gf_status st = launch_prepare<true>(p, src, first, n, base, d->eps / root, s); st != GF_OK) return st;
     }
-    float* O = reinterpret_cast<float*>(base + p.off_o);
-    if (gf_status st = ns_iterate(p, base, d->steps, h_coeffs, O, 0, s); st != GF_OK) return st;
+    if (gf_status st = ns_iterate(p, base, d->steps, h_coeffs, s); st != GF_OK) return st;
     for (int first = 0; first < d->count; first += kMaxLayers) {
         const int n = d->count - first < kMaxLayers ? d->count - first : kMaxLayers;
-        UpdateArgs u = {};
-        for (int k = 0; k < n; ++k) { u.w[k] = h_weight[first + k]; u.w_out[k] = h_weight_out[first + k]; }
-        u.n = (long long)d->rows * d->cols;
-        u.O = O + (size_t)first * u.n;
-        u.taps = d->taps; u.bf16 = d->weight_dtype == GF_BF16;
-        u.keep = 1.f - d->lr * d->weight_decay;
-        u.f = d->lr * d->scale / root;
-        const long long blocks = (u.n * u.taps + 1023) / 1024;
-        const long long most = cdiv64(8LL * sm_count(), n);
-        if (gf_status st = launch_pdl(muon_update_kernel, dim3((unsigned)(blocks < most ? blocks : most), n), dim3(256), 0, s, u); st != GF_OK) return st;
+        FinishArgs f = finish_args(p, base, d->steps, first);
+        for (int k = 0; k < n; ++k) { f.w[k] = h_weight[first + k]; f.w_out[k] = h_weight_out[first + k]; }
+        f.taps = d->taps; f.div_taps = FastDiv((uint32_t)d->taps); f.bf16 = d->weight_dtype == GF_BF16;
+        f.keep = 1.f - d->lr * d->weight_decay;
+        f.f = d->lr * d->scale / root;
+        if (gf_status st = launch_pdl(ns_finish_kernel<true>, finish_grid(p, n), dim3(256), 0, s, f); st != GF_OK) return st;
     }
     return GF_OK;
 }

@@ -58,6 +58,22 @@ bool make_tmap_u8_2d(CUtensorMap* out, const void* base, uint64_t width, uint64_
     return r == CUDA_SUCCESS;
 }
 
+bool make_tmap_u64(CUtensorMap* out, const void* base, uint64_t d0, uint64_t d1, uint64_t d2, uint64_t stride1, uint64_t stride2,
+                   uint32_t box0, uint32_t box1) {
+    PFN_cuTensorMapEncodeTiled enc = encoder();
+    if (!enc) return false;
+    if ((reinterpret_cast<uintptr_t>(base) & 15u) != 0 || stride1 % 2 != 0 || stride2 % 2 != 0) return false;
+    if (box0 < 2 || box0 > 256 || box0 % 2 != 0 || box1 < 1 || box1 > 256) return false;
+    cuuint64_t dims[3] = {d0, d1, d2};
+    cuuint64_t strides[2] = {stride1 * 8, stride2 * 8};
+    cuuint32_t box[3] = {box0, box1, 1};
+    cuuint32_t estr[3] = {1, 1, 1};
+    const CUresult r = enc(out, CU_TENSOR_MAP_DATA_TYPE_UINT64, 3, const_cast<void*>(base), dims, strides, box, estr,
+                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS;
+}
+
 bool make_tmap_plain(CUtensorMap* out, const void* base, int elem_bytes, uint64_t d0, uint64_t d1, uint64_t d2,
                      uint64_t stride1, uint64_t stride2, uint32_t box0, uint32_t box1, uint32_t box2) {
     PFN_cuTensorMapEncodeTiled enc = encoder();

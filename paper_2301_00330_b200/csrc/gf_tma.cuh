@@ -38,6 +38,10 @@ bool make_tmap_plain(CUtensorMap* out, const void* base, int elem_bytes, uint64_
 // 128-byte swizzle: a box lands as a K-major tile of 128-byte rows.  pitch is a multiple of 16.
 bool make_tmap_u8_2d(CUtensorMap* out, const void* base, uint64_t width, uint64_t rows, uint64_t pitch, uint32_t box_rows);
 
+// Plain map of a dense array [d2][d1][d0] of 8-byte units, strides in units, box = {box0, box1, 1}; an even box0 <= 256.
+bool make_tmap_u64(CUtensorMap* out, const void* base, uint64_t d0, uint64_t d1, uint64_t d2, uint64_t stride1, uint64_t stride2,
+                   uint32_t box0, uint32_t box1);
+
 #ifdef __CUDACC__
 __device__ __forceinline__ void tma_load_2d(void* dst_smem, const CUtensorMap* m, int x, int y, uint64_t* bar) {
     asm volatile(
