@@ -423,6 +423,13 @@ __device__ __forceinline__ uint32_t cluster_rank() {
     return r;
 }
 
+// One thread of a converged warp.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
+}
+
 // All blocks of a cooperative launch meet: the writes before it are visible to all after it.  `ok` false in any thread ends the
 // kernel of every block: the error word tells the others.  The wait is bounded like every other.
 __device__ __forceinline__ bool grid_meet(const IterateArgs& p, uint32_t target, bool ok, int* flag) {
@@ -447,10 +454,10 @@ __device__ __forceinline__ bool grid_meet(const IterateArgs& p, uint32_t target,
             }
         }
         *flag = go;
-        // what the other blocks wrote through the generic proxy is read by this thread's copies through the asynchronous one
-        asm volatile("fence.proxy.async;" ::: "memory");
     }
     __syncthreads();
+    // what the other blocks wrote through the generic proxy is read by this warp's copies through the asynchronous one
+    if (threadIdx.x < 32) asm volatile("fence.proxy.async;" ::: "memory");
     return *flag != 0;
 }
 
@@ -463,7 +470,7 @@ template <int SPLIT, bool PAIR> __global__ void __launch_bounds__(kThreads, 1) n
     __shared__ uint32_t tmem_base;
     __shared__ int flag;
     constexpr int kRows = PAIR ? 256 : 128;                 // of a tile
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;      // uniform
     const uint32_t rank = PAIR ? cluster_rank() : 0u;
     const int unit = PAIR ? blockIdx.x >> 1 : blockIdx.x, units = PAIR ? gridDim.x >> 1 : gridDim.x;
     if (threadIdx.x == 0) {
@@ -481,7 +488,7 @@ template <int SPLIT, bool PAIR> __global__ void __launch_bounds__(kThreads, 1) n
     __syncthreads();
     if constexpr (PAIR) cluster_meet();                     // the other CTA's barriers are ready
     tc_fence_after_sync();
-    const uint32_t tmem = tmem_base;
+    const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_base, 0);
     asm volatile("fence.proxy.async;" ::: "memory");
     bool ok = true;
     uint32_t ring = 0;                 // one bit per stage: the parity of its next use
@@ -503,18 +510,21 @@ template <int SPLIT, bool PAIR> __global__ void __launch_bounds__(kThreads, 1) n
             if (symmetric) lower_tile(tt, ps.bn == kRows, ti, tj);
             else { ti = tt / ps.tiles_n; tj = tt - ti * ps.tiles_n; }
         };
+        // The two issuing warps run their loops as whole warps and elect the thread that issues: descriptors and addresses
+        // then stay in uniform registers.  (With the loop under `lane == 0` every product took 110 clocks to issue, whatever its
+        // size.)
         if (warp == 0) {
-            if (lane == 0) {
-                const CUtensorMap* ta = phase == PH_GRAM ? &p.tm_a[step & 1] : phase == PH_POLY ? &p.tm_a[2] : &p.tm_a[3];
-                const CUtensorMap* tb = phase == PH_GRAM ? &p.tm_g[step & 1] : phase == PH_POLY ? &p.tm_g[2] : &p.tm_n[step & 1];
-                int s = 0;
-                for (int t = unit; t < total && ok; t += units) {
-                    int b, ti, tj;
-                    tile_at(t, b, ti, tj);
-                    const int row = ti * kRows + (int)rank * 128, col = tj * ps.bn + (int)rank * share;
-                    for (int q = 0; q < chunks; ++q) {
-                        ok = mbar_wait_bounded(&empty[s], ((ring >> s) & 1u) ^ 1u);
-                        if (!ok) break;
+            const CUtensorMap* ta = phase == PH_GRAM ? &p.tm_a[step & 1] : phase == PH_POLY ? &p.tm_a[2] : &p.tm_a[3];
+            const CUtensorMap* tb = phase == PH_GRAM ? &p.tm_g[step & 1] : phase == PH_POLY ? &p.tm_g[2] : &p.tm_n[step & 1];
+            int s = 0;
+            for (int t = unit; t < total && ok; t += units) {
+                int b, ti, tj;
+                tile_at(t, b, ti, tj);
+                const int row = ti * kRows + (int)rank * 128, col = tj * ps.bn + (int)rank * share;
+                for (int q = 0; q < chunks; ++q) {
+                    ok = __all_sync(0xffffffffu, mbar_wait_bounded(&empty[s], ((ring >> s) & 1u) ^ 1u));
+                    if (!ok) break;
+                    if (elect_one()) {
                         unsigned char* st = dyn + (size_t)s * ps.stage_bytes;
                         if (rank == 0) mbar_expect_tx(&full[s], (uint32_t)ps.stage_bytes * (PAIR ? 2u : 1u));
 #pragma unroll
@@ -525,17 +535,20 @@ template <int SPLIT, bool PAIR> __global__ void __launch_bounds__(kThreads, 1) n
                             if (symmetric) load_box<PAIR>(sb, tb, col * 2, q * 8, z, &full[s]);
                             else load_box<PAIR>(sb, tb, q * 128, col / 8, z, &full[s]);
                         }
-                        ring ^= 1u << s;
-                        if (++s == ps.stages) s = 0;
                     }
+                    __syncwarp();
+                    ring ^= 1u << s;
+                    if (++s == ps.stages) s = 0;
                 }
             }
         } else if (warp == 1) {
-            if (lane == 0 && rank == 0) {
+            if (rank == 0) {
                 // fp16 x fp16 -> fp32; B is K-major in the symmetric products, MN-major otherwise
                 const uint32_t idesc = (1u << 4) | ((symmetric ? 0u : 1u) << 16) | ((uint32_t)(ps.bn >> 3) << 17) | ((uint32_t)(kRows >> 4) << 24);
-                const uint32_t b_step = symmetric ? (uint32_t)share * 32u : 256u;      // 16 k further
-                const uint32_t b_lbo = symmetric ? (uint32_t)share * 16u : 128u, b_sbo = symmetric ? 128u : 1024u;
+                const uint64_t a_form = plain_smem_desc(0, 2048, 128);
+                const uint64_t b_form = symmetric ? plain_smem_desc(0, (uint32_t)share * 16u, 128) : plain_smem_desc(0, 128, 1024);
+                const uint32_t b_step = (symmetric ? (uint32_t)share * 32u : 256u) >> 4;      // 16 k further, in 16 bytes
+                const uint32_t ring0 = smem_u32(dyn) >> 4;
                 int s = 0;
                 for (int t = unit; t < total && ok; t += units) {
                     for (int q = 0; q < chunks; ++q) {
@@ -543,24 +556,29 @@ template <int SPLIT, bool PAIR> __global__ void __launch_bounds__(kThreads, 1) n
                         const bool first = q % segment == 0, last = q % segment == segment - 1 || q == chunks - 1;
                         if (first && use >= 2) ok = mbar_wait_bounded(&drained[buf], ((use >> 1) - 1) & 1u);
                         if (ok) ok = mbar_wait_bounded(&full[s], (ring >> s) & 1u);
+                        ok = __all_sync(0xffffffffu, ok);
                         if (!ok) break;
                         tc_fence_after_sync();
-                        const uint32_t d = tmem + (uint32_t)(buf * 256);
-                        const uint32_t a_hi = smem_u32(dyn + (size_t)s * ps.stage_bytes), a_lo = a_hi + a_bytes;
-                        const uint32_t b_hi = a_hi + SPLIT * a_bytes, b_lo = b_hi + b_bytes;
+                        if (elect_one()) {
+                            const uint32_t d = tmem + (uint32_t)(buf * 256);
+                            const uint32_t at = ring0 + (uint32_t)s * ((uint32_t)ps.stage_bytes >> 4);
+                            const uint64_t a_hi = a_form + at, a_lo = a_hi + (a_bytes >> 4);
+                            const uint64_t b_hi = b_form + at + SPLIT * (a_bytes >> 4), b_lo = b_hi + (b_bytes >> 4);
 #pragma unroll
-                        for (int ks = 0; ks < 4; ++ks) {
-                            const uint64_t ad = plain_smem_desc(a_hi + ks * 4096, 2048, 128), bd = plain_smem_desc(b_hi + ks * b_step, b_lbo, b_sbo);
-                            mma_f16<PAIR>(d, ad, bd, idesc, !(first && ks == 0));
-                            if constexpr (SPLIT == 2) {
-                                mma_f16<PAIR>(d, ad, plain_smem_desc(b_lo + ks * b_step, b_lbo, b_sbo), idesc, 1u);
-                                mma_f16<PAIR>(d, plain_smem_desc(a_lo + ks * 4096, 2048, 128), bd, idesc, 1u);
+                            for (int ks = 0; ks < 4; ++ks) {
+                                mma_f16<PAIR>(d, a_hi + ks * 256, b_hi + ks * b_step, idesc, !(first && ks == 0));
+                                if constexpr (SPLIT == 2) {
+                                    mma_f16<PAIR>(d, a_hi + ks * 256, b_lo + ks * b_step, idesc, 1u);
+                                    mma_f16<PAIR>(d, a_lo + ks * 256, b_hi + ks * b_step, idesc, 1u);
+                                }
                             }
+                            commit<PAIR>(&empty[s]);
+                            if (last) commit<PAIR>(&done[buf]);
                         }
-                        commit<PAIR>(&empty[s]);
+                        __syncwarp();
                         ring ^= 1u << s;
                         if (++s == ps.stages) s = 0;
-                        if (last) { commit<PAIR>(&done[buf]); ++use; }
+                        if (last) ++use;
                     }
                 }
             }
