@@ -50,7 +50,7 @@ ProfScope::~ProfScope() {
 // (gf_stash_forward).  The address is looked up once per device.
 static __device__ uint32_t g_err_word_dev;
 
-static uint32_t* global_err_word() {
+uint32_t* global_err_word() {
     static uint32_t* cached[kMaxDevices] = {};
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return nullptr;

@@ -168,6 +168,9 @@ struct Geo {
 
 Geo make_geo(const gf_conv_desc& d);
 
+// Error word of the current device for kernels that run without a workspace (NULL: a CUDA call failed).
+uint32_t* global_err_word();
+
 // ---- workspace layout of gf_backward ---------------------------------------
 // [ error word (256 B) | theta sum fp32 [C_out,C_ig] | gbar fp32 [N,C_out,Hp,Wp] |
 //   split partials fp32 [S, C_out, C_ig] | fp32 tensor-core layers: stash as bf16 (high, low) ]

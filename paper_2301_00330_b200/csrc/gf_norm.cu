@@ -2,6 +2,8 @@
 #include <type_traits>
 
 #include "gf_common.cuh"
+#include "gf_pipe.cuh"
+#include "gf_tma.cuh"
 #include "gf_train.h"
 
 namespace gf {
@@ -286,6 +288,256 @@ template <typename T> __global__ void __launch_bounds__(1024) ln_rows_bwd_long_k
     }
 }
 
+// ---- rows through shared memory ---------------------------------------------------------------------
+// For more rows than there are teams of threads: a team (part of a block that shares a row) has its own ring of batches
+// of whole rows, which the copy engine fills some batches ahead, so that the loads of the next rows run under
+// the sums and stores of the present one.  A batch is one contiguous piece of memory, copied from the 16-byte
+// boundary before it to the one after it: rows of any length take the same path.  The last bytes of a tensor whose
+// size is no multiple of 16 are fetched with plain loads.
+struct RingArgs {
+    int warps;                 // per team
+    int stages, rows;          // batches in flight per team; rows per batch
+    int stage_bytes;           // of one tensor's batch
+    long long batches;
+    uint32_t* err_word;
+};
+
+template <bool TEAM> __device__ __forceinline__ void team_sync(int team, int warps) {
+    if constexpr (TEAM) asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(warps * 32) : "memory");
+    else __syncwarp();
+}
+
+// Sums of N values over the threads that share a row (part of a warp, or a team of warps through `red` [N][16]).
+template <bool TEAM, int N> __device__ __forceinline__ void team_sum(float (&s)[N], int log_tpr, float* red, int team, int warps) {
+    if constexpr (TEAM) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+            for (int n = 0; n < N; ++n) s[n] += __shfl_xor_sync(0xffffffffu, s[n], o);
+        const int w = (threadIdx.x >> 5) - team * warps;
+        if ((threadIdx.x & 31) == 0) {
+#pragma unroll
+            for (int n = 0; n < N; ++n) red[n * 16 + w] = s[n];
+        }
+        team_sync<TEAM>(team, warps);
+#pragma unroll
+        for (int n = 0; n < N; ++n) s[n] = red[n * 16];
+        for (int k = 1; k < warps; ++k)
+#pragma unroll
+            for (int n = 0; n < N; ++n) s[n] += red[n * 16 + k];
+    } else {
+        for (int o = (1 << log_tpr) >> 1; o > 0; o >>= 1)
+#pragma unroll
+            for (int n = 0; n < N; ++n) s[n] += __shfl_xor_sync(0xffffffffu, s[n], o);
+    }
+}
+
+template <typename T, int V, int E, bool TEAM, bool BWD>
+__global__ void __launch_bounds__(512) ln_rows_ring_kernel(const __grid_constant__ NormArgs a, const __grid_constant__ RingArgs r) {
+    constexpr int NV = E / V, NT = BWD ? 2 : 1;
+    extern __shared__ __align__(128) unsigned char dyn[];
+    __shared__ uint64_t full[8 * 8];                       // [team][stage]
+    __shared__ float red[8][2][2 * 16];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int team = warp / r.warps, teams = (int)(blockDim.x >> 5) / r.warps;
+    const int tid = threadIdx.x - team * r.warps * 32;      // within the team
+    const int tpr = 1 << a.log_tpr, g = TEAM ? tid : tid & (tpr - 1);
+    const int rows_at_once = TEAM ? 1 : 32 >> a.log_tpr;
+    const int step = tpr * V;                               // columns between a thread's vectors
+    const long long teams_all = (long long)gridDim.x * teams, first = (long long)blockIdx.x * teams + team;
+    const int row_bytes = a.C * (int)sizeof(T);
+    const long long total16 = (a.R * row_bytes) & ~15LL;    // whole 16-byte pieces of the tensor
+    unsigned char* ring = dyn + (size_t)team * r.stages * NT * r.stage_bytes;
+    if (threadIdx.x == 0) {
+        for (int k = 0; k < teams * r.stages; ++k) mbar_init(&full[k], 1);
+        mbar_fence_init();
+    }
+    __syncthreads();
+    auto load = [&](long long b, int s) {                   // by one thread
+        const long long lo = (b * r.rows * row_bytes) & ~15LL;
+        long long hi = ((b + 1) * r.rows < a.R ? (b + 1) * r.rows : a.R) * row_bytes;
+        hi = (hi + 15) & ~15LL;
+        if (hi > total16) hi = total16;
+        const uint32_t bytes = hi > lo ? (uint32_t)(hi - lo) : 0u;
+        uint64_t* bar = &full[team * r.stages + s];
+        mbar_expect_tx(bar, bytes * NT);
+        if (bytes == 0) return;
+        unsigned char* dst = ring + (size_t)s * NT * r.stage_bytes;
+        bulk_g2s(dst, static_cast<const unsigned char*>(a.x) + lo, bytes, bar);
+        if constexpr (BWD) bulk_g2s(dst + r.stage_bytes, static_cast<const unsigned char*>(a.gy) + lo, bytes, bar);
+    };
+    if (tid == 0)
+        for (int s = 0; s < r.stages; ++s)
+            if (first + s * teams_all < r.batches) load(first + s * teams_all, s);
+
+    float gam[NV][V], bet[BWD ? 1 : NV][V], ag[BWD ? NV : 1][V], ab[BWD ? NV : 1][V];
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int c = k * step + g * V + i;
+            gam[k][i] = c < a.C ? a.gamma.at(c, 1.f) : 0.f;
+            if constexpr (!BWD) bet[k][i] = c < a.C ? a.beta.at(c, 0.f) : 0.f;
+            else ag[k][i] = ab[k][i] = 0.f;
+        }
+    float mean_n = 0.f, rstd_n = 0.f;                       // of row `lane` of the next batch
+    auto stats = [&](long long b) {
+        const long long row = b * r.rows + lane;
+        const bool there = b < r.batches && lane < r.rows && row < a.R;
+        mean_n = there ? a.mean_in[row] : 0.f;
+        rstd_n = there ? a.rstd_in[row] : 0.f;
+    };
+    if constexpr (BWD) stats(first);
+
+    bool ok = true;
+    int s = 0, slot = 0;
+    uint32_t parity = 0;
+    for (long long b = first; b < r.batches; b += teams_all) {
+        ok = mbar_wait_bounded(&full[team * r.stages + s], parity);
+        if constexpr (TEAM) ok = !bar_any(team + 1, r.warps * 32, !ok);
+        else ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        const long long r0 = b * r.rows, lo = (r0 * row_bytes) & ~15LL;
+        const int nr = (int)(a.R - r0 < r.rows ? a.R - r0 : r.rows);
+        unsigned char* sx = ring + (size_t)s * NT * r.stage_bytes;
+        if ((r0 + nr) * row_bytes > total16) {              // the tensor's last bytes
+            const long long from = lo > total16 ? lo : total16;
+            const int n = (int)(((r0 + nr) * row_bytes - from) / (long long)sizeof(T));
+            if (tid < n) {
+                reinterpret_cast<T*>(sx + (from - lo))[tid] = reinterpret_cast<const T*>(static_cast<const unsigned char*>(a.x) + from)[tid];
+                if constexpr (BWD)
+                    reinterpret_cast<T*>(sx + r.stage_bytes + (from - lo))[tid] =
+                        reinterpret_cast<const T*>(static_cast<const unsigned char*>(a.gy) + from)[tid];
+            }
+            team_sync<TEAM>(team, r.warps);
+        }
+        const float mean_b = mean_n, rstd_b = rstd_n;
+        if constexpr (BWD) stats(b + teams_all);
+        const int row_in = TEAM ? 0 : lane >> a.log_tpr;    // of the rows that the warp has at once
+        const T* x = reinterpret_cast<const T*>(sx + (int)(r0 * row_bytes - lo) + row_in * row_bytes) + g * V;
+        T* out = static_cast<T*>(a.out) + (r0 + row_in) * a.C + g * V;
+        for (int q = 0; q < nr; q += rows_at_once, slot ^= 1, x += rows_at_once * a.C, out += rows_at_once * a.C) {
+            const int k_row = q + row_in;
+            const int width = TEAM || k_row < nr ? a.C - g * V : 0;      // columns from this thread's first on
+            float v[NV][V];
+            if constexpr (!BWD) {
+                float sum[1] = {0.f}, var[1] = {0.f};
+#pragma unroll
+                for (int k = 0; k < NV; ++k) {
+                    if (k * step >= a.C) break;             // the same for all threads
+                    if (k * step < width) load_vec<T, V>(x + k * step, v[k]);
+                    else {
+#pragma unroll
+                        for (int i = 0; i < V; ++i) v[k][i] = 0.f;
+                    }
+#pragma unroll
+                    for (int i = 0; i < V; ++i) sum[0] += v[k][i];
+                }
+                team_sum<TEAM, 1>(sum, a.log_tpr, red[team][0], team, r.warps);
+                const float mean = sum[0] / (float)a.C;
+#pragma unroll
+                for (int k = 0; k < NV; ++k) {
+                    if (k * step >= a.C) break;
+                    if (k * step < width) {
+#pragma unroll
+                        for (int i = 0; i < V; ++i) { v[k][i] -= mean; var[0] += v[k][i] * v[k][i]; }
+                    }
+                }
+                team_sum<TEAM, 1>(var, a.log_tpr, red[team][1], team, r.warps);
+                const float rstd = rsqrtf(var[0] * a.inv_c + a.eps);
+#pragma unroll
+                for (int k = 0; k < NV; ++k) {
+                    if (k * step >= a.C) break;
+                    if (k * step < width) {
+#pragma unroll
+                        for (int i = 0; i < V; ++i) v[k][i] = v[k][i] * rstd * gam[k][i] + bet[k][i];
+                        store_vec<T, V>(out + k * step, v[k]);
+                    }
+                }
+                if (a.mean && g == 0 && width > 0) { a.mean[r0 + k_row] = mean; a.rstd[r0 + k_row] = rstd; }
+            } else {
+                const T* gy = reinterpret_cast<const T*>(reinterpret_cast<const unsigned char*>(x) + r.stage_bytes);
+                const float mean = __shfl_sync(0xffffffffu, mean_b, k_row & 31), rstd = __shfl_sync(0xffffffffu, rstd_b, k_row & 31);
+                float gv[NV][V];
+                float sum[2] = {0.f, 0.f};
+#pragma unroll
+                for (int k = 0; k < NV; ++k) {
+                    if (k * step >= a.C) break;
+                    if (k * step < width) {
+                        load_vec<T, V>(x + k * step, v[k]);
+                        load_vec<T, V>(gy + k * step, gv[k]);
+                    } else {                                // xh = 0 and gy = 0: adds nothing
+#pragma unroll
+                        for (int i = 0; i < V; ++i) { v[k][i] = mean; gv[k][i] = 0.f; }
+                    }
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        v[k][i] = (v[k][i] - mean) * rstd;
+                        ag[k][i] += gv[k][i] * v[k][i];
+                        ab[k][i] += gv[k][i];
+                        gv[k][i] *= gam[k][i];
+                        sum[0] += gv[k][i];
+                        sum[1] += gv[k][i] * v[k][i];
+                    }
+                }
+                if (a.out) {
+                    team_sum<TEAM, 2>(sum, a.log_tpr, red[team][slot], team, r.warps);
+                    const float m1 = sum[0] * a.inv_c * rstd, m2 = sum[1] * a.inv_c * rstd;
+#pragma unroll
+                    for (int k = 0; k < NV; ++k) {
+                        if (k * step >= a.C) break;
+                        if (k * step < width) {
+#pragma unroll
+                            for (int i = 0; i < V; ++i) v[k][i] = (gv[k][i] * rstd - m1) - v[k][i] * m2;
+                            store_vec<T, V>(out + k * step, v[k]);
+                        }
+                    }
+                }
+            }
+        }
+        team_sync<TEAM>(team, r.warps);                     // the batch has been read
+        if (tid == 0 && b + r.stages * teams_all < r.batches) load(b + r.stages * teams_all, s);
+        if (++s == r.stages) { s = 0; parity ^= 1u; }
+    }
+    if (!ok) {
+        atomicOr(r.err_word, 8192u);
+        const long long t0 = clock64();                     // copies may still be on their way to this block's shared memory
+        while (clock64() - t0 < 2000000LL) {}
+    }
+    if constexpr (BWD) {
+        if (!a.part) return;
+        float* cols = reinterpret_cast<float*>(dyn);        // [2][C], over the rings
+        float* part = a.part + (size_t)blockIdx.x * 2 * a.C;
+        if constexpr (!TEAM) {
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    for (int o = tpr; o < 32; o <<= 1) {    // lanes of a warp that hold the same columns
+                        ag[k][i] += __shfl_xor_sync(0xffffffffu, ag[k][i], o);
+                        ab[k][i] += __shfl_xor_sync(0xffffffffu, ab[k][i], o);
+                    }
+        }
+        __syncthreads();
+        for (int w = 0; w < teams; ++w) {                   // the teams of the block in order
+            if (team == w && tid < tpr) {
+#pragma unroll
+                for (int k = 0; k < NV; ++k)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        const int c = k * step + g * V + i;
+                        if (c < a.C) {
+                            const float p = w == 0 ? ag[k][i] : cols[c] + ag[k][i], q = w == 0 ? ab[k][i] : cols[a.C + c] + ab[k][i];
+                            if (w == teams - 1) { part[c] = p; part[a.C + c] = q; }
+                            else { cols[c] = p; cols[a.C + c] = q; }
+                        }
+                    }
+            }
+            __syncthreads();
+        }
+    }
+}
+
 // ---- channels first --------------------------------------------------------------------------
 // A block takes 32 V consecutive pixels (lane = pixel, V per lane) and all channels; warp w of CG
 // has channels w, w + CG, ...  Pixels are numbered through all images, so that small planes fill
@@ -565,6 +817,287 @@ __global__ void __launch_bounds__(512) ln_planes_bwd_long_kernel(const __grid_co
     }
 }
 
+// ---- channels first, through shared memory ------------------------------------------------------------
+// A block takes the same few consecutive pixels of all channels of an image at a time: a tile of C short rows, of
+// which several are on their way while one is worked on.  LP lanes lie along the pixels, 32 / LP along the
+// channels, so that the sums over channels (per pixel) are sums in registers and a few exchanges per tile,
+// and the sums over pixels (per channel) stay in a thread's registers for the whole kernel.  The tile is read
+// from shared memory once per pass over it (two backward, three forward).
+//   WHOLE: every row of a plane starts on a 16-byte boundary; tiles come as boxes of the copy engine, a lane has a
+//          16-byte vector of pixels.
+//   else : planes of odd size.  Each row is copied in 16-byte pieces from the boundary before it (its offset differs from
+//          channel to channel); 32 lanes read and write single pixels, PX of them each.
+constexpr int kPlaneThreads = 512, kPlaneWarps = kPlaneThreads / 32;
+constexpr int kPX = 4;
+struct PlaneArgs {
+    CUtensorMap tm_x, tm_gy;   // WHOLE
+    int boxes, box_rows;       // boxes of a tile (channels), rows of each
+    int px, tiles_per_img;
+    int pitch;                 // bytes of a channel's row in shared memory
+    int stage_bytes;           // of one tensor's tile
+    int stages;
+    long long tiles;
+    FastDiv div_tiles;
+    int log_pieces;            // else: 16-byte pieces of a row, rounded up to a power of two
+    uint32_t* err_word;
+};
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+
+template <typename T, int LP, int KC, bool WHOLE, bool BWD>
+__global__ void __launch_bounds__(kPlaneThreads) ln_planes_tile_kernel(const __grid_constant__ NormArgs a, const __grid_constant__ PlaneArgs t) {
+    constexpr int NT = BWD ? 2 : 1, E = (int)sizeof(T);
+    constexpr int V = WHOLE ? 16 / E : kPX;                 // pixels of a thread
+    constexpr int PT = LP * V;                              // pixels of a tile
+    constexpr int CL = 32 / LP;                             // channels of a warp at once
+    extern __shared__ __align__(128) unsigned char dyn[];
+    __shared__ uint64_t full[8];
+    __shared__ float red[2][kPlaneWarps][PT];
+    __shared__ float stat[2][PT];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int cl = lane / LP, pl = lane % LP;
+    auto pixel = [&](int i) { return WHOLE ? pl * V + i : pl + 32 * i; };
+    auto place = [&](long long tile, uint32_t& n, int& p0) {
+        uint32_t k;
+        t.div_tiles.divmod((uint32_t)tile, n, k);
+        p0 = (int)k * t.px;
+    };
+    auto load = [&](long long tile, int s) {
+        unsigned char* dst = dyn + (size_t)s * NT * t.stage_bytes;
+        if constexpr (WHOLE) {
+            if (tid != 0 || tile >= t.tiles) return;
+            uint32_t n;
+            int p0;
+            place(tile, n, p0);
+            mbar_expect_tx(&full[s], (uint32_t)(t.boxes * t.box_rows * t.pitch * NT));
+            for (int k = 0; k < t.boxes; ++k) {
+                tma_load_3d(dst + k * t.box_rows * t.pitch, &t.tm_x, p0, k * t.box_rows, (int)n, &full[s]);
+                if constexpr (BWD) tma_load_3d(dst + t.stage_bytes + k * t.box_rows * t.pitch, &t.tm_gy, p0, k * t.box_rows, (int)n, &full[s]);
+            }
+        } else {
+            if (tile < t.tiles) {
+                uint32_t n;
+                int p0;
+                place(tile, n, p0);
+                const int np = min(t.px, a.HW - p0);
+                const int piece = tid & ((1 << t.log_pieces) - 1), c0 = tid >> t.log_pieces, dc = kPlaneThreads >> t.log_pieces;
+                const long long plane = (long long)a.HW * E, total = a.R * a.C * E, skip = plane * dc;
+                long long row = (long long)n * a.C * plane + (long long)p0 * E + c0 * plane;
+                uint32_t to = smem_u32(dst) + c0 * t.pitch + piece * 16;
+                for (int c = c0; c < a.C; c += dc, row += skip, to += dc * t.pitch) {
+                    const long long at = (row & ~15LL) + piece * 16;
+                    if (at < row + np * E) {
+                        const int bytes = total - at < 16 ? (int)(total - at) : 16;
+                        cp_async16(to, static_cast<const unsigned char*>(a.x) + at, bytes);
+                        if constexpr (BWD) cp_async16(to + t.stage_bytes, static_cast<const unsigned char*>(a.gy) + at, bytes);
+                    }
+                }
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        }
+    };
+    if constexpr (WHOLE) {
+        if (tid == 0) {
+            for (int s = 0; s < t.stages; ++s) mbar_init(&full[s], 1);
+            mbar_fence_init();
+        }
+        __syncthreads();
+    }
+    for (int s = 0; s < t.stages - (WHOLE ? 0 : 1); ++s) load(blockIdx.x + (long long)s * gridDim.x, s);
+
+    float gam[KC], bet[BWD ? 1 : KC], ag[BWD ? KC : 1], ab[BWD ? KC : 1];
+#pragma unroll
+    for (int k = 0; k < KC; ++k) {
+        const int c = (k * kPlaneWarps + warp) * CL + cl;
+        gam[k] = c < a.C ? a.gamma.at(c, 1.f) : 0.f;
+        if constexpr (!BWD) bet[k] = c < a.C ? a.beta.at(c, 0.f) : 0.f;
+        else ag[k] = ab[k] = 0.f;
+    }
+    // sums over the channels of N values per pixel: lanes of the warp, then the warps through `red`; they end in stat[n][pixel]
+    auto over_channels = [&](float (&v)[NT][V], int n_values) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            if (n >= n_values) break;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+#pragma unroll
+                for (int o = LP; o < 32; o <<= 1) v[n][i] += __shfl_xor_sync(0xffffffffu, v[n][i], o);
+                if (cl == 0) red[n][warp][pixel(i)] = v[n][i];
+            }
+        }
+        __syncthreads();
+        for (int k = tid; k < n_values * PT; k += kPlaneThreads) {
+            const int n = k / PT, p = k - n * PT;
+            float s = 0.f;
+#pragma unroll
+            for (int w = 0; w < kPlaneWarps; ++w) s += red[n][w][p];
+            stat[n][p] = s;
+        }
+        __syncthreads();
+    };
+    bool ok = true;
+    int s = 0;
+    uint32_t parity = 0;
+    for (long long tile = blockIdx.x; tile < t.tiles; tile += gridDim.x) {
+        uint32_t n;
+        int p0;
+        place(tile, n, p0);
+        const int np = min(t.px, a.HW - p0);
+        const long long q0 = (long long)n * a.HW + p0;
+        float mean[V], rstd[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            mean[i] = rstd[i] = 0.f;
+            if constexpr (BWD) {
+                if (pixel(i) < np) { mean[i] = a.mean_in[q0 + pixel(i)]; rstd[i] = a.rstd_in[q0 + pixel(i)]; }
+            }
+        }
+        if constexpr (WHOLE) {
+            ok = mbar_wait_bounded(&full[s], parity);
+            if (__syncthreads_or(!ok)) { ok = false; break; }
+        } else {
+            if (t.stages == 3) asm volatile("cp.async.wait_group 1;" ::: "memory");
+            else asm volatile("cp.async.wait_group 0;" ::: "memory");
+            __syncthreads();                                // this tile is here; the one before it has been read
+            load(tile + (long long)(t.stages - 1) * gridDim.x, s == 0 ? t.stages - 1 : s - 1);
+        }
+        const unsigned char* sx = dyn + (size_t)s * NT * t.stage_bytes;
+        const long long base = ((long long)n * a.C * a.HW + p0);      // of channel 0, in elements
+        const uint32_t b16 = (uint32_t)(base * E) & 15u, hw16 = (uint32_t)((long long)a.HW * E) & 15u;
+        auto fetch = [&](const unsigned char* from, int c, float (&f)[V]) {
+            if constexpr (WHOLE) load_vec<T, V>(reinterpret_cast<const T*>(from + c * (PT * E)) + pl * V, f);
+            else {
+                const T* row = reinterpret_cast<const T*>(from + c * t.pitch + ((b16 + (uint32_t)c * hw16) & 15u));
+#pragma unroll
+                for (int i = 0; i < V; ++i) f[i] = pixel(i) < np ? to_f32(row[pixel(i)]) : 0.f;
+            }
+        };
+        auto put = [&](int c, const float (&f)[V]) {
+            T* dst = static_cast<T*>(a.out) + base + (long long)c * a.HW;
+            if constexpr (WHOLE) {
+                if (pl * V < np) store_vec<T, V>(dst + pl * V, f);
+            } else {
+#pragma unroll
+                for (int i = 0; i < V; ++i) if (pixel(i) < np) dst[pixel(i)] = from_f32<T>(f[i]);
+            }
+        };
+        float sum[NT][V];
+#pragma unroll
+        for (int q = 0; q < NT; ++q)
+#pragma unroll
+            for (int i = 0; i < V; ++i) sum[q][i] = 0.f;
+        if constexpr (BWD) {
+#pragma unroll
+            for (int k = 0; k < KC; ++k) {
+                const int c = (k * kPlaneWarps + warp) * CL + cl;
+                if (c < a.C) {
+                    float x[V], g[V];
+                    fetch(sx, c, x);
+                    fetch(sx + t.stage_bytes, c, g);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        const float xh = (x[i] - mean[i]) * rstd[i];
+                        ag[k] += g[i] * xh;
+                        ab[k] += g[i];
+                        const float h = g[i] * gam[k];
+                        sum[0][i] += h;
+                        sum[1][i] += h * xh;
+                    }
+                }
+            }
+            if (a.out) {
+                over_channels(sum, 2);
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    sum[0][i] = stat[0][pixel(i)] * a.inv_c * rstd[i];
+                    sum[1][i] = stat[1][pixel(i)] * a.inv_c * rstd[i] * rstd[i];
+                }
+#pragma unroll
+                for (int k = 0; k < KC; ++k) {
+                    const int c = (k * kPlaneWarps + warp) * CL + cl;
+                    if (c < a.C) {
+                        float x[V], g[V];
+                        fetch(sx, c, x);
+                        fetch(sx + t.stage_bytes, c, g);
+#pragma unroll
+                        for (int i = 0; i < V; ++i) x[i] = (g[i] * gam[k] * rstd[i] - sum[0][i]) - (x[i] - mean[i]) * sum[1][i];
+                        put(c, x);
+                    }
+                }
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < KC; ++k) {
+                const int c = (k * kPlaneWarps + warp) * CL + cl;
+                if (c < a.C) {
+                    float x[V];
+                    fetch(sx, c, x);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) sum[0][i] += x[i];
+                }
+            }
+            over_channels(sum, 1);
+#pragma unroll
+            for (int i = 0; i < V; ++i) { mean[i] = stat[0][pixel(i)] / (float)a.C; sum[0][i] = 0.f; }
+#pragma unroll
+            for (int k = 0; k < KC; ++k) {
+                const int c = (k * kPlaneWarps + warp) * CL + cl;
+                if (c < a.C) {
+                    float x[V];
+                    fetch(sx, c, x);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) { const float d = x[i] - mean[i]; sum[0][i] += d * d; }
+                }
+            }
+            over_channels(sum, 1);
+#pragma unroll
+            for (int i = 0; i < V; ++i) rstd[i] = rsqrtf(stat[0][pixel(i)] * a.inv_c + a.eps);
+            if (a.mean && warp == 0 && cl == 0) {
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    if (pixel(i) < np) { a.mean[q0 + pixel(i)] = mean[i]; a.rstd[q0 + pixel(i)] = rstd[i]; }
+            }
+#pragma unroll
+            for (int k = 0; k < KC; ++k) {
+                const int c = (k * kPlaneWarps + warp) * CL + cl;
+                if (c < a.C) {
+                    float x[V];
+                    fetch(sx, c, x);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) x[i] = (x[i] - mean[i]) * rstd[i] * gam[k] + bet[k];
+                    put(c, x);
+                }
+            }
+        }
+        if constexpr (WHOLE) {
+            __syncthreads();                                // the tile has been read
+            load(tile + (long long)t.stages * gridDim.x, s);
+        }
+        if (++s == t.stages) { s = 0; parity ^= 1u; }
+    }
+    if (!ok) {
+        atomicOr(t.err_word, 8192u);
+        const long long t0 = clock64();                     // copies may still be on their way to this block's shared memory
+        while (clock64() - t0 < 2000000LL) {}
+    }
+    if constexpr (BWD) {
+        if (!a.part) return;
+        float* part = a.part + (size_t)blockIdx.x * 2 * a.C;
+#pragma unroll
+        for (int k = 0; k < KC; ++k) {
+#pragma unroll
+            for (int o = LP >> 1; o > 0; o >>= 1) {
+                ag[k] += __shfl_xor_sync(0xffffffffu, ag[k], o);
+                ab[k] += __shfl_xor_sync(0xffffffffu, ab[k], o);
+            }
+            const int c = (k * kPlaneWarps + warp) * CL + cl;
+            if (pl == 0 && c < a.C) { part[c] = ag[k]; part[a.C + c] = ab[k]; }
+        }
+    }
+}
+
 // ---- sums of the blocks' lines -------------------------------------------------------------------
 // part [blocks][2 C] -> g_gamma, g_beta: the blocks in a fixed order.
 constexpr int kFinX = 32, kFinY = 16;
@@ -600,14 +1133,21 @@ gf_status norm_validate(const gf_norm_desc* d) {
 
 bool misaligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 
+// Which kernel a call takes.
+enum NormKind { ROWS_DIRECT, ROWS_LONG, ROWS_RING, PLANES_DIRECT, PLANES_LONG, PLANES_TILE };
 struct NormPlan {
-    bool planes;          // channels first with more than one pixel per plane
+    NormKind kind;
     int V;                // elements per load
-    int log_tpr, NV;      // rows: threads per row; loads per thread (0: long rows)
-    int CG, NCH;          // planes: warps, channels per warp (0: read again)
+    int log_tpr, E;       // rows: threads per row; elements per thread
+    int CG, NCH;          // planes, direct: warps, channels per warp
     int threads;
     long long work;       // blocks of work (row groups, or pixel tiles)
-    int grid;             // backward: persistent blocks
+    int grid;             // persistent blocks
+    size_t smem;
+    RingArgs ring;
+    PlaneArgs tile;
+    int KC, LP;
+    bool whole;
 };
 
 // Widest load that keeps every row (plane) on its boundary.
@@ -617,99 +1157,259 @@ int vec_for(long long n, int esize) {
     return v;
 }
 
+constexpr size_t kNormSmem = 220 * 1024;
+
+void plan_rows(const gf_norm_desc& d, bool backward, long long R, NormPlan& p) {
+    const int e = d.dtype == GF_F32 ? 4 : 2;
+    p.V = vec_for(d.C, e);
+    const int most = backward ? 16 : 32;                 // elements a thread holds
+    const int max_log = 9;
+    const long long vecs = (d.C + p.V - 1) / p.V;
+    // A thread holds up to `most` elements, so that the work per row (exchanges, statistics) is shared by many of them;
+    // two lanes at least share a row of more than 8.
+    auto fits = [&](int lt, int el) { return vecs <= (long long)(el / p.V) << lt; };
+    p.E = 8;
+    p.log_tpr = 0;
+    if (!fits(1, 8)) p.E = 16;
+    if (!fits(2, 16)) p.E = most;
+    while (p.log_tpr < max_log && !fits(p.log_tpr, p.E)) ++p.log_tpr;
+    if (!fits(p.log_tpr, p.E)) {
+        p.kind = ROWS_LONG;
+        p.threads = 1024;
+        p.work = R;
+        p.grid = (int)(R < sm_count() ? R : sm_count());
+        return;
+    }
+    p.threads = p.log_tpr > 8 ? 1 << p.log_tpr : kRowThreads;
+    const int rows_pb = p.threads >> p.log_tpr;
+    p.work = (R + rows_pb - 1) / rows_pb;
+    // The ring: per team of warps, batches of whole rows; two blocks per SM while their rings fit.
+    const int nt = backward ? 2 : 1;
+    const int warps = p.log_tpr > 5 ? 1 << (p.log_tpr - 5) : 1, teams = p.threads / 32 / warps;
+    const int at_once = p.log_tpr > 5 ? 1 : 32 >> p.log_tpr;
+    const long long row_bytes = (long long)d.C * e;
+    const long long blocks = 2LL * sm_count();
+    RingArgs& r = p.ring;
+    r.warps = warps;
+    const size_t budget = kNormSmem / 2 / teams;
+    long long rows = 4096 / row_bytes;
+    const long long fair = R / (blocks * teams * 2);     // at least two batches for every team
+    if (rows > fair) rows = fair;
+    if (rows > 32) rows = 32;
+    rows = rows / at_once * at_once;
+    if (rows < at_once) rows = at_once;
+    r.rows = (int)rows;
+    r.stage_bytes = (int)((rows * row_bytes + 32 + 127) / 128 * 128);
+    int per_sm = 2;
+    long long st = (long long)(budget / ((size_t)nt * r.stage_bytes));
+    if (st < 2) { per_sm = 1; st = (long long)(kNormSmem / teams / ((size_t)nt * r.stage_bytes)); }
+    r.stages = (int)(st > 4 ? 4 : st);
+    r.batches = (R + rows - 1) / rows;
+    const long long grid = (r.batches + teams - 1) / teams;
+    // Fewer rows than two rounds of teams: every row is on its way at once in the direct kernel, and nothing is left to
+    // prefetch
+    if (r.stages < 2 || r.batches < 2 * (long long)sm_count() * teams) {
+        p.kind = ROWS_DIRECT;
+        if (p.log_tpr > 5) { p.threads = 1 << p.log_tpr; p.work = R; }      // one row per block
+        const int resident = p.threads > 512 ? 1 : 1024 / p.threads;
+        p.grid = (int)(p.work < (long long)sm_count() * resident ? p.work : (long long)sm_count() * resident);
+        p.smem = backward && p.log_tpr <= 5 ? (size_t)2 * d.C * 4 : 0;
+        return;
+    }
+    p.kind = ROWS_RING;
+    p.grid = (int)(grid < (long long)per_sm * sm_count() ? grid : (long long)per_sm * sm_count());
+    p.smem = (size_t)teams * r.stages * nt * r.stage_bytes;
+    if (backward && p.smem < (size_t)8 * d.C) p.smem = (size_t)8 * d.C;
+}
+
+void plan_planes(const gf_norm_desc& d, bool backward, long long R, NormPlan& p) {
+    const int e = d.dtype == GF_F32 ? 4 : 2, nt = backward ? 2 : 1;
+    const long long HW = (long long)d.H * d.W;
+    const bool whole = HW * e % 16 == 0;                 // every row of a plane starts on a 16-byte boundary
+    auto tiles = [&](int px) {
+        PlaneArgs& t = p.tile;
+        t.px = px;
+        t.tiles_per_img = (int)((HW + px - 1) / px);
+        t.tiles = (long long)d.N * t.tiles_per_img;
+        t.div_tiles = FastDiv((uint32_t)t.tiles_per_img);
+        p.threads = kPlaneThreads;
+        p.kind = PLANES_TILE;
+        p.whole = whole;
+    };
+    if (whole) {
+        // Rows of 128 bytes, of 64 or of 32, as long as three tiles are in flight (two of the shortest).
+        for (int lp = 8; lp >= 2; lp >>= 1) {
+            PlaneArgs& t = p.tile;
+            t.boxes = (d.C + 255) / 256;
+            t.box_rows = ((d.C + t.boxes - 1) / t.boxes + 3) / 4 * 4;       // boxes land on 128-byte boundaries
+            t.pitch = lp * 16;
+            const long long stage = ((long long)t.boxes * t.box_rows * t.pitch + 127) / 128 * 128;
+            const long long fit = (long long)(kNormSmem - 40 * 1024) / (nt * stage);
+            const int kc = (d.C + kPlaneWarps * (32 / lp) - 1) / (kPlaneWarps * (32 / lp));
+            if (fit < (lp > 2 ? 3 : 2) || kc > 8) continue;
+            const int px = lp * 16 / e;
+            if (lp > 2 && HW <= px / 2) continue;        // shorter rows would do
+            if ((long long)d.N * ((HW + px - 1) / px) > 0x7fffffffLL) continue;
+            tiles(px);
+            p.LP = lp;
+            p.KC = kc <= 1 ? 1 : kc <= 2 ? 2 : kc <= 4 ? 4 : 8;
+            t.stage_bytes = (int)stage;
+            // two blocks per SM where both can have three tiles in flight
+            const int per_sm = fit >= 6 ? 2 : 1;
+            t.stages = (int)(fit / per_sm > 6 ? 6 : fit / per_sm);
+            p.smem = (size_t)t.stages * nt * stage;
+            p.grid = (int)(t.tiles < (long long)per_sm * sm_count() ? t.tiles : (long long)per_sm * sm_count());
+            return;
+        }
+    } else if (HW * e >= 64) {
+        PlaneArgs& t = p.tile;
+        const int kc = (d.C + kPlaneWarps - 1) / kPlaneWarps;
+        const int pieces = 32 * kPX * e / 16 + 1;
+        t.log_pieces = 0;
+        while ((1 << t.log_pieces) < pieces) ++t.log_pieces;
+        t.pitch = pieces * 16;
+        const long long stage = ((long long)d.C * t.pitch + 127) / 128 * 128;
+        const long long fit = (long long)(kNormSmem - 40 * 1024) / (nt * stage);
+        if (fit >= 2 && kc <= 32) {
+            tiles(32 * kPX);
+            p.LP = 32;
+            p.KC = kc <= 4 ? 4 : kc <= 8 ? 8 : kc <= 16 ? 16 : 32;
+            t.stage_bytes = (int)stage;
+            const int per_sm = fit >= 4 ? 2 : 1;
+            t.stages = fit / per_sm >= 3 ? 3 : 2;
+            p.smem = (size_t)t.stages * nt * stage;
+            p.grid = (int)(t.tiles < (long long)per_sm * sm_count() ? t.tiles : (long long)per_sm * sm_count());
+            return;
+        }
+    }
+    // Small planes (pixels are numbered through all images), and more channels than shared memory holds.
+    p.V = vec_for(HW, e);
+    if (p.V > 4) p.V = 4;
+    p.CG = 4;
+    while (p.CG < 16 && (long long)p.CG * 8 < d.C) p.CG *= 2;
+    const int most = 32;                                 // values per thread (of each tensor)
+    while (p.V > 1 && (long long)p.CG * (most / p.V) < d.C) p.V >>= 1;
+    p.NCH = 8;
+    while (p.NCH * p.V < most && (long long)p.CG * p.NCH < d.C) p.NCH *= 2;
+    p.kind = PLANES_DIRECT;
+    if ((long long)p.CG * p.NCH < d.C) { p.kind = PLANES_LONG; p.V = vec_for(HW, e) >= 2 ? 2 : 1; }
+    p.threads = 32 * p.CG;
+    p.work = (R + 32LL * p.V - 1) / (32LL * p.V);
+    const int per_sm = 1024 / p.threads;
+    p.grid = (int)(p.work < (long long)sm_count() * per_sm ? p.work : (long long)sm_count() * per_sm);
+    p.smem = (size_t)(backward ? 4 : 2) * p.CG * 32 * p.V * 4;
+}
+
 NormPlan norm_plan(const gf_norm_desc& d, bool backward) {
     NormPlan p = {};
-    const int e = d.dtype == GF_F32 ? 4 : 2;
     const long long R = (long long)d.N * d.H * d.W;
-    p.planes = d.layout == GF_NCHW && (long long)d.H * d.W > 1;
-    if (!p.planes) {
-        p.V = vec_for(d.C, e);
-        const int most = backward ? 16 : 32;             // elements a thread holds
-        const int max_log = backward ? 9 : 10;
-        const long long vecs = (d.C + p.V - 1) / p.V;
-        // few elements per thread while a warp is enough for the row, then more threads, then more elements
-        int per = 8;
-        auto fits = [&](int lt, int el) { return vecs <= (long long)(el / p.V) << lt; };
-        p.log_tpr = 0;
-        while (p.log_tpr < 5 && !fits(p.log_tpr, per)) ++p.log_tpr;
-        if (!fits(p.log_tpr, per)) {
-            per = most;
-            while (p.log_tpr < max_log && !fits(p.log_tpr, per)) ++p.log_tpr;
-        }
-        p.NV = fits(p.log_tpr, per) ? per / p.V : 0;
-        if (p.NV == 0) p.log_tpr = 10;
-        p.threads = p.log_tpr > 5 ? 1 << p.log_tpr : kRowThreads;
-        const int rows_pb = p.threads >> p.log_tpr;
-        p.work = (R + rows_pb - 1) / rows_pb;
-        const int per_sm = p.threads > 512 ? 1 : 1024 / p.threads;
-        p.grid = (int)(p.work < (long long)sm_count() * per_sm ? p.work : (long long)sm_count() * per_sm);
-    } else {
-        p.V = vec_for((long long)d.H * d.W, e);
-        if (p.V > 4) p.V = 4;
-        const int max_cg = 16;
-        p.CG = 4;
-        while (p.CG < max_cg && (long long)p.CG * 8 < d.C) p.CG *= 2;
-        const int most = 32;                             // values per thread (of each tensor)
-        while (p.V > 1 && (long long)p.CG * (most / p.V) < d.C) p.V >>= 1;
-        p.NCH = 8;
-        while (p.NCH * p.V < most && (long long)p.CG * p.NCH < d.C) p.NCH *= 2;
-        if ((long long)p.CG * p.NCH < d.C) { p.NCH = 0; p.V = vec_for((long long)d.H * d.W, e) >= 2 ? 2 : 1; }
-        p.threads = 32 * p.CG;
-        p.work = (R + 32LL * p.V - 1) / (32LL * p.V);
-        const int per_sm = 1024 / p.threads;
-        p.grid = (int)(p.work < (long long)sm_count() * per_sm ? p.work : (long long)sm_count() * per_sm);
-    }
+    if (d.layout == GF_NCHW && (long long)d.H * d.W > 1) plan_planes(d, backward, R, p);
+    else plan_rows(d, backward, R, p);
     return p;
 }
 
-template <typename T, int V, int NV> gf_status launch_rows(const NormArgs& a, const NormPlan& p, bool backward, cudaStream_t s) {
-    if (!backward) {
-        if (p.log_tpr > 5) ln_rows_fwd_kernel<T, V, NV, true><<<(unsigned)p.work, p.threads, 0, s>>>(a);
-        else ln_rows_fwd_kernel<T, V, NV, false><<<(unsigned)p.work, p.threads, 0, s>>>(a);
-    } else {
-        if constexpr (V * NV <= 16) {
-            if (p.log_tpr > 5) ln_rows_bwd_kernel<T, V, NV, true><<<p.grid, p.threads, 0, s>>>(a);
-            else ln_rows_bwd_kernel<T, V, NV, false><<<p.grid, p.threads, (size_t)2 * a.C * 4, s>>>(a);
-        } else return GF_ERR_UNSUPPORTED;
+template <typename T, int V, int E, bool TEAM, bool BWD> gf_status launch_ring(const NormArgs& a, const NormPlan& p, cudaStream_t s) {
+    static size_t configured[kMaxDevices] = {};
+    if (gf_status st = ensure_dyn_smem(ln_rows_ring_kernel<T, V, E, TEAM, BWD>, p.smem, configured); st != GF_OK) return st;
+    RingArgs r = p.ring;
+    r.err_word = global_err_word();
+    if (!r.err_word) return GF_ERR_CUDA;
+    ln_rows_ring_kernel<T, V, E, TEAM, BWD><<<p.grid, p.threads, p.smem, s>>>(a, r);
+    return after_launch();
+}
+template <typename T, int V, int E> gf_status launch_rows(const NormArgs& a, const NormPlan& p, bool backward, cudaStream_t s) {
+    constexpr int NV = E / V;
+    const bool team = p.log_tpr > 5;
+    if (p.kind == ROWS_RING) {
+        if (!backward) return team ? launch_ring<T, V, E, true, false>(a, p, s) : launch_ring<T, V, E, false, false>(a, p, s);
+        if constexpr (E <= 16) return team ? launch_ring<T, V, E, true, true>(a, p, s) : launch_ring<T, V, E, false, true>(a, p, s);
+        return GF_ERR_UNSUPPORTED;
     }
+    if (!backward) {
+        if (team) ln_rows_fwd_kernel<T, V, NV, true><<<(unsigned)p.work, p.threads, 0, s>>>(a);
+        else ln_rows_fwd_kernel<T, V, NV, false><<<(unsigned)p.work, p.threads, 0, s>>>(a);
+    } else if constexpr (E <= 16) {
+        if (team) ln_rows_bwd_kernel<T, V, NV, true><<<p.grid, p.threads, 0, s>>>(a);
+        else ln_rows_bwd_kernel<T, V, NV, false><<<p.grid, p.threads, p.smem, s>>>(a);
+    } else return GF_ERR_UNSUPPORTED;
     return after_launch();
 }
 template <typename T, int V> gf_status launch_rows_v(const NormArgs& a, const NormPlan& p, bool backward, cudaStream_t s) {
-    switch (p.NV * V) {
-        case 8: return launch_rows<T, V, 8 / V>(a, p, backward, s);
-        case 16: return launch_rows<T, V, 16 / V>(a, p, backward, s);
-        default: return launch_rows<T, V, 32 / V>(a, p, backward, s);
+    switch (p.E) {
+        case 8: return launch_rows<T, V, 8>(a, p, backward, s);
+        case 16: return launch_rows<T, V, 16>(a, p, backward, s);
+        default: return launch_rows<T, V, 32>(a, p, backward, s);
     }
 }
 template <typename T, int V> gf_status launch_planes_v(const NormArgs& a, const NormPlan& p, bool backward, cudaStream_t s) {
-    const size_t smem = (size_t)(backward ? 4 : 2) * p.CG * 32 * V * 4;
     if (!backward) {
         const unsigned grid = (unsigned)p.work;
-        switch (p.NCH) {
-            case 8: ln_planes_fwd_kernel<T, V, 8><<<grid, p.threads, smem, s>>>(a); break;
-            case 16: if constexpr (V <= 2) { ln_planes_fwd_kernel<T, V, 16><<<grid, p.threads, smem, s>>>(a); break; }
-            case 32: if constexpr (V == 1) { ln_planes_fwd_kernel<T, V, 32><<<grid, p.threads, smem, s>>>(a); break; }
-            default: ln_planes_fwd_kernel<T, V, 0><<<grid, p.threads, smem, s>>>(a);
+        switch (p.kind == PLANES_LONG ? 0 : p.NCH) {
+            case 8: ln_planes_fwd_kernel<T, V, 8><<<grid, p.threads, p.smem, s>>>(a); break;
+            case 16: if constexpr (V <= 2) { ln_planes_fwd_kernel<T, V, 16><<<grid, p.threads, p.smem, s>>>(a); break; }
+            case 32: if constexpr (V == 1) { ln_planes_fwd_kernel<T, V, 32><<<grid, p.threads, p.smem, s>>>(a); break; }
+            default: ln_planes_fwd_kernel<T, V, 0><<<grid, p.threads, p.smem, s>>>(a);
         }
     } else {
-        switch (p.NCH) {
-            case 8: ln_planes_bwd_kernel<T, V, 8><<<p.grid, p.threads, smem, s>>>(a, p.work); break;
-            case 16: if constexpr (V <= 2) { ln_planes_bwd_kernel<T, V, 16><<<p.grid, p.threads, smem, s>>>(a, p.work); break; }
-            case 32: if constexpr (V == 1) { ln_planes_bwd_kernel<T, V, 32><<<p.grid, p.threads, smem, s>>>(a, p.work); break; }
-            default: ln_planes_bwd_long_kernel<T, V><<<p.grid, p.threads, smem, s>>>(a, p.work);
+        switch (p.kind == PLANES_LONG ? 0 : p.NCH) {
+            case 8: ln_planes_bwd_kernel<T, V, 8><<<p.grid, p.threads, p.smem, s>>>(a, p.work); break;
+            case 16: if constexpr (V <= 2) { ln_planes_bwd_kernel<T, V, 16><<<p.grid, p.threads, p.smem, s>>>(a, p.work); break; }
+            case 32: if constexpr (V == 1) { ln_planes_bwd_kernel<T, V, 32><<<p.grid, p.threads, p.smem, s>>>(a, p.work); break; }
+            default: ln_planes_bwd_long_kernel<T, V><<<p.grid, p.threads, p.smem, s>>>(a, p.work);
         }
     }
     return after_launch();
 }
-template <typename T> gf_status launch_norm(const NormArgs& a, const NormPlan& p, bool backward, cudaStream_t s) {
-    if (p.planes) {
+template <typename T, int LP, int KC, bool WHOLE, bool BWD>
+gf_status launch_tile_inst(const NormArgs& a, const gf_norm_desc& d, const NormPlan& p, cudaStream_t s) {
+    static size_t configured[kMaxDevices] = {};
+    if (gf_status st = ensure_dyn_smem(ln_planes_tile_kernel<T, LP, KC, WHOLE, BWD>, p.smem, configured); st != GF_OK) return st;
+    PlaneArgs t = p.tile;
+    t.err_word = global_err_word();
+    if (!t.err_word) return GF_ERR_CUDA;
+    if constexpr (WHOLE) {
+        const uint64_t hw = (uint64_t)a.HW, c = (uint64_t)a.C;
+        if (!make_tmap_plain(&t.tm_x, a.x, sizeof(T), hw, c, (uint64_t)d.N, hw, hw * c, (uint32_t)t.px, (uint32_t)t.box_rows, 1) ||
+            (BWD && !make_tmap_plain(&t.tm_gy, a.gy, sizeof(T), hw, c, (uint64_t)d.N, hw, hw * c, (uint32_t)t.px, (uint32_t)t.box_rows, 1)))
+            return GF_ERR_CUDA;
+    }
+    ln_planes_tile_kernel<T, LP, KC, WHOLE, BWD><<<p.grid, p.threads, p.smem, s>>>(a, t);
+    return after_launch();
+}
+template <typename T, int LP, int KC, bool WHOLE>
+gf_status launch_tile_way(const NormArgs& a, const gf_norm_desc& d, const NormPlan& p, bool backward, cudaStream_t s) {
+    return backward ? launch_tile_inst<T, LP, KC, WHOLE, true>(a, d, p, s) : launch_tile_inst<T, LP, KC, WHOLE, false>(a, d, p, s);
+}
+template <typename T, int LP> gf_status launch_tile_whole(const NormArgs& a, const gf_norm_desc& d, const NormPlan& p, bool backward, cudaStream_t s) {
+    switch (p.KC) {
+        case 1: return launch_tile_way<T, LP, 1, true>(a, d, p, backward, s);
+        case 2: return launch_tile_way<T, LP, 2, true>(a, d, p, backward, s);
+        case 4: return launch_tile_way<T, LP, 4, true>(a, d, p, backward, s);
+        default: return launch_tile_way<T, LP, 8, true>(a, d, p, backward, s);
+    }
+}
+template <typename T> gf_status launch_tile(const NormArgs& a, const gf_norm_desc& d, const NormPlan& p, bool backward, cudaStream_t s) {
+    if (p.whole) {
+        if (p.LP == 8) return launch_tile_whole<T, 8>(a, d, p, backward, s);
+        return p.LP == 4 ? launch_tile_whole<T, 4>(a, d, p, backward, s) : launch_tile_whole<T, 2>(a, d, p, backward, s);
+    }
+    switch (p.KC) {
+        case 4: return launch_tile_way<T, 32, 4, false>(a, d, p, backward, s);
+        case 8: return launch_tile_way<T, 32, 8, false>(a, d, p, backward, s);
+        case 16: return launch_tile_way<T, 32, 16, false>(a, d, p, backward, s);
+        default: return launch_tile_way<T, 32, 32, false>(a, d, p, backward, s);
+    }
+}
+template <typename T> gf_status launch_norm(const NormArgs& a, const gf_norm_desc& d, const NormPlan& p, bool backward, cudaStream_t s) {
+    if (p.kind == PLANES_TILE) return launch_tile<T>(a, d, p, backward, s);
+    if (p.kind == PLANES_DIRECT || p.kind == PLANES_LONG) {
         switch (p.V) {
             case 4: return launch_planes_v<T, 4>(a, p, backward, s);
             case 2: return launch_planes_v<T, 2>(a, p, backward, s);
             default: return launch_planes_v<T, 1>(a, p, backward, s);
         }
     }
-    if (p.NV == 0) {
+    if (p.kind == ROWS_LONG) {
         if (!backward) ln_rows_fwd_long_kernel<T><<<(unsigned)a.R, 1024, 0, s>>>(a);
         else ln_rows_bwd_long_kernel<T><<<p.grid, 1024, 0, s>>>(a);
         return after_launch();
@@ -755,7 +1455,7 @@ gf_status gf_layer_norm_forward(const gf_norm_desc* desc, const void* x, const v
     a.gamma = {gamma, desc->param_dtype == GF_BF16};
     a.beta = {beta, desc->param_dtype == GF_BF16};
     ProfScope prof(K_NORM_FWD, s);
-    return desc->dtype == GF_F32 ? launch_norm<float>(a, p, false, s) : launch_norm<__nv_bfloat16>(a, p, false, s);
+    return desc->dtype == GF_F32 ? launch_norm<float>(a, *desc, p, false, s) : launch_norm<__nv_bfloat16>(a, *desc, p, false, s);
 }
 
 gf_status gf_layer_norm_backward_workspace_bytes(const gf_norm_desc* desc, size_t* bytes) {
@@ -788,7 +1488,7 @@ gf_status gf_layer_norm_backward(const gf_norm_desc* desc, const void* g_y, cons
         a.gamma = {gamma, desc->param_dtype == GF_BF16};
         a.part = sums ? static_cast<float*>(workspace) : nullptr;
         ProfScope prof(K_NORM_BWD, s);
-        st = desc->dtype == GF_F32 ? launch_norm<float>(a, p, true, s) : launch_norm<__nv_bfloat16>(a, p, true, s);
+        st = desc->dtype == GF_F32 ? launch_norm<float>(a, *desc, p, true, s) : launch_norm<__nv_bfloat16>(a, *desc, p, true, s);
         if (st != GF_OK) return st;
     }
     if (!sums) return GF_OK;

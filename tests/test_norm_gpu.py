@@ -104,6 +104,11 @@ ROWS = [(1, 2), (3, 3), (7, 8), (33, 31), (300, 64), (257, 100), (5, 255), (130,
         (17, 1025), (9, 2056), (700, 2048), (3, 4096), (5, 8190), (6, 8192), (3, 8200), (2, 16384), (3, 20001), (2, 33000), (1, 40000)]
 
 
+# many rows: batches of rows in flight per team of threads, rows that start anywhere in a 16-byte piece, a
+# tensor whose size is no multiple of 16 bytes, one team per block
+ROWS += [(20001, 19), (30000, 1), (9001, 96), (6001, 257), (5003, 1001), (2500, 4096), (1500, 8192), (1201, 7001), (700, 16384), (40000, 8)]
+
+
 @pytest.mark.parametrize("dtype", DTYPES, ids=["f32", "bf16"])
 @pytest.mark.parametrize("R,C", ROWS, ids=lambda v: str(v))
 def test_rows(gf, R, C, dtype):
@@ -115,7 +120,7 @@ def test_rows(gf, R, C, dtype):
 
 PLANES = [(1, 1, 1, 1), (2, 3, 1, 1), (2, 5, 1, 2), (3, 8, 7, 7), (2, 33, 5, 5), (1, 96, 9, 11), (4, 64, 14, 14), (2, 100, 16, 16),
           (3, 130, 6, 6), (2, 256, 7, 7), (1, 257, 4, 4), (2, 511, 3, 5), (2, 512, 8, 8), (1, 513, 6, 6), (1, 1024, 3, 3),
-          (2, 1500, 4, 4), (1, 12, 56, 57), (64, 96, 28, 28), (5, 16, 33, 31)]
+          (2, 1500, 4, 4), (1, 2100, 5, 5), (1, 2048, 4, 8), (3, 700, 13, 13), (40, 130, 31, 33), (300, 64, 16, 16), (1, 12, 56, 57), (64, 96, 28, 28), (5, 16, 33, 31)]
 
 
 @pytest.mark.parametrize("dtype", DTYPES, ids=["f32", "bf16"])
