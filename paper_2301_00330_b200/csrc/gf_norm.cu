@@ -156,7 +156,7 @@ template <typename T> __global__ void __launch_bounds__(1024) ln_rows_fwd_long_k
 template <typename T, int V, int NV, bool WHOLE_BLOCK>
 __global__ void __launch_bounds__(WHOLE_BLOCK ? 512 : kRowThreads) ln_rows_bwd_kernel(const __grid_constant__ NormArgs a) {
     __shared__ float red[4][32];
-    extern __shared__ float cols[];                       // !WHOLE_BLOCK: [2][C]
+    extern __shared__ float cols[];                       // !WHOLE_BLOCK: [warps][2][C], at most 32 KB
     const int tpr = 1 << a.log_tpr;
     const int g = threadIdx.x & (tpr - 1);
     const int rows_pb = blockDim.x >> a.log_tpr;
@@ -236,22 +236,22 @@ __global__ void __launch_bounds__(WHOLE_BLOCK ? 512 : kRowThreads) ln_rows_bwd_k
                     ag[k][i] += __shfl_xor_sync(0xffffffffu, ag[k][i], o);
                     ab[k][i] += __shfl_xor_sync(0xffffffffu, ab[k][i], o);
                 }
-        for (int w = 0; w < (int)(blockDim.x >> 5); ++w) {
-            if ((int)(threadIdx.x >> 5) == w && (int)(threadIdx.x & 31) < tpr) {
+        float* mine = cols + (size_t)(threadIdx.x >> 5) * 2 * a.C;
+        if ((int)(threadIdx.x & 31) < tpr) {
 #pragma unroll
-                for (int k = 0; k < NV; ++k)
+            for (int k = 0; k < NV; ++k)
 #pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        const int c = (k * tpr + g) * V + i;
-                        if (c < a.C) {
-                            cols[c] = w == 0 ? ag[k][i] : cols[c] + ag[k][i];
-                            cols[a.C + c] = w == 0 ? ab[k][i] : cols[a.C + c] + ab[k][i];
-                        }
-                    }
-            }
-            __syncthreads();
+                for (int i = 0; i < V; ++i) {
+                    const int c = (k * tpr + g) * V + i;
+                    if (c < a.C) { mine[c] = ag[k][i]; mine[a.C + c] = ab[k][i]; }
+                }
         }
-        for (int c = threadIdx.x; c < 2 * a.C; c += blockDim.x) part[c] = cols[c];
+        __syncthreads();
+        for (int c = threadIdx.x; c < 2 * a.C; c += blockDim.x) {
+            float p = cols[c];
+            for (int w = 1; w < (int)(blockDim.x >> 5); ++w) p += cols[(size_t)w * 2 * a.C + c];
+            part[c] = p;
+        }
     }
 }
 
@@ -321,10 +321,14 @@ template <bool TEAM, int N> __device__ __forceinline__ void team_sum(float (&s)[
         }
         team_sync<TEAM>(team, warps);
 #pragma unroll
-        for (int n = 0; n < N; ++n) s[n] = red[n * 16];
-        for (int k = 1; k < warps; ++k)
-#pragma unroll
-            for (int n = 0; n < N; ++n) s[n] += red[n * 16 + k];
+        for (int n = 0; n < N; ++n) {                       // places past the team's warps hold zeros
+            const float4 p = *reinterpret_cast<const float4*>(red + n * 16);
+            s[n] = (p.x + p.y) + (p.z + p.w);
+            for (int k = 4; k < warps; k += 4) {
+                const float4 q = *reinterpret_cast<const float4*>(red + n * 16 + k);
+                s[n] += (q.x + q.y) + (q.z + q.w);
+            }
+        }
     } else {
         for (int o = (1 << log_tpr) >> 1; o > 0; o >>= 1)
 #pragma unroll
@@ -333,11 +337,11 @@ template <bool TEAM, int N> __device__ __forceinline__ void team_sum(float (&s)[
 }
 
 template <typename T, int V, int E, bool TEAM, bool BWD>
-__global__ void __launch_bounds__(512) ln_rows_ring_kernel(const __grid_constant__ NormArgs a, const __grid_constant__ RingArgs r) {
+__global__ void __launch_bounds__(BWD ? 256 : 512) ln_rows_ring_kernel(const __grid_constant__ NormArgs a, const __grid_constant__ RingArgs r) {
     constexpr int NV = E / V, NT = BWD ? 2 : 1;
     extern __shared__ __align__(128) unsigned char dyn[];
     __shared__ uint64_t full[8 * 8];                       // [team][stage]
-    __shared__ float red[8][2][2 * 16];
+    __shared__ __align__(16) float red[8][2][2 * 16];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int team = warp / r.warps, teams = (int)(blockDim.x >> 5) / r.warps;
     const int tid = threadIdx.x - team * r.warps * 32;      // within the team
@@ -352,6 +356,8 @@ __global__ void __launch_bounds__(512) ln_rows_ring_kernel(const __grid_constant
         for (int k = 0; k < teams * r.stages; ++k) mbar_init(&full[k], 1);
         mbar_fence_init();
     }
+    if (TEAM)
+        for (int k = threadIdx.x; k < 8 * 2 * 2 * 16; k += blockDim.x) (&red[0][0][0])[k] = 0.f;
     __syncthreads();
     auto load = [&](long long b, int s) {                   // by one thread
         const long long lo = (b * r.rows * row_bytes) & ~15LL;
@@ -393,10 +399,8 @@ __global__ void __launch_bounds__(512) ln_rows_ring_kernel(const __grid_constant
     int s = 0, slot = 0;
     uint32_t parity = 0;
     for (long long b = first; b < r.batches; b += teams_all) {
-        ok = mbar_wait_bounded(&full[team * r.stages + s], parity);
-        if constexpr (TEAM) ok = !bar_any(team + 1, r.warps * 32, !ok);
-        else ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
+        // once a wait has run out nothing is waited for any more: the results are void, which the error word says
+        if (ok) ok = mbar_wait_bounded(&full[team * r.stages + s], parity);
         const long long r0 = b * r.rows, lo = (r0 * row_bytes) & ~15LL;
         const int nr = (int)(a.R - r0 < r.rows ? a.R - r0 : r.rows);
         unsigned char* sx = ring + (size_t)s * NT * r.stage_bytes;
@@ -506,7 +510,7 @@ __global__ void __launch_bounds__(512) ln_rows_ring_kernel(const __grid_constant
     }
     if constexpr (BWD) {
         if (!a.part) return;
-        float* cols = reinterpret_cast<float*>(dyn);        // [2][C], over the rings
+        float* cols = reinterpret_cast<float*>(dyn);        // [teams][2][C]
         float* part = a.part + (size_t)blockIdx.x * 2 * a.C;
         if constexpr (!TEAM) {
 #pragma unroll
@@ -519,21 +523,22 @@ __global__ void __launch_bounds__(512) ln_rows_ring_kernel(const __grid_constant
                     }
         }
         __syncthreads();
-        for (int w = 0; w < teams; ++w) {                   // the teams of the block in order
-            if (team == w && tid < tpr) {
+        // every team leaves its sums over the rings; then a thread per column adds them in the teams' order
+        if (tid < tpr) {
+            float* mine = cols + (size_t)team * 2 * a.C;
 #pragma unroll
-                for (int k = 0; k < NV; ++k)
+            for (int k = 0; k < NV; ++k)
 #pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        const int c = k * step + g * V + i;
-                        if (c < a.C) {
-                            const float p = w == 0 ? ag[k][i] : cols[c] + ag[k][i], q = w == 0 ? ab[k][i] : cols[a.C + c] + ab[k][i];
-                            if (w == teams - 1) { part[c] = p; part[a.C + c] = q; }
-                            else { cols[c] = p; cols[a.C + c] = q; }
-                        }
-                    }
-            }
-            __syncthreads();
+                for (int i = 0; i < V; ++i) {
+                    const int c = k * step + g * V + i;
+                    if (c < a.C) { mine[c] = ag[k][i]; mine[a.C + c] = ab[k][i]; }
+                }
+        }
+        __syncthreads();
+        for (int c = threadIdx.x; c < 2 * a.C; c += blockDim.x) {
+            float p = cols[c];
+            for (int w = 1; w < teams; ++w) p += cols[(size_t)w * 2 * a.C + c];
+            part[c] = p;
         }
     }
 }
@@ -827,8 +832,7 @@ __global__ void __launch_bounds__(512) ln_planes_bwd_long_kernel(const __grid_co
 //          16-byte vector of pixels.
 //   else : planes of odd size.  Each row is copied in 16-byte pieces from the boundary before it (its offset differs from
 //          channel to channel); 32 lanes read and write single pixels, PX of them each.
-constexpr int kPlaneThreads = 512, kPlaneWarps = kPlaneThreads / 32;
-constexpr int kPX = 4;
+constexpr int kPlaneThreads = 256, kPlaneWarps = kPlaneThreads / 32;
 struct PlaneArgs {
     CUtensorMap tm_x, tm_gy;   // WHOLE
     int boxes, box_rows;       // boxes of a tile (channels), rows of each
@@ -846,16 +850,17 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int by
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 
-template <typename T, int LP, int KC, bool WHOLE, bool BWD>
+template <typename T, int LP, int KC, int PX, bool BWD>        // PX = 0: WHOLE
 __global__ void __launch_bounds__(kPlaneThreads) ln_planes_tile_kernel(const __grid_constant__ NormArgs a, const __grid_constant__ PlaneArgs t) {
+    constexpr bool WHOLE = PX == 0;
     constexpr int NT = BWD ? 2 : 1, E = (int)sizeof(T);
-    constexpr int V = WHOLE ? 16 / E : kPX;                 // pixels of a thread
+    constexpr int V = WHOLE ? 16 / E : PX;                 // pixels of a thread
     constexpr int PT = LP * V;                              // pixels of a tile
     constexpr int CL = 32 / LP;                             // channels of a warp at once
     extern __shared__ __align__(128) unsigned char dyn[];
     __shared__ uint64_t full[8];
-    __shared__ float red[2][kPlaneWarps][PT];
-    __shared__ float stat[2][PT];
+    __shared__ float red[kPlaneWarps * NT * PT];
+    __shared__ float stat[NT * PT];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int cl = lane / LP, pl = lane % LP;
     auto pixel = [&](int i) { return WHOLE ? pl * V + i : pl + 32 * i; };
@@ -907,33 +912,54 @@ __global__ void __launch_bounds__(kPlaneThreads) ln_planes_tile_kernel(const __g
     }
     for (int s = 0; s < t.stages - (WHOLE ? 0 : 1); ++s) load(blockIdx.x + (long long)s * gridDim.x, s);
 
-    float gam[KC], bet[BWD ? 1 : KC], ag[BWD ? KC : 1], ab[BWD ? KC : 1];
+    constexpr bool kPar = KC <= 16;                         // gamma and beta in registers (else from L1)
+    constexpr bool kHold = KC * V * NT <= 64;               // the tile in registers between the passes (else from shared memory)
+    float gam[kPar ? KC : 1], bet[kPar && !BWD ? KC : 1], ag[BWD ? KC : 1], ab[BWD ? KC : 1];
 #pragma unroll
     for (int k = 0; k < KC; ++k) {
         const int c = (k * kPlaneWarps + warp) * CL + cl;
-        gam[k] = c < a.C ? a.gamma.at(c, 1.f) : 0.f;
-        if constexpr (!BWD) bet[k] = c < a.C ? a.beta.at(c, 0.f) : 0.f;
-        else ag[k] = ab[k] = 0.f;
+        if constexpr (kPar) gam[k] = c < a.C ? a.gamma.at(c, 1.f) : 0.f;
+        if constexpr (kPar && !BWD) bet[k] = c < a.C ? a.beta.at(c, 0.f) : 0.f;
+        if constexpr (BWD) ag[k] = ab[k] = 0.f;
     }
-    // sums over the channels of N values per pixel: lanes of the warp, then the warps through `red`; they end in stat[n][pixel]
-    auto over_channels = [&](float (&v)[NT][V], int n_values) {
+    auto gamma_of = [&](int k, int c) { if constexpr (kPar) return gam[k]; else return a.gamma.at(c, 1.f); };
+    auto beta_of = [&](int k, int c) { if constexpr (kPar && !BWD) return bet[k]; else return a.beta.at(c, 0.f); };
+    // Sums over the channels of N values per pixel.  Over the CL lanes of a warp that hold the same pixels an exchange halves the
+    // values a lane is responsible for, as long as there are two; then the warps through `red`; they end in stat[n * PT + pixel].
+    auto over_channels = [&](auto& v) {
+        constexpr int N = (int)(sizeof(v) / sizeof(float)) / V;
+        constexpr int M = N * V;
+        float w[M];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            if (n >= n_values) break;
+        for (int k = 0; k < M; ++k) w[k] = v[k / V][k % V];
+        int at = 0;                                         // first of the values that this lane is left with
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
+        for (int step = 0; (CL >> step) > 1; ++step) {
+            const int o = 16 >> step, m = M >> step;
+            if (m > 1) {
+                const bool up_half = (lane & o) != 0;
+                at += up_half ? m / 2 : 0;
 #pragma unroll
-                for (int o = LP; o < 32; o <<= 1) v[n][i] += __shfl_xor_sync(0xffffffffu, v[n][i], o);
-                if (cl == 0) red[n][warp][pixel(i)] = v[n][i];
-            }
+                for (int k = 0; k < M / 2; ++k)
+                    if (k < m / 2) {
+                        const float send = up_half ? w[k] : w[k + m / 2];
+                        w[k] = (up_half ? w[k + m / 2] : w[k]) + __shfl_xor_sync(0xffffffffu, send, o);
+                    }
+            } else w[0] += __shfl_xor_sync(0xffffffffu, w[0], o);
+        }
+        constexpr int left = M / CL > 0 ? M / CL : 1;
+        // (lanes that share a value write it together)
+#pragma unroll
+        for (int k = 0; k < left; ++k) {
+            const int q = at + k, n = q / V, i = q - n * V;
+            red[warp * (NT * PT) + n * PT + pixel(i)] = w[k];
         }
         __syncthreads();
-        for (int k = tid; k < n_values * PT; k += kPlaneThreads) {
-            const int n = k / PT, p = k - n * PT;
+        for (int k = tid; k < N * PT; k += kPlaneThreads) {
             float s = 0.f;
 #pragma unroll
-            for (int w = 0; w < kPlaneWarps; ++w) s += red[n][w][p];
-            stat[n][p] = s;
+            for (int u = 0; u < kPlaneWarps; ++u) s += red[u * (NT * PT) + k];
+            stat[k] = s;
         }
         __syncthreads();
     };
@@ -955,8 +981,8 @@ __global__ void __launch_bounds__(kPlaneThreads) ln_planes_tile_kernel(const __g
             }
         }
         if constexpr (WHOLE) {
-            ok = mbar_wait_bounded(&full[s], parity);
-            if (__syncthreads_or(!ok)) { ok = false; break; }
+            // once a wait has run out nothing is waited for any more: the results are void, which the error word says
+            if (ok) ok = mbar_wait_bounded(&full[s], parity);
         } else {
             if (t.stages == 3) asm volatile("cp.async.wait_group 1;" ::: "memory");
             else asm volatile("cp.async.wait_group 0;" ::: "memory");
@@ -969,91 +995,96 @@ __global__ void __launch_bounds__(kPlaneThreads) ln_planes_tile_kernel(const __g
         auto fetch = [&](const unsigned char* from, int c, float (&f)[V]) {
             if constexpr (WHOLE) load_vec<T, V>(reinterpret_cast<const T*>(from + c * (PT * E)) + pl * V, f);
             else {
-                const T* row = reinterpret_cast<const T*>(from + c * t.pitch + ((b16 + (uint32_t)c * hw16) & 15u));
+                const T* row = reinterpret_cast<const T*>(from + c * t.pitch + ((b16 + (uint32_t)c * hw16) & 15u)) + pl;
 #pragma unroll
-                for (int i = 0; i < V; ++i) f[i] = pixel(i) < np ? to_f32(row[pixel(i)]) : 0.f;
+                for (int i = 0; i < V; ++i) f[i] = !BWD || pl + 32 * i < np ? to_f32(row[32 * i]) : 0.f;      // forward, a pixel is alone
             }
         };
         auto put = [&](int c, const float (&f)[V]) {
-            T* dst = static_cast<T*>(a.out) + base + (long long)c * a.HW;
+            T* dst = static_cast<T*>(a.out) + base + (long long)c * a.HW + (WHOLE ? pl * V : pl);
             if constexpr (WHOLE) {
-                if (pl * V < np) store_vec<T, V>(dst + pl * V, f);
+                if (pl * V < np) store_vec<T, V>(dst, f);
             } else {
 #pragma unroll
-                for (int i = 0; i < V; ++i) if (pixel(i) < np) dst[pixel(i)] = from_f32<T>(f[i]);
+                for (int i = 0; i < V; ++i) if (pl + 32 * i < np) dst[32 * i] = from_f32<T>(f[i]);
             }
         };
-        float sum[NT][V];
-#pragma unroll
-        for (int q = 0; q < NT; ++q)
-#pragma unroll
-            for (int i = 0; i < V; ++i) sum[q][i] = 0.f;
+        float xs[kHold ? KC : 1][V], gs[kHold && BWD ? KC : 1][V];
         if constexpr (BWD) {
+            float sum[2][V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) sum[0][i] = sum[1][i] = 0.f;
 #pragma unroll
             for (int k = 0; k < KC; ++k) {
-                const int c = (k * kPlaneWarps + warp) * CL + cl;
+                const int c = (k * kPlaneWarps + warp) * CL + cl, at = kHold ? k : 0;
                 if (c < a.C) {
-                    float x[V], g[V];
-                    fetch(sx, c, x);
-                    fetch(sx + t.stage_bytes, c, g);
+                    fetch(sx, c, xs[at]);
+                    fetch(sx + t.stage_bytes, c, gs[at]);
+                    const float gm = gamma_of(k, c);
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
-                        const float xh = (x[i] - mean[i]) * rstd[i];
-                        ag[k] += g[i] * xh;
-                        ab[k] += g[i];
-                        const float h = g[i] * gam[k];
-                        sum[0][i] += h;
-                        sum[1][i] += h * xh;
+                        xs[at][i] = (xs[at][i] - mean[i]) * rstd[i];
+                        ag[k] += gs[at][i] * xs[at][i];
+                        ab[k] += gs[at][i];
+                        gs[at][i] *= gm;
+                        sum[0][i] += gs[at][i];
+                        sum[1][i] += gs[at][i] * xs[at][i];
                     }
                 }
             }
             if (a.out) {
-                over_channels(sum, 2);
+                over_channels(sum);
+                float m1[V], m2[V];
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    sum[0][i] = stat[0][pixel(i)] * a.inv_c * rstd[i];
-                    sum[1][i] = stat[1][pixel(i)] * a.inv_c * rstd[i] * rstd[i];
+                    m1[i] = stat[pixel(i)] * a.inv_c * rstd[i];
+                    m2[i] = stat[PT + pixel(i)] * a.inv_c * rstd[i];
                 }
 #pragma unroll
                 for (int k = 0; k < KC; ++k) {
-                    const int c = (k * kPlaneWarps + warp) * CL + cl;
+                    const int c = (k * kPlaneWarps + warp) * CL + cl, at = kHold ? k : 0;
                     if (c < a.C) {
-                        float x[V], g[V];
-                        fetch(sx, c, x);
-                        fetch(sx + t.stage_bytes, c, g);
+                        if constexpr (!kHold) {
+                            fetch(sx, c, xs[at]);
+                            fetch(sx + t.stage_bytes, c, gs[at]);
+                            const float gm = gamma_of(k, c);
 #pragma unroll
-                        for (int i = 0; i < V; ++i) x[i] = (g[i] * gam[k] * rstd[i] - sum[0][i]) - (x[i] - mean[i]) * sum[1][i];
-                        put(c, x);
+                            for (int i = 0; i < V; ++i) { xs[at][i] = (xs[at][i] - mean[i]) * rstd[i]; gs[at][i] *= gm; }
+                        }
+#pragma unroll
+                        for (int i = 0; i < V; ++i) xs[at][i] = (gs[at][i] * rstd[i] - m1[i]) - xs[at][i] * m2[i];
+                        put(c, xs[at]);
                     }
                 }
             }
         } else {
+            float sum[1][V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) sum[0][i] = 0.f;
 #pragma unroll
             for (int k = 0; k < KC; ++k) {
-                const int c = (k * kPlaneWarps + warp) * CL + cl;
+                const int c = (k * kPlaneWarps + warp) * CL + cl, at = kHold ? k : 0;
                 if (c < a.C) {
-                    float x[V];
-                    fetch(sx, c, x);
+                    fetch(sx, c, xs[at]);
 #pragma unroll
-                    for (int i = 0; i < V; ++i) sum[0][i] += x[i];
+                    for (int i = 0; i < V; ++i) sum[0][i] += xs[at][i];
                 }
             }
-            over_channels(sum, 1);
+            over_channels(sum);
 #pragma unroll
-            for (int i = 0; i < V; ++i) { mean[i] = stat[0][pixel(i)] / (float)a.C; sum[0][i] = 0.f; }
+            for (int i = 0; i < V; ++i) { mean[i] = stat[pixel(i)] / (float)a.C; sum[0][i] = 0.f; }
 #pragma unroll
             for (int k = 0; k < KC; ++k) {
-                const int c = (k * kPlaneWarps + warp) * CL + cl;
+                const int c = (k * kPlaneWarps + warp) * CL + cl, at = kHold ? k : 0;
                 if (c < a.C) {
-                    float x[V];
-                    fetch(sx, c, x);
+                    if constexpr (!kHold) fetch(sx, c, xs[at]);
 #pragma unroll
-                    for (int i = 0; i < V; ++i) { const float d = x[i] - mean[i]; sum[0][i] += d * d; }
+                    for (int i = 0; i < V; ++i) { xs[at][i] -= mean[i]; sum[0][i] += xs[at][i] * xs[at][i]; }
                 }
             }
-            over_channels(sum, 1);
+            over_channels(sum);
 #pragma unroll
-            for (int i = 0; i < V; ++i) rstd[i] = rsqrtf(stat[0][pixel(i)] * a.inv_c + a.eps);
+            for (int i = 0; i < V; ++i) rstd[i] = rsqrtf(stat[pixel(i)] * a.inv_c + a.eps);
             if (a.mean && warp == 0 && cl == 0) {
 #pragma unroll
                 for (int i = 0; i < V; ++i)
@@ -1061,13 +1092,17 @@ __global__ void __launch_bounds__(kPlaneThreads) ln_planes_tile_kernel(const __g
             }
 #pragma unroll
             for (int k = 0; k < KC; ++k) {
-                const int c = (k * kPlaneWarps + warp) * CL + cl;
+                const int c = (k * kPlaneWarps + warp) * CL + cl, at = kHold ? k : 0;
                 if (c < a.C) {
-                    float x[V];
-                    fetch(sx, c, x);
+                    if constexpr (!kHold) {
+                        fetch(sx, c, xs[at]);
 #pragma unroll
-                    for (int i = 0; i < V; ++i) x[i] = (x[i] - mean[i]) * rstd[i] * gam[k] + bet[k];
-                    put(c, x);
+                        for (int i = 0; i < V; ++i) xs[at][i] -= mean[i];
+                    }
+                    const float gm = gamma_of(k, c), bt = beta_of(k, c);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) xs[at][i] = xs[at][i] * rstd[i] * gm + bt;
+                    put(c, xs[at]);
                 }
             }
         }
@@ -1100,14 +1135,14 @@ __global__ void __launch_bounds__(kPlaneThreads) ln_planes_tile_kernel(const __g
 
 // ---- sums of the blocks' lines -------------------------------------------------------------------
 // part [blocks][2 C] -> g_gamma, g_beta: the blocks in a fixed order.
-constexpr int kFinX = 32, kFinY = 16;
+constexpr int kFinX = 32, kFinY = 32;
 __global__ void __launch_bounds__(kFinX * kFinY) ln_finish_kernel(const float* part, int blocks, int C, float* g_gamma, float* g_beta) {
     __shared__ float red[kFinY][kFinX + 1];
     pdl_wait();
     const long long col = (long long)blockIdx.x * kFinX + threadIdx.x;
     float s = 0.f;
     if (col < 2LL * C) {
-#pragma unroll 4
+#pragma unroll 10
         for (int b = threadIdx.y; b < blocks; b += kFinY) s += part[(size_t)b * 2 * C + col];
     }
     red[threadIdx.y][threadIdx.x] = s;
@@ -1146,8 +1181,7 @@ struct NormPlan {
     size_t smem;
     RingArgs ring;
     PlaneArgs tile;
-    int KC, LP;
-    bool whole;
+    int KC, LP, PX;       // planes, tiles (PX = 0: whole 16-byte pieces)
 };
 
 // Widest load that keeps every row (plane) on its boundary.
@@ -1162,16 +1196,15 @@ constexpr size_t kNormSmem = 220 * 1024;
 void plan_rows(const gf_norm_desc& d, bool backward, long long R, NormPlan& p) {
     const int e = d.dtype == GF_F32 ? 4 : 2;
     p.V = vec_for(d.C, e);
-    const int most = backward ? 16 : 32;                 // elements a thread holds
-    const int max_log = 9;
+    const int max_log = backward ? 8 : 9;
     const long long vecs = (d.C + p.V - 1) / p.V;
-    // A thread holds up to `most` elements, so that the work per row (exchanges, statistics) is shared by many of them;
+    // A thread holds up to 32 elements, so that the work per row (exchanges, statistics) is shared by many of them;
     // two lanes at least share a row of more than 8.
     auto fits = [&](int lt, int el) { return vecs <= (long long)(el / p.V) << lt; };
     p.E = 8;
     p.log_tpr = 0;
     if (!fits(1, 8)) p.E = 16;
-    if (!fits(2, 16)) p.E = most;
+    if (!fits(2, 16)) p.E = 32;
     while (p.log_tpr < max_log && !fits(p.log_tpr, p.E)) ++p.log_tpr;
     if (!fits(p.log_tpr, p.E)) {
         p.kind = ROWS_LONG;
@@ -1181,45 +1214,50 @@ void plan_rows(const gf_norm_desc& d, bool backward, long long R, NormPlan& p) {
         return;
     }
     p.threads = p.log_tpr > 8 ? 1 << p.log_tpr : kRowThreads;
-    const int rows_pb = p.threads >> p.log_tpr;
-    p.work = (R + rows_pb - 1) / rows_pb;
-    // The ring: per team of warps, batches of whole rows; two blocks per SM while their rings fit.
+    // The ring: per team of warps, batches of whole rows, three on their way.  Forward, two blocks per SM; backward a
+    // thread's sums take the registers of one.
     const int nt = backward ? 2 : 1;
     const int warps = p.log_tpr > 5 ? 1 << (p.log_tpr - 5) : 1, teams = p.threads / 32 / warps;
     const int at_once = p.log_tpr > 5 ? 1 : 32 >> p.log_tpr;
     const long long row_bytes = (long long)d.C * e;
-    const long long blocks = 2LL * sm_count();
     RingArgs& r = p.ring;
     r.warps = warps;
-    const size_t budget = kNormSmem / 2 / teams;
-    long long rows = 4096 / row_bytes;
-    const long long fair = R / (blocks * teams * 2);     // at least two batches for every team
+    int per_sm = backward ? 1 : 2;
+    if (kNormSmem / per_sm / teams / nt < (size_t)(2 * (row_bytes + 160))) per_sm = 1;
+    const long long all = (long long)per_sm * sm_count() * teams;
+    const long long budget = (long long)(kNormSmem / per_sm / teams / nt);       // of one tensor's batches
+    long long rows = (budget / 3 - 160) / row_bytes;
+    const long long fair = R / (all * 3);                // at least three batches for every team
     if (rows > fair) rows = fair;
     if (rows > 32) rows = 32;
     rows = rows / at_once * at_once;
     if (rows < at_once) rows = at_once;
     r.rows = (int)rows;
     r.stage_bytes = (int)((rows * row_bytes + 32 + 127) / 128 * 128);
-    int per_sm = 2;
-    long long st = (long long)(budget / ((size_t)nt * r.stage_bytes));
-    if (st < 2) { per_sm = 1; st = (long long)(kNormSmem / teams / ((size_t)nt * r.stage_bytes)); }
-    r.stages = (int)(st > 4 ? 4 : st);
+    r.stages = (int)(budget / r.stage_bytes > 4 ? 4 : budget / r.stage_bytes);
     r.batches = (R + rows - 1) / rows;
-    const long long grid = (r.batches + teams - 1) / teams;
     // Fewer rows than two rounds of teams: every row is on its way at once in the direct kernel, and nothing is left to
     // prefetch
     if (r.stages < 2 || r.batches < 2 * (long long)sm_count() * teams) {
         p.kind = ROWS_DIRECT;
-        if (p.log_tpr > 5) { p.threads = 1 << p.log_tpr; p.work = R; }      // one row per block
-        const int resident = p.threads > 512 ? 1 : 1024 / p.threads;
+        if (backward && p.E > 16) {                      // the direct kernel holds 16 elements per thread
+            p.E = 16;
+            ++p.log_tpr;
+            p.threads = p.log_tpr > 8 ? 1 << p.log_tpr : kRowThreads;
+        }
+        if (p.log_tpr > 5) p.threads = 1 << p.log_tpr;   // one row per block
+        const int rows_pb = p.threads >> p.log_tpr;
+        p.work = (R + rows_pb - 1) / rows_pb;
+        const int resident = 1024 / p.threads;
         p.grid = (int)(p.work < (long long)sm_count() * resident ? p.work : (long long)sm_count() * resident);
-        p.smem = backward && p.log_tpr <= 5 ? (size_t)2 * d.C * 4 : 0;
+        p.smem = backward && p.log_tpr <= 5 ? (size_t)p.threads / 32 * 2 * d.C * 4 : 0;
         return;
     }
+    const long long grid = (r.batches + teams - 1) / teams;
     p.kind = ROWS_RING;
     p.grid = (int)(grid < (long long)per_sm * sm_count() ? grid : (long long)per_sm * sm_count());
     p.smem = (size_t)teams * r.stages * nt * r.stage_bytes;
-    if (backward && p.smem < (size_t)8 * d.C) p.smem = (size_t)8 * d.C;
+    if (backward && p.smem < (size_t)teams * 8 * d.C) p.smem = (size_t)teams * 8 * d.C;
 }
 
 void plan_planes(const gf_norm_desc& d, bool backward, long long R, NormPlan& p) {
@@ -1234,7 +1272,6 @@ void plan_planes(const gf_norm_desc& d, bool backward, long long R, NormPlan& p)
         t.div_tiles = FastDiv((uint32_t)t.tiles_per_img);
         p.threads = kPlaneThreads;
         p.kind = PLANES_TILE;
-        p.whole = whole;
     };
     if (whole) {
         // Rows of 128 bytes, of 64 or of 32, as long as three tiles are in flight (two of the shortest).
@@ -1244,15 +1281,16 @@ void plan_planes(const gf_norm_desc& d, bool backward, long long R, NormPlan& p)
             t.box_rows = ((d.C + t.boxes - 1) / t.boxes + 3) / 4 * 4;       // boxes land on 128-byte boundaries
             t.pitch = lp * 16;
             const long long stage = ((long long)t.boxes * t.box_rows * t.pitch + 127) / 128 * 128;
-            const long long fit = (long long)(kNormSmem - 40 * 1024) / (nt * stage);
+            const long long fixed = kPlaneWarps * nt * lp * 16 / e * 4 + nt * lp * 16 / e * 4 + 2048;      // exchange, and what a block takes
+            const long long fit = ((long long)kNormSmem - 2 * fixed) / (nt * stage);
             const int kc = (d.C + kPlaneWarps * (32 / lp) - 1) / (kPlaneWarps * (32 / lp));
-            if (fit < (lp > 2 ? 3 : 2) || kc > 8) continue;
+            if (fit < (lp > 2 ? 3 : 2) || kc > 16) continue;
             const int px = lp * 16 / e;
             if (lp > 2 && HW <= px / 2) continue;        // shorter rows would do
             if ((long long)d.N * ((HW + px - 1) / px) > 0x7fffffffLL) continue;
             tiles(px);
             p.LP = lp;
-            p.KC = kc <= 1 ? 1 : kc <= 2 ? 2 : kc <= 4 ? 4 : 8;
+            p.KC = kc <= 2 ? 2 : kc <= 4 ? 4 : kc <= 8 ? 8 : 16;
             t.stage_bytes = (int)stage;
             // two blocks per SM where both can have three tiles in flight
             const int per_sm = fit >= 6 ? 2 : 1;
@@ -1262,18 +1300,21 @@ void plan_planes(const gf_norm_desc& d, bool backward, long long R, NormPlan& p)
             return;
         }
     } else if (HW * e >= 64) {
-        PlaneArgs& t = p.tile;
+        // Rows of 128 pixels, or of 32, as long as two tiles are in flight.
         const int kc = (d.C + kPlaneWarps - 1) / kPlaneWarps;
-        const int pieces = 32 * kPX * e / 16 + 1;
-        t.log_pieces = 0;
-        while ((1 << t.log_pieces) < pieces) ++t.log_pieces;
-        t.pitch = pieces * 16;
-        const long long stage = ((long long)d.C * t.pitch + 127) / 128 * 128;
-        const long long fit = (long long)(kNormSmem - 40 * 1024) / (nt * stage);
-        if (fit >= 2 && kc <= 32) {
-            tiles(32 * kPX);
-            p.LP = 32;
-            p.KC = kc <= 4 ? 4 : kc <= 8 ? 8 : kc <= 16 ? 16 : 32;
+        for (int px = 4; px >= 1 && kc <= 64; px -= 3) {
+            PlaneArgs& t = p.tile;
+            const int pieces = 32 * px * e / 16 + 1;
+            t.log_pieces = 0;
+            while ((1 << t.log_pieces) < pieces) ++t.log_pieces;
+            t.pitch = pieces * 16;
+            const long long stage = ((long long)d.C * t.pitch + 127) / 128 * 128;
+            const long long fixed = (kPlaneWarps + 1) * nt * 32 * px * 4 + 2048;
+            const long long fit = ((long long)kNormSmem - 2 * fixed) / (nt * stage);
+            if (fit < 2 || (px > 1 && HW <= 32)) continue;
+            tiles(32 * px);
+            p.PX = px;
+            p.KC = kc <= 8 ? 8 : kc <= 16 ? 16 : kc <= 32 ? 32 : 64;
             t.stage_bytes = (int)stage;
             const int per_sm = fit >= 4 ? 2 : 1;
             t.stages = fit / per_sm >= 3 ? 3 : 2;
@@ -1322,8 +1363,7 @@ template <typename T, int V, int E> gf_status launch_rows(const NormArgs& a, con
     const bool team = p.log_tpr > 5;
     if (p.kind == ROWS_RING) {
         if (!backward) return team ? launch_ring<T, V, E, true, false>(a, p, s) : launch_ring<T, V, E, false, false>(a, p, s);
-        if constexpr (E <= 16) return team ? launch_ring<T, V, E, true, true>(a, p, s) : launch_ring<T, V, E, false, true>(a, p, s);
-        return GF_ERR_UNSUPPORTED;
+        return team ? launch_ring<T, V, E, true, true>(a, p, s) : launch_ring<T, V, E, false, true>(a, p, s);
     }
     if (!backward) {
         if (team) ln_rows_fwd_kernel<T, V, NV, true><<<(unsigned)p.work, p.threads, 0, s>>>(a);
@@ -1360,45 +1400,47 @@ template <typename T, int V> gf_status launch_planes_v(const NormArgs& a, const 
     }
     return after_launch();
 }
-template <typename T, int LP, int KC, bool WHOLE, bool BWD>
+template <typename T, int LP, int KC, int PX, bool BWD>
 gf_status launch_tile_inst(const NormArgs& a, const gf_norm_desc& d, const NormPlan& p, cudaStream_t s) {
     static size_t configured[kMaxDevices] = {};
-    if (gf_status st = ensure_dyn_smem(ln_planes_tile_kernel<T, LP, KC, WHOLE, BWD>, p.smem, configured); st != GF_OK) return st;
+    if (gf_status st = ensure_dyn_smem(ln_planes_tile_kernel<T, LP, KC, PX, BWD>, p.smem, configured); st != GF_OK) return st;
     PlaneArgs t = p.tile;
     t.err_word = global_err_word();
     if (!t.err_word) return GF_ERR_CUDA;
-    if constexpr (WHOLE) {
+    if constexpr (PX == 0) {
         const uint64_t hw = (uint64_t)a.HW, c = (uint64_t)a.C;
         if (!make_tmap_plain(&t.tm_x, a.x, sizeof(T), hw, c, (uint64_t)d.N, hw, hw * c, (uint32_t)t.px, (uint32_t)t.box_rows, 1) ||
             (BWD && !make_tmap_plain(&t.tm_gy, a.gy, sizeof(T), hw, c, (uint64_t)d.N, hw, hw * c, (uint32_t)t.px, (uint32_t)t.box_rows, 1)))
             return GF_ERR_CUDA;
     }
-    ln_planes_tile_kernel<T, LP, KC, WHOLE, BWD><<<p.grid, p.threads, p.smem, s>>>(a, t);
+    ln_planes_tile_kernel<T, LP, KC, PX, BWD><<<p.grid, p.threads, p.smem, s>>>(a, t);
     return after_launch();
 }
-template <typename T, int LP, int KC, bool WHOLE>
+template <typename T, int LP, int KC, int PX>
 gf_status launch_tile_way(const NormArgs& a, const gf_norm_desc& d, const NormPlan& p, bool backward, cudaStream_t s) {
-    return backward ? launch_tile_inst<T, LP, KC, WHOLE, true>(a, d, p, s) : launch_tile_inst<T, LP, KC, WHOLE, false>(a, d, p, s);
+    return backward ? launch_tile_inst<T, LP, KC, PX, true>(a, d, p, s) : launch_tile_inst<T, LP, KC, PX, false>(a, d, p, s);
 }
 template <typename T, int LP> gf_status launch_tile_whole(const NormArgs& a, const gf_norm_desc& d, const NormPlan& p, bool backward, cudaStream_t s) {
     switch (p.KC) {
-        case 1: return launch_tile_way<T, LP, 1, true>(a, d, p, backward, s);
-        case 2: return launch_tile_way<T, LP, 2, true>(a, d, p, backward, s);
-        case 4: return launch_tile_way<T, LP, 4, true>(a, d, p, backward, s);
-        default: return launch_tile_way<T, LP, 8, true>(a, d, p, backward, s);
+        case 2: return launch_tile_way<T, LP, 2, 0>(a, d, p, backward, s);
+        case 4: return launch_tile_way<T, LP, 4, 0>(a, d, p, backward, s);
+        case 8: return launch_tile_way<T, LP, 8, 0>(a, d, p, backward, s);
+        default: return launch_tile_way<T, LP, 16, 0>(a, d, p, backward, s);
+    }
+}
+template <typename T, int PX> gf_status launch_tile_odd(const NormArgs& a, const gf_norm_desc& d, const NormPlan& p, bool backward, cudaStream_t s) {
+    switch (p.KC) {
+        case 8: return launch_tile_way<T, 32, 8, PX>(a, d, p, backward, s);
+        case 16: return launch_tile_way<T, 32, 16, PX>(a, d, p, backward, s);
+        case 32: return launch_tile_way<T, 32, 32, PX>(a, d, p, backward, s);
+        default: return launch_tile_way<T, 32, 64, PX>(a, d, p, backward, s);
     }
 }
 template <typename T> gf_status launch_tile(const NormArgs& a, const gf_norm_desc& d, const NormPlan& p, bool backward, cudaStream_t s) {
-    if (p.whole) {
-        if (p.LP == 8) return launch_tile_whole<T, 8>(a, d, p, backward, s);
-        return p.LP == 4 ? launch_tile_whole<T, 4>(a, d, p, backward, s) : launch_tile_whole<T, 2>(a, d, p, backward, s);
-    }
-    switch (p.KC) {
-        case 4: return launch_tile_way<T, 32, 4, false>(a, d, p, backward, s);
-        case 8: return launch_tile_way<T, 32, 8, false>(a, d, p, backward, s);
-        case 16: return launch_tile_way<T, 32, 16, false>(a, d, p, backward, s);
-        default: return launch_tile_way<T, 32, 32, false>(a, d, p, backward, s);
-    }
+    if (p.PX == 4) return launch_tile_odd<T, 4>(a, d, p, backward, s);
+    if (p.PX == 1) return launch_tile_odd<T, 1>(a, d, p, backward, s);
+    if (p.LP == 8) return launch_tile_whole<T, 8>(a, d, p, backward, s);
+    return p.LP == 4 ? launch_tile_whole<T, 4>(a, d, p, backward, s) : launch_tile_whole<T, 2>(a, d, p, backward, s);
 }
 template <typename T> gf_status launch_norm(const NormArgs& a, const gf_norm_desc& d, const NormPlan& p, bool backward, cudaStream_t s) {
     if (p.kind == PLANES_TILE) return launch_tile<T>(a, d, p, backward, s);
