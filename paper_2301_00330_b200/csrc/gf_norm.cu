@@ -292,8 +292,11 @@ template <typename T> __global__ void __launch_bounds__(1024) ln_rows_bwd_long_k
 // For more rows than there are teams of threads: a team (part of a block that shares a row) has its own ring of batches
 // of whole rows, which the copy engine fills some batches ahead, so that the loads of the next rows run under
 // the sums and stores of the present one.  A batch is one contiguous piece of memory, copied from the 16-byte
-// boundary before it to the one after it: rows of any length take the same path.  The last bytes of a tensor whose
-// size is no multiple of 16 are fetched with plain loads.
+// boundary before it to the one after it.  The last bytes of a tensor whose size is no multiple of 16 are fetched with
+// plain loads.
+//   SHIFT: rows whose length is no multiple of 16 bytes, one to a batch.  The number of teams is a multiple of the period (at most
+//   8) with which the rows' offsets from a 16-byte boundary repeat, so that all rows of a team have the same
+//   offset: its threads own whole aligned vectors, the first and last of which are partly the neighbouring rows'.
 struct RingArgs {
     int warps;                 // per team
     int stages, rows;          // batches in flight per team; rows per batch
@@ -336,7 +339,7 @@ template <bool TEAM, int N> __device__ __forceinline__ void team_sum(float (&s)[
     }
 }
 
-template <typename T, int V, int E, bool TEAM, bool BWD>
+template <typename T, int V, int E, bool TEAM, bool BWD, bool SHIFT>
 __global__ void __launch_bounds__(BWD ? 256 : 512) ln_rows_ring_kernel(const __grid_constant__ NormArgs a, const __grid_constant__ RingArgs r) {
     constexpr int NV = E / V, NT = BWD ? 2 : 1;
     extern __shared__ __align__(128) unsigned char dyn[];
@@ -359,6 +362,12 @@ __global__ void __launch_bounds__(BWD ? 256 : 512) ln_rows_ring_kernel(const __g
     if (TEAM)
         for (int k = threadIdx.x; k < 8 * 2 * 2 * 16; k += blockDim.x) (&red[0][0][0])[k] = 0.f;
     __syncthreads();
+    const int shift = SHIFT ? (int)((first * row_bytes) & 15) / (int)sizeof(T) : 0;      // elements before the row in its first vector
+    const int C = a.C + shift;                              // end of the row, counted from there
+    // element i of the thread's vector k is in the row
+    auto inside = [&](int k, int i) { const int c = k * step + g * V + i; return c >= shift && c < C; };
+    // the vector is wholly in the row (for all vectors but a row's first and last one)
+    auto whole = [&](int k) { return !SHIFT || ((k > 0 || g > 0 || shift == 0) && k * step + g * V + V <= C); };
     auto load = [&](long long b, int s) {                   // by one thread
         const long long lo = (b * r.rows * row_bytes) & ~15LL;
         long long hi = ((b + 1) * r.rows < a.R ? (b + 1) * r.rows : a.R) * row_bytes;
@@ -381,9 +390,9 @@ __global__ void __launch_bounds__(BWD ? 256 : 512) ln_rows_ring_kernel(const __g
     for (int k = 0; k < NV; ++k)
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const int c = k * step + g * V + i;
-            gam[k][i] = c < a.C ? a.gamma.at(c, 1.f) : 0.f;
-            if constexpr (!BWD) bet[k][i] = c < a.C ? a.beta.at(c, 0.f) : 0.f;
+            const int c = k * step + g * V + i - shift;
+            gam[k][i] = inside(k, i) ? a.gamma.at(c, 1.f) : 0.f;
+            if constexpr (!BWD) bet[k][i] = inside(k, i) ? a.beta.at(c, 0.f) : 0.f;
             else ag[k][i] = ab[k][i] = 0.f;
         }
     float mean_n = 0.f, rstd_n = 0.f;                       // of row `lane` of the next batch
@@ -418,19 +427,31 @@ __global__ void __launch_bounds__(BWD ? 256 : 512) ln_rows_ring_kernel(const __g
         const float mean_b = mean_n, rstd_b = rstd_n;
         if constexpr (BWD) stats(b + teams_all);
         const int row_in = TEAM ? 0 : lane >> a.log_tpr;    // of the rows that the warp has at once
-        const T* x = reinterpret_cast<const T*>(sx + (int)(r0 * row_bytes - lo) + row_in * row_bytes) + g * V;
-        T* out = static_cast<T*>(a.out) + (r0 + row_in) * a.C + g * V;
+        const T* x = reinterpret_cast<const T*>(sx + (SHIFT ? 0 : (int)(r0 * row_bytes - lo)) + row_in * row_bytes) + g * V;
+        T* out = static_cast<T*>(a.out) + ((r0 + row_in) * a.C - shift) + g * V;
         for (int q = 0; q < nr; q += rows_at_once, slot ^= 1, x += rows_at_once * a.C, out += rows_at_once * a.C) {
             const int k_row = q + row_in;
-            const int width = TEAM || k_row < nr ? a.C - g * V : 0;      // columns from this thread's first on
+            const int width = TEAM || k_row < nr ? C - g * V : 0;        // columns from this thread's first on
             float v[NV][V];
+            auto put = [&](int k) {
+                if (whole(k)) store_vec<T, V>(out + k * step, v[k]);
+                else {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) if (inside(k, i)) out[k * step + i] = from_f32<T>(v[k][i]);
+                }
+            };
             if constexpr (!BWD) {
                 float sum[1] = {0.f}, var[1] = {0.f};
 #pragma unroll
                 for (int k = 0; k < NV; ++k) {
-                    if (k * step >= a.C) break;             // the same for all threads
-                    if (k * step < width) load_vec<T, V>(x + k * step, v[k]);
-                    else {
+                    if (k * step >= C) break;               // the same for all threads
+                    if (k * step < width) {
+                        load_vec<T, V>(x + k * step, v[k]);
+                        if (!whole(k)) {
+#pragma unroll
+                            for (int i = 0; i < V; ++i) if (!inside(k, i)) v[k][i] = 0.f;
+                        }
+                    } else {
 #pragma unroll
                         for (int i = 0; i < V; ++i) v[k][i] = 0.f;
                     }
@@ -441,21 +462,27 @@ __global__ void __launch_bounds__(BWD ? 256 : 512) ln_rows_ring_kernel(const __g
                 const float mean = sum[0] / (float)a.C;
 #pragma unroll
                 for (int k = 0; k < NV; ++k) {
-                    if (k * step >= a.C) break;
+                    if (k * step >= C) break;
                     if (k * step < width) {
 #pragma unroll
-                        for (int i = 0; i < V; ++i) { v[k][i] -= mean; var[0] += v[k][i] * v[k][i]; }
+                        for (int i = 0; i < V; ++i) v[k][i] -= mean;
+                        if (!whole(k)) {
+#pragma unroll
+                            for (int i = 0; i < V; ++i) if (!inside(k, i)) v[k][i] = 0.f;
+                        }
+#pragma unroll
+                        for (int i = 0; i < V; ++i) var[0] += v[k][i] * v[k][i];
                     }
                 }
                 team_sum<TEAM, 1>(var, a.log_tpr, red[team][1], team, r.warps);
                 const float rstd = rsqrtf(var[0] * a.inv_c + a.eps);
 #pragma unroll
                 for (int k = 0; k < NV; ++k) {
-                    if (k * step >= a.C) break;
+                    if (k * step >= C) break;
                     if (k * step < width) {
 #pragma unroll
                         for (int i = 0; i < V; ++i) v[k][i] = v[k][i] * rstd * gam[k][i] + bet[k][i];
-                        store_vec<T, V>(out + k * step, v[k]);
+                        put(k);
                     }
                 }
                 if (a.mean && g == 0 && width > 0) { a.mean[r0 + k_row] = mean; a.rstd[r0 + k_row] = rstd; }
@@ -466,10 +493,14 @@ __global__ void __launch_bounds__(BWD ? 256 : 512) ln_rows_ring_kernel(const __g
                 float sum[2] = {0.f, 0.f};
 #pragma unroll
                 for (int k = 0; k < NV; ++k) {
-                    if (k * step >= a.C) break;
+                    if (k * step >= C) break;
                     if (k * step < width) {
                         load_vec<T, V>(x + k * step, v[k]);
                         load_vec<T, V>(gy + k * step, gv[k]);
+                        if (!whole(k)) {
+#pragma unroll
+                            for (int i = 0; i < V; ++i) if (!inside(k, i)) { v[k][i] = mean; gv[k][i] = 0.f; }
+                        }
                     } else {                                // xh = 0 and gy = 0: adds nothing
 #pragma unroll
                         for (int i = 0; i < V; ++i) { v[k][i] = mean; gv[k][i] = 0.f; }
@@ -489,11 +520,11 @@ __global__ void __launch_bounds__(BWD ? 256 : 512) ln_rows_ring_kernel(const __g
                     const float m1 = sum[0] * a.inv_c * rstd, m2 = sum[1] * a.inv_c * rstd;
 #pragma unroll
                     for (int k = 0; k < NV; ++k) {
-                        if (k * step >= a.C) break;
+                        if (k * step >= C) break;
                         if (k * step < width) {
 #pragma unroll
                             for (int i = 0; i < V; ++i) v[k][i] = (gv[k][i] * rstd - m1) - v[k][i] * m2;
-                            store_vec<T, V>(out + k * step, v[k]);
+                            put(k);
                         }
                     }
                 }
@@ -530,8 +561,8 @@ __global__ void __launch_bounds__(BWD ? 256 : 512) ln_rows_ring_kernel(const __g
             for (int k = 0; k < NV; ++k)
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    const int c = k * step + g * V + i;
-                    if (c < a.C) { mine[c] = ag[k][i]; mine[a.C + c] = ab[k][i]; }
+                    const int c = k * step + g * V + i - shift;
+                    if (inside(k, i)) { mine[c] = ag[k][i]; mine[a.C + c] = ab[k][i]; }
                 }
         }
         __syncthreads();
@@ -1174,6 +1205,7 @@ struct NormPlan {
     NormKind kind;
     int V;                // elements per load
     int log_tpr, E;       // rows: threads per row; elements per thread
+    bool shift;           // rows off 16-byte boundaries, taken as aligned vectors
     int CG, NCH;          // planes, direct: warps, channels per warp
     int threads;
     long long work;       // blocks of work (row groups, or pixel tiles)
@@ -1195,18 +1227,34 @@ constexpr size_t kNormSmem = 220 * 1024;
 
 void plan_rows(const gf_norm_desc& d, bool backward, long long R, NormPlan& p) {
     const int e = d.dtype == GF_F32 ? 4 : 2;
-    p.V = vec_for(d.C, e);
     const int max_log = backward ? 8 : 9;
-    const long long vecs = (d.C + p.V - 1) / p.V;
+    const long long row_bytes = (long long)d.C * e;
     // A thread holds up to 32 elements, so that the work per row (exchanges, statistics) is shared by many of them;
     // two lanes at least share a row of more than 8.
-    auto fits = [&](int lt, int el) { return vecs <= (long long)(el / p.V) << lt; };
-    p.E = 8;
-    p.log_tpr = 0;
-    if (!fits(1, 8)) p.E = 16;
-    if (!fits(2, 16)) p.E = 32;
-    while (p.log_tpr < max_log && !fits(p.log_tpr, p.E)) ++p.log_tpr;
-    if (!fits(p.log_tpr, p.E)) {
+    auto share_out = [&](int V, long long vecs) {
+        auto fits = [&](int lt, int el) { return vecs <= (long long)(el / V) << lt; };
+        p.V = V;
+        p.E = 8;
+        p.log_tpr = 0;
+        if (!fits(1, 8)) p.E = 16;
+        if (!fits(2, 16)) p.E = 32;
+        while (p.log_tpr < max_log && !fits(p.log_tpr, p.E)) ++p.log_tpr;
+        return fits(p.log_tpr, p.E);
+    };
+    auto plain = [&] { const int V = vec_for(d.C, e); return share_out(V, d.C / V); };
+    // Long rows off the 16-byte boundaries: aligned vectors, with a row of their own for each copy (short rows are
+    // better copied many at a time, and read element by element).
+    const int full = 16 / e;
+    auto shifted = [&] {
+        const long long vecs = (d.C + 2 * full - 2) / full;
+        p.V = full;
+        p.log_tpr = 5;                                   // a warp at least: the batch is one row
+        for (p.E = 8; p.E < 32 && vecs > 32LL * (p.E / full); p.E *= 2) {}
+        while (p.log_tpr < max_log && vecs > (long long)(p.E / full) << p.log_tpr) ++p.log_tpr;
+        return vecs <= (long long)(p.E / full) << p.log_tpr;
+    };
+    p.shift = row_bytes % 16 != 0 && row_bytes >= 512;
+    if (!(p.shift ? shifted() : plain())) {
         p.kind = ROWS_LONG;
         p.threads = 1024;
         p.work = R;
@@ -1219,7 +1267,6 @@ void plan_rows(const gf_norm_desc& d, bool backward, long long R, NormPlan& p) {
     const int nt = backward ? 2 : 1;
     const int warps = p.log_tpr > 5 ? 1 << (p.log_tpr - 5) : 1, teams = p.threads / 32 / warps;
     const int at_once = p.log_tpr > 5 ? 1 : 32 >> p.log_tpr;
-    const long long row_bytes = (long long)d.C * e;
     RingArgs& r = p.ring;
     r.warps = warps;
     int per_sm = backward ? 1 : 2;
@@ -1232,6 +1279,7 @@ void plan_rows(const gf_norm_desc& d, bool backward, long long R, NormPlan& p) {
     if (rows > 32) rows = 32;
     rows = rows / at_once * at_once;
     if (rows < at_once) rows = at_once;
+    if (p.shift) rows = 1;                               // at_once is 1 too
     r.rows = (int)rows;
     r.stage_bytes = (int)((rows * row_bytes + 32 + 127) / 128 * 128);
     r.stages = (int)(budget / r.stage_bytes > 4 ? 4 : budget / r.stage_bytes);
@@ -1240,12 +1288,14 @@ void plan_rows(const gf_norm_desc& d, bool backward, long long R, NormPlan& p) {
     // prefetch
     if (r.stages < 2 || r.batches < 2 * (long long)sm_count() * teams) {
         p.kind = ROWS_DIRECT;
+        if (p.shift && !plain()) p.kind = ROWS_LONG;
+        p.shift = false;
         if (backward && p.E > 16) {                      // the direct kernel holds 16 elements per thread
             p.E = 16;
             ++p.log_tpr;
-            p.threads = p.log_tpr > 8 ? 1 << p.log_tpr : kRowThreads;
         }
-        if (p.log_tpr > 5) p.threads = 1 << p.log_tpr;   // one row per block
+        if (p.kind == ROWS_LONG) { p.threads = 1024; p.work = R; p.grid = (int)(R < sm_count() ? R : sm_count()); return; }
+        p.threads = p.log_tpr > 5 ? 1 << p.log_tpr : kRowThreads;        // one row per block when a warp is not enough
         const int rows_pb = p.threads >> p.log_tpr;
         p.work = (R + rows_pb - 1) / rows_pb;
         const int resident = 1024 / p.threads;
@@ -1256,6 +1306,7 @@ void plan_rows(const gf_norm_desc& d, bool backward, long long R, NormPlan& p) {
     const long long grid = (r.batches + teams - 1) / teams;
     p.kind = ROWS_RING;
     p.grid = (int)(grid < (long long)per_sm * sm_count() ? grid : (long long)per_sm * sm_count());
+    if (p.shift && teams < 8) p.grid = p.grid / (8 / teams) * (8 / teams);      // a multiple of 8 teams (there are 2 x 148 x teams rows at least)
     p.smem = (size_t)teams * r.stages * nt * r.stage_bytes;
     if (backward && p.smem < (size_t)teams * 8 * d.C) p.smem = (size_t)teams * 8 * d.C;
 }
@@ -1349,21 +1400,32 @@ NormPlan norm_plan(const gf_norm_desc& d, bool backward) {
     return p;
 }
 
-template <typename T, int V, int E, bool TEAM, bool BWD> gf_status launch_ring(const NormArgs& a, const NormPlan& p, cudaStream_t s) {
+template <typename T, int V, int E, bool TEAM, bool BWD, bool SHIFT> gf_status launch_ring(const NormArgs& a, const NormPlan& p, cudaStream_t s) {
     static size_t configured[kMaxDevices] = {};
-    if (gf_status st = ensure_dyn_smem(ln_rows_ring_kernel<T, V, E, TEAM, BWD>, p.smem, configured); st != GF_OK) return st;
+    if (gf_status st = ensure_dyn_smem(ln_rows_ring_kernel<T, V, E, TEAM, BWD, SHIFT>, p.smem, configured); st != GF_OK) return st;
     RingArgs r = p.ring;
     r.err_word = global_err_word();
     if (!r.err_word) return GF_ERR_CUDA;
-    ln_rows_ring_kernel<T, V, E, TEAM, BWD><<<p.grid, p.threads, p.smem, s>>>(a, r);
+    ln_rows_ring_kernel<T, V, E, TEAM, BWD, SHIFT><<<p.grid, p.threads, p.smem, s>>>(a, r);
     return after_launch();
 }
 template <typename T, int V, int E> gf_status launch_rows(const NormArgs& a, const NormPlan& p, bool backward, cudaStream_t s) {
     constexpr int NV = E / V;
     const bool team = p.log_tpr > 5;
     if (p.kind == ROWS_RING) {
-        if (!backward) return team ? launch_ring<T, V, E, true, false>(a, p, s) : launch_ring<T, V, E, false, false>(a, p, s);
-        return team ? launch_ring<T, V, E, true, true>(a, p, s) : launch_ring<T, V, E, false, true>(a, p, s);
+        if constexpr (V * (int)sizeof(T) == 16) {
+            if (p.shift) {
+                if (!backward) return team ? launch_ring<T, V, E, true, false, true>(a, p, s) : launch_ring<T, V, E, false, false, true>(a, p, s);
+                return team ? launch_ring<T, V, E, true, true, true>(a, p, s) : launch_ring<T, V, E, false, true, true>(a, p, s);
+            }
+        }
+        if (V * (int)sizeof(T) < 16 && team) return GF_ERR_UNSUPPORTED;      // (such rows are short, or taken as shifted ones)
+        if (!backward) {
+            if constexpr (V * (int)sizeof(T) == 16) if (team) return launch_ring<T, V, E, true, false, false>(a, p, s);
+            return launch_ring<T, V, E, false, false, false>(a, p, s);
+        }
+        if constexpr (V * (int)sizeof(T) == 16) if (team) return launch_ring<T, V, E, true, true, false>(a, p, s);
+        return launch_ring<T, V, E, false, true, false>(a, p, s);
     }
     if (!backward) {
         if (team) ln_rows_fwd_kernel<T, V, NV, true><<<(unsigned)p.work, p.threads, 0, s>>>(a);
