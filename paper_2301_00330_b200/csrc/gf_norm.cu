@@ -863,7 +863,6 @@ __global__ void __launch_bounds__(512) ln_planes_bwd_long_kernel(const __grid_co
 //          16-byte vector of pixels.
 //   else : planes of odd size.  Each row is copied in 16-byte pieces from the boundary before it (its offset differs from
 //          channel to channel); 32 lanes read and write single pixels, PX of them each.
-constexpr int kPlaneThreads = 256, kPlaneWarps = kPlaneThreads / 32;
 struct PlaneArgs {
     CUtensorMap tm_x, tm_gy;   // WHOLE
     int boxes, box_rows;       // boxes of a tile (channels), rows of each
@@ -881,9 +880,12 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int by
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 
-template <typename T, int LP, int KC, int PX, bool BWD>        // PX = 0: WHOLE
-__global__ void __launch_bounds__(kPlaneThreads) ln_planes_tile_kernel(const __grid_constant__ NormArgs a, const __grid_constant__ PlaneArgs t) {
+// PX = 0: WHOLE, with 8 warps; 16 warps else (more instructions per byte)
+constexpr int plane_warps(int PX) { return PX == 0 ? 8 : 16; }
+template <typename T, int LP, int KC, int PX, bool BWD>
+__global__ void __launch_bounds__((PX == 0 ? 8 : 16) * 32) ln_planes_tile_kernel(const __grid_constant__ NormArgs a, const __grid_constant__ PlaneArgs t) {
     constexpr bool WHOLE = PX == 0;
+    constexpr int kPlaneWarps = PX == 0 ? 8 : 16, kPlaneThreads = kPlaneWarps * 32;
     constexpr int NT = BWD ? 2 : 1, E = (int)sizeof(T);
     constexpr int V = WHOLE ? 16 / E : PX;                 // pixels of a thread
     constexpr int PT = LP * V;                              // pixels of a tile
@@ -1321,7 +1323,7 @@ void plan_planes(const gf_norm_desc& d, bool backward, long long R, NormPlan& p)
         t.tiles_per_img = (int)((HW + px - 1) / px);
         t.tiles = (long long)d.N * t.tiles_per_img;
         t.div_tiles = FastDiv((uint32_t)t.tiles_per_img);
-        p.threads = kPlaneThreads;
+        p.threads = plane_warps(p.PX) * 32;
         p.kind = PLANES_TILE;
     };
     if (whole) {
@@ -1332,6 +1334,7 @@ void plan_planes(const gf_norm_desc& d, bool backward, long long R, NormPlan& p)
             t.box_rows = ((d.C + t.boxes - 1) / t.boxes + 3) / 4 * 4;       // boxes land on 128-byte boundaries
             t.pitch = lp * 16;
             const long long stage = ((long long)t.boxes * t.box_rows * t.pitch + 127) / 128 * 128;
+            constexpr int kPlaneWarps = plane_warps(0);
             const long long fixed = kPlaneWarps * nt * lp * 16 / e * 4 + nt * lp * 16 / e * 4 + 2048;      // exchange, and what a block takes
             const long long fit = ((long long)kNormSmem - 2 * fixed) / (nt * stage);
             const int kc = (d.C + kPlaneWarps * (32 / lp) - 1) / (kPlaneWarps * (32 / lp));
@@ -1352,8 +1355,9 @@ void plan_planes(const gf_norm_desc& d, bool backward, long long R, NormPlan& p)
         }
     } else if (HW * e >= 64) {
         // Rows of 128 pixels, or of 32, as long as two tiles are in flight.
+        constexpr int kPlaneWarps = plane_warps(1);
         const int kc = (d.C + kPlaneWarps - 1) / kPlaneWarps;
-        for (int px = 4; px >= 1 && kc <= 64; px -= 3) {
+        for (int px = 4; px >= 1 && kc <= 32; px -= 3) {
             PlaneArgs& t = p.tile;
             const int pieces = 32 * px * e / 16 + 1;
             t.log_pieces = 0;
@@ -1363,11 +1367,11 @@ void plan_planes(const gf_norm_desc& d, bool backward, long long R, NormPlan& p)
             const long long fixed = (kPlaneWarps + 1) * nt * 32 * px * 4 + 2048;
             const long long fit = ((long long)kNormSmem - 2 * fixed) / (nt * stage);
             if (fit < 2 || (px > 1 && HW <= 32)) continue;
-            tiles(32 * px);
             p.PX = px;
-            p.KC = kc <= 8 ? 8 : kc <= 16 ? 16 : kc <= 32 ? 32 : 64;
+            tiles(32 * px);
+            p.KC = kc <= 8 ? 8 : kc <= 16 ? 16 : 32;
             t.stage_bytes = (int)stage;
-            const int per_sm = fit >= 4 ? 2 : 1;
+            const int per_sm = fit >= 4 && p.KC <= 8 ? 2 : 1;        // registers of 512 threads
             t.stages = fit / per_sm >= 3 ? 3 : 2;
             p.smem = (size_t)t.stages * nt * stage;
             p.grid = (int)(t.tiles < (long long)per_sm * sm_count() ? t.tiles : (long long)per_sm * sm_count());
@@ -1494,8 +1498,7 @@ template <typename T, int PX> gf_status launch_tile_odd(const NormArgs& a, const
     switch (p.KC) {
         case 8: return launch_tile_way<T, 32, 8, PX>(a, d, p, backward, s);
         case 16: return launch_tile_way<T, 32, 16, PX>(a, d, p, backward, s);
-        case 32: return launch_tile_way<T, 32, 32, PX>(a, d, p, backward, s);
-        default: return launch_tile_way<T, 32, 64, PX>(a, d, p, backward, s);
+        default: return launch_tile_way<T, 32, 32, PX>(a, d, p, backward, s);
     }
 }
 template <typename T> gf_status launch_tile(const NormArgs& a, const gf_norm_desc& d, const NormPlan& p, bool backward, cudaStream_t s) {
