@@ -26,8 +26,8 @@ namespace {
 
 constexpr float kScale = 1024.f, kInvScale = 1.f / 1024.f;
 constexpr int kMaxLayers = 48;              // layers whose pointers travel in one launch's arguments
-constexpr int kNormBlocks = 128;            // partial sums per matrix, at most
-constexpr int kNormThreads = 512;
+constexpr int kNormBlocks = 256;            // partial sums per matrix, at most
+constexpr int kNormThreads = 256;
 
 inline size_t up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
@@ -38,14 +38,37 @@ struct Source {
     const float* mom[kMaxLayers];           // momentum before the step (NULL in g-only sources)
     float* mom_out[kMaxLayers];
     int batched, bf16, taps, nesterov;
+    int vec;                                // four elements at a time: one value per 4 or 2 bytes, rows and pointers on boundaries of them
     float momentum;
     int rows, cols;
 };
 
-__device__ __forceinline__ float source_grad(const Source& s, int b, long long e) {
+// Elements e .. e + 3 of matrix b's gradient; `live` of them exist (four where s.vec).
+__device__ __forceinline__ void source_grad4(const Source& s, int b, long long e, int live, float (&g)[4]) {
     const long long at = (s.batched ? (long long)b * s.rows * s.cols : 0) + e * s.taps;
     const void* p = s.g[s.batched ? 0 : b];
-    return s.bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p)[at]) : static_cast<const float*>(p)[at];
+    if (s.vec) {
+        if (s.bf16) {
+            const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(p) + at);
+            g[0] = __uint_as_float(w.x << 16); g[1] = __uint_as_float(w.x & 0xffff0000u);
+            g[2] = __uint_as_float(w.y << 16); g[3] = __uint_as_float(w.y & 0xffff0000u);
+        } else {
+            const float4 w = *reinterpret_cast<const float4*>(static_cast<const float*>(p) + at);
+            g[0] = w.x; g[1] = w.y; g[2] = w.z; g[3] = w.w;
+        }
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        g[k] = 0.f;
+        if (k < live) g[k] = s.bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p)[at + k * s.taps]) : static_cast<const float*>(p)[at + k * s.taps];
+    }
+}
+// Four floats of a momentum buffer.
+__device__ __forceinline__ void momentum4(const float* p, int vec, int live, float (&m)[4]) {
+    if (vec) { const float4 w = *reinterpret_cast<const float4*>(p); m[0] = w.x; m[1] = w.y; m[2] = w.z; m[3] = w.w; return; }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) { m[k] = 0.f; if (k < live) m[k] = p[k]; }
 }
 
 // Sums of squares of the matrices to be orthogonalised, one partial per block; a Muon step also
@@ -57,25 +80,36 @@ template <bool MUON> __global__ void __launch_bounds__(kNormThreads) ns_norm_ker
     const int b = blockIdx.y;
     const long long n = (long long)s.rows * s.cols;
     float q = 0.f;
-    const long long stride = (long long)gridDim.x * kNormThreads;
-    constexpr int kAtOnce = 8;                            // loads in flight per thread
-    for (long long e0 = (long long)blockIdx.x * kNormThreads + threadIdx.x; e0 < n; e0 += kAtOnce * stride) {
-        float g[kAtOnce], m[kAtOnce];
+    const long long stride = 4LL * gridDim.x * kNormThreads;
+    constexpr int kAtOnce = 4;                            // groups of four in flight per thread
+    for (long long e0 = 4LL * (blockIdx.x * kNormThreads + threadIdx.x); e0 < n; e0 += kAtOnce * stride) {
+        float g[kAtOnce][4], m[kAtOnce][4];
 #pragma unroll
         for (int k = 0; k < kAtOnce; ++k) {
             const long long e = e0 + k * stride;
-            g[k] = e < n ? source_grad(s, b, e) : 0.f;
-            if constexpr (MUON) m[k] = e < n ? s.mom[b][e] : 0.f;
+            const int live = e < n ? (n - e < 4 ? (int)(n - e) : 4) : 0;
+            if (live > 0) {
+                source_grad4(s, b, e, live, g[k]);
+                if constexpr (MUON) momentum4(s.mom[b] + e, s.vec, live, m[k]);
+            } else g[k][0] = g[k][1] = g[k][2] = g[k][3] = m[k][0] = m[k][1] = m[k][2] = m[k][3] = 0.f;
         }
 #pragma unroll
         for (int k = 0; k < kAtOnce; ++k) {
-            float u = g[k];
+            const long long e = e0 + k * stride;
             if constexpr (MUON) {
-                const float mo = s.momentum * m[k] + (1.f - s.momentum) * u;
-                if (e0 + k * stride < n) s.mom_out[b][e0 + k * stride] = mo;
-                u = s.nesterov ? (1.f - s.momentum) * u + s.momentum * mo : mo;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    m[k][i] = s.momentum * m[k][i] + (1.f - s.momentum) * g[k][i];
+                    g[k][i] = s.nesterov ? (1.f - s.momentum) * g[k][i] + s.momentum * m[k][i] : m[k][i];
+                }
+                if (s.vec) { if (e < n) *reinterpret_cast<float4*>(s.mom_out[b] + e) = make_float4(m[k][0], m[k][1], m[k][2], m[k][3]); }
+                else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) if (e + i < n) s.mom_out[b][e + i] = m[k][i];
+                }
             }
-            q += u * u;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) q += g[k][i] * g[k][i];
         }
     }
     double d = q;
@@ -102,17 +136,21 @@ __global__ void __launch_bounds__(256) ns_cast_kernel(const __grid_constant__ So
     pdl_wait();
     const int b = blockIdx.z, tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
     const int j0 = blockIdx.x * kCast, i0 = blockIdx.y * kCast;     // in the matrix as it was given
-    float u[16];
+    const int cx = (threadIdx.x & 15) * 4, cy = threadIdx.x >> 4;   // four columns of every 16th row
+    float u[4][4];
 #pragma unroll
-    for (int k = 0; k < 16; ++k) {
-        const int i = i0 + ty + 4 * k, j = j0 + tx;
-        u[k] = 0.f;
+    for (int k = 0; k < 4; ++k) {
+        const int i = i0 + cy + 16 * k, j = j0 + cx;
+        u[k][0] = u[k][1] = u[k][2] = u[k][3] = 0.f;
         if (i < s.rows && j < s.cols) {
             const long long e = (long long)i * s.cols + j;
-            u[k] = source_grad(s, b, e);
+            const int live = min(4, s.cols - j);
+            source_grad4(s, b, e, live, u[k]);
             if constexpr (MUON) {
-                const float mo = s.mom_out[b][e];
-                u[k] = s.nesterov ? (1.f - s.momentum) * u[k] + s.momentum * mo : mo;
+                float mo[4];
+                momentum4(s.mom_out[b] + e, s.vec, live, mo);
+#pragma unroll
+                for (int d = 0; d < 4; ++d) u[k][d] = s.nesterov ? (1.f - s.momentum) * u[k][d] + s.momentum * mo[d] : mo[d];
             }
         }
     }
@@ -125,7 +163,9 @@ __global__ void __launch_bounds__(256) ns_cast_kernel(const __grid_constant__ So
         if (threadIdx.x == 0) scale_sh = isinf(scale) ? 0.f : scale;
     }
 #pragma unroll
-    for (int k = 0; k < 16; ++k) tile[ty + 4 * k][tx] = u[k];
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int d = 0; d < 4; ++d) tile[cy + 16 * k][cx + d] = u[k][d];
     __syncthreads();
     const float scale = scale_sh;
     const int x0 = transposed ? i0 : j0, y0 = transposed ? j0 : i0;
@@ -168,39 +208,41 @@ struct FinishArgs {
     float keep, f;
     FastDiv div_taps;
 };
+constexpr int kFinRows = 16;                       // rows of the result per block, 64 columns
 template <bool MUON> __global__ void __launch_bounds__(256) ns_finish_kernel(const __grid_constant__ FinishArgs a) {
-    __shared__ float tile[kCast][kCast + 1];       // [row][column] of the result as it is wanted
+    __shared__ float tile[kFinRows][kCast + 1];    // [row][column] of the result as it is wanted
     pdl_launch_dependents();
     pdl_wait();
-    const int b = blockIdx.z, tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
-    const int c0 = blockIdx.x * kCast, r0 = blockIdx.y * kCast;
-    const int x0 = a.transposed ? r0 : c0, y0 = a.transposed ? c0 : r0;
+    const int b = blockIdx.z;
+    const int c0 = blockIdx.x * kCast, r0 = blockIdx.y * kFinRows;
+    if (threadIdx.x < 128) {
+        // a thread has 8 columns of a row of X: 16 rows x 8 pieces, or (transposed) 64 rows x 2 pieces
+        const int row = a.transposed ? threadIdx.x & 63 : threadIdx.x & 15, piece = a.transposed ? threadIdx.x >> 6 : threadIdx.x >> 4;
+        const int i = (a.transposed ? c0 : r0) + row, j = (a.transposed ? r0 : c0) + piece * 8;
+        if (i < a.m && j < a.n) {
+            const __half* src = a.x + (((long long)b * a.pieces + (j >> 3)) * a.m + i) * 8;
+            const uint4 hv = *reinterpret_cast<const uint4*>(src), lv = *reinterpret_cast<const uint4*>(src + a.lo);
+            const uint32_t h[4] = {hv.x, hv.y, hv.z, hv.w}, l[4] = {lv.x, lv.y, lv.z, lv.w};
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const int row = tx, piece = ty + 4 * k;
-        const int i = y0 + row, j = x0 + piece * 8;
-        if (i >= a.m || j >= a.n) continue;
-        const __half* src = a.x + (((long long)b * a.pieces + (j >> 3)) * a.m + i) * 8;
-        const uint4 hv = *reinterpret_cast<const uint4*>(src), lv = *reinterpret_cast<const uint4*>(src + a.lo);
-        const uint32_t h[4] = {hv.x, hv.y, hv.z, hv.w}, l[4] = {lv.x, lv.y, lv.z, lv.w};
+            for (int e = 0; e < 4; ++e) {
+                const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&h[e])), q = __half22float2(*reinterpret_cast<const __half2*>(&l[e]));
+                const float v[2] = {(p.x + q.x) * kInvScale, (p.y + q.y) * kInvScale};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&h[e])), q = __half22float2(*reinterpret_cast<const __half2*>(&l[e]));
-            const float v[2] = {(p.x + q.x) * kInvScale, (p.y + q.y) * kInvScale};
-#pragma unroll
-            for (int d = 0; d < 2; ++d) {
-                const int c = piece * 8 + 2 * e + d;
-                if (a.transposed) tile[c][row] = v[d];
-                else tile[row][c] = v[d];
+                for (int d = 0; d < 2; ++d) {
+                    const int c = piece * 8 + 2 * e + d;
+                    if (a.transposed) tile[c][row] = v[d];
+                    else tile[row][c] = v[d];
+                }
             }
         }
     }
     __syncthreads();
-    const int nr = min(kCast, a.rows - r0), nc = min(kCast, a.cols - c0);
+    const int nr = min(kFinRows, a.rows - r0), nc = min(kCast, a.cols - c0);
     if constexpr (!MUON) {
+        const int tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
         const long long base = (long long)b * a.rows * a.cols;
 #pragma unroll
-        for (int k = 0; k < 16; ++k) {
+        for (int k = 0; k < kFinRows / 4; ++k) {
             const int r = ty + 4 * k;
             if (r < nr && tx < nc) {
                 const long long o = base + (long long)(r0 + r) * a.cols + c0 + tx;
@@ -209,17 +251,32 @@ template <bool MUON> __global__ void __launch_bounds__(256) ns_finish_kernel(con
             }
         }
     } else {
-        // a row of the tile is nc * taps consecutive weights; a warp takes rows in turn
+        // a row of the tile is nc * taps consecutive weights; a warp takes two rows
         const int span = nc * a.taps, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
         for (int r = warp; r < nr; r += 8) {
             const long long o = ((long long)(r0 + r) * a.cols + c0) * a.taps;
-#pragma unroll 4
-            for (int e = lane; e < span; e += 32) {
-                const float x = tile[r][a.div_taps.div((uint32_t)e)];
-                if (a.bf16)
-                    static_cast<__nv_bfloat16*>(a.w_out[b])[o + e] =
-                        __float2bfloat16_rn(a.keep * __bfloat162float(static_cast<const __nv_bfloat16*>(a.w[b])[o + e]) - a.f * x);
-                else static_cast<float*>(a.w_out[b])[o + e] = a.keep * static_cast<const float*>(a.w[b])[o + e] - a.f * x;
+            if (a.bf16) {
+                const __nv_bfloat16* w = static_cast<const __nv_bfloat16*>(a.w[b]) + o;
+                __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.w_out[b]) + o;
+                for (int e0 = lane; e0 < span; e0 += 32 * 8) {
+                    float v[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) if (e0 + 32 * k < span) v[k] = __bfloat162float(w[e0 + 32 * k]);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if (e0 + 32 * k < span) out[e0 + 32 * k] = __float2bfloat16_rn(a.keep * v[k] - a.f * tile[r][a.div_taps.div((uint32_t)(e0 + 32 * k))]);
+                }
+            } else {
+                const float* w = static_cast<const float*>(a.w[b]) + o;
+                float* out = static_cast<float*>(a.w_out[b]) + o;
+                for (int e0 = lane; e0 < span; e0 += 32 * 8) {
+                    float v[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) if (e0 + 32 * k < span) v[k] = w[e0 + 32 * k];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if (e0 + 32 * k < span) out[e0 + 32 * k] = a.keep * v[k] - a.f * tile[r][a.div_taps.div((uint32_t)(e0 + 32 * k))];
+                }
             }
         }
     }
@@ -687,7 +744,7 @@ NsPlan ns_plan(int batch, int rows, int cols, int precision) {
     p.split = precision == GF_NS_F32 ? 2 : 1;
     p.x_pieces = (p.n + 7) / 8;
     p.a_pieces = (p.m + 7) / 8;
-    const long long per = ((long long)rows * cols + 8 * kNormThreads - 1) / (8 * kNormThreads);
+    const long long per = ((long long)rows * cols + 8 * kNormThreads - 1) / (8 * kNormThreads);      // two groups of four per thread
     p.norm_blocks = (int)(per < kNormBlocks ? per : kNormBlocks);
     p.x_lo = 8LL * batch * p.m * p.x_pieces;
     p.a_lo = 8LL * batch * p.m * p.a_pieces;
@@ -807,7 +864,7 @@ gf_status ns_iterate(const NsPlan& p, char* base, int steps, const float* coeffs
     return p.split == 2 ? launch_iterate<2, false>(a, units, s) : launch_iterate<1, false>(a, units, s);
 }
 
-dim3 finish_grid(const NsPlan& p, int count) { return dim3((p.cols + kCast - 1) / kCast, (p.rows + kCast - 1) / kCast, count); }
+dim3 finish_grid(const NsPlan& p, int count) { return dim3((p.cols + kCast - 1) / kCast, (p.rows + kFinRows - 1) / kFinRows, count); }
 FinishArgs finish_args(const NsPlan& p, char* base, int steps, int first) {
     FinishArgs f = {};
     f.x = reinterpret_cast<const __half*>(base + p.off_x[steps & 1]) + 8LL * first * p.x_pieces * p.m;
@@ -864,6 +921,7 @@ gf_status gf_newton_schulz(const gf_ns_desc* d, const void* G, void* O, void* wo
     char* base = static_cast<char*>(workspace);
     Source src = {};
     src.g[0] = G; src.batched = 1; src.bf16 = d->in_dtype == GF_BF16; src.taps = 1; src.rows = d->rows; src.cols = d->cols;
+    src.vec = d->cols % 4 == 0;                 // G is on a 16-byte boundary, and so are its rows and matrices, or 8 in bf16
     if (gf_status st = launch_prepare<false>(p, src, 0, d->batch, base, d->eps, s); st != GF_OK) return st;
     if (gf_status st = ns_iterate(p, base, d->steps, h_coeffs, s); st != GF_OK) return st;
     FinishArgs f = finish_args(p, base, d->steps, 0);
@@ -911,6 +969,9 @@ gf_status gf_muon_step(const gf_muon_desc* d, const void* const* h_grad, const f
         }
         src.bf16 = d->grad_dtype == GF_BF16; src.taps = d->taps; src.nesterov = d->nesterov; src.momentum = d->momentum;
         src.rows = d->rows; src.cols = d->cols;
+        src.vec = d->taps == 1 && d->cols % 4 == 0;
+        for (int k = 0; k < n; ++k)
+            if (off16(src.g[k]) || off16(src.mom[k]) || off16(src.mom_out[k])) src.vec = 0;
         // the flattened matrix is u (x) (1 .. 1): its norm is sqrt(taps) times that of u
         if (gf_status st = launch_prepare<true>(p, src, first, n, base, d->eps / root, s); st != GF_OK) return st;
     }
