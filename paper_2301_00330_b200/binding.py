@@ -343,10 +343,26 @@ def _nbytes(workspace) -> int:
     return 0 if workspace is None else workspace.numel() * workspace.element_size()
 
 
+def _addr(t):
+    """Device address of a dense tensor, as ctypes takes it for a pointer (None: NULL).  These calls are short beside
+    their marshalling, so that it is kept short: no intermediate objects."""
+    if t is None:
+        return None
+    if not t.is_contiguous() and not (t.dim() == 4 and t.is_contiguous(memory_format=torch.channels_last)):
+        raise ValueError("tensors passed to the gf_* calls must be dense")
+    return t.data_ptr()
+
+
+def _raw_stream(stream):
+    if stream is None:
+        stream = torch.cuda.current_stream()
+    return stream.cuda_stream if isinstance(stream, torch.cuda.Stream) else int(stream)
+
+
 def gf_layer_norm_forward(desc: gf_norm_desc, x, gamma, beta, y, mean=None, rstd=None, stream=None) -> None:
     """y <- (x - mean) rstd gamma + beta over the channels; mean and rstd (fp32, one per pixel) for the backward pass."""
-    _check(lib().gf_layer_norm_forward(ctypes.byref(desc), _ptr(x), _ptr(gamma), _ptr(beta), _ptr(y), _ptr(mean), _ptr(rstd),
-                                       _stream(stream)), "gf_layer_norm_forward")
+    _check(lib().gf_layer_norm_forward(ctypes.byref(desc), _addr(x), _addr(gamma), _addr(beta), _addr(y), _addr(mean), _addr(rstd),
+                                       _raw_stream(stream)), "gf_layer_norm_forward")
 
 
 def gf_layer_norm_backward_workspace_bytes(desc: gf_norm_desc) -> int:
@@ -357,8 +373,8 @@ def gf_layer_norm_backward(desc: gf_norm_desc, g_y, x, gamma, mean, rstd, g_x, g
                            workspace_bytes=None, stream=None) -> None:
     if workspace_bytes is None:
         workspace_bytes = _nbytes(workspace)
-    _check(lib().gf_layer_norm_backward(ctypes.byref(desc), _ptr(g_y), _ptr(x), _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(g_x),
-                                        _ptr(g_gamma), _ptr(g_beta), _ptr(workspace), workspace_bytes, _stream(stream)),
+    _check(lib().gf_layer_norm_backward(ctypes.byref(desc), _addr(g_y), _addr(x), _addr(gamma), _addr(mean), _addr(rstd), _addr(g_x),
+                                        _addr(g_gamma), _addr(g_beta), _addr(workspace), workspace_bytes, _raw_stream(stream)),
            "gf_layer_norm_backward")
 
 
@@ -380,8 +396,8 @@ def gf_newton_schulz(desc: gf_ns_desc, G, O, workspace, workspace_bytes=None, co
     """O <- the Newton-Schulz iterates of the matrices G [batch, rows, cols]; coeffs: (a, b, c) for each step."""
     if workspace_bytes is None:
         workspace_bytes = _nbytes(workspace)
-    _check(lib().gf_newton_schulz(ctypes.byref(desc), _ptr(G), _ptr(O), _ptr(workspace), workspace_bytes,
-                                  _coeffs(coeffs, desc.steps), _stream(stream)), "gf_newton_schulz")
+    _check(lib().gf_newton_schulz(ctypes.byref(desc), _addr(G), _addr(O), _addr(workspace), workspace_bytes,
+                                  _coeffs(coeffs, desc.steps), _raw_stream(stream)), "gf_newton_schulz")
 
 
 def gf_muon_workspace_bytes(desc: gf_muon_desc) -> int:
@@ -391,7 +407,7 @@ def gf_muon_workspace_bytes(desc: gf_muon_desc) -> int:
 def _ptrs(tensors, count: int):
     if len(tensors) != count:
         raise ValueError(f"{count} tensors expected, got {len(tensors)}")
-    return (ctypes.c_void_p * count)(*[_ptr(t).value for t in tensors])
+    return (ctypes.c_void_p * count)(*map(_addr, tensors))
 
 
 def gf_muon_step(desc: gf_muon_desc, grads, momenta, weights, momenta_out, weights_out, workspace, workspace_bytes=None,
@@ -401,8 +417,8 @@ def gf_muon_step(desc: gf_muon_desc, grads, momenta, weights, momenta_out, weigh
         workspace_bytes = _nbytes(workspace)
     n = desc.count
     _check(lib().gf_muon_step(ctypes.byref(desc), _ptrs(grads, n), _ptrs(momenta, n), _ptrs(weights, n), _ptrs(momenta_out, n),
-                              _ptrs(weights_out, n), _ptr(workspace), workspace_bytes, _coeffs(coeffs, desc.steps),
-                              _stream(stream)), "gf_muon_step")
+                              _ptrs(weights_out, n), _addr(workspace), workspace_bytes, _coeffs(coeffs, desc.steps),
+                              _raw_stream(stream)), "gf_muon_step")
 
 
 def gf_selftest_bounded_wait(workspace, limit_cycles: int, stream=None) -> None:

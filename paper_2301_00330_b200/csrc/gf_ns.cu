@@ -16,6 +16,8 @@
 // boxes of 8 KB fed 44 bytes per clock and SM, and results written row by row took 10 us a tile.)
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "gf_common.cuh"
 #include "gf_tc.cuh"
 #include "gf_tma.cuh"
@@ -300,6 +302,8 @@ struct IterateArgs {
     float coeff[GF_NS_MAX_STEPS][3];
     int batch, m, n, steps;
     __half *x[2], *a, *b;
+    float* trace;                  // [matrix][rows / 32]: sums of A's diagonal over 32 rows, times kScale
+    int blocks;                    // of 32 rows
     int x_pieces, a_pieces;        // of 8 columns
     long long x_lo, a_lo;          // elements from the high to the low parts
     uint32_t *err_word, *barrier;
@@ -381,6 +385,13 @@ __device__ __forceinline__ void store_pairs(__half* p, long long piece, long lon
     }
 }
 
+// B = b A + c A A near convergence is close to a multiple of the identity, -2.7 I, against which a X = 3.4 X is then set: most of
+// what rounding B and X to fp16 costs is lost on that multiple.  It is taken out: with s = b t + c t^2, t the mean
+// eigenvalue of A (its trace / m), B - s I is what is rounded and multiplied, and (a + s) X is added in fp32.  Pairs do
+// not need it.  (96 x 576
+// in fp16 operands: error of O 1.8e-3 without, 1.1e-3 with it.)
+__device__ __forceinline__ float shift_of(float mean, float cb, float cc) { return mean * (cb + cc * mean); }
+
 // The values that the results of a block of 32 x 32 need besides the sums: A for the polynomial, X for the
 // last product of a step.  Row i, columns j0 ...
 template <int SPLIT>
@@ -397,18 +408,31 @@ __device__ __forceinline__ void fetch(const IterateArgs& p, int phase, int step,
 // blocks above it not at all; a block is a warp's, so that nothing here diverges.  Columns past the matrix hold
 // zeros: their sums are of zeros.
 template <int SPLIT>
-__device__ __forceinline__ void emit(const IterateArgs& p, int phase, int step, int b, int i, int j0, const Pairs& r, float (&v)[32]) {
+__device__ __forceinline__ void emit(const IterateArgs& p, int phase, int step, int b, int i, int j0, float shift, const Pairs& r, float (&v)[32]) {
     if (phase == PH_APPLY) {
         if (i >= p.m) return;
         // a X is added in fp32 from the pair, so that only the smaller part of the step sees rounded operands
-        add_pairs(r, true, p.coeff[step][0], kInvScale, v);
+        add_pairs(r, true, p.coeff[step][0] + shift, kInvScale, v);
         store_pairs(p.x[(step + 1) & 1] + (((long long)b * p.x_pieces + (j0 >> 3)) * p.m + i) * 8, 8LL * p.m, p.x_lo, true,
                     p.x_pieces - (j0 >> 3), v);
         return;
     }
+    const bool on_diagonal = j0 == (i & ~31);                 // the same for the whole warp
+    if (SPLIT == 1 && phase == PH_GRAM && on_diagonal) {
+        float d = 0.f;
+#pragma unroll
+        for (int k = 0; k < 32; ++k) if (k == (i & 31) && i < p.m) d = v[k];
+        d = warp_sum(d) * kInvScale;
+        if ((i & 31) == 0) p.trace[b * p.blocks + (i >> 5)] = d;
+    }
     if (i >= 8 * p.a_pieces) return;
-    if (phase == PH_POLY) add_pairs(r, SPLIT == 2, p.coeff[step][1], p.coeff[step][2] * kInvScale, v);
-    else {
+    if (phase == PH_POLY) {
+        add_pairs(r, SPLIT == 2, p.coeff[step][1], p.coeff[step][2] * kInvScale, v);
+        if (SPLIT == 1 && on_diagonal) {
+#pragma unroll
+            for (int k = 0; k < 32; ++k) if (k == (i & 31)) v[k] -= shift * kScale;
+        }
+    } else {
 #pragma unroll
         for (int k = 0; k < 32; ++k) v[k] *= kInvScale;
     }
@@ -518,8 +542,38 @@ __device__ __forceinline__ bool grid_meet(const IterateArgs& p, uint32_t target,
     return *flag != 0;
 }
 
+// Matrix, row and column of tile t of a phase.
+template <int ROWS> __device__ __forceinline__ void tile_of(const PhaseShape& ps, bool symmetric, int t, int& b, int& ti, int& tj) {
+    b = t / ps.tiles;
+    const int tt = t - b * ps.tiles;
+    if (symmetric) lower_tile(tt, ps.bn == ROWS, ti, tj);
+    else { ti = tt / ps.tiles_n; tj = tt - ti * ps.tiles_n; }
+}
+
+// What a phase multiplies, and how.
+struct PhaseView {
+    int step, phase, chunks, segment, total, share;
+    bool symmetric;
+    uint32_t a_bytes, b_bytes;
+};
+template <int SPLIT, bool PAIR> __device__ __forceinline__ PhaseView phase_view(const IterateArgs& p, int turn) {
+    PhaseView v;
+    v.step = turn / 3;
+    v.phase = turn - 3 * v.step;
+    v.symmetric = v.phase != PH_APPLY;
+    v.chunks = ((v.phase == PH_GRAM ? p.n : p.m) + 63) / 64;
+    v.segment = SPLIT == 2 ? kSegment : v.chunks;
+    v.total = p.shape[v.phase].tiles * p.batch;
+    v.share = PAIR ? p.shape[v.phase].bn / 2 : p.shape[v.phase].bn;         // columns of the second operand held here
+    v.a_bytes = 128 * 128;
+    v.b_bytes = (uint32_t)v.share * 128;
+    return v;
+}
+
 // The whole iteration in one launch: every phase deals its tiles (of all matrices) to the CTAs or pairs in turn, and
-// all meet between phases.
+// all meet between phases.  Each role has a loop over the phases of its own, so that its registers are its own.
+// The two issuing warps run as whole warps and elect the thread that issues: descriptors and addresses then stay in
+// uniform registers.  (With the loop under `lane == 0` every product took 110 clocks to issue, whatever its size.)
 template <int SPLIT, bool PAIR> __global__ void __launch_bounds__(kThreads, 1) ns_iterate_kernel(const __grid_constant__ IterateArgs p) {
     extern __shared__ unsigned char dyn_raw[];
     unsigned char* dyn = align1024(dyn_raw);
@@ -530,6 +584,7 @@ template <int SPLIT, bool PAIR> __global__ void __launch_bounds__(kThreads, 1) n
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;      // uniform
     const uint32_t rank = PAIR ? cluster_rank() : 0u;
     const int unit = PAIR ? blockIdx.x >> 1 : blockIdx.x, units = PAIR ? gridDim.x >> 1 : gridDim.x;
+    const int turns = 3 * p.steps;
     if (threadIdx.x == 0) {
         for (int s = 0; s < kMaxStages; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
         for (int s = 0; s < 2; ++s) { mbar_init(&done[s], 1); mbar_init(&drained[s], PAIR ? 16 : 8); }
@@ -548,37 +603,21 @@ template <int SPLIT, bool PAIR> __global__ void __launch_bounds__(kThreads, 1) n
     const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_base, 0);
     asm volatile("fence.proxy.async;" ::: "memory");
     bool ok = true;
-    uint32_t ring = 0;                 // one bit per stage: the parity of its next use
-    uint32_t use = 0;                  // accumulators taken so far (products), emptied so far (results)
+    auto meet = [&](int turn) { return turn + 1 == turns || grid_meet(p, (uint32_t)(turn + 1) * gridDim.x, ok, &flag); };
 
-    for (int turn = 0; turn < 3 * p.steps; ++turn) {
-        const int step = turn / 3, phase = turn - 3 * step;
-        const PhaseShape ps = p.shape[phase];
-        const bool symmetric = phase != PH_APPLY;
-        const int K = phase == PH_GRAM ? p.n : p.m;
-        const int chunks = (K + 63) / 64;
-        const int segment = SPLIT == 2 ? kSegment : chunks;
-        const int total = ps.tiles * p.batch;
-        const int share = PAIR ? ps.bn / 2 : ps.bn;         // columns of the second operand held here
-        const uint32_t a_bytes = 128 * 128, b_bytes = (uint32_t)share * 128;
-        auto tile_at = [&](int t, int& b, int& ti, int& tj) {
-            b = t / ps.tiles;
-            const int tt = t - b * ps.tiles;
-            if (symmetric) lower_tile(tt, ps.bn == kRows, ti, tj);
-            else { ti = tt / ps.tiles_n; tj = tt - ti * ps.tiles_n; }
-        };
-        // The two issuing warps run their loops as whole warps and elect the thread that issues: descriptors and addresses
-        // then stay in uniform registers.  (With the loop under `lane == 0` every product took 110 clocks to issue, whatever its
-        // size.)
-        if (warp == 0) {
-            const CUtensorMap* ta = phase == PH_GRAM ? &p.tm_a[step & 1] : phase == PH_POLY ? &p.tm_a[2] : &p.tm_a[3];
-            const CUtensorMap* tb = phase == PH_GRAM ? &p.tm_g[step & 1] : phase == PH_POLY ? &p.tm_g[2] : &p.tm_n[step & 1];
+    if (warp == 0) {
+        uint32_t ring = 0;             // one bit per stage: the parity of its next use
+        for (int turn = 0; turn < turns && ok; ++turn) {
+            const PhaseView v = phase_view<SPLIT, PAIR>(p, turn);
+            const PhaseShape& ps = p.shape[v.phase];
+            const CUtensorMap* ta = v.phase == PH_GRAM ? &p.tm_a[v.step & 1] : v.phase == PH_POLY ? &p.tm_a[2] : &p.tm_a[3];
+            const CUtensorMap* tb = v.phase == PH_GRAM ? &p.tm_g[v.step & 1] : v.phase == PH_POLY ? &p.tm_g[2] : &p.tm_n[v.step & 1];
             int s = 0;
-            for (int t = unit; t < total && ok; t += units) {
+            for (int t = unit; t < v.total && ok; t += units) {
                 int b, ti, tj;
-                tile_at(t, b, ti, tj);
-                const int row = ti * kRows + (int)rank * 128, col = tj * ps.bn + (int)rank * share;
-                for (int q = 0; q < chunks; ++q) {
+                tile_of<kRows>(ps, v.symmetric, t, b, ti, tj);
+                const int row = ti * kRows + (int)rank * 128, col = tj * ps.bn + (int)rank * v.share;
+                for (int q = 0; q < v.chunks; ++q) {
                     ok = __all_sync(0xffffffffu, mbar_wait_bounded(&empty[s], ((ring >> s) & 1u) ^ 1u));
                     if (!ok) break;
                     if (elect_one()) {
@@ -587,9 +626,9 @@ template <int SPLIT, bool PAIR> __global__ void __launch_bounds__(kThreads, 1) n
 #pragma unroll
                         for (int h = 0; h < SPLIT; ++h) {
                             const int z = h * p.batch + b;
-                            unsigned char* sb = st + SPLIT * a_bytes + h * b_bytes;
-                            load_box<PAIR>(st + h * a_bytes, ta, row * 2, q * 8, z, &full[s]);
-                            if (symmetric) load_box<PAIR>(sb, tb, col * 2, q * 8, z, &full[s]);
+                            unsigned char* sb = st + SPLIT * v.a_bytes + h * v.b_bytes;
+                            load_box<PAIR>(st + h * v.a_bytes, ta, row * 2, q * 8, z, &full[s]);
+                            if (v.symmetric) load_box<PAIR>(sb, tb, col * 2, q * 8, z, &full[s]);
                             else load_box<PAIR>(sb, tb, q * 128, col / 8, z, &full[s]);
                         }
                     }
@@ -598,19 +637,25 @@ template <int SPLIT, bool PAIR> __global__ void __launch_bounds__(kThreads, 1) n
                     if (++s == ps.stages) s = 0;
                 }
             }
-        } else if (warp == 1) {
+            ok = meet(turn);
+        }
+    } else if (warp == 1) {
+        uint32_t ring = 0, use = 0;    // use: accumulators taken so far
+        for (int turn = 0; turn < turns && ok; ++turn) {
+            const PhaseView v = phase_view<SPLIT, PAIR>(p, turn);
+            const PhaseShape& ps = p.shape[v.phase];
             if (rank == 0) {
                 // fp16 x fp16 -> fp32; B is K-major in the symmetric products, MN-major otherwise
-                const uint32_t idesc = (1u << 4) | ((symmetric ? 0u : 1u) << 16) | ((uint32_t)(ps.bn >> 3) << 17) | ((uint32_t)(kRows >> 4) << 24);
+                const uint32_t idesc = (1u << 4) | ((v.symmetric ? 0u : 1u) << 16) | ((uint32_t)(ps.bn >> 3) << 17) | ((uint32_t)(kRows >> 4) << 24);
                 const uint64_t a_form = plain_smem_desc(0, 2048, 128);
-                const uint64_t b_form = symmetric ? plain_smem_desc(0, (uint32_t)share * 16u, 128) : plain_smem_desc(0, 128, 1024);
-                const uint32_t b_step = (symmetric ? (uint32_t)share * 32u : 256u) >> 4;      // 16 k further, in 16 bytes
-                const uint32_t ring0 = smem_u32(dyn) >> 4;
+                const uint64_t b_form = v.symmetric ? plain_smem_desc(0, (uint32_t)v.share * 16u, 128) : plain_smem_desc(0, 128, 1024);
+                const uint32_t b_step = (v.symmetric ? (uint32_t)v.share * 32u : 256u) >> 4;      // 16 k further, in 16 bytes
+                const uint32_t ring0 = smem_u32(dyn) >> 4;      // (in the first CTA of a pair, whose addresses carry no rank)
                 int s = 0;
-                for (int t = unit; t < total && ok; t += units) {
-                    for (int q = 0; q < chunks; ++q) {
+                for (int t = unit; t < v.total && ok; t += units) {
+                    for (int q = 0; q < v.chunks; ++q) {
                         const int buf = (int)(use & 1u);
-                        const bool first = q % segment == 0, last = q % segment == segment - 1 || q == chunks - 1;
+                        const bool first = q % v.segment == 0, last = q % v.segment == v.segment - 1 || q == v.chunks - 1;
                         if (first && use >= 2) ok = mbar_wait_bounded(&drained[buf], ((use >> 1) - 1) & 1u);
                         if (ok) ok = mbar_wait_bounded(&full[s], (ring >> s) & 1u);
                         ok = __all_sync(0xffffffffu, ok);
@@ -619,8 +664,8 @@ template <int SPLIT, bool PAIR> __global__ void __launch_bounds__(kThreads, 1) n
                         if (elect_one()) {
                             const uint32_t d = tmem + (uint32_t)(buf * 256);
                             const uint32_t at = ring0 + (uint32_t)s * ((uint32_t)ps.stage_bytes >> 4);
-                            const uint64_t a_hi = a_form + at, a_lo = a_hi + (a_bytes >> 4);
-                            const uint64_t b_hi = b_form + at + SPLIT * (a_bytes >> 4), b_lo = b_hi + (b_bytes >> 4);
+                            const uint64_t a_hi = a_form + at, a_lo = a_hi + (v.a_bytes >> 4);
+                            const uint64_t b_hi = b_form + at + SPLIT * (v.a_bytes >> 4), b_lo = b_hi + (v.b_bytes >> 4);
 #pragma unroll
                             for (int ks = 0; ks < 4; ++ks) {
                                 mma_f16<PAIR>(d, a_hi + ks * 256, b_hi + ks * b_step, idesc, !(first && ks == 0));
@@ -639,20 +684,34 @@ template <int SPLIT, bool PAIR> __global__ void __launch_bounds__(kThreads, 1) n
                     }
                 }
             }
-        } else {
+            ok = meet(turn);
+        }
+    } else {
+        uint32_t use = 0;              // accumulators emptied so far
+        for (int turn = 0; turn < turns && ok; ++turn) {
+            const PhaseView view = phase_view<SPLIT, PAIR>(p, turn);
+            const PhaseShape& ps = p.shape[view.phase];
+            const int step = view.step, phase = view.phase, chunks = view.chunks, segment = view.segment, total = view.total;
+            const bool symmetric = view.symmetric;
             const int quarter = warp & 3, half = (warp - 2) >> 2;
             const int cols = ps.bn / 2;                       // of this warp
             constexpr int kChunks = PAIR ? 4 : 2;             // of 32 columns, at most
             const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * cols);
             for (int t = unit; t < total && ok; t += units) {
                 int b, ti, tj;
-                tile_at(t, b, ti, tj);
+                tile_of<kRows>(ps, symmetric, t, b, ti, tj);
                 const int i0 = ti * kRows + (int)rank * 128 + quarter * 32, i = i0 + lane;
                 const int j0 = tj * ps.bn + half * cols;
                 // columns past the matrix, or past the diagonal of the warp's rows, are not read (the same for the whole warp)
                 const int reach = i0 >= p.m ? 0 : symmetric ? min(p.m, i0 + 32) : p.n;
                 Pairs pr;
                 if (j0 < reach) fetch<SPLIT>(p, phase, step, b, i, j0, pr);        // on its way while the product runs
+                float shift = 0.f;
+                if (SPLIT == 1 && phase != PH_GRAM) {
+                    float trace = 0.f;
+                    for (int k = lane; k < p.blocks; k += 32) trace += p.trace[b * p.blocks + k];
+                    shift = shift_of(warp_sum(trace) * kInvScale / (float)p.m, p.coeff[step][1], p.coeff[step][2]);
+                }
                 float acc[SPLIT == 2 ? kChunks : 1][32];
                 if constexpr (SPLIT == 2) {
 #pragma unroll
@@ -678,7 +737,7 @@ template <int SPLIT, bool PAIR> __global__ void __launch_bounds__(kThreads, 1) n
                                 tmem_ld_wait();
 #pragma unroll
                                 for (int k = 0; k < 32; ++k) acc[0][k] = __uint_as_float(raw[k]);
-                                emit<SPLIT>(p, phase, step, b, i, j, now, acc[0]);
+                                emit<SPLIT>(p, phase, step, b, i, j, shift, now, acc[0]);
                                 __syncwarp();                 // the next read of tensor memory is the whole warp's
                             } else {
                                 tmem_ld_wait();
@@ -700,16 +759,13 @@ template <int SPLIT, bool PAIR> __global__ void __launch_bounds__(kThreads, 1) n
                     for (int c = 0; c < kChunks; ++c) {
                         if (c * 32 < cols && j0 + c * 32 < reach) {
                             if (c > 0) fetch<SPLIT>(p, phase, step, b, i, j0 + c * 32, pr);
-                            emit<SPLIT>(p, phase, step, b, i, j0 + c * 32, pr, acc[c]);
+                            emit<SPLIT>(p, phase, step, b, i, j0 + c * 32, shift, pr, acc[c]);
                         }
                         __syncwarp();
                     }
                 }
             }
-        }
-        if (turn + 1 < 3 * p.steps) {
-            ok = grid_meet(p, (uint32_t)(turn + 1) * gridDim.x, ok, &flag);
-            if (!ok) break;
+            ok = meet(turn);
         }
     }
     if (!ok) {
@@ -727,13 +783,476 @@ template <int SPLIT, bool PAIR> __global__ void __launch_bounds__(kThreads, 1) n
     }
 }
 
+// ---- small matrices ---------------------------------------------------------------------------------------
+// m <= 128 and n <= 2048: a cluster of CTAs per matrix holds everything on chip for the whole call, in one launch.  A CTA has a slice
+// of at most 256 columns of X: as fp32 in tensor memory and as fp16 (pairs) in shared memory.  Only X X^T needs the other
+// slices: every CTA owns some of its columns, the others send it their partial sums of these (stores into its shared
+// memory), it adds them in the order of the ranks and sends the result to all.  The polynomial is computed by every
+// CTA, B X by each for its slice.  (The general kernel takes 4 to 5 us per product of this size, of which the product
+// itself is a tenth: two passes through L2 and a meeting of the grid.  Reading the others' sums instead of being sent
+// them took 4500 clocks per step, three times as long.)
+constexpr int kSmallThreads = 256;
+constexpr int kSmallCols = 256;            // columns of a slice, at most
+constexpr int kSmallCluster = 8;
+constexpr int kSmallPart = 86016;          // partial sums that a CTA is sent: at most 7 x 3 pieces of 4 KB; also tiles on their way in and out
+// A or B: 32 KB, as pairs 64, then in the partial sums' place (all together would not fit)
+constexpr int small_region(int split) { return split == 1 ? kSmallPart + 32768 : kSmallPart; }
+
+struct SmallArgs {
+    Source src;
+    const void* w[kMaxLayers];             // Muon: weights
+    void* w_out[kMaxLayers];
+    void* out;                             // O
+    int m, n, slice, cluster, transposed, steps;
+    int out_bf16, taps;
+    float keep, f, eps;
+    float coeff[GF_NS_MAX_STEPS][3];
+    FastDiv div_taps;
+    uint32_t *err_word, *status;           // the library's word for waits that run out; the workspace's, cleared here
+};
+
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]),
+        "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]),
+        "r"(r[31])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ uint32_t peer_addr(uint32_t addr, int rank) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void peer_store4(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ uint32_t pack_half2(float x, float y) {
+    const __half2 h = __floats2half2_rn(x, y);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+// (hi, lo) of a pair of values as fp16
+__device__ __forceinline__ void split_half2(float x, float y, uint32_t& hi, uint32_t& lo) {
+    const __half2 h = __floats2half2_rn(x, y);
+    const float2 back = __half22float2(h);
+    hi = *reinterpret_cast<const uint32_t*>(&h);
+    lo = pack_half2(x - back.x, y - back.y);
+}
+
+template <int SPLIT, bool MUON> __global__ void __launch_bounds__(kSmallThreads, 1) ns_small_kernel(const __grid_constant__ SmallArgs p) {
+    extern __shared__ unsigned char dyn_raw[];
+    unsigned char* const region = align1024(dyn_raw);                     // partial sums, tiles
+    unsigned char* const as = region + (SPLIT == 1 ? kSmallPart : 0);     // A / B: [part][16][128][8] fp16
+    unsigned char* const xs = region + (SPLIT == 1 ? kSmallPart + 32768 : kSmallPart);      // X: [part][slice / 8][128][8] fp16
+    __shared__ uint64_t bar;
+    __shared__ uint32_t tmem_base;
+    __shared__ double red[kSmallThreads / 32], total;
+    __shared__ uint32_t send_to[16];                                      // where the partial sums of a piece of 8 columns go
+    const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
+    const int quarter = warp & 3, half = warp >> 2, row = quarter * 32 + lane;      // tensor memory: this thread's lane
+    const int rank = p.cluster > 1 ? (int)cluster_rank() : 0, b = blockIdx.x / p.cluster;
+    const int c0 = rank * p.slice, width = max(0, min(p.slice, p.n - c0));          // columns of X that this CTA has
+    const uint32_t x_lo = (uint32_t)p.slice * 256u;                                 // bytes to the low parts
+    const Source& s = p.src;
+    auto all_meet = [&] { if (p.cluster > 1) cluster_meet(); else __syncthreads(); };
+    if (tid == 0) {
+        mbar_init(&bar, 1);
+        mbar_fence_init();
+        if (blockIdx.x == 0) *p.status = 0;
+    }
+    if (warp == 0) { tmem_alloc(&tmem_base, 512); tmem_relinquish(); }
+    tc_fence_before_sync();
+    all_meet();
+    tc_fence_after_sync();
+    const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_base, 0);
+    const uint32_t tx = tmem + ((uint32_t)(quarter * 32) << 16), td = tx + 256u;    // X; sums
+    bool ok = true;
+    uint32_t phase = 0;
+
+    // ---- in: 64 columns of X at a time through a tile [column][row], raw into tensor memory
+    float* tile = reinterpret_cast<float*>(region);                       // [64][129]
+    // Pieces of 8 columns of A: rank r owns those from r P / cluster on.  Rows and pieces past the matrix stay out.
+    const int P = (p.m + 7) / 8;
+    auto first_of = [&](int r) { return (r * P + p.cluster - 1) / p.cluster; };
+    const int mine = first_of(rank), count = first_of(rank + 1) - mine;   // at most 8
+    if (p.cluster > 1 && tid < P) {
+        const int owner = tid * p.cluster / P, first = first_of(owner), n = first_of(owner + 1) - first;
+        send_to[tid] = peer_addr(smem_u32(region) + (uint32_t)((rank * n + tid - first) * 4096), owner);      // there: [rank][piece][column / 4][row][4]
+    }
+    float q = 0.f;
+    for (int j0 = 0; j0 < p.slice; j0 += 64) {
+        float u[32];
+        // the type is asked for outside the loop, so that all 32 loads are on their way at once
+        auto take = [&](const auto* g) {
+            const int i = p.transposed ? tid & 127 : tid >> 6, j = j0 + (p.transposed ? tid >> 7 : tid & 63);
+            const int di = p.transposed ? 0 : 4, dj = p.transposed ? 2 : 0;
+            const long long e0 = p.transposed ? (long long)(c0 + j) * s.cols + i : (long long)i * s.cols + c0 + j;
+            const long long de = p.transposed ? 2LL * s.cols : 4LL * s.cols;
+            g += (s.batched ? (long long)b * s.rows * s.cols : 0) + e0 * s.taps;
+#pragma unroll
+            for (int k = 0; k < 32; ++k) u[k] = i + di * k < p.m && j + dj * k < width ? to_f32(g[de * s.taps * k]) : 0.f;
+            if constexpr (MUON) {
+                const float* from = s.mom[b] + e0;
+                float* to = s.mom_out[b] + e0;
+                float mo[32];
+#pragma unroll
+                for (int k = 0; k < 32; ++k) mo[k] = i + di * k < p.m && j + dj * k < width ? from[de * k] : 0.f;
+#pragma unroll
+                for (int k = 0; k < 32; ++k) {
+                    mo[k] = s.momentum * mo[k] + (1.f - s.momentum) * u[k];
+                    u[k] = s.nesterov ? (1.f - s.momentum) * u[k] + s.momentum * mo[k] : mo[k];
+                    if (i + di * k < p.m && j + dj * k < width) to[de * k] = mo[k];
+                }
+            }
+        };
+        if (s.bf16) take(static_cast<const __nv_bfloat16*>(s.g[s.batched ? 0 : b]));
+        else take(static_cast<const float*>(s.g[s.batched ? 0 : b]));
+#pragma unroll
+        for (int k = 0; k < 32; ++k) {
+            const int i = p.transposed ? tid & 127 : (tid >> 6) + 4 * k, j = p.transposed ? (tid >> 7) + 2 * k : tid & 63;
+            tile[j * 129 + i] = u[k];
+            q += u[k] * u[k];
+        }
+        __syncthreads();
+        if (j0 + half * 32 < p.slice) {
+            uint32_t v[32];
+#pragma unroll
+            for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(tile[(half * 32 + k) * 129 + row]);
+            tmem_st32(tx + (uint32_t)(j0 + half * 32), v);
+        }
+        __syncthreads();
+    }
+    tmem_st_wait();
+    // ---- norm of the whole matrix: the CTAs' sums in the order of their ranks
+    {
+        double d = q;
+        for (int o = 16; o > 0; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
+        if (lane == 0) red[warp] = d;
+        __syncthreads();
+        if (tid == 0) {
+            for (int w = 1; w < kSmallThreads / 32; ++w) d += red[w];
+            total = d;
+        }
+        all_meet();
+        d = 0;
+        for (int k = 0; k < p.cluster; ++k) {
+            double v = total;
+            if (p.cluster > 1) asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(peer_addr(smem_u32(&total), k)) : "memory");
+            d += v;
+        }
+        const float scale0 = kScale / ((float)sqrt(d) + p.eps);
+        const float scale = isinf(scale0) ? 0.f : scale0;                 // a matrix of zeros with eps = 0 gives zeros
+        for (int j = half * 32; j < p.slice; j += 64) {
+            uint32_t v[32];
+            tmem_ld32(tx + (uint32_t)j, v);
+            tmem_ld_wait();
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                uint32_t h[4], l[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float x = __uint_as_float(v[8 * g + 2 * e]) * scale, y = __uint_as_float(v[8 * g + 2 * e + 1]) * scale;
+                    v[8 * g + 2 * e] = __float_as_uint(x);
+                    v[8 * g + 2 * e + 1] = __float_as_uint(y);
+                    split_half2(x, y, h[e], l[e]);
+                }
+                if (j + 8 * g < p.slice) {
+                    unsigned char* dst = xs + ((j >> 3) + g) * 2048 + row * 16;
+                    *reinterpret_cast<uint4*>(dst) = make_uint4(h[0], h[1], h[2], h[3]);
+                    if constexpr (SPLIT == 2) *reinterpret_cast<uint4*>(dst + x_lo) = make_uint4(l[0], l[1], l[2], l[3]);
+                }
+            }
+            tmem_st32(tx + (uint32_t)j, v);
+        }
+        tmem_st_wait();
+    }
+
+    // One product, issued by one thread and waited for by all: D (columns from `col` on) = A B over `steps16` steps of 16.
+    // K-major operands: 16-byte columns 2048 bytes apart; B of the last product MN-major.
+    // (in a cluster the bits above a shared address' own 18 name the CTA: they are not the descriptor's)
+    const uint32_t a_at = (smem_u32(as) >> 4) & 0x3FFFu, x_at = (smem_u32(xs) >> 4) & 0x3FFFu;
+    const uint64_t k_major = plain_smem_desc(0, 2048, 128), mn_major = plain_smem_desc(0, 128, 2048);
+    auto begin = [&] {                                       // operands were written through the generic proxy
+        fence_proxy_async_smem();
+        tc_fence_before_sync();
+        all_meet();
+        asm volatile("fence.proxy.async;" ::: "memory");     // those that other CTAs wrote
+        tc_fence_after_sync();
+    };
+    auto finish = [&] {
+        if (ok) ok = mbar_wait_bounded(&bar, phase);         // (after a wait that ran out nothing is waited for any more)
+        phase ^= 1u;
+        tc_fence_after_sync();
+    };
+    const uint32_t rows16 = (uint32_t)(p.m + 15) / 16u;
+
+    for (int step = 0; step < p.steps; ++step) {
+        // ---- partial X X^T: two accumulators of at most 8 steps each (24 additions with pairs)
+        begin();
+        const int k16 = p.slice / 16, first = (k16 + 1) / 2;
+        if (warp == 0 && elect_one()) {
+            const uint32_t idesc = (1u << 4) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
+            for (int k = 0; k < k16; ++k) {
+                const uint64_t hi = k_major + x_at + (uint32_t)k * 256u, lo = hi + (x_lo >> 4);
+                const uint32_t d = tmem + 256u + (k >= first ? 128u : 0u);
+                umma_bf16(d, hi, hi, idesc, k != 0 && k != first);
+                if constexpr (SPLIT == 2) { umma_bf16(d, hi, lo, idesc, 1u); umma_bf16(d, lo, hi, idesc, 1u); }
+            }
+            umma_commit(&bar);
+        }
+        __syncwarp();
+        finish();
+        // this thread's row, 64 columns of half `half`; then to where they are added up
+        const bool two = k16 > first;
+        if (p.cluster == 1) {
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const int j = half * 64 + c * 32;
+                uint32_t v[32], w[32];
+                tmem_ld32(td + (uint32_t)j, v);
+                if (two) tmem_ld32(td + 128u + (uint32_t)j, w);
+                tmem_ld_wait();
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    uint32_t h[4], l[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int k = 8 * g + 2 * e;
+                        const float x = __uint_as_float(v[k]) + (two ? __uint_as_float(w[k]) : 0.f);
+                        const float y = __uint_as_float(v[k + 1]) + (two ? __uint_as_float(w[k + 1]) : 0.f);
+                        split_half2(x * kInvScale, y * kInvScale, h[e], l[e]);
+                    }
+                    unsigned char* dst = as + ((j >> 3) + g) * 2048 + row * 16;
+                    *reinterpret_cast<uint4*>(dst) = make_uint4(h[0], h[1], h[2], h[3]);
+                    if constexpr (SPLIT == 2) *reinterpret_cast<uint4*>(dst + 32768) = make_uint4(l[0], l[1], l[2], l[3]);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const int j = half * 64 + c * 32;
+                if (j >= p.m || quarter * 32 >= p.m) continue;            // the same for the whole warp
+                uint32_t v[32], w[32];
+                tmem_ld32(td + (uint32_t)j, v);
+                if (two) tmem_ld32(td + 128u + (uint32_t)j, w);
+                tmem_ld_wait();
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const int piece = (j >> 3) + g;
+                    if (piece >= P) continue;
+                    float f[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(v[8 * g + e]) + (two ? __uint_as_float(w[8 * g + e]) : 0.f);
+                    const uint32_t to = send_to[piece] + (uint32_t)(row * 16);
+                    peer_store4(to, __float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+                    peer_store4(to + 2048u, __float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7]));
+                }
+            }
+            cluster_meet();
+            float sum[4][8];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int piece = (tid >> 7) + 2 * k, i = tid & 127;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[k][e] = 0.f;
+                if (piece < count && i < p.m)
+                    for (int r = 0; r < p.cluster; ++r) {
+                        const float4 x = *reinterpret_cast<const float4*>(region + (r * count + piece) * 4096 + i * 16);
+                        const float4 y = *reinterpret_cast<const float4*>(region + (r * count + piece) * 4096 + 2048 + i * 16);
+                        sum[k][0] += x.x; sum[k][1] += x.y; sum[k][2] += x.z; sum[k][3] += x.w;
+                        sum[k][4] += y.x; sum[k][5] += y.y; sum[k][6] += y.z; sum[k][7] += y.w;
+                    }
+            }
+            if constexpr (SPLIT == 2) cluster_meet();        // all have added: A may take the partial sums' place
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int piece = (tid >> 7) + 2 * k, i = tid & 127;
+                if (piece < count) {
+                    uint32_t h[4], l[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) split_half2(sum[k][2 * e] * kInvScale, sum[k][2 * e + 1] * kInvScale, h[e], l[e]);
+                    const uint32_t at = smem_u32(as) + (uint32_t)((mine + piece) * 2048 + i * 16);
+                    for (int r = 0; r < p.cluster; ++r) {
+                        const uint32_t to = peer_addr(at, r);
+                        peer_store4(to, h[0], h[1], h[2], h[3]);
+                        if constexpr (SPLIT == 2) peer_store4(to + 32768u, l[0], l[1], l[2], l[3]);
+                    }
+                }
+            }
+            // the odd piece that fills up 16 contracted columns
+            if (P & 1) {
+                if (tid < 128) {
+                    *reinterpret_cast<uint4*>(as + P * 2048 + tid * 16) = make_uint4(0u, 0u, 0u, 0u);
+                    if constexpr (SPLIT == 2) *reinterpret_cast<uint4*>(as + 32768 + P * 2048 + tid * 16) = make_uint4(0u, 0u, 0u, 0u);
+                }
+            }
+        }
+        // ---- A A, and B = b A + c A A in A's place
+        begin();
+        if (warp == 0 && elect_one()) {
+            const uint32_t idesc = (1u << 4) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
+            for (uint32_t k = 0; k < rows16; ++k) {
+                const uint64_t hi = k_major + a_at + k * 256u, lo = hi + (32768u >> 4);
+                umma_bf16(tmem + 256u, hi, hi, idesc, k != 0);
+                if constexpr (SPLIT == 2) { umma_bf16(tmem + 256u, hi, lo, idesc, 1u); umma_bf16(tmem + 256u, lo, hi, idesc, 1u); }
+            }
+            umma_commit(&bar);
+        }
+        __syncwarp();
+        finish();
+        // the mean eigenvalue of A is taken out of B (see `shift_of`); every warp adds the diagonal itself
+        float shift = 0.f;
+        if constexpr (SPLIT == 1) {
+            float trace = 0.f;
+            for (int i = lane; i < p.m; i += 32) trace += __half2float(*reinterpret_cast<const __half*>(as + (i >> 3) * 2048 + i * 16 + (i & 7) * 2));
+            shift = shift_of(warp_sum(trace) * kInvScale / (float)p.m, p.coeff[step][1], p.coeff[step][2]);
+            __syncthreads();                                 // before B takes A's place
+        }
+        const float ca = p.coeff[step][0] + shift, cb = p.coeff[step][1], cc = p.coeff[step][2] * kInvScale;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const int j = half * 64 + c * 32;
+            uint32_t v[32];
+            tmem_ld32(td + (uint32_t)j, v);
+            tmem_ld_wait();
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                unsigned char* at = as + ((j >> 3) + g) * 2048 + row * 16;
+                const uint4 hv = *reinterpret_cast<const uint4*>(at);
+                uint4 lv = make_uint4(0u, 0u, 0u, 0u);
+                if constexpr (SPLIT == 2) lv = *reinterpret_cast<const uint4*>(at + 32768);
+                const uint32_t hw[4] = {hv.x, hv.y, hv.z, hv.w}, lw[4] = {lv.x, lv.y, lv.z, lv.w};
+                uint32_t h[4], l[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int k = 8 * g + 2 * e;
+                    float2 f = __half22float2(*reinterpret_cast<const __half2*>(&hw[e]));
+                    if constexpr (SPLIT == 2) {
+                        const float2 o = __half22float2(*reinterpret_cast<const __half2*>(&lw[e]));
+                        f.x += o.x; f.y += o.y;
+                    }
+                    split_half2(cb * f.x + cc * __uint_as_float(v[k]) - (j + k == row ? shift * kScale : 0.f),
+                                cb * f.y + cc * __uint_as_float(v[k + 1]) - (j + k + 1 == row ? shift * kScale : 0.f), h[e], l[e]);
+                }
+                *reinterpret_cast<uint4*>(at) = make_uint4(h[0], h[1], h[2], h[3]);
+                if constexpr (SPLIT == 2) *reinterpret_cast<uint4*>(at + 32768) = make_uint4(l[0], l[1], l[2], l[3]);
+            }
+        }
+        // ---- B X for this slice, X = a X + B X
+        fence_proxy_async_smem();
+        tc_fence_before_sync();
+        __syncthreads();
+        tc_fence_after_sync();
+        if (warp == 0 && elect_one()) {
+            const uint32_t idesc = (1u << 4) | (1u << 16) | ((uint32_t)(p.slice >> 3) << 17) | ((128u >> 4) << 24);
+            for (uint32_t k = 0; k < rows16; ++k) {
+                const uint64_t hi = k_major + a_at + k * 256u, lo = hi + (32768u >> 4);
+                const uint64_t xhi = mn_major + x_at + k * 16u, xlo = xhi + (x_lo >> 4);
+                umma_bf16(tmem + 256u, hi, xhi, idesc, k != 0);
+                if constexpr (SPLIT == 2) { umma_bf16(tmem + 256u, hi, xlo, idesc, 1u); umma_bf16(tmem + 256u, lo, xhi, idesc, 1u); }
+            }
+            umma_commit(&bar);
+        }
+        __syncwarp();
+        finish();
+        const bool last = step + 1 == p.steps;
+        for (int j = half * 32; j < p.slice; j += 64) {
+            uint32_t v[32], w[32];
+            tmem_ld32(tx + (uint32_t)j, v);
+            tmem_ld32(td + (uint32_t)j, w);
+            tmem_ld_wait();
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                uint32_t h[4], l[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int k = 8 * g + 2 * e;
+                    const float x = ca * __uint_as_float(v[k]) + kInvScale * __uint_as_float(w[k]);
+                    const float y = ca * __uint_as_float(v[k + 1]) + kInvScale * __uint_as_float(w[k + 1]);
+                    v[k] = __float_as_uint(x);
+                    v[k + 1] = __float_as_uint(y);
+                    split_half2(x, y, h[e], l[e]);
+                }
+                if (!last && j + 8 * g < p.slice) {
+                    unsigned char* dst = xs + ((j >> 3) + g) * 2048 + row * 16;
+                    *reinterpret_cast<uint4*>(dst) = make_uint4(h[0], h[1], h[2], h[3]);
+                    if constexpr (SPLIT == 2) *reinterpret_cast<uint4*>(dst + x_lo) = make_uint4(l[0], l[1], l[2], l[3]);
+                }
+            }
+            tmem_st32(tx + (uint32_t)j, v);
+        }
+        tmem_st_wait();
+    }
+
+    // ---- out, through the same tile
+    for (int j0 = 0; j0 < width; j0 += 64) {
+        __syncthreads();
+        if (j0 + half * 32 < p.slice) {
+            uint32_t v[32];
+            tmem_ld32(tx + (uint32_t)(j0 + half * 32), v);
+            tmem_ld_wait();
+#pragma unroll
+            for (int k = 0; k < 32; ++k) tile[(half * 32 + k) * 129 + row] = __uint_as_float(v[k]) * kInvScale;
+        }
+        __syncthreads();
+        const int cols = min(64, width - j0);
+        if constexpr (!MUON) {
+            auto give = [&](auto* o) {
+                const int i = p.transposed ? tid & 127 : tid >> 6, j = p.transposed ? tid >> 7 : tid & 63;
+                const int di = p.transposed ? 0 : 4, dj = p.transposed ? 2 : 0;
+                const long long de = p.transposed ? 2LL * s.cols : 4LL * s.cols;
+                using Out = typename std::remove_pointer<decltype(o)>::type;
+                o += (long long)b * s.rows * s.cols + (p.transposed ? (long long)(c0 + j0 + j) * s.cols + i : (long long)i * s.cols + c0 + j0 + j);
+#pragma unroll
+                for (int k = 0; k < 32; ++k)
+                    if (i + di * k < p.m && j + dj * k < cols) o[de * k] = from_f32<Out>(tile[(j + dj * k) * 129 + i + di * k]);
+            };
+            if (p.out_bf16) give(static_cast<__nv_bfloat16*>(p.out));
+            else give(static_cast<float*>(p.out));
+        } else {
+            // rows of W as they lie in memory: columns j of row i, or (transposed) all i of row j; taps values each
+            const int nr = p.transposed ? cols : p.m, nc = p.transposed ? p.m : cols, span = nc * p.taps;
+            for (int r = warp; r < nr; r += kSmallThreads / 32) {
+                const long long o = (p.transposed ? (long long)(c0 + j0 + r) * s.cols : (long long)r * s.cols + c0 + j0) * p.taps;
+                auto update = [&](const auto* w, auto* out) {
+                    using Weight = typename std::remove_pointer<decltype(out)>::type;
+                    for (int e0 = lane; e0 < span; e0 += 32 * 8) {
+                        float v[8];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) v[k] = e0 + 32 * k < span ? to_f32(w[o + e0 + 32 * k]) : 0.f;
+#pragma unroll
+                        for (int k = 0; k < 8; ++k)
+                            if (e0 + 32 * k < span) {
+                                const int c = (int)p.div_taps.div((uint32_t)(e0 + 32 * k));
+                                out[o + e0 + 32 * k] = from_f32<Weight>(p.keep * v[k] - p.f * tile[p.transposed ? r * 129 + c : c * 129 + r]);
+                            }
+                    }
+                };
+                if (p.out_bf16) update(static_cast<const __nv_bfloat16*>(p.w[b]), static_cast<__nv_bfloat16*>(p.w_out[b]));
+                else update(static_cast<const float*>(p.w[b]), static_cast<float*>(p.w_out[b]));
+            }
+        }
+    }
+    if (!ok) atomicOr(p.err_word, 16384u);
+    tc_fence_before_sync();
+    all_meet();                                              // no CTA leaves while its memory may be read
+    tc_fence_after_sync();
+    if (warp == 0) tmem_dealloc(tmem, 512);
+}
+
 // ---- host side --------------------------------------------------------------------------------------------
 struct NsPlan {
     int batch, rows, cols, m, n, x_pieces, a_pieces, split, transposed;
     int norm_blocks;
-    size_t off_part, off_x[2], off_a, off_b, total;
+    size_t off_part, off_x[2], off_a, off_b, off_trace, total;
     long long x_lo, a_lo;          // elements from the high to the low parts
 };
+
+bool use_small(const NsPlan& p) { return p.m <= 128 && p.n <= kSmallCols * kSmallCluster; }
 
 NsPlan ns_plan(int batch, int rows, int cols, int precision) {
     NsPlan p = {};
@@ -753,7 +1272,8 @@ NsPlan ns_plan(int batch, int rows, int cols, int precision) {
     for (int k = 0; k < 2; ++k) { p.off_x[k] = off; off += up((size_t)p.x_lo * 4, 256); }
     p.off_a = off; off += up((size_t)p.a_lo * 2 * p.split, 256);
     p.off_b = off; off += up((size_t)p.a_lo * 2 * p.split, 256);
-    p.total = off;
+    p.off_trace = off; off += up((size_t)batch * ((p.m + 31) / 32) * 4, 256);
+    p.total = use_small(p) ? 256 : off;
     return p;
 }
 
@@ -837,6 +1357,8 @@ gf_status ns_iterate(const NsPlan& p, char* base, int steps, const float* coeffs
     a.x[1] = reinterpret_cast<__half*>(base + p.off_x[1]);
     a.a = reinterpret_cast<__half*>(base + p.off_a);
     a.b = reinterpret_cast<__half*>(base + p.off_b);
+    a.trace = reinterpret_cast<float*>(base + p.off_trace);
+    a.blocks = (p.m + 31) / 32;
     a.x_pieces = p.x_pieces; a.a_pieces = p.a_pieces; a.x_lo = p.x_lo; a.a_lo = p.a_lo;
     a.err_word = reinterpret_cast<uint32_t*>(base);
     a.barrier = reinterpret_cast<uint32_t*>(base + 128);
@@ -883,6 +1405,35 @@ template <bool MUON> gf_status launch_prepare(const NsPlan& p, const Source& src
     return launch_pdl(ns_cast_kernel<MUON>, grid, block, 0, s, src, (const double*)part, p.norm_blocks, eps, X, p.m, p.n, p.x_pieces, p.x_lo, p.transposed);
 }
 
+template <int SPLIT, bool MUON> gf_status launch_small_t(const SmallArgs& a, int count, cudaStream_t s) {
+    const size_t smem = (size_t)small_region(SPLIT) + (size_t)a.slice * 256 * SPLIT + 1024;
+    static size_t configured[kMaxDevices] = {};
+    if (gf_status st = ensure_dyn_smem(ns_small_kernel<SPLIT, MUON>, smem, configured); st != GF_OK) return st;
+    ProfScope prof(K_NS_PRODUCT, s);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(count * a.cluster)); cfg.blockDim = dim3(kSmallThreads); cfg.dynamicSmemBytes = smem; cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = a.cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, ns_small_kernel<SPLIT, MUON>, a);
+    count_launch();
+    return e == cudaSuccess ? GF_OK : GF_ERR_CUDA;
+}
+// `a` holds the source, the outputs and the update's factors; count matrices.
+gf_status launch_small(const NsPlan& p, SmallArgs& a, bool muon, int count, int steps, const float* coeffs, float eps, char* base, cudaStream_t s) {
+    a.m = p.m; a.n = p.n; a.transposed = p.transposed; a.steps = steps; a.eps = eps;
+    a.cluster = (p.n + kSmallCols - 1) / kSmallCols;
+    a.slice = ((p.n + a.cluster - 1) / a.cluster + 15) / 16 * 16;
+    for (int k = 0; k < steps; ++k)
+        for (int e = 0; e < 3; ++e) a.coeff[k][e] = coeffs ? coeffs[3 * k + e] : kDefaultCoeffs[e];
+    a.err_word = global_err_word();
+    if (!a.err_word) return GF_ERR_CUDA;
+    a.status = reinterpret_cast<uint32_t*>(base);
+    if (muon) return p.split == 2 ? launch_small_t<2, true>(a, count, s) : launch_small_t<1, true>(a, count, s);
+    return p.split == 2 ? launch_small_t<2, false>(a, count, s) : launch_small_t<1, false>(a, count, s);
+}
+
 bool off16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 bool bad_dtype(int d) { return d != GF_F32 && d != GF_BF16; }
 
@@ -922,6 +1473,12 @@ gf_status gf_newton_schulz(const gf_ns_desc* d, const void* G, void* O, void* wo
     Source src = {};
     src.g[0] = G; src.batched = 1; src.bf16 = d->in_dtype == GF_BF16; src.taps = 1; src.rows = d->rows; src.cols = d->cols;
     src.vec = d->cols % 4 == 0;                 // G is on a 16-byte boundary, and so are its rows and matrices, or 8 in bf16
+    if (use_small(p)) {
+        SmallArgs a = {};
+        a.src = src;
+        a.out = O; a.out_bf16 = d->out_dtype == GF_BF16; a.taps = 1;
+        return launch_small(p, a, false, d->batch, d->steps, h_coeffs, d->eps, base, s);
+    }
     if (gf_status st = launch_prepare<false>(p, src, 0, d->batch, base, d->eps, s); st != GF_OK) return st;
     if (gf_status st = ns_iterate(p, base, d->steps, h_coeffs, s); st != GF_OK) return st;
     FinishArgs f = finish_args(p, base, d->steps, 0);
@@ -973,8 +1530,20 @@ gf_status gf_muon_step(const gf_muon_desc* d, const void* const* h_grad, const f
         for (int k = 0; k < n; ++k)
             if (off16(src.g[k]) || off16(src.mom[k]) || off16(src.mom_out[k])) src.vec = 0;
         // the flattened matrix is u (x) (1 .. 1): its norm is sqrt(taps) times that of u
+        if (use_small(p)) {
+            SmallArgs a = {};
+            a.src = src;
+            for (int k = 0; k < n; ++k) { a.w[k] = h_weight[first + k]; a.w_out[k] = h_weight_out[first + k]; }
+            a.out_bf16 = d->weight_dtype == GF_BF16;
+            a.taps = d->taps; a.div_taps = FastDiv((uint32_t)d->taps);
+            a.keep = 1.f - d->lr * d->weight_decay;
+            a.f = d->lr * d->scale / root;
+            if (gf_status st = launch_small(p, a, true, n, d->steps, h_coeffs, d->eps / root, base, s); st != GF_OK) return st;
+            continue;
+        }
         if (gf_status st = launch_prepare<true>(p, src, first, n, base, d->eps / root, s); st != GF_OK) return st;
     }
+    if (use_small(p)) return GF_OK;
     if (gf_status st = ns_iterate(p, base, d->steps, h_coeffs, s); st != GF_OK) return st;
     for (int first = 0; first < d->count; first += kMaxLayers) {
         const int n = d->count - first < kMaxLayers ? d->count - first : kMaxLayers;
