@@ -28,6 +28,7 @@ namespace {
 
 constexpr float kScale = 1024.f, kInvScale = 1.f / 1024.f;
 constexpr int kMaxLayers = 48;              // layers whose pointers travel in one launch's arguments
+constexpr int kArrived = 4096;              // counters of split tiles
 constexpr int kNormBlocks = 256;            // partial sums per matrix, at most
 constexpr int kNormThreads = 256;
 
@@ -79,6 +80,8 @@ template <bool MUON> __global__ void __launch_bounds__(kNormThreads) ns_norm_ker
     pdl_launch_dependents();
     pdl_wait();
     if (err_word && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) { err_word[0] = 0; err_word[32] = 0; }   // and the barrier
+    if (err_word && blockIdx.x == 0 && blockIdx.y == 0)
+        for (int k = threadIdx.x; k < kArrived; k += kNormThreads) err_word[64 + k] = 0;               // and the counters of split tiles
     const int b = blockIdx.y;
     const long long n = (long long)s.rows * s.cols;
     float q = 0.f;
@@ -293,6 +296,7 @@ struct PhaseShape {
     int bn;                        // columns of a tile
     int stages, stage_bytes;       // operand ring of a CTA
     int tiles, tiles_n;            // tiles per matrix; per row of tiles (not symmetric)
+    int splits, per;               // parts of the contracted index that a tile is dealt out in; chunks of 64 of each
 };
 struct IterateArgs {
     CUtensorMap tm_a[4];           // first operands, 128 rows x 64 k: X[0], X[1], A, B
@@ -306,11 +310,14 @@ struct IterateArgs {
     int blocks;                    // of 32 rows
     int x_pieces, a_pieces;        // of 8 columns
     long long x_lo, a_lo;          // elements from the high to the low parts
+    float* partial;                // sums of the parts of split tiles: [tile, CTA of a pair][part][warp][column][lane]
+    uint32_t* arrived;             // [tile, CTA of a pair][warp]: parts that are there; zero between phases
     uint32_t *err_word, *barrier;
 };
 
 constexpr int kMaxStages = 8;
 constexpr int kRing = 196608;              // bytes of the operand ring
+constexpr int kMaxSplits = 8;
 constexpr int kThreads = 320;              // copies, products, eight warps of results
 // k chunks of 64 that one accumulator takes when results are wanted to 32 bits: the tensor core
 // adds without rounding to nearest, so that long sums drift towards zero (K = 2048 in one accumulator: 2e-5
@@ -365,23 +372,46 @@ __device__ __forceinline__ void add_pairs(const Pairs& r, bool has_lo, float sca
         }
     }
 }
-__device__ __forceinline__ void store_pairs(__half* p, long long piece, long long lo, bool has_lo, int live, const float (&f)[32]) {
+// 32 values as packed fp16, and what is left of them.
+__device__ __forceinline__ void pack_pairs(const float (&f)[32], bool has_lo, uint32_t (&h)[16], uint32_t (&l)[16]) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        uint32_t h[4], l[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float x = f[q * 8 + 2 * e], y = f[q * 8 + 2 * e + 1];
-            const __half2 hv = __floats2half2_rn(x, y);
+    for (int e = 0; e < 16; ++e) {
+        const __half2 hv = __floats2half2_rn(f[2 * e], f[2 * e + 1]);
+        h[e] = *reinterpret_cast<const uint32_t*>(&hv);
+        if (has_lo) {
             const float2 back = __half22float2(hv);
-            const __half2 lv = __floats2half2_rn(x - back.x, y - back.y);
-            h[e] = *reinterpret_cast<const uint32_t*>(&hv);
+            const __half2 lv = __floats2half2_rn(f[2 * e] - back.x, f[2 * e + 1] - back.y);
             l[e] = *reinterpret_cast<const uint32_t*>(&lv);
         }
-        if (q < live) {
-            *reinterpret_cast<uint4*>(p + q * piece) = make_uint4(h[0], h[1], h[2], h[3]);
-            if (has_lo) *reinterpret_cast<uint4*>(p + q * piece + lo) = make_uint4(l[0], l[1], l[2], l[3]);
-        }
+    }
+}
+__device__ __forceinline__ void store_row(__half* p, long long piece, int live, const uint32_t (&w)[16]) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        if (q < live) *reinterpret_cast<uint4*>(p + q * piece) = make_uint4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]);
+}
+// The mirror image of a warp's 32 x 32 block (a row per lane): through shared memory in rows of 80 bytes (no bank conflicts), back as
+// transposed 8 x 8 matrices, out as 128 consecutive bytes per instruction.  `out`: row j0 of piece i0 / 8; pieces from
+// `live` on do not exist.
+__device__ __forceinline__ void store_mirror(__half* out, long long piece, int live, unsigned char* buf, const uint32_t (&w)[16]) {
+    const int lane = threadIdx.x & 31;
+    __syncwarp();
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<uint4*>(buf + lane * 80 + q * 16) = make_uint4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]);
+    __syncwarp();
+#pragma unroll
+    for (int o = 0; o < 4; ++o) {
+        if (o >= live) break;
+        uint32_t r[4];
+        const uint32_t at = smem_u32(buf) + (uint32_t)((8 * o + (lane & 7)) * 80 + (lane >> 3) * 16);
+        asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                     : "r"(at)
+                     : "memory");
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            *reinterpret_cast<uint32_t*>(out + o * piece + (8 * q + (lane >> 2)) * 8 + (lane & 3) * 2) = r[q];
     }
 }
 
@@ -408,13 +438,18 @@ __device__ __forceinline__ void fetch(const IterateArgs& p, int phase, int step,
 // blocks above it not at all; a block is a warp's, so that nothing here diverges.  Columns past the matrix hold
 // zeros: their sums are of zeros.
 template <int SPLIT>
-__device__ __forceinline__ void emit(const IterateArgs& p, int phase, int step, int b, int i, int j0, float shift, const Pairs& r, float (&v)[32]) {
+__device__ __forceinline__ void emit(const IterateArgs& p, int phase, int step, int b, int i, int j0, float shift, const Pairs& r, unsigned char* buf,
+                                     float (&v)[32]) {
+    uint32_t h[16], l[16];
     if (phase == PH_APPLY) {
         if (i >= p.m) return;
         // a X is added in fp32 from the pair, so that only the smaller part of the step sees rounded operands
         add_pairs(r, true, p.coeff[step][0] + shift, kInvScale, v);
-        store_pairs(p.x[(step + 1) & 1] + (((long long)b * p.x_pieces + (j0 >> 3)) * p.m + i) * 8, 8LL * p.m, p.x_lo, true,
-                    p.x_pieces - (j0 >> 3), v);
+        pack_pairs(v, true, h, l);
+        __half* out = p.x[(step + 1) & 1] + (((long long)b * p.x_pieces + (j0 >> 3)) * p.m + i) * 8;
+        const int live = p.x_pieces - (j0 >> 3);
+        store_row(out, 8LL * p.m, live, h);
+        store_row(out + p.x_lo, 8LL * p.m, live, l);
         return;
     }
     const bool on_diagonal = j0 == (i & ~31);                 // the same for the whole warp
@@ -425,7 +460,6 @@ __device__ __forceinline__ void emit(const IterateArgs& p, int phase, int step, 
         d = warp_sum(d) * kInvScale;
         if ((i & 31) == 0) p.trace[b * p.blocks + (i >> 5)] = d;
     }
-    if (i >= 8 * p.a_pieces) return;
     if (phase == PH_POLY) {
         add_pairs(r, SPLIT == 2, p.coeff[step][1], p.coeff[step][2] * kInvScale, v);
         if (SPLIT == 1 && on_diagonal) {
@@ -436,20 +470,22 @@ __device__ __forceinline__ void emit(const IterateArgs& p, int phase, int step, 
 #pragma unroll
         for (int k = 0; k < 32; ++k) v[k] *= kInvScale;
     }
-    __half* out = (phase == PH_GRAM ? p.a : p.b) + (long long)b * p.a_pieces * p.m * 8;
-    if (i < p.m) store_pairs(out + ((long long)(j0 >> 3) * p.m + i) * 8, 8LL * p.m, p.a_lo, SPLIT == 2, p.a_pieces - (j0 >> 3), v);
-    else {
+    if (i >= p.m) {                                           // the columns that fill up the last piece of the mirror image
 #pragma unroll
-        for (int k = 0; k < 32; ++k) v[k] = 0.f;       // the columns that fill up the last piece
+        for (int k = 0; k < 32; ++k) v[k] = 0.f;
     }
-    if (j0 < (i & ~31)) {                              // j0 + 31 < m
-        __half* col = out + ((long long)(i >> 3) * p.m + j0) * 8 + (i & 7);
-#pragma unroll
-        for (int k = 0; k < 32; ++k) {
-            const __half h = __float2half_rn(v[k]);
-            col[k * 8] = h;
-            if constexpr (SPLIT == 2) col[k * 8 + p.a_lo] = __float2half_rn(v[k] - __half2float(h));
-        }
+    pack_pairs(v, SPLIT == 2, h, l);
+    __half* out = (phase == PH_GRAM ? p.a : p.b) + (long long)b * p.a_pieces * p.m * 8;
+    if (i < p.m) {
+        __half* row = out + ((long long)(j0 >> 3) * p.m + i) * 8;
+        store_row(row, 8LL * p.m, p.a_pieces - (j0 >> 3), h);
+        if constexpr (SPLIT == 2) store_row(row + p.a_lo, 8LL * p.m, p.a_pieces - (j0 >> 3), l);
+    }
+    if (!on_diagonal) {                                       // below it: j0 + 31 < m
+        const int piece = (i & ~31) >> 3;
+        __half* col = out + ((long long)piece * p.m + j0) * 8;
+        store_mirror(col, 8LL * p.m, p.a_pieces - piece, buf, h);
+        if constexpr (SPLIT == 2) store_mirror(col + p.a_lo, 8LL * p.m, p.a_pieces - piece, buf, l);
     }
 }
 
@@ -552,7 +588,7 @@ template <int ROWS> __device__ __forceinline__ void tile_of(const PhaseShape& ps
 
 // What a phase multiplies, and how.
 struct PhaseView {
-    int step, phase, chunks, segment, total, share;
+    int step, phase, chunks, segment, total, share, splits, per;
     bool symmetric;
     uint32_t a_bytes, b_bytes;
 };
@@ -563,7 +599,9 @@ template <int SPLIT, bool PAIR> __device__ __forceinline__ PhaseView phase_view(
     v.symmetric = v.phase != PH_APPLY;
     v.chunks = ((v.phase == PH_GRAM ? p.n : p.m) + 63) / 64;
     v.segment = SPLIT == 2 ? kSegment : v.chunks;
-    v.total = p.shape[v.phase].tiles * p.batch;
+    v.splits = p.shape[v.phase].splits;
+    v.per = p.shape[v.phase].per;
+    v.total = p.shape[v.phase].tiles * p.batch * v.splits;      // units of work: (tile, part), parts of a tile side by side
     v.share = PAIR ? p.shape[v.phase].bn / 2 : p.shape[v.phase].bn;         // columns of the second operand held here
     v.a_bytes = 128 * 128;
     v.b_bytes = (uint32_t)v.share * 128;
@@ -580,6 +618,7 @@ template <int SPLIT, bool PAIR> __global__ void __launch_bounds__(kThreads, 1) n
     __shared__ uint64_t full[kMaxStages], empty[kMaxStages], done[2], drained[2];
     __shared__ uint32_t tmem_base;
     __shared__ int flag;
+    __shared__ __align__(16) unsigned char mirrors[8][32 * 80];
     constexpr int kRows = PAIR ? 256 : 128;                 // of a tile
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;      // uniform
     const uint32_t rank = PAIR ? cluster_rank() : 0u;
@@ -609,15 +648,16 @@ template <int SPLIT, bool PAIR> __global__ void __launch_bounds__(kThreads, 1) n
         uint32_t ring = 0;             // one bit per stage: the parity of its next use
         for (int turn = 0; turn < turns && ok; ++turn) {
             const PhaseView v = phase_view<SPLIT, PAIR>(p, turn);
-            const PhaseShape& ps = p.shape[v.phase];
+            const PhaseShape ps = p.shape[v.phase];
             const CUtensorMap* ta = v.phase == PH_GRAM ? &p.tm_a[v.step & 1] : v.phase == PH_POLY ? &p.tm_a[2] : &p.tm_a[3];
             const CUtensorMap* tb = v.phase == PH_GRAM ? &p.tm_g[v.step & 1] : v.phase == PH_POLY ? &p.tm_g[2] : &p.tm_n[v.step & 1];
             int s = 0;
             for (int t = unit; t < v.total && ok; t += units) {
                 int b, ti, tj;
-                tile_of<kRows>(ps, v.symmetric, t, b, ti, tj);
+                tile_of<kRows>(ps, v.symmetric, t / v.splits, b, ti, tj);
                 const int row = ti * kRows + (int)rank * 128, col = tj * ps.bn + (int)rank * v.share;
-                for (int q = 0; q < v.chunks; ++q) {
+                const int q0 = t % v.splits * v.per, q1 = min(q0 + v.per, v.chunks);
+                for (int q = q0; q < q1; ++q) {
                     ok = __all_sync(0xffffffffu, mbar_wait_bounded(&empty[s], ((ring >> s) & 1u) ^ 1u));
                     if (!ok) break;
                     if (elect_one()) {
@@ -643,7 +683,7 @@ template <int SPLIT, bool PAIR> __global__ void __launch_bounds__(kThreads, 1) n
         uint32_t ring = 0, use = 0;    // use: accumulators taken so far
         for (int turn = 0; turn < turns && ok; ++turn) {
             const PhaseView v = phase_view<SPLIT, PAIR>(p, turn);
-            const PhaseShape& ps = p.shape[v.phase];
+            const PhaseShape ps = p.shape[v.phase];
             if (rank == 0) {
                 // fp16 x fp16 -> fp32; B is K-major in the symmetric products, MN-major otherwise
                 const uint32_t idesc = (1u << 4) | ((v.symmetric ? 0u : 1u) << 16) | ((uint32_t)(ps.bn >> 3) << 17) | ((uint32_t)(kRows >> 4) << 24);
@@ -653,9 +693,12 @@ template <int SPLIT, bool PAIR> __global__ void __launch_bounds__(kThreads, 1) n
                 const uint32_t ring0 = smem_u32(dyn) >> 4;      // (in the first CTA of a pair, whose addresses carry no rank)
                 int s = 0;
                 for (int t = unit; t < v.total && ok; t += units) {
-                    for (int q = 0; q < v.chunks; ++q) {
+                    const int n = min(v.per, v.chunks - t % v.splits * v.per);
+                    int in = 0;                                 // chunks in the present accumulator
+                    for (int q = 0; q < n; ++q) {
                         const int buf = (int)(use & 1u);
-                        const bool first = q % v.segment == 0, last = q % v.segment == v.segment - 1 || q == v.chunks - 1;
+                        const bool first = in == 0, last = in == v.segment - 1 || q == n - 1;
+                        in = last ? 0 : in + 1;
                         if (first && use >= 2) ok = mbar_wait_bounded(&drained[buf], ((use >> 1) - 1) & 1u);
                         if (ok) ok = mbar_wait_bounded(&full[s], (ring >> s) & 1u);
                         ok = __all_sync(0xffffffffu, ok);
@@ -690,22 +733,29 @@ template <int SPLIT, bool PAIR> __global__ void __launch_bounds__(kThreads, 1) n
         uint32_t use = 0;              // accumulators emptied so far
         for (int turn = 0; turn < turns && ok; ++turn) {
             const PhaseView view = phase_view<SPLIT, PAIR>(p, turn);
-            const PhaseShape& ps = p.shape[view.phase];
-            const int step = view.step, phase = view.phase, chunks = view.chunks, segment = view.segment, total = view.total;
+            const PhaseShape ps = p.shape[view.phase];
+            const int step = view.step, phase = view.phase, segment = view.segment, total = view.total;
             const bool symmetric = view.symmetric;
+            unsigned char* const mirror = mirrors[warp - 2];
             const int quarter = warp & 3, half = (warp - 2) >> 2;
             const int cols = ps.bn / 2;                       // of this warp
             constexpr int kChunks = PAIR ? 4 : 2;             // of 32 columns, at most
             const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * cols);
             for (int t = unit; t < total && ok; t += units) {
                 int b, ti, tj;
-                tile_of<kRows>(ps, symmetric, t, b, ti, tj);
+                tile_of<kRows>(ps, symmetric, t / view.splits, b, ti, tj);
+                const int part = t % view.splits, chunks = min(view.per, view.chunks - part * view.per);
+                const bool split = view.splits > 1;
                 const int i0 = ti * kRows + (int)rank * 128 + quarter * 32, i = i0 + lane;
                 const int j0 = tj * ps.bn + half * cols;
                 // columns past the matrix, or past the diagonal of the warp's rows, are not read (the same for the whole warp)
                 const int reach = i0 >= p.m ? 0 : symmetric ? min(p.m, i0 + 32) : p.n;
+                // where this warp's sums go when the tile is split
+                const int slot = (t / view.splits * (PAIR ? 2 : 1) + (int)rank) * 8 + warp - 2;
+                const long long tile_floats = (long long)cols * 32, part_floats = 8 * tile_floats;
+                float* const place = p.partial + ((long long)(slot >> 3) * view.splits * 8 + (slot & 7)) * tile_floats + lane;
                 Pairs pr;
-                if (j0 < reach) fetch<SPLIT>(p, phase, step, b, i, j0, pr);        // on its way while the product runs
+                if (!split && j0 < reach) fetch<SPLIT>(p, phase, step, b, i, j0, pr);        // on its way while the product runs
                 float shift = 0.f;
                 if (SPLIT == 1 && phase != PH_GRAM) {
                     float trace = 0.f;
@@ -733,11 +783,14 @@ template <int SPLIT, bool PAIR> __global__ void __launch_bounds__(kThreads, 1) n
                             tmem_ld32(lanes + (uint32_t)(buf * 256 + c * 32), raw);
                             if constexpr (SPLIT == 1) {
                                 const Pairs now = pr;
-                                if (c + 1 < kChunks && (c + 1) * 32 < cols && j + 32 < reach) fetch<SPLIT>(p, phase, step, b, i, j + 32, pr);
+                                if (!split && c + 1 < kChunks && (c + 1) * 32 < cols && j + 32 < reach) fetch<SPLIT>(p, phase, step, b, i, j + 32, pr);
                                 tmem_ld_wait();
 #pragma unroll
                                 for (int k = 0; k < 32; ++k) acc[0][k] = __uint_as_float(raw[k]);
-                                emit<SPLIT>(p, phase, step, b, i, j, shift, now, acc[0]);
+                                if (split) {
+#pragma unroll
+                                    for (int k = 0; k < 32; ++k) place[part * part_floats + (c * 32 + k) * 32] = acc[0][k];
+                                } else emit<SPLIT>(p, phase, step, b, i, j, shift, now, mirror, acc[0]);
                                 __syncwarp();                 // the next read of tensor memory is the whole warp's
                             } else {
                                 tmem_ld_wait();
@@ -754,12 +807,50 @@ template <int SPLIT, bool PAIR> __global__ void __launch_bounds__(kThreads, 1) n
                     }
                 }
                 if (!ok) break;
-                if constexpr (SPLIT == 2) {
+                if (split) {
+                    // The warp that brings a tile's last part adds all parts, in their order whoever it is, and goes on.
+                    if constexpr (SPLIT == 2) {
+#pragma unroll
+                        for (int c = 0; c < kChunks; ++c)
+                            if (c * 32 < cols && j0 + c * 32 < reach) {
+#pragma unroll
+                                for (int k = 0; k < 32; ++k) place[part * part_floats + (c * 32 + k) * 32] = acc[c][k];
+                            }
+                    }
+                    __threadfence();
+                    __syncwarp();
+                    uint32_t before = 0;
+                    if (lane == 0) before = atomicAdd(p.arrived + slot, 1u);
+                    before = __shfl_sync(0xffffffffu, before, 0);
+                    if (before != (uint32_t)view.splits - 1u) continue;
+                    __threadfence();
+                    if (lane == 0) p.arrived[slot] = 0;
+#pragma unroll 1
+                    for (int c = 0; c * 32 < cols && j0 + c * 32 < reach; ++c) {
+                        fetch<SPLIT>(p, phase, step, b, i, j0 + c * 32, pr);
+                        float sum[32];
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) sum[k] = 0.f;
+#pragma unroll 1
+                        for (int r = 0; r < view.splits; r += 2) {          // two parts on their way at once, added in order
+                            float x[32], y[32];
+                            const bool two = r + 1 < view.splits;
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) x[k] = __ldcg(place + r * part_floats + (c * 32 + k) * 32);
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) y[k] = two ? __ldcg(place + (r + 1) * part_floats + (c * 32 + k) * 32) : 0.f;
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) sum[k] = (sum[k] + x[k]) + y[k];
+                        }
+                        emit<SPLIT>(p, phase, step, b, i, j0 + c * 32, shift, pr, mirror, sum);
+                        __syncwarp();
+                    }
+                } else if constexpr (SPLIT == 2) {
 #pragma unroll
                     for (int c = 0; c < kChunks; ++c) {
                         if (c * 32 < cols && j0 + c * 32 < reach) {
                             if (c > 0) fetch<SPLIT>(p, phase, step, b, i, j0 + c * 32, pr);
-                            emit<SPLIT>(p, phase, step, b, i, j0 + c * 32, shift, pr, acc[c]);
+                            emit<SPLIT>(p, phase, step, b, i, j0 + c * 32, shift, pr, mirror, acc[c]);
                         }
                         __syncwarp();
                     }
@@ -1245,12 +1336,77 @@ template <int SPLIT, bool MUON> __global__ void __launch_bounds__(kSmallThreads,
 }
 
 // ---- host side --------------------------------------------------------------------------------------------
+struct Shapes {
+    PhaseShape shape[3];
+    bool pair;
+    int units;                     // CTAs or pairs that run at once
+    size_t partial_bytes;
+};
 struct NsPlan {
     int batch, rows, cols, m, n, x_pieces, a_pieces, split, transposed;
     int norm_blocks;
-    size_t off_part, off_x[2], off_a, off_b, off_trace, total;
+    size_t off_part, off_x[2], off_a, off_b, off_trace, off_partial, total;
     long long x_lo, a_lo;          // elements from the high to the low parts
+    Shapes shapes;                 // (not of small matrices)
 };
+
+// Clocks that a phase takes, and its shape with the fewest.  A chunk of 64 of the contracted index costs what its bytes take
+// to come from L2 (58 per clock and SM, measured) or its products take to run, whichever is more; a tile's results cost
+// by their width, under the next tile's products except for the last; a split tile costs the way through L2.  (Splitting:
+// 300 x 3000 219 -> 140 us, 1001 x 2048 264 -> 239, both with pairs of fp16.)
+PhaseShape phase_shape(const NsPlan& p, int phase, bool pair, int units, double* clocks) {
+    PhaseShape best = {};
+    double least = 0;
+    const int rows = pair ? 256 : 128;
+    const bool symmetric = phase != PH_APPLY;
+    const int chunks = ((phase == PH_GRAM ? p.n : p.m) + 63) / 64;
+    for (int bn = rows; bn >= rows / 2; bn >>= 1) {
+        PhaseShape s;
+        s.bn = bn;
+        s.stage_bytes = p.split * (128 + (pair ? bn / 2 : bn)) * 128;
+        s.stages = kRing / s.stage_bytes < kMaxStages ? kRing / s.stage_bytes : kMaxStages;
+        s.tiles_n = ((symmetric ? p.m : p.n) + bn - 1) / bn;
+        s.tiles = symmetric ? lower_tiles(p.m, rows, bn) : (p.m + rows - 1) / rows * s.tiles_n;
+        const double products = (p.split == 2 ? 12 : 4) * (double)(bn / 2 > 48 ? bn / 2 : 48);
+        const double chunk = s.stage_bytes / 58.0 > products ? s.stage_bytes / 58.0 : products;
+        const double results = 1000.0 + 32.0 * bn;
+        const long long all = (long long)s.tiles * p.batch;
+        for (s.splits = 1; s.splits <= kMaxSplits; ++s.splits) {
+            s.per = (chunks + s.splits - 1) / s.splits;
+            if (s.splits > 1 && (all * s.splits > units || s.per < 2 || (s.splits - 1) * s.per >= chunks)) continue;
+            const double t = (double)cdiv64(all * s.splits, units) * s.per * chunk + results + (s.splits > 1 ? 2500.0 + 4.0 * s.splits * bn : 0.0);
+            if (least == 0 || t < least) { least = t; best = s; }
+        }
+    }
+    *clocks = least;
+    return best;
+}
+
+template <int SPLIT> int resident_pairs();
+Shapes choose_shapes(const NsPlan& p) {
+    Shapes best = {};
+    double least = 0;
+    const int pairs = p.split == 2 ? resident_pairs<2>() : resident_pairs<1>();
+    for (int pair = 0; pair <= (pairs > 0 ? 1 : 0); ++pair) {
+        Shapes c = {};
+        c.pair = pair != 0;
+        c.units = pair ? pairs : sm_count();
+        double sum = 0;
+        for (int ph = 0; ph < 3; ++ph) {
+            double t;
+            PhaseShape& s = c.shape[ph];
+            s = phase_shape(p, ph, c.pair, c.units, &t);
+            sum += t;
+            const size_t bytes = s.splits > 1 ? (size_t)s.tiles * p.batch * (pair ? 2 : 1) * s.splits * 8 * (s.bn / 2) * 128 : 0;
+            if (bytes > c.partial_bytes) c.partial_bytes = bytes;
+        }
+        // Pairs take 1.6 times this estimate, with pairs of fp16 1.35 times (measured on both sides of where it decides, fp16 operands: 2048 x 2048 pairs 350 us,
+        // single CTAs 316; 4096 x 4096 1350 and 1770; pairs of fp16: 1001 x 2048 293 and 239, 4096 x 4096 3950 and 4370).
+        if (c.pair) sum *= p.split == 1 ? 1.6 : 1.35;
+        if (least == 0 || sum < least) { least = sum; best = c; }
+    }
+    return best;
+}
 
 bool use_small(const NsPlan& p) { return p.m <= 128 && p.n <= kSmallCols * kSmallCluster; }
 
@@ -1267,48 +1423,30 @@ NsPlan ns_plan(int batch, int rows, int cols, int precision) {
     p.norm_blocks = (int)(per < kNormBlocks ? per : kNormBlocks);
     p.x_lo = 8LL * batch * p.m * p.x_pieces;
     p.a_lo = 8LL * batch * p.m * p.a_pieces;
-    size_t off = 256;
+    size_t off = 256 + kArrived * 4;
     p.off_part = off; off += up((size_t)batch * p.norm_blocks * 8, 256);
     for (int k = 0; k < 2; ++k) { p.off_x[k] = off; off += up((size_t)p.x_lo * 4, 256); }
     p.off_a = off; off += up((size_t)p.a_lo * 2 * p.split, 256);
     p.off_b = off; off += up((size_t)p.a_lo * 2 * p.split, 256);
     p.off_trace = off; off += up((size_t)batch * ((p.m + 31) / 32) * 4, 256);
-    p.total = use_small(p) ? 256 : off;
+    if (use_small(p)) { p.total = 256; return p; }
+    p.shapes = choose_shapes(p);
+    p.off_partial = off; off += up(p.shapes.partial_bytes, 256);
+    p.total = off;
     return p;
 }
 
 const float kDefaultCoeffs[3] = {3.4445f, -4.7750f, 2.0315f};
-
-// Pairs of CTAs where every pair gets a tile of the largest product.
-bool use_pairs(const NsPlan& p, int pairs) {
-    return (long long)((p.m + 255) / 256) * ((p.n + 127) / 128) * p.batch >= pairs;
-}
-
-// The tile width with the least estimated time: rounds of tiles over the CTAs (pairs), times the width plus what a tile
-// costs whatever its width (its rows of the first operand).
-PhaseShape phase_shape(const NsPlan& p, bool symmetric, bool pair, int units) {
-    PhaseShape best = {};
-    double least = 0;
-    const int rows = pair ? 256 : 128;
-    for (int bn = rows; bn >= rows / 2; bn >>= 1) {
-        PhaseShape s;
-        s.bn = bn;
-        s.stage_bytes = p.split * (128 + (pair ? bn / 2 : bn)) * 128;
-        s.stages = kRing / s.stage_bytes < kMaxStages ? kRing / s.stage_bytes : kMaxStages;
-        s.tiles_n = ((symmetric ? p.m : p.n) + bn - 1) / bn;
-        s.tiles = symmetric ? lower_tiles(p.m, rows, bn) : (p.m + rows - 1) / rows * s.tiles_n;
-        const double cost = (double)cdiv64((long long)s.tiles * p.batch, units) * (bn + 64);
-        if (least == 0 || cost < least) { least = cost; best = s; }
-    }
-    return best;
-}
 
 template <int SPLIT, bool PAIR> gf_status launch_iterate(const IterateArgs& a, int units, cudaStream_t s) {
     constexpr size_t smem = (size_t)kRing + 1024;
     static size_t configured[kMaxDevices] = {};
     if (gf_status st = ensure_dyn_smem(ns_iterate_kernel<SPLIT, PAIR>, smem, configured); st != GF_OK) return st;
     long long most = 1;
-    for (const PhaseShape& ps : a.shape) most = (long long)ps.tiles * a.batch > most ? (long long)ps.tiles * a.batch : most;
+    for (const PhaseShape& ps : a.shape) {
+        const long long all = (long long)ps.tiles * a.batch * ps.splits;
+        if (all > most) most = all;
+    }
     const int used = most < units ? (int)most : units;
     ProfScope prof(K_NS_PRODUCT, s);
     cudaLaunchConfig_t cfg = {};
@@ -1362,25 +1500,24 @@ gf_status ns_iterate(const NsPlan& p, char* base, int steps, const float* coeffs
     a.x_pieces = p.x_pieces; a.a_pieces = p.a_pieces; a.x_lo = p.x_lo; a.a_lo = p.a_lo;
     a.err_word = reinterpret_cast<uint32_t*>(base);
     a.barrier = reinterpret_cast<uint32_t*>(base + 128);
-    const int pairs = p.split == 2 ? resident_pairs<2>() : resident_pairs<1>();
-    const bool pair = pairs > 0 && use_pairs(p, pairs);
-    const int units = pair ? pairs : sm_count();
-    a.shape[PH_GRAM] = a.shape[PH_POLY] = phase_shape(p, true, pair, units);
-    a.shape[PH_APPLY] = phase_shape(p, false, pair, units);
+    a.partial = reinterpret_cast<float*>(base + p.off_partial);
+    a.arrived = reinterpret_cast<uint32_t*>(base + 256);
+    const bool pair = p.shapes.pair;
+    const int units = p.shapes.units;
+    for (int k = 0; k < 3; ++k) a.shape[k] = p.shapes.shape[k];
     for (const PhaseShape& ps : a.shape)
         if ((long long)ps.tiles * p.batch > 0x3fffffffLL) return GF_ERR_UNSUPPORTED;
     const uint64_t m = (uint64_t)p.m, b = (uint64_t)p.batch, xp = (uint64_t)p.x_pieces, ap = (uint64_t)p.a_pieces;
-    const uint32_t g_rows = (uint32_t)(pair ? a.shape[PH_GRAM].bn / 2 : a.shape[PH_GRAM].bn);
-    const uint32_t n_cols = (uint32_t)(pair ? a.shape[PH_APPLY].bn / 2 : a.shape[PH_APPLY].bn);
+    auto share = [&](int phase) { return (uint32_t)(pair ? a.shape[phase].bn / 2 : a.shape[phase].bn); };
     // two 8-byte units are the 8 columns of a row
     auto map = [&](CUtensorMap* out, const __half* src, uint64_t pieces, uint64_t planes, uint32_t rows, uint32_t columns) {
         return make_tmap_u64(out, src, 2 * m, pieces, planes, 2 * m, 2 * m * pieces, 2 * rows, columns / 8);
     };
     bool good = map(&a.tm_a[2], a.a, ap, b * p.split, 128, 64) && map(&a.tm_a[3], a.b, ap, b * p.split, 128, 64) &&
-                map(&a.tm_g[2], a.a, ap, b * p.split, g_rows, 64);
+                map(&a.tm_g[2], a.a, ap, b * p.split, share(PH_POLY), 64);
     for (int k = 0; k < 2 && good; ++k)
-        good = map(&a.tm_a[k], a.x[k], xp, 2 * b, 128, 64) && map(&a.tm_g[k], a.x[k], xp, 2 * b, g_rows, 64) &&
-               map(&a.tm_n[k], a.x[k], xp, 2 * b, 64, n_cols);
+        good = map(&a.tm_a[k], a.x[k], xp, 2 * b, 128, 64) && map(&a.tm_g[k], a.x[k], xp, 2 * b, share(PH_GRAM), 64) &&
+               map(&a.tm_n[k], a.x[k], xp, 2 * b, 64, share(PH_APPLY));
     if (!good) return GF_ERR_CUDA;
     if (pair) return p.split == 2 ? launch_iterate<2, true>(a, units, s) : launch_iterate<1, true>(a, units, s);
     return p.split == 2 ? launch_iterate<2, false>(a, units, s) : launch_iterate<1, false>(a, units, s);
