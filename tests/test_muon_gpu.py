@@ -68,7 +68,7 @@ def _run(gf, G, precision="f32", out=torch.float32, steps=5, eps=1e-7, coeffs=No
 SHAPES = [(1, 1, 1), (2, 1, 7), (1, 9, 1), (3, 5, 3), (1, 16, 16), (2, 31, 33), (5, 64, 64), (1, 64, 200), (2, 127, 129), (1, 128, 128),
           (3, 129, 100), (1, 96, 576), (2, 576, 96), (1, 200, 1000), (1, 255, 257), (1, 256, 256), (4, 257, 255), (1, 300, 301),
           (1, 385, 640), (2, 1001, 130), (1, 512, 2048), (1, 700, 513), (3, 100, 1025), (1, 2048, 128), (2, 17, 2047), (1, 128, 2049),
-          (1, 3, 5000), (30, 33, 40)]
+          (1, 3, 5000), (30, 33, 40), (1, 300, 3000), (2, 129, 2500), (1, 700, 1500)]
 
 
 @pytest.mark.parametrize("precision", ["f16", "f32"])
