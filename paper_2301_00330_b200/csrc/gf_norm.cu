@@ -48,6 +48,78 @@ template <typename T, int V> __device__ __forceinline__ void store_vec(T* p, con
     }
 }
 
+// ---- pairs of fp32 --------------------------------------------------------------------------
+// Two fp32 operations per instruction, each half rounded as the scalar operation is; the loops below are bound by instructions
+// and their latency (8192 x 4096 bf16 backward 53 -> 51 us).
+__device__ __forceinline__ void fma2(float (&d)[2], float a0, float a1, float b0, float b1, float c0, float c1) {
+    asm("{\n\t.reg .b64 a, b, c;\n\t"
+        "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+        "fma.rn.f32x2 c, a, b, c;\n\t"
+        "mov.b64 {%0, %1}, c;\n\t}"
+        : "=f"(d[0]), "=f"(d[1])
+        : "f"(a0), "f"(a1), "f"(b0), "f"(b1), "f"(c0), "f"(c1));
+}
+__device__ __forceinline__ void mul2(float (&d)[2], float a0, float a1, float b0, float b1) {
+    asm("{\n\t.reg .b64 a, b;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmul.rn.f32x2 a, a, b;\n\tmov.b64 {%0, %1}, a;\n\t}"
+        : "=f"(d[0]), "=f"(d[1])
+        : "f"(a0), "f"(a1), "f"(b0), "f"(b1));
+}
+__device__ __forceinline__ void add2(float (&d)[2], float a0, float a1, float b0, float b1) {
+    asm("{\n\t.reg .b64 a, b;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 a, a, b;\n\tmov.b64 {%0, %1}, a;\n\t}"
+        : "=f"(d[0]), "=f"(d[1])
+        : "f"(a0), "f"(a1), "f"(b0), "f"(b1));
+}
+// d = a b + c, a b, a + b over V values; S: a scalar in b's (c's) place.
+template <int V> __device__ __forceinline__ void v_fma(float (&d)[V], const float (&a)[V], const float (&b)[V], const float (&c)[V]) {
+    if constexpr (V == 1) d[0] = a[0] * b[0] + c[0];
+    else {
+#pragma unroll
+        for (int i = 0; i < V; i += 2) {
+            float r[2];
+            fma2(r, a[i], a[i + 1], b[i], b[i + 1], c[i], c[i + 1]);
+            d[i] = r[0]; d[i + 1] = r[1];
+        }
+    }
+}
+template <int V> __device__ __forceinline__ void v_fma(float (&d)[V], const float (&a)[V], float b, const float (&c)[V]) {
+    float bb[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) bb[i] = b;
+    v_fma<V>(d, a, bb, c);
+}
+template <int V> __device__ __forceinline__ void v_mul(float (&d)[V], const float (&a)[V], const float (&b)[V]) {
+    if constexpr (V == 1) d[0] = a[0] * b[0];
+    else {
+#pragma unroll
+        for (int i = 0; i < V; i += 2) {
+            float r[2];
+            mul2(r, a[i], a[i + 1], b[i], b[i + 1]);
+            d[i] = r[0]; d[i + 1] = r[1];
+        }
+    }
+}
+template <int V> __device__ __forceinline__ void v_add(float (&d)[V], const float (&a)[V], const float (&b)[V]) {
+    if constexpr (V == 1) d[0] = a[0] + b[0];
+    else {
+#pragma unroll
+        for (int i = 0; i < V; i += 2) {
+            float r[2];
+            add2(r, a[i], a[i + 1], b[i], b[i + 1]);
+            d[i] = r[0]; d[i + 1] = r[1];
+        }
+    }
+}
+template <int V> __device__ __forceinline__ void v_fill(float (&d)[V], float x) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) d[i] = x;
+}
+template <int V> __device__ __forceinline__ float v_sum(const float (&a)[V]) {
+    float s = a[0];
+#pragma unroll
+    for (int i = 1; i < V; ++i) s += a[i];
+    return s;
+}
+
 // gamma or beta: fp32 or bf16, absent = `none`
 struct Param {
     const void* p;
@@ -300,9 +372,9 @@ template <typename T> __global__ void __launch_bounds__(1024) ln_rows_bwd_long_k
 // the sums and stores of the present one.  A batch is one contiguous piece of memory, copied from the 16-byte
 // boundary before it to the one after it.  The last bytes of a tensor whose size is no multiple of 16 are fetched with
 // plain loads.
-// Measured: 100352 x 576 fp32 forward 88 us, 5.2 TB/s (0.80 of the copy bandwidth); 8192 x 4096 bf16 backward 49 us and 4 us
-// for the lines of sums, 4.1 TB/s: with 8 warps per SM (the sums take their registers) it is bound by the latency of
-// each row's exchanges, 22 instructions per element; 16 elements per thread and 16 warps measured 56 us in all.
+// Measured: 100352 x 576 fp32 forward 88 us, 5.2 TB/s (0.80 of the copy bandwidth); 8192 x 4096 bf16 backward 47 us and 4 us
+// for the lines of sums, 4.3 TB/s: with 8 warps per SM (the sums take their registers) it is bound by the latency of
+// each row's exchanges; 16 elements per thread and 16 warps measured 56 us in all.
 //   SHIFT: rows whose length is no multiple of 16 bytes, one to a batch.  The number of teams is a multiple of the period (at most
 //   8) with which the rows' offsets from a 16-byte boundary repeat, so that all rows of a team have the same
 //   offset: its threads own whole aligned vectors, the first and last of which are partly the neighbouring rows'.
@@ -451,7 +523,8 @@ __global__ void __launch_bounds__(BWD ? 256 : 512) ln_rows_ring_kernel(const __g
                 }
             };
             if constexpr (!BWD) {
-                float sum[1] = {0.f}, var[1] = {0.f};
+                float sum[1], var[1], s1[V], minus_mean[V], rstd_v[V];
+                v_fill<V>(s1, 0.f);
 #pragma unroll
                 for (int k = 0; k < NV; ++k) {
                     if (k * step >= C) break;               // the same for all threads
@@ -465,33 +538,35 @@ __global__ void __launch_bounds__(BWD ? 256 : 512) ln_rows_ring_kernel(const __g
 #pragma unroll
                         for (int i = 0; i < V; ++i) v[k][i] = 0.f;
                     }
-#pragma unroll
-                    for (int i = 0; i < V; ++i) sum[0] += v[k][i];
+                    v_add<V>(s1, s1, v[k]);
                 }
+                sum[0] = v_sum<V>(s1);
                 team_sum<TEAM, 1>(sum, a.log_tpr, red[team][0], team, r.warps);
                 const float mean = sum[0] / (float)a.C;
+                v_fill<V>(minus_mean, -mean);
+                v_fill<V>(s1, 0.f);
 #pragma unroll
                 for (int k = 0; k < NV; ++k) {
                     if (k * step >= C) break;
                     if (k * step < width) {
-#pragma unroll
-                        for (int i = 0; i < V; ++i) v[k][i] -= mean;
+                        v_add<V>(v[k], v[k], minus_mean);
                         if (!whole(k)) {
 #pragma unroll
                             for (int i = 0; i < V; ++i) if (!inside(k, i)) v[k][i] = 0.f;
                         }
-#pragma unroll
-                        for (int i = 0; i < V; ++i) var[0] += v[k][i] * v[k][i];
+                        v_fma<V>(s1, v[k], v[k], s1);
                     }
                 }
+                var[0] = v_sum<V>(s1);
                 team_sum<TEAM, 1>(var, a.log_tpr, red[team][1], team, r.warps);
                 const float rstd = rsqrtf(var[0] * a.inv_c + a.eps);
+                v_fill<V>(rstd_v, rstd);
 #pragma unroll
                 for (int k = 0; k < NV; ++k) {
                     if (k * step >= C) break;
                     if (k * step < width) {
-#pragma unroll
-                        for (int i = 0; i < V; ++i) v[k][i] = v[k][i] * rstd * gam[k][i] + bet[k][i];
+                        v_mul<V>(v[k], v[k], rstd_v);
+                        v_fma<V>(v[k], v[k], gam[k], bet[k]);
                         put(k);
                     }
                 }
@@ -499,8 +574,11 @@ __global__ void __launch_bounds__(BWD ? 256 : 512) ln_rows_ring_kernel(const __g
             } else {
                 const T* gy = reinterpret_cast<const T*>(reinterpret_cast<const unsigned char*>(x) + r.stage_bytes);
                 const float mean = __shfl_sync(0xffffffffu, mean_b, k_row & 31), rstd = __shfl_sync(0xffffffffu, rstd_b, k_row & 31);
-                float gv[NV][V];
-                float sum[2] = {0.f, 0.f};
+                float gv[NV][V], s1[V], s2[V], minus_mean[V], rstd_v[V];
+                v_fill<V>(s1, 0.f);
+                v_fill<V>(s2, 0.f);
+                v_fill<V>(minus_mean, -mean);
+                v_fill<V>(rstd_v, rstd);
 #pragma unroll
                 for (int k = 0; k < NV; ++k) {
                     if (k * step >= C) break;
@@ -515,25 +593,26 @@ __global__ void __launch_bounds__(BWD ? 256 : 512) ln_rows_ring_kernel(const __g
 #pragma unroll
                         for (int i = 0; i < V; ++i) { v[k][i] = mean; gv[k][i] = 0.f; }
                     }
-#pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        v[k][i] = (v[k][i] - mean) * rstd;
-                        ag[k][i] += gv[k][i] * v[k][i];
-                        ab[k][i] += gv[k][i];
-                        gv[k][i] *= gam[k][i];
-                        sum[0] += gv[k][i];
-                        sum[1] += gv[k][i] * v[k][i];
-                    }
+                    v_add<V>(v[k], v[k], minus_mean);
+                    v_mul<V>(v[k], v[k], rstd_v);
+                    v_fma<V>(ag[k], gv[k], v[k], ag[k]);
+                    v_add<V>(ab[k], ab[k], gv[k]);
+                    v_mul<V>(gv[k], gv[k], gam[k]);
+                    v_add<V>(s1, s1, gv[k]);
+                    v_fma<V>(s2, gv[k], v[k], s2);
                 }
+                float sum[2] = {v_sum<V>(s1), v_sum<V>(s2)};
                 if (a.out) {
                     team_sum<TEAM, 2>(sum, a.log_tpr, red[team][slot], team, r.warps);
-                    const float m1 = sum[0] * a.inv_c * rstd, m2 = sum[1] * a.inv_c * rstd;
+                    float minus_m1[V], minus_m2[V];
+                    v_fill<V>(minus_m1, -(sum[0] * a.inv_c * rstd));
+                    v_fill<V>(minus_m2, -(sum[1] * a.inv_c * rstd));
 #pragma unroll
                     for (int k = 0; k < NV; ++k) {
                         if (k * step >= C) break;
                         if (k * step < width) {
-#pragma unroll
-                            for (int i = 0; i < V; ++i) v[k][i] = (gv[k][i] * rstd - m1) - v[k][i] * m2;
+                            v_fma<V>(gv[k], gv[k], rstd_v, minus_m1);
+                            v_fma<V>(v[k], v[k], minus_m2, gv[k]);
                             put(k);
                         }
                     }
@@ -1055,7 +1134,9 @@ __global__ void __launch_bounds__((PX == 0 ? 8 : 16) * 32) ln_planes_tile_kernel
                 for (int i = 0; i < V; ++i) if (pl + 32 * i < np) dst[32 * i] = from_f32<T>(f[i]);
             }
         };
-        float xs[kHold ? KC : 1][V], gs[kHold && BWD ? KC : 1][V];
+        float xs[kHold ? KC : 1][V], gs[kHold && BWD ? KC : 1][V], minus_mean[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) minus_mean[i] = -mean[i];
         if constexpr (BWD) {
             float sum[2][V];
 #pragma unroll
@@ -1067,15 +1148,16 @@ __global__ void __launch_bounds__((PX == 0 ? 8 : 16) * 32) ln_planes_tile_kernel
                     fetch(sx, c, xs[at]);
                     fetch(sx + t.stage_bytes, c, gs[at]);
                     const float gm = gamma_of(k, c);
-#pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        xs[at][i] = (xs[at][i] - mean[i]) * rstd[i];
-                        ag[k] += gs[at][i] * xs[at][i];
-                        ab[k] += gs[at][i];
-                        gs[at][i] *= gm;
-                        sum[0][i] += gs[at][i];
-                        sum[1][i] += gs[at][i] * xs[at][i];
-                    }
+                    float w[V];
+                    v_add<V>(xs[at], xs[at], minus_mean);
+                    v_mul<V>(xs[at], xs[at], rstd);
+                    v_mul<V>(w, gs[at], xs[at]);
+                    ag[k] += v_sum<V>(w);
+                    ab[k] += v_sum<V>(gs[at]);
+                    v_fill<V>(w, gm);
+                    v_mul<V>(gs[at], gs[at], w);
+                    v_add<V>(sum[0], sum[0], gs[at]);
+                    v_fma<V>(sum[1], gs[at], xs[at], sum[1]);
                 }
             }
             if (a.out) {
@@ -1083,8 +1165,8 @@ __global__ void __launch_bounds__((PX == 0 ? 8 : 16) * 32) ln_planes_tile_kernel
                 float m1[V], m2[V];
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    m1[i] = stat[pixel(i)] * a.inv_c * rstd[i];
-                    m2[i] = stat[PT + pixel(i)] * a.inv_c * rstd[i];
+                    m1[i] = -(stat[pixel(i)] * a.inv_c * rstd[i]);
+                    m2[i] = -(stat[PT + pixel(i)] * a.inv_c * rstd[i]);
                 }
 #pragma unroll
                 for (int k = 0; k < KC; ++k) {
@@ -1097,8 +1179,8 @@ __global__ void __launch_bounds__((PX == 0 ? 8 : 16) * 32) ln_planes_tile_kernel
 #pragma unroll
                             for (int i = 0; i < V; ++i) { xs[at][i] = (xs[at][i] - mean[i]) * rstd[i]; gs[at][i] *= gm; }
                         }
-#pragma unroll
-                        for (int i = 0; i < V; ++i) xs[at][i] = (gs[at][i] * rstd[i] - m1[i]) - xs[at][i] * m2[i];
+                        v_fma<V>(gs[at], gs[at], rstd, m1);
+                        v_fma<V>(xs[at], xs[at], m2, gs[at]);
                         put(c, xs[at]);
                     }
                 }

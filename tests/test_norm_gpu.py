@@ -275,3 +275,46 @@ def test_module_through_autograd(gf, form):
     assert relerr(f64(m.weight.grad), ref["ggamma"]) <= 2e-5 and relerr(f64(m.bias.grad), ref["gbeta"]) <= 2e-5
     if form == "channels_last":
         assert y.is_contiguous(memory_format=torch.channels_last) and xa.grad.is_contiguous(memory_format=torch.channels_last)
+
+
+def test_more_elements_than_32_bits_count(gf):
+    """270001 rows of 8192 (2.2e9 elements): the last rows against a plain form on the device, the rest by their statistics."""
+    R, C = 270001, 8192
+    g = torch.Generator(device="cuda")
+    g.manual_seed(40)
+    x = torch.empty((R, C), dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    desc = gf.make_norm_desc(R, C, dtype=torch.bfloat16)
+    y, mean, rstd = torch.empty_like(x), torch.empty(R, device="cuda"), torch.empty(R, device="cuda")
+    gf.gf_layer_norm_forward(desc, x, None, None, y, mean, rstd)
+    ws = torch.empty(gf.gf_layer_norm_backward_workspace_bytes(desc), dtype=torch.uint8, device="cuda")
+    gw, gb, gx = torch.empty(C, device="cuda"), torch.empty(C, device="cuda"), torch.empty_like(x)
+    gf.gf_layer_norm_backward(desc, y, x, None, mean, rstd, gx, gw, gb, ws)          # g_y = y
+    torch.cuda.synchronize()
+    tail = x[-3:].double()
+    xh = (tail - tail.mean(1, keepdim=True)) / (tail.var(1, unbiased=False, keepdim=True) + 1e-5).sqrt()
+    assert float((y[-3:].double() - xh).abs().max()) <= 2.0 ** -8 * float(xh.abs().max())
+    assert float((mean.double().mean())) == pytest.approx(0.0, abs=1e-4) and float(rstd.double().mean()) == pytest.approx(1.0, abs=1e-3)
+    # g_y = y = xh (rounded): g_x is what is left of it, rounding; g_gamma sums xh^2
+    assert float(gx[-3:].float().abs().max()) <= 2.0 ** -8 * float(xh.abs().max()) * 3
+    assert float((gw.double() / R - 1).abs().max()) <= 0.02
+    del x, y, gx
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("nchw,shape", [(False, (3000, 1, 1, 768)), (True, (8, 96, 28, 28))])
+def test_calls_can_be_captured_in_a_graph(gf, nchw, shape):
+    x, gy = _draw(shape, 41).cuda(), _draw(shape, 42).cuda()
+    want = _run(gf, x, gy, None, None, nchw)                     # first calls set function attributes
+    N, H, W = (shape[0], shape[2], shape[3]) if nchw else shape[:3]
+    C = shape[1] if nchw else shape[-1]
+    desc = gf.make_norm_desc(N, C, H, W, layout=gf.GF_NCHW if nchw else gf.GF_NHWC)
+    ws = torch.empty(gf.gf_layer_norm_backward_workspace_bytes(desc), dtype=torch.uint8, device="cuda")
+    out = [torch.zeros_like(t) for t in want]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        gf.gf_layer_norm_forward(desc, x, None, None, out[0], out[1], out[2])
+        gf.gf_layer_norm_backward(desc, gy, x, None, out[1], out[2], out[3], out[4], out[5], ws)
+    graph.replay()
+    torch.cuda.synchronize()
+    for a, b in zip(out, want):
+        assert torch.equal(a, b)
