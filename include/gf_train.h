@@ -58,6 +58,7 @@ gf_status gf_layer_norm_backward(const gf_norm_desc* desc, const void* g_y, cons
  * (A = X^T X from the other side when rows > cols: the same result from the smaller products);
  * O = X.  A step maps every singular value s to a s + b s^3 + c s^5 and keeps the singular
  * vectors; with the default coefficients five steps bring the singular values near 1.
+ * Results repeat bit for bit on one device.
  *   precision GF_NS_F16: the products' operands are rounded to fp16 under a fixed scale (11
  *     significant bits), sums are fp32 -- for updates that are applied in 16 bits or that are
  *     small beside the weights.
@@ -81,7 +82,8 @@ typedef struct gf_ns_desc {
 } gf_ns_desc;
 
 /* h_coeffs: HOST array of 3 * steps floats (a, b, c of each step; read before the call returns),
- * or NULL for (3.4445, -4.7750, 2.0315) at every step.  O must not be G. */
+ * or NULL for (3.4445, -4.7750, 2.0315) at every step.  O must not be G.  The size of the
+ * workspace is that for the device which is current. */
 gf_status gf_newton_schulz_workspace_bytes(const gf_ns_desc* desc, size_t* bytes);
 gf_status gf_newton_schulz(const gf_ns_desc* desc, const void* G, void* O, void* workspace,
                            size_t workspace_bytes, const float* h_coeffs, void* stream);

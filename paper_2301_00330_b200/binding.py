@@ -354,8 +354,8 @@ def _addr(t):
 
 
 def _raw_stream(stream):
-    if stream is None:
-        stream = torch.cuda.current_stream()
+    if stream is None:      # what torch.cuda.current_stream().cuda_stream gives, without the stream object
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     return stream.cuda_stream if isinstance(stream, torch.cuda.Stream) else int(stream)
 
 

@@ -1305,27 +1305,33 @@ template <int SPLIT, bool MUON> __global__ void __launch_bounds__(kSmallThreads,
             if (p.out_bf16) give(static_cast<__nv_bfloat16*>(p.out));
             else give(static_cast<float*>(p.out));
         } else {
-            // rows of W as they lie in memory: columns j of row i, or (transposed) all i of row j; taps values each
-            const int nr = p.transposed ? cols : p.m, nc = p.transposed ? p.m : cols, span = nc * p.taps;
-            for (int r = warp; r < nr; r += kSmallThreads / 32) {
-                const long long o = (p.transposed ? (long long)(c0 + j0 + r) * s.cols : (long long)r * s.cols + c0 + j0) * p.taps;
-                auto update = [&](const auto* w, auto* out) {
-                    using Weight = typename std::remove_pointer<decltype(out)>::type;
-                    for (int e0 = lane; e0 < span; e0 += 32 * 8) {
-                        float v[8];
+            // rows of W as they lie in memory: columns j of row i, or (transposed) all i of row j; taps values each.  All rows of the
+            // tile in one sequence, eight values on their way per thread.
+            const int nr = p.transposed ? cols : p.m, nc = p.transposed ? p.m : cols, span = nc * p.taps, all = nr * span;
+            const long long base = (p.transposed ? (long long)(c0 + j0) * s.cols : (long long)(c0 + j0)) * p.taps, pitch = (long long)s.cols * p.taps;
+            auto update = [&](const auto* w, auto* out) {
+                using Weight = typename std::remove_pointer<decltype(out)>::type;
+                for (int e0 = tid; e0 < all; e0 += kSmallThreads * 8) {
+                    float v[8];
+                    int r[8], e[8];
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) v[k] = e0 + 32 * k < span ? to_f32(w[o + e0 + 32 * k]) : 0.f;
-#pragma unroll
-                        for (int k = 0; k < 8; ++k)
-                            if (e0 + 32 * k < span) {
-                                const int c = (int)p.div_taps.div((uint32_t)(e0 + 32 * k));
-                                out[o + e0 + 32 * k] = from_f32<Weight>(p.keep * v[k] - p.f * tile[p.transposed ? r * 129 + c : c * 129 + r]);
-                            }
+                    for (int k = 0; k < 8; ++k) {
+                        const int at = e0 + kSmallThreads * k;
+                        r[k] = at / span;
+                        e[k] = at - r[k] * span;
+                        v[k] = at < all ? to_f32(w[base + r[k] * pitch + e[k]]) : 0.f;
                     }
-                };
-                if (p.out_bf16) update(static_cast<const __nv_bfloat16*>(p.w[b]), static_cast<__nv_bfloat16*>(p.w_out[b]));
-                else update(static_cast<const float*>(p.w[b]), static_cast<float*>(p.w_out[b]));
-            }
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if (e0 + kSmallThreads * k < all) {
+                            const int c = (int)p.div_taps.div((uint32_t)e[k]);
+                            out[base + r[k] * pitch + e[k]] =
+                                from_f32<Weight>(p.keep * v[k] - p.f * tile[p.transposed ? r[k] * 129 + c : c * 129 + r[k]]);
+                        }
+                }
+            };
+            if (p.out_bf16) update(static_cast<const __nv_bfloat16*>(p.w[b]), static_cast<__nv_bfloat16*>(p.w_out[b]));
+            else update(static_cast<const float*>(p.w[b]), static_cast<float*>(p.w_out[b]));
         }
     }
     if (!ok) atomicOr(p.err_word, 16384u);
@@ -1505,8 +1511,6 @@ gf_status ns_iterate(const NsPlan& p, char* base, int steps, const float* coeffs
     const bool pair = p.shapes.pair;
     const int units = p.shapes.units;
     for (int k = 0; k < 3; ++k) a.shape[k] = p.shapes.shape[k];
-    for (const PhaseShape& ps : a.shape)
-        if ((long long)ps.tiles * p.batch > 0x3fffffffLL) return GF_ERR_UNSUPPORTED;
     const uint64_t m = (uint64_t)p.m, b = (uint64_t)p.batch, xp = (uint64_t)p.x_pieces, ap = (uint64_t)p.a_pieces;
     auto share = [&](int phase) { return (uint32_t)(pair ? a.shape[phase].bn / 2 : a.shape[phase].bn); };
     // two 8-byte units are the 8 columns of a row
@@ -1577,7 +1581,7 @@ bool bad_dtype(int d) { return d != GF_F32 && d != GF_BF16; }
 gf_status check_shape(int batch, int rows, int cols, int precision, int steps, float eps) {
     if (batch < 0 || rows < 1 || cols < 1 || steps < 1 || steps > GF_NS_MAX_STEPS || !(eps >= 0.f)) return GF_ERR_BAD_DESC;
     if (precision != GF_NS_F16 && precision != GF_NS_F32) return GF_ERR_BAD_DESC;
-    if (rows > 16384 || cols > 16384 || batch > 32767) return GF_ERR_UNSUPPORTED;
+    if (rows > 16384 || cols > 16384 || batch > 32767) return GF_ERR_UNSUPPORTED;      // at most 2^14 tiles of a matrix: units of work fit 32 bits
     return GF_OK;
 }
 

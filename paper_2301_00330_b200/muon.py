@@ -50,17 +50,20 @@ class Muon(torch.optim.Optimizer):
 
     A parameter whose attribute `filtered_taps` is true has gradients with one value for all taps of a
     kernel -- the weights of FilteredConv2d with r >= 2 -- and its update then costs the products of
-    [C_out, C_in / groups] alone; the result is the same.  Parameters of one shape and kind go through
-    one call of the library."""
+    [C_out, C_in / groups] alone; the result is the same.  This reads each gradient at its first tap: whatever
+    else is added to such a gradient (an L2 term in the loss, another use of the weight) has to have one value
+    for all taps too, or the parameter's attribute, or `filtered_taps` here, is set to False.  Parameters of one
+    shape and kind go through one call of the library."""
 
     def __init__(self, params, lr: float = 1e-3, momentum: float = 0.95, nesterov: bool = True, weight_decay: float = 0.0,
-                 steps: int = 5, eps: float = 1e-7, precision: str | None = None):
+                 steps: int = 5, eps: float = 1e-7, precision: str | None = None,
+                 filtered_taps: bool = True):
         if lr < 0 or not 0 <= momentum < 1 or weight_decay < 0:
             raise ValueError("lr >= 0, 0 <= momentum < 1 and weight_decay >= 0 expected")
         if precision is not None and precision not in _PRECISION:
             raise ValueError("precision is 'f16', 'f32' or None")
         super().__init__(params, dict(lr=lr, momentum=momentum, nesterov=nesterov, weight_decay=weight_decay, steps=steps, eps=eps,
-                                      precision=precision))
+                                      precision=precision, filtered_taps=filtered_taps))
         for group in self.param_groups:
             for p in group["params"]:
                 if p.dim() not in (2, 4):
@@ -91,7 +94,7 @@ class Muon(torch.optim.Optimizer):
                 if not p.is_contiguous():
                     raise ValueError("Muon updates parameters in place: they have to be contiguous")
                 rows, taps = p.shape[0], math.prod(p.shape[2:])
-                uniform = taps if getattr(p, "filtered_taps", False) else 1
+                uniform = taps if group["filtered_taps"] and getattr(p, "filtered_taps", False) else 1
                 cols = p.numel() // rows // uniform
                 alike.setdefault((p.device, rows, cols, uniform, p.grad.dtype, p.dtype), []).append(p)
             for (device, rows, cols, taps, gdt, wdt), ps in alike.items():
@@ -100,7 +103,13 @@ class Muon(torch.optim.Optimizer):
                     state = self.state[p]
                     if "momentum" not in state:
                         state["momentum"] = torch.zeros((rows, cols), dtype=torch.float32, device=device)
-                    momenta.append(state["momentum"])
+                    m = state["momentum"]
+                    if m.shape != (rows, cols):
+                        raise ValueError(f"a momentum of shape {(rows, cols)} expected, got {tuple(m.shape)}: was it kept with another "
+                                         "setting of filtered_taps?")
+                    if m.dtype != torch.float32 or not m.is_contiguous():      # loading a state casts it to the parameter's dtype
+                        m = state["momentum"] = m.to(torch.float32).contiguous()
+                    momenta.append(m)
                 precision = group["precision"] or ("f32" if wdt == torch.float32 else "f16")
                 desc = B.make_muon_desc(len(ps), rows, cols, taps, grad_dtype=gdt, weight_dtype=wdt, precision=_PRECISION[precision],
                                         steps=group["steps"], nesterov=group["nesterov"], eps=group["eps"],

@@ -7,6 +7,7 @@ channels.  Only marshalling happens here.
 from __future__ import annotations
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as B
 
@@ -55,6 +56,7 @@ class _LayerNormFn(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, g_y):
         x, weight, stats = ctx.saved_tensors
         desc, (need_x, need_w, need_b) = ctx.desc, ctx.had_grad

@@ -265,6 +265,28 @@ def test_optimizer_trains_filtered_layers(gf):
     assert opt.state[kernels[0]]["momentum"].shape == (32, 16) and other.state[twins[0]]["momentum"].shape == (32, 144)
 
 
+def test_optimizer_state_survives_saving(gf):
+    """A state that was saved and loaded (torch casts it to the parameters' dtype) goes on as fp32; one kept with taps is
+    refused where taps are used, and the other way round."""
+    conv = gf.FilteredConv2d(8, 16, 3, r=2, bias=False, device="cuda", dtype=torch.bfloat16)
+    grad = _draw((16, 8, 1, 1), 70).expand(16, 8, 3, 3).contiguous().to("cuda", torch.bfloat16)
+    opt = gf.Muon([conv.weight], lr=0.1)
+    conv.weight.grad = grad
+    opt.step()
+    again = gf.Muon([conv.weight], lr=0.1)
+    again.load_state_dict(opt.state_dict())
+    again.step()
+    m = again.state[conv.weight]["momentum"]
+    assert m.dtype == torch.float32 and m.shape == (16, 8) and bool(torch.isfinite(conv.weight).all())
+    flat = gf.Muon([conv.weight], lr=0.1, filtered_taps=False)
+    flat.step()
+    assert flat.state[conv.weight]["momentum"].shape == (16, 72)
+    flat.load_state_dict(opt.state_dict())           # brings filtered_taps = True along with the state
+    flat.param_groups[0]["filtered_taps"] = False
+    with pytest.raises(ValueError, match="filtered_taps"):
+        flat.step()
+
+
 def test_muon_takes_slices_of_a_flat_buffer(gf):
     """Parameters, momenta and gradients that lie one behind the other, off 16-byte boundaries."""
     rows, cols = 13, 9
