@@ -1306,28 +1306,32 @@ template <int SPLIT, bool MUON> __global__ void __launch_bounds__(kSmallThreads,
             else give(static_cast<float*>(p.out));
         } else {
             // rows of W as they lie in memory: columns j of row i, or (transposed) all i of row j; taps values each.  All rows of the
-            // tile in one sequence, eight values on their way per thread.
+            // tile in one sequence, 24 values on their way per thread (8: 13 us of the 59 for 576 x 96).
             const int nr = p.transposed ? cols : p.m, nc = p.transposed ? p.m : cols, span = nc * p.taps, all = nr * span;
             const long long base = (p.transposed ? (long long)(c0 + j0) * s.cols : (long long)(c0 + j0)) * p.taps, pitch = (long long)s.cols * p.taps;
             auto update = [&](const auto* w, auto* out) {
                 using Weight = typename std::remove_pointer<decltype(out)>::type;
-                for (int e0 = tid; e0 < all; e0 += kSmallThreads * 8) {
-                    float v[8];
-                    int r[8], e[8];
+                constexpr int kAtOnce = 24;
+                // place `at` = row r, value e of the row; the next of this thread lies kSmallThreads further
+                const int dr = kSmallThreads / span, de = kSmallThreads - dr * span;
+                int r = tid / span, e = tid - r * span;
+                for (int at = tid; at < all; at += kSmallThreads * kAtOnce) {
+                    float v[kAtOnce];
+                    long long o[kAtOnce];
+                    int from[kAtOnce];
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const int at = e0 + kSmallThreads * k;
-                        r[k] = at / span;
-                        e[k] = at - r[k] * span;
-                        v[k] = at < all ? to_f32(w[base + r[k] * pitch + e[k]]) : 0.f;
+                    for (int k = 0; k < kAtOnce; ++k) {
+                        const int c = (int)p.div_taps.div((uint32_t)e);
+                        o[k] = base + r * pitch + e;
+                        from[k] = p.transposed ? r * 129 + c : c * 129 + r;
+                        v[k] = at + kSmallThreads * k < all ? to_f32(w[o[k]]) : 0.f;
+                        r += dr;
+                        e += de;
+                        if (e >= span) { e -= span; ++r; }
                     }
 #pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        if (e0 + kSmallThreads * k < all) {
-                            const int c = (int)p.div_taps.div((uint32_t)e[k]);
-                            out[base + r[k] * pitch + e[k]] =
-                                from_f32<Weight>(p.keep * v[k] - p.f * tile[p.transposed ? r[k] * 129 + c : c * 129 + r[k]]);
-                        }
+                    for (int k = 0; k < kAtOnce; ++k)
+                        if (at + kSmallThreads * k < all) out[o[k]] = from_f32<Weight>(p.keep * v[k] - p.f * tile[from[k]]);
                 }
             };
             if (p.out_bf16) update(static_cast<const __nv_bfloat16*>(p.w[b]), static_cast<__nv_bfloat16*>(p.w_out[b]));
