@@ -1116,22 +1116,32 @@ __global__ void __launch_bounds__((PX == 0 ? 8 : 16) * 32) ln_planes_tile_kernel
         }
         const unsigned char* sx = dyn + (size_t)s * NT * t.stage_bytes;
         const long long base = ((long long)n * a.C * a.HW + p0);      // of channel 0, in elements
-        const uint32_t b16 = (uint32_t)(base * E) & 15u, hw16 = (uint32_t)((long long)a.HW * E) & 15u;
-        auto fetch = [&](const unsigned char* from, int c, float (&f)[V]) {
-            if constexpr (WHOLE) load_vec<T, V>(reinterpret_cast<const T*>(from + c * (PT * E)) + pl * V, f);
-            else {
-                const T* row = reinterpret_cast<const T*>(from + c * t.pitch + ((b16 + (uint32_t)c * hw16) & 15u)) + pl;
+        // A thread's channels lie kPlaneWarps * CL apart: 16 with planes of odd size, so that all of them have the same offset
+        // from a 16-byte boundary.
+        const int c_first = warp * CL + cl;
+        const uint32_t off16 = ((uint32_t)(base * E) + (uint32_t)c_first * (uint32_t)((long long)a.HW * E & 15)) & 15u;
+        const uint32_t in_tile = WHOLE ? (uint32_t)(c_first * (PT * E) + pl * 16) : (uint32_t)(c_first * t.pitch + pl * E) + off16;
+        const uint32_t in_step = (uint32_t)(kPlaneWarps * CL) * (WHOLE ? (uint32_t)(PT * E) : (uint32_t)t.pitch);
+        T* const out0 = static_cast<T*>(a.out) + base + (long long)c_first * a.HW + (WHOLE ? pl * V : pl);
+        const long long out_step = (long long)(kPlaneWarps * CL) * a.HW;
+        bool there[V];                                      // the thread's pixels are in the tile
 #pragma unroll
-                for (int i = 0; i < V; ++i) f[i] = !BWD || pl + 32 * i < np ? to_f32(row[32 * i]) : 0.f;      // forward, a pixel is alone
+        for (int i = 0; i < V; ++i) there[i] = pixel(i) < np;
+        auto fetch = [&](const unsigned char* from, int k, float (&f)[V]) {
+            const T* row = reinterpret_cast<const T*>(from + in_tile + (uint32_t)k * in_step);
+            if constexpr (WHOLE) load_vec<T, V>(row, f);
+            else {
+#pragma unroll
+                for (int i = 0; i < V; ++i) f[i] = !BWD || there[i] ? to_f32(row[32 * i]) : 0.f;      // forward, a pixel is alone
             }
         };
-        auto put = [&](int c, const float (&f)[V]) {
-            T* dst = static_cast<T*>(a.out) + base + (long long)c * a.HW + (WHOLE ? pl * V : pl);
+        auto put = [&](int k, const float (&f)[V]) {
+            T* dst = out0 + k * out_step;
             if constexpr (WHOLE) {
-                if (pl * V < np) store_vec<T, V>(dst, f);
+                if (there[0]) store_vec<T, V>(dst, f);
             } else {
 #pragma unroll
-                for (int i = 0; i < V; ++i) if (pl + 32 * i < np) dst[32 * i] = from_f32<T>(f[i]);
+                for (int i = 0; i < V; ++i) if (there[i]) dst[32 * i] = from_f32<T>(f[i]);
             }
         };
         float xs[kHold ? KC : 1][V], gs[kHold && BWD ? KC : 1][V], minus_mean[V];
@@ -1145,8 +1155,8 @@ __global__ void __launch_bounds__((PX == 0 ? 8 : 16) * 32) ln_planes_tile_kernel
             for (int k = 0; k < KC; ++k) {
                 const int c = (k * kPlaneWarps + warp) * CL + cl, at = kHold ? k : 0;
                 if (c < a.C) {
-                    fetch(sx, c, xs[at]);
-                    fetch(sx + t.stage_bytes, c, gs[at]);
+                    fetch(sx, k, xs[at]);
+                    fetch(sx + t.stage_bytes, k, gs[at]);
                     const float gm = gamma_of(k, c);
                     float w[V];
                     v_add<V>(xs[at], xs[at], minus_mean);
@@ -1173,15 +1183,15 @@ __global__ void __launch_bounds__((PX == 0 ? 8 : 16) * 32) ln_planes_tile_kernel
                     const int c = (k * kPlaneWarps + warp) * CL + cl, at = kHold ? k : 0;
                     if (c < a.C) {
                         if constexpr (!kHold) {
-                            fetch(sx, c, xs[at]);
-                            fetch(sx + t.stage_bytes, c, gs[at]);
+                            fetch(sx, k, xs[at]);
+                            fetch(sx + t.stage_bytes, k, gs[at]);
                             const float gm = gamma_of(k, c);
 #pragma unroll
                             for (int i = 0; i < V; ++i) { xs[at][i] = (xs[at][i] - mean[i]) * rstd[i]; gs[at][i] *= gm; }
                         }
                         v_fma<V>(gs[at], gs[at], rstd, m1);
                         v_fma<V>(xs[at], xs[at], m2, gs[at]);
-                        put(c, xs[at]);
+                        put(k, xs[at]);
                     }
                 }
             }
@@ -1193,7 +1203,7 @@ __global__ void __launch_bounds__((PX == 0 ? 8 : 16) * 32) ln_planes_tile_kernel
             for (int k = 0; k < KC; ++k) {
                 const int c = (k * kPlaneWarps + warp) * CL + cl, at = kHold ? k : 0;
                 if (c < a.C) {
-                    fetch(sx, c, xs[at]);
+                    fetch(sx, k, xs[at]);
 #pragma unroll
                     for (int i = 0; i < V; ++i) sum[0][i] += xs[at][i];
                 }
@@ -1205,7 +1215,7 @@ __global__ void __launch_bounds__((PX == 0 ? 8 : 16) * 32) ln_planes_tile_kernel
             for (int k = 0; k < KC; ++k) {
                 const int c = (k * kPlaneWarps + warp) * CL + cl, at = kHold ? k : 0;
                 if (c < a.C) {
-                    if constexpr (!kHold) fetch(sx, c, xs[at]);
+                    if constexpr (!kHold) fetch(sx, k, xs[at]);
 #pragma unroll
                     for (int i = 0; i < V; ++i) { xs[at][i] -= mean[i]; sum[0][i] += xs[at][i] * xs[at][i]; }
                 }
@@ -1223,14 +1233,14 @@ __global__ void __launch_bounds__((PX == 0 ? 8 : 16) * 32) ln_planes_tile_kernel
                 const int c = (k * kPlaneWarps + warp) * CL + cl, at = kHold ? k : 0;
                 if (c < a.C) {
                     if constexpr (!kHold) {
-                        fetch(sx, c, xs[at]);
+                        fetch(sx, k, xs[at]);
 #pragma unroll
                         for (int i = 0; i < V; ++i) xs[at][i] -= mean[i];
                     }
                     const float gm = gamma_of(k, c), bt = beta_of(k, c);
 #pragma unroll
                     for (int i = 0; i < V; ++i) xs[at][i] = xs[at][i] * rstd[i] * gm + bt;
-                    put(c, xs[at]);
+                    put(k, xs[at]);
                 }
             }
         }
@@ -1449,10 +1459,10 @@ void plan_planes(const gf_norm_desc& d, bool backward, long long R, NormPlan& p)
             return;
         }
     } else if (HW * e >= 64) {
-        // Rows of 128 pixels, or of 32, as long as two tiles are in flight.
+        // Rows of 256 pixels (bf16, few channels: the tile stays in registers), of 128, or of 32, as long as two tiles are in flight.
         constexpr int kPlaneWarps = plane_warps(1);
         const int kc = (d.C + kPlaneWarps - 1) / kPlaneWarps;
-        for (int px = 4; px >= 1 && kc <= 32; px -= 3) {
+        for (int px = e == 2 && kc <= 8 ? 8 : 4; px >= 1 && kc <= 32; px = px == 8 ? 4 : px - 3) {
             PlaneArgs& t = p.tile;
             const int pieces = 32 * px * e / 16 + 1;
             t.log_pieces = 0;
@@ -1461,7 +1471,7 @@ void plan_planes(const gf_norm_desc& d, bool backward, long long R, NormPlan& p)
             const long long stage = ((long long)d.C * t.pitch + 127) / 128 * 128;
             const long long fixed = (kPlaneWarps + 1) * nt * 32 * px * 4 + 2048;
             const long long fit = ((long long)kNormSmem - 2 * fixed) / (nt * stage);
-            if (fit < 2 || (px > 1 && HW <= 32)) continue;
+            if (fit < 2 || (px > 1 && HW <= 32) || (px > 4 && HW <= 128)) continue;
             p.PX = px;
             tiles(32 * px);
             p.KC = kc <= 8 ? 8 : kc <= 16 ? 16 : 32;
@@ -1599,6 +1609,9 @@ template <typename T, int PX> gf_status launch_tile_odd(const NormArgs& a, const
     }
 }
 template <typename T> gf_status launch_tile(const NormArgs& a, const gf_norm_desc& d, const NormPlan& p, bool backward, cudaStream_t s) {
+    if constexpr (sizeof(T) == 2) {
+        if (p.PX == 8) return launch_tile_way<T, 32, 8, 8>(a, d, p, backward, s);
+    }
     if (p.PX == 4) return launch_tile_odd<T, 4>(a, d, p, backward, s);
     if (p.PX == 1) return launch_tile_odd<T, 1>(a, d, p, backward, s);
     if (p.LP == 8) return launch_tile_whole<T, 8>(a, d, p, backward, s);
