@@ -949,8 +949,9 @@ __global__ void __launch_bounds__(512) ln_planes_bwd_long_kernel(const __grid_co
 // channels, so that the sums over channels (per pixel) are sums in registers and a few exchanges per tile,
 // and the sums over pixels (per channel) stay in a thread's registers for the whole kernel.  The tile is read
 // from shared memory once per pass over it (two backward, three forward).
-// Measured: 256 x 512 x 16 x 16 fp32 backward 77 us and 3 us for the lines of sums, 5.2 TB/s; 64 x 96 x 55 x 55 bf16 forward 37 us,
-// 2.0 TB/s: planes of odd size are read and written a pixel at a time, about 30 instructions per pixel and channel.
+// Measured: 256 x 512 x 16 x 16 fp32 backward 77 us and 3 us for the lines of sums, 5.2 TB/s; 64 x 96 x 55 x 55 bf16 forward 35 us,
+// 2.2 TB/s: planes of odd size are read and written a pixel at a time, about 30 instructions per pixel and channel (tiles of
+// 128 pixels 37 us, of 8 warps 53).
 //   WHOLE: every row of a plane starts on a 16-byte boundary; tiles come as boxes of the copy engine, a lane has a
 //          16-byte vector of pixels.
 //   else : planes of odd size.  Each row is copied in 16-byte pieces from the boundary before it (its offset differs from

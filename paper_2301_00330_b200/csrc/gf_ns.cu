@@ -74,6 +74,7 @@ __device__ __forceinline__ void momentum4(const float* p, int vec, int live, flo
     for (int k = 0; k < 4; ++k) { m[k] = 0.f; if (k < live) m[k] = p[k]; }
 }
 
+// (Bound by memory; with the cast and the last kernel about 40 us of the 1.3 ms of 4096 x 4096.)
 // Sums of squares of the matrices to be orthogonalised, one partial per block; a Muon step also
 // writes the new momentum here.  Squares are added in fp32 within a thread, in fp64 across threads.
 template <bool MUON> __global__ void __launch_bounds__(kNormThreads) ns_norm_kernel(const __grid_constant__ Source s, double* part, uint32_t* err_word) {
@@ -612,6 +613,10 @@ template <int SPLIT, bool PAIR> __device__ __forceinline__ PhaseView phase_view(
 // all meet between phases.  Each role has a loop over the phases of its own, so that its registers are its own.
 // The two issuing warps run as whole warps and elect the thread that issues: descriptors and addresses then stay in
 // uniform registers.  (With the loop under `lane == 0` every product took 110 clocks to issue, whatever its size.)
+// Measured, five steps: 4096 x 4096 in fp16 operands 1.3 ms with the kernels around it, a pair's chunk of 64 in 528 clocks where the
+// products alone take 512, under the power cap; 4 x 2048 x 512 with pairs of fp16 244 us, bound by operands from L2 (58
+// bytes per clock and SM), 3000 clocks per meeting and 2500 to 9000 per tile's results; 6 x 256 x 256 105 us, 12000 clocks per
+// phase of which the products take 3600.
 template <int SPLIT, bool PAIR> __global__ void __launch_bounds__(kThreads, 1) ns_iterate_kernel(const __grid_constant__ IterateArgs p) {
     extern __shared__ unsigned char dyn_raw[];
     unsigned char* dyn = align1024(dyn_raw);
@@ -880,7 +885,9 @@ template <int SPLIT, bool PAIR> __global__ void __launch_bounds__(kThreads, 1) n
 // slices: every CTA owns some of its columns, the others send it their partial sums of these (stores into its shared
 // memory), it adds them in the order of the ranks and sends the result to all.  The polynomial is computed by every
 // CTA, B X by each for its slice.  (The general kernel takes 4 to 5 us per product of this size, of which the product
-// itself is a tenth: two passes through L2 and a meeting of the grid.  Reading the others' sums instead of being sent
+// itself is a tenth: two passes through L2 and a meeting of the grid; 96 x 576 took 71 us there and takes 45 here, 11000
+// clocks per step: 3000 the partial sums and A, 4000 meetings, 2000 products, 2000 results.  More rows do not fit one
+// accumulator, more columns not a cluster of 8.  Reading the others' sums instead of being sent
 // them took 4500 clocks per step, three times as long.)
 constexpr int kSmallThreads = 256;
 constexpr int kSmallCols = 256;            // columns of a slice, at most
