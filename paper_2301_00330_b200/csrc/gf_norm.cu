@@ -373,8 +373,8 @@ template <typename T> __global__ void __launch_bounds__(1024) ln_rows_bwd_long_k
 // boundary before it to the one after it.  The last bytes of a tensor whose size is no multiple of 16 are fetched with
 // plain loads.
 // Measured: 100352 x 576 fp32 forward 88 us, 5.2 TB/s (0.80 of the copy bandwidth); 8192 x 4096 bf16 backward 47 us and 4 us
-// for the lines of sums, 4.3 TB/s: with 8 warps per SM (the sums take their registers) it is bound by the latency of
-// each row's exchanges; 16 elements per thread and 16 warps measured 56 us in all.
+// for the lines of sums, 4.3 TB/s: 8 warps per SM (the sums take their registers), about 7 us of it start and
+// end; two rows at once with one exchange measured the same, 16 elements per thread and 16 warps measured 56 us in all.
 //   SHIFT: rows whose length is no multiple of 16 bytes, one to a batch.  The number of teams is a multiple of the period (at most
 //   8) with which the rows' offsets from a 16-byte boundary repeat, so that all rows of a team have the same
 //   offset: its threads own whole aligned vectors, the first and last of which are partly the neighbouring rows'.
