@@ -5,7 +5,11 @@
  *
  * The conventions of gf.h hold: device pointers 16-byte aligned and dense, inputs read-only,
  * outputs overwritten, work enqueued on `stream` without synchronising, errors that the host can
- * detect returned before anything is launched, device scratch supplied by the caller.
+ * detect returned before anything is launched, device scratch supplied by the caller.  A
+ * device-side wait that runs out is reported by gf_last_async_status on the call's workspace.
+ * The layer norms report to the library-wide word that the same call reads: any workspace serves
+ * there, a layer norm's own from a backward with g_gamma or g_beta and N > 0, which clears the
+ * workspace's word.
  */
 #ifndef GF_TRAIN_H_
 #define GF_TRAIN_H_

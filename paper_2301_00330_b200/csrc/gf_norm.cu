@@ -1275,9 +1275,10 @@ __global__ void __launch_bounds__((PX == 0 ? 8 : 16) * 32) ln_planes_tile_kernel
 // ---- sums of the blocks' lines -------------------------------------------------------------------
 // part [blocks][2 C] -> g_gamma, g_beta: the blocks in a fixed order.
 constexpr int kFinX = 32, kFinY = 32;
-__global__ void __launch_bounds__(kFinX * kFinY) ln_finish_kernel(const float* part, int blocks, int C, float* g_gamma, float* g_beta) {
+__global__ void __launch_bounds__(kFinX * kFinY) ln_finish_kernel(const float* part, int blocks, int C, float* g_gamma, float* g_beta, uint32_t* status) {
     __shared__ float red[kFinY][kFinX + 1];
     pdl_wait();
+    if (status && blockIdx.x == 0 && threadIdx.x == 0 && threadIdx.y == 0) *status = 0;
     const long long col = (long long)blockIdx.x * kFinX + threadIdx.x;
     float s = 0.f;
     if (col < 2LL * C) {
@@ -1681,7 +1682,7 @@ gf_status gf_layer_norm_backward_workspace_bytes(const gf_norm_desc* desc, size_
     gf_status st = norm_validate(desc);
     if (st != GF_OK) return st;
     const NormPlan p = norm_plan(*desc, true);
-    *bytes = (size_t)(p.grid > 0 ? p.grid : 1) * 2 * desc->C * 4;
+    *bytes = 256 + (size_t)(p.grid > 0 ? p.grid : 1) * 2 * desc->C * 4;      // error word | lines of sums
     return GF_OK;
 }
 
@@ -1700,11 +1701,12 @@ gf_status gf_layer_norm_backward(const gf_norm_desc* desc, const void* g_y, cons
     if (!g_x && !sums) return GF_OK;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const NormPlan p = norm_plan(*desc, true);
+    float* part = sums && desc->N > 0 ? reinterpret_cast<float*>(static_cast<char*>(workspace) + 256) : nullptr;
     if (desc->N > 0) {
         NormArgs a = norm_args(*desc);
         a.x = x; a.gy = g_y; a.out = g_x; a.mean_in = mean; a.rstd_in = rstd; a.log_tpr = p.log_tpr;
         a.gamma = {gamma, desc->param_dtype == GF_BF16};
-        a.part = sums ? static_cast<float*>(workspace) : nullptr;
+        a.part = part;
         ProfScope prof(K_NORM_BWD, s);
         st = desc->dtype == GF_F32 ? launch_norm<float>(a, *desc, p, true, s) : launch_norm<__nv_bfloat16>(a, *desc, p, true, s);
         if (st != GF_OK) return st;
@@ -1713,7 +1715,8 @@ gf_status gf_layer_norm_backward(const gf_norm_desc* desc, const void* g_y, cons
     ProfScope prof(K_NORM_SUMS, s);
     const long long cols = 2LL * desc->C;
     return launch_pdl(ln_finish_kernel, dim3((unsigned)((cols + kFinX - 1) / kFinX)), dim3(kFinX, kFinY), 0, s,
-                      (const float*)workspace, desc->N > 0 ? p.grid : 0, (int)desc->C, g_gamma, g_beta);
+                      (const float*)part, desc->N > 0 ? p.grid : 0, (int)desc->C, g_gamma, g_beta,
+                      desc->N > 0 ? static_cast<uint32_t*>(workspace) : nullptr);
 }
 
 }  // extern "C"

@@ -76,7 +76,7 @@ def _run(gf, x, gy, gamma, beta, nchw, eps=1e-5, inplace=False):
         gy_src = gy
     gf.gf_layer_norm_forward(desc, src, gamma, beta, y.t, mean.t, rstd.t)
     gf.gf_layer_norm_backward(desc, gy_src, x, gamma, mean.t, rstd.t, gx.t, gw.t, gb.t, ws.t)
-    torch.cuda.synchronize()
+    assert gf.gf_last_async_status(ws.t) == gf.GF_OK
     assert gf.gf_kernel_launch_count() >= before + 3
     for g in (y, gx, mean, rstd, gw, gb, ws):
         g.check()
