@@ -46,6 +46,13 @@ int32_t gf_profile_read(gf_kernel_time* out, int32_t max_entries);
  * workspace clears the word again. */
 gf_status gf_selftest_bounded_wait(void* workspace, int64_t limit_cycles, void* stream);
 
+/* Self-test, on the host, of the rule by which the Newton-Schulz kernel ends a turn (a product that
+ * all blocks have part in): what a role goes on with when its own waits of turn `turn` of `turns`
+ * went well (ok != 0) or ran out, and the meeting of the blocks after it reports `met`.  Nonzero: on
+ * to the next turn, or done; 0: the failure is reported and the kernel ends.  There is no meeting
+ * after the last turn. */
+int32_t gf_selftest_end_of_turn(int32_t turn, int32_t turns, int32_t ok, int32_t met);
+
 /* Name of a kernel id (ids are 0 .. gf_kernel_id_count()-1), NULL if out of range. */
 const char* gf_kernel_name(int32_t kernel_id);
 int32_t gf_kernel_id_count(void);

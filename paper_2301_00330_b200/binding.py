@@ -33,6 +33,7 @@ EXPORTS = (
     "gf_backward_int8", "gf_backward_int8_workspace_bytes", "gf_selftest_bounded_wait",
     "gf_layer_norm_forward", "gf_layer_norm_backward_workspace_bytes", "gf_layer_norm_backward",
     "gf_newton_schulz_workspace_bytes", "gf_newton_schulz", "gf_muon_workspace_bytes", "gf_muon_step",
+    "gf_selftest_end_of_turn",
 )
 
 
@@ -137,6 +138,8 @@ def lib() -> ctypes.CDLL:
             getattr(L, name).restype = ctypes.c_int
         L.gf_selftest_bounded_wait.argtypes = [vp, ctypes.c_int64, vp]
         L.gf_selftest_bounded_wait.restype = ctypes.c_int
+        L.gf_selftest_end_of_turn.argtypes = [i32, i32, i32, i32]
+        L.gf_selftest_end_of_turn.restype = i32
         L.gf_status_string.argtypes = [ctypes.c_int]
         L.gf_status_string.restype = ctypes.c_char_p
         for name in ("gf_stash_dims", "gf_stash_bytes", "gf_backward_workspace_bytes", "gf_stash_forward",
@@ -425,6 +428,11 @@ def gf_selftest_bounded_wait(workspace, limit_cycles: int, stream=None) -> None:
     """Launches a block whose bounded wait must expire; it records that in the workspace's error word."""
     _check(lib().gf_selftest_bounded_wait(_ptr(workspace), ctypes.c_int64(int(limit_cycles)), _stream(stream)),
            "gf_selftest_bounded_wait")
+
+
+def gf_selftest_end_of_turn(turn: int, turns: int, ok: bool, met: bool) -> bool:
+    """Whether a role of the Newton-Schulz kernel goes on after turn `turn` of `turns` (evaluated on the host)."""
+    return bool(lib().gf_selftest_end_of_turn(int(turn), int(turns), int(ok), int(met)))
 
 
 def gf_kernel_launch_count() -> int:

@@ -776,6 +776,10 @@ int32_t gf_profile_read(gf_kernel_time* out, int32_t max_entries) {
     return n;
 }
 
+int32_t gf_selftest_end_of_turn(int32_t turn, int32_t turns, int32_t ok, int32_t met) {
+    return end_of_turn((int)turn, (int)turns, ok != 0, [&](bool good) { return good && met != 0; });
+}
+
 const char* gf_kernel_name(int32_t kernel_id) {
     return (kernel_id >= 0 && kernel_id < K_COUNT) ? kKernelNames[kernel_id] : nullptr;
 }

@@ -647,7 +647,9 @@ template <int SPLIT, bool PAIR> __global__ void __launch_bounds__(kThreads, 1) n
     const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_base, 0);
     asm volatile("fence.proxy.async;" ::: "memory");
     bool ok = true;
-    auto meet = [&](int turn) { return turn + 1 == turns || grid_meet(p, (uint32_t)(turn + 1) * gridDim.x, ok, &flag); };
+    auto meet = [&](int turn) {
+        return end_of_turn(turn, turns, ok, [&](bool good) { return grid_meet(p, (uint32_t)(turn + 1) * gridDim.x, good, &flag); });
+    };
 
     if (warp == 0) {
         uint32_t ring = 0;             // one bit per stage: the parity of its next use

@@ -85,6 +85,13 @@ __device__ __forceinline__ void fence_proxy_async_smem() {
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
 }
 
+// What a role of a kernel that works in turns, between which all blocks meet, goes on with: `ok` false says that one of
+// its waits has run out.  After the last turn nobody meets, and a failure of that turn is still to be reported.
+#pragma nv_exec_check_disable
+template <typename Meet> __host__ __device__ __forceinline__ bool end_of_turn(int turn, int turns, bool ok, Meet&& meet) {
+    return turn + 1 == turns ? ok : meet(ok);
+}
+
 // Named barrier `id` over `nthreads` threads that also tells every one of them whether ANY
 // of them passed a true predicate: a failed (timed-out) wait of one thread ends the loop of all,
 // so that no thread is left alone at a later barrier.
