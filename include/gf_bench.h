@@ -46,6 +46,13 @@ int32_t gf_profile_read(gf_kernel_time* out, int32_t max_entries);
  * workspace clears the word again. */
 gf_status gf_selftest_bounded_wait(void* workspace, int64_t limit_cycles, void* stream);
 
+/* Self-test of the wait that a whole warp makes: its lanes have to give up together, or those that
+ * went on would wait for the others at the next instruction of the whole warp.  One warp waits on a
+ * barrier that another thread arrives on after 8 * `limit_cycles` clocks (limit_cycles 1 .. 1e8); its
+ * even lanes wait for limit_cycles at most, its odd ones for 64 times that.  result (device memory, 32
+ * words) gets what each lane went on with. */
+gf_status gf_selftest_warp_wait(uint32_t* result, int64_t limit_cycles, void* stream);
+
 /* Self-test, on the host, of the rule by which the Newton-Schulz kernel ends a turn (a product that
  * all blocks have part in): what a role goes on with when its own waits of turn `turn` of `turns`
  * went well (ok != 0) or ran out, and the meeting of the blocks after it reports `met`.  Nonzero: on

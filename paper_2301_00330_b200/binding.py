@@ -33,7 +33,7 @@ EXPORTS = (
     "gf_backward_int8", "gf_backward_int8_workspace_bytes", "gf_selftest_bounded_wait",
     "gf_layer_norm_forward", "gf_layer_norm_backward_workspace_bytes", "gf_layer_norm_backward",
     "gf_newton_schulz_workspace_bytes", "gf_newton_schulz", "gf_muon_workspace_bytes", "gf_muon_step",
-    "gf_selftest_end_of_turn",
+    "gf_selftest_end_of_turn", "gf_selftest_warp_wait",
 )
 
 
@@ -138,6 +138,8 @@ def lib() -> ctypes.CDLL:
             getattr(L, name).restype = ctypes.c_int
         L.gf_selftest_bounded_wait.argtypes = [vp, ctypes.c_int64, vp]
         L.gf_selftest_bounded_wait.restype = ctypes.c_int
+        L.gf_selftest_warp_wait.argtypes = [vp, ctypes.c_int64, vp]
+        L.gf_selftest_warp_wait.restype = ctypes.c_int
         L.gf_selftest_end_of_turn.argtypes = [i32, i32, i32, i32]
         L.gf_selftest_end_of_turn.restype = i32
         L.gf_status_string.argtypes = [ctypes.c_int]
@@ -428,6 +430,11 @@ def gf_selftest_bounded_wait(workspace, limit_cycles: int, stream=None) -> None:
     """Launches a block whose bounded wait must expire; it records that in the workspace's error word."""
     _check(lib().gf_selftest_bounded_wait(_ptr(workspace), ctypes.c_int64(int(limit_cycles)), _stream(stream)),
            "gf_selftest_bounded_wait")
+
+
+def gf_selftest_warp_wait(result, limit_cycles: int, stream=None) -> None:
+    """A warp whose lanes wait with different limits; result (32 words on the device) <- what each lane went on with."""
+    _check(lib().gf_selftest_warp_wait(_ptr(result), ctypes.c_int64(int(limit_cycles)), _stream(stream)), "gf_selftest_warp_wait")
 
 
 def gf_selftest_end_of_turn(turn: int, turns: int, ok: bool, met: bool) -> bool:

@@ -737,6 +737,19 @@ __global__ void selftest_wait_kernel(uint32_t* err_word, long long limit) {
     __syncthreads();
     if (threadIdx.x == 0 && !gf::mbar_wait_bounded(&bar, 0, limit)) atomicOr(err_word, 128u);
 }
+
+// Lanes with different patience: all of them have to come out of the wait alike.
+__global__ void selftest_warp_wait_kernel(uint32_t* result, long long limit) {
+    __shared__ uint64_t bar;
+    if (threadIdx.x == 0) { gf::mbar_init(&bar, 1); gf::mbar_fence_init(); }
+    __syncthreads();
+    if (threadIdx.x < 32) result[threadIdx.x] = gf::mbar_wait_warp(&bar, 0, threadIdx.x % 2 == 0 ? limit : 64 * limit) ? 1u : 0u;
+    else if (threadIdx.x == 32) {
+        const long long t0 = clock64();
+        while (clock64() - t0 < 8 * limit) {}
+        gf::mbar_arrive(&bar);
+    }
+}
 }  // namespace gf
 
 extern "C" {
@@ -746,6 +759,14 @@ gf_status gf_selftest_bounded_wait(void* workspace, int64_t limit_cycles, void* 
     if (limit_cycles < 1 || limit_cycles > 2000000000LL) return GF_ERR_BAD_DESC;
     if (misaligned(workspace)) return GF_ERR_ALIGN;
     selftest_wait_kernel<<<1, 32, 0, static_cast<cudaStream_t>(stream)>>>(static_cast<uint32_t*>(workspace), (long long)limit_cycles);
+    return after_launch();
+}
+
+gf_status gf_selftest_warp_wait(uint32_t* result, int64_t limit_cycles, void* stream) {
+    if (!result) return GF_ERR_NULL;
+    if (limit_cycles < 1 || limit_cycles > 100000000LL) return GF_ERR_BAD_DESC;
+    if (misaligned(result)) return GF_ERR_ALIGN;
+    selftest_warp_wait_kernel<<<1, 64, 0, static_cast<cudaStream_t>(stream)>>>(result, (long long)limit_cycles);
     return after_launch();
 }
 

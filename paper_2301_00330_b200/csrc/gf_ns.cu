@@ -665,7 +665,7 @@ template <int SPLIT, bool PAIR> __global__ void __launch_bounds__(kThreads, 1) n
                 const int row = ti * kRows + (int)rank * 128, col = tj * ps.bn + (int)rank * v.share;
                 const int q0 = t % v.splits * v.per, q1 = min(q0 + v.per, v.chunks);
                 for (int q = q0; q < q1; ++q) {
-                    ok = __all_sync(0xffffffffu, mbar_wait_bounded(&empty[s], ((ring >> s) & 1u) ^ 1u));
+                    ok = mbar_wait_warp(&empty[s], ((ring >> s) & 1u) ^ 1u);
                     if (!ok) break;
                     if (elect_one()) {
                         unsigned char* st = dyn + (size_t)s * ps.stage_bytes;
@@ -706,9 +706,8 @@ template <int SPLIT, bool PAIR> __global__ void __launch_bounds__(kThreads, 1) n
                         const int buf = (int)(use & 1u);
                         const bool first = in == 0, last = in == v.segment - 1 || q == n - 1;
                         in = last ? 0 : in + 1;
-                        if (first && use >= 2) ok = mbar_wait_bounded(&drained[buf], ((use >> 1) - 1) & 1u);
-                        if (ok) ok = mbar_wait_bounded(&full[s], (ring >> s) & 1u);
-                        ok = __all_sync(0xffffffffu, ok);
+                        if (first && use >= 2) ok = mbar_wait_warp(&drained[buf], ((use >> 1) - 1) & 1u);
+                        if (ok) ok = mbar_wait_warp(&full[s], (ring >> s) & 1u);
                         if (!ok) break;
                         tc_fence_after_sync();
                         if (elect_one()) {
@@ -778,7 +777,7 @@ template <int SPLIT, bool PAIR> __global__ void __launch_bounds__(kThreads, 1) n
                 }
                 for (int q = 0; q < chunks; q += segment) {
                     const int buf = (int)(use & 1u);
-                    ok = mbar_wait_bounded(&done[buf], (use >> 1) & 1u);
+                    ok = mbar_wait_warp(&done[buf], (use >> 1) & 1u);
                     ++use;
                     if (!ok) break;
                     tc_fence_after_sync();

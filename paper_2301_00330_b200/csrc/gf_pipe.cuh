@@ -54,6 +54,12 @@ __device__ __forceinline__ bool mbar_wait_bounded(uint64_t* bar, uint32_t parity
     return true;
 }
 
+// The same for a whole converged warp, whose lanes give up together: what follows a wait is often an instruction of
+// the whole warp, at which lanes that went on would wait for those that did not.
+__device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, long long limit = kWaitCycles) {
+    return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, limit));
+}
+
 // One contiguous global -> shared copy by the copy engine; both addresses 16-byte
 // aligned, bytes a multiple of 16.  Completion is signalled on `bar` as tx bytes.
 __device__ __forceinline__ void bulk_g2s(void* dst_smem, const void* src_gmem, uint32_t bytes, uint64_t* bar) {

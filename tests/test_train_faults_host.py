@@ -11,3 +11,13 @@ def test_a_wait_that_runs_out_in_any_turn_is_reported(gf, turns):
         assert gf.gf_selftest_end_of_turn(turn, turns, ok=True, met=True), turn
     for turn in range(turns - 1):
         assert not gf.gf_selftest_end_of_turn(turn, turns, ok=True, met=False), turn
+
+
+def test_the_warp_wait_checks_its_arguments(gf):
+    for bad in (0, -1, 10 ** 8 + 1):
+        with pytest.raises(gf.GfError) as e:
+            gf.gf_selftest_warp_wait(0x1000, bad, 0)
+        assert e.value.status == gf.GF_ERR_BAD_DESC
+    with pytest.raises(gf.GfError) as e:
+        gf.gf_selftest_warp_wait(None, 1000, 0)
+    assert e.value.status == gf.GF_ERR_NULL
