@@ -620,7 +620,8 @@ __global__ void __launch_bounds__(BWD ? 256 : 512) ln_rows_ring_kernel(const __g
             }
         }
         team_sync<TEAM>(team, r.warps);                     // the batch has been read
-        if (tid == 0 && b + r.stages * teams_all < r.batches) load(b + r.stages * teams_all, s);
+        // after a wait that ran out no copy is started: its barrier may still be in the phase before
+        if (tid == 0 && ok && b + r.stages * teams_all < r.batches) load(b + r.stages * teams_all, s);
         if (++s == r.stages) { s = 0; parity ^= 1u; }
     }
     if (!ok) {
@@ -1247,7 +1248,7 @@ __global__ void __launch_bounds__((PX == 0 ? 8 : 16) * 32) ln_planes_tile_kernel
         }
         if constexpr (WHOLE) {
             __syncthreads();                                // the tile has been read
-            load(tile + (long long)t.stages * gridDim.x, s);
+            if (ok) load(tile + (long long)t.stages * gridDim.x, s);      // (none after a wait that ran out: its barrier may be in the phase before)
         }
         if (++s == t.stages) { s = 0; parity ^= 1u; }
     }
