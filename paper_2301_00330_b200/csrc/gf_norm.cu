@@ -626,8 +626,7 @@ __global__ void __launch_bounds__(BWD ? 256 : 512) ln_rows_ring_kernel(const __g
     }
     if (!ok) {
         atomicOr(r.err_word, 8192u);
-        const long long t0 = clock64();                     // copies may still be on their way to this block's shared memory
-        while (clock64() - t0 < 2000000LL) {}
+        let_settle();
     }
     if constexpr (BWD) {
         if (!a.part) return;
@@ -1254,8 +1253,7 @@ __global__ void __launch_bounds__((PX == 0 ? 8 : 16) * 32) ln_planes_tile_kernel
     }
     if (!ok) {
         atomicOr(t.err_word, 8192u);
-        const long long t0 = clock64();                     // copies may still be on their way to this block's shared memory
-        while (clock64() - t0 < 2000000LL) {}
+        let_settle();
     }
     if constexpr (BWD) {
         if (!a.part) return;

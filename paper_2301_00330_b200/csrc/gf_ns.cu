@@ -867,8 +867,7 @@ template <int SPLIT, bool PAIR> __global__ void __launch_bounds__(kThreads, 1) n
     }
     if (!ok) {
         atomicOr(p.err_word, 4096u);
-        const long long t0 = clock64();           // copies may still be on their way to this CTA's shared memory
-        while (clock64() - t0 < 2000000LL) {}
+        let_settle();
     }
     tc_fence_before_sync();
     __syncthreads();
@@ -1346,7 +1345,10 @@ template <int SPLIT, bool MUON> __global__ void __launch_bounds__(kSmallThreads,
             else update(static_cast<const float*>(p.w[b]), static_cast<float*>(p.w_out[b]));
         }
     }
-    if (!ok) atomicOr(p.err_word, 16384u);
+    if (!ok) {
+        atomicOr(p.err_word, 16384u);
+        let_settle();
+    }
     tc_fence_before_sync();
     all_meet();                                              // no CTA leaves while its memory may be read
     tc_fence_after_sync();

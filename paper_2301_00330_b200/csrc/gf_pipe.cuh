@@ -60,6 +60,13 @@ __device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, l
     return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, limit));
 }
 
+// After a wait that ran out: copies or products that were started may still be under way in this block's shared and
+// tensor memory.  About a millisecond, after which the block may end.
+__device__ __forceinline__ void let_settle() {
+    const long long t0 = clock64();
+    while (clock64() - t0 < 2000000LL) {}
+}
+
 // One contiguous global -> shared copy by the copy engine; both addresses 16-byte
 // aligned, bytes a multiple of 16.  Completion is signalled on `bar` as tx bytes.
 __device__ __forceinline__ void bulk_g2s(void* dst_smem, const void* src_gmem, uint32_t bytes, uint64_t* bar) {
