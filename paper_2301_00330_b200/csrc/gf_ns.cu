@@ -1402,11 +1402,13 @@ PhaseShape phase_shape(const NsPlan& p, int phase, bool pair, int units, double*
     return best;
 }
 
-template <int SPLIT> int resident_pairs();
+int resident_pairs();
 Shapes choose_shapes(const NsPlan& p) {
     Shapes best = {};
     double least = 0;
-    const int pairs = p.split == 2 ? resident_pairs<2>() : resident_pairs<1>();
+    // Pairs of fp16 always run on single CTAs: CTA pairs measured slower on every size (1536 x 1536 334 us single, 363 paired;
+    // 2560 x 2560 1176 and 1326; 4096 x 4096 4350 and 4830; 8192 x 8192 36.8 and 38.2 ms, all back to back under the power cap).
+    const int pairs = p.split == 1 ? resident_pairs() : 0;
     for (int pair = 0; pair <= (pairs > 0 ? 1 : 0); ++pair) {
         Shapes c = {};
         c.pair = pair != 0;
@@ -1420,9 +1422,10 @@ Shapes choose_shapes(const NsPlan& p) {
             const size_t bytes = s.splits > 1 ? (size_t)s.tiles * p.batch * (pair ? 2 : 1) * s.splits * 8 * (s.bn / 2) * 128 : 0;
             if (bytes > c.partial_bytes) c.partial_bytes = bytes;
         }
-        // Pairs take 1.6 times this estimate, with pairs of fp16 1.35 times (measured on both sides of where it decides, fp16 operands: 2048 x 2048 pairs 350 us,
-        // single CTAs 316; 4096 x 4096 1350 and 1770; pairs of fp16: 1001 x 2048 293 and 239, 4096 x 4096 3950 and 4370).
-        if (c.pair) sum *= p.split == 1 ? 1.6 : 1.35;
+        // CTA pairs take 1.25 times this estimate (measured on both sides of where it decides, us back to back, single CTAs and pairs: by the
+        // estimate, single / pairs = 1.06: 1024 x 4096 217 and 250; 1.22: 1536 x 1536 191 and 194; 1.31: 1500 x 2100 239 and 227;
+        // 1.36: 2048 x 2048 279 and 267; 1.47: 2560 x 2560 517 and 454; 1.76: 4096 x 4096 1750 and 1375).
+        if (c.pair) sum *= 1.25;
         if (least == 0 || sum < least) { least = sum; best = c; }
     }
     return best;
@@ -1483,7 +1486,7 @@ template <int SPLIT, bool PAIR> gf_status launch_iterate(const IterateArgs& a, i
 }
 
 // Pairs of CTAs that are resident at once (0: none).
-template <int SPLIT> int resident_pairs() {
+int resident_pairs() {
     static int cached[kMaxDevices] = {};                  // pairs + 1
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return 0;
@@ -1497,8 +1500,8 @@ template <int SPLIT> int resident_pairs() {
         attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
         cfg.attrs = attr; cfg.numAttrs = 1;
         int n = 0;
-        if (ensure_dyn_smem(ns_iterate_kernel<SPLIT, true>, smem, configured) != GF_OK ||
-            cudaOccupancyMaxActiveClusters(&n, ns_iterate_kernel<SPLIT, true>, &cfg) != cudaSuccess)
+        if (ensure_dyn_smem(ns_iterate_kernel<1, true>, smem, configured) != GF_OK ||
+            cudaOccupancyMaxActiveClusters(&n, ns_iterate_kernel<1, true>, &cfg) != cudaSuccess)
             n = 0;
         cached[dev] = n + 1;
     }
@@ -1537,7 +1540,7 @@ gf_status ns_iterate(const NsPlan& p, char* base, int steps, const float* coeffs
         good = map(&a.tm_a[k], a.x[k], xp, 2 * b, 128, 64) && map(&a.tm_g[k], a.x[k], xp, 2 * b, share(PH_GRAM), 64) &&
                map(&a.tm_n[k], a.x[k], xp, 2 * b, 64, share(PH_APPLY));
     if (!good) return GF_ERR_CUDA;
-    if (pair) return p.split == 2 ? launch_iterate<2, true>(a, units, s) : launch_iterate<1, true>(a, units, s);
+    if (pair) return launch_iterate<1, true>(a, units, s);        // (pairs of fp16: single CTAs, see choose_shapes)
     return p.split == 2 ? launch_iterate<2, false>(a, units, s) : launch_iterate<1, false>(a, units, s);
 }
 
