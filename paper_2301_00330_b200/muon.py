@@ -70,6 +70,10 @@ class Muon(torch.optim.Optimizer):
                     raise ValueError(f"Muon takes matrices and convolution kernels, got a parameter of shape {tuple(p.shape)}")
         self._workspaces = {}
 
+    def __setstate__(self, state):      # of a copy, or of one that was pickled: a base class without the workspaces
+        super().__setstate__(state)
+        self.__dict__.setdefault("_workspaces", {})
+
     def _workspace(self, device, nbytes: int) -> torch.Tensor:
         # one per device and stream: calls on one stream follow one another
         key = device, torch.cuda.current_stream(device).cuda_stream

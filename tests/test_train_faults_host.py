@@ -1,6 +1,10 @@
 """What goes wrong on the way of the fine-tuning operators has to be seen: waits that run out, copies of an optimiser or a
 layer, settings that change between steps.  No GPU needed."""
+import copy
+import pickle
+
 import pytest
+import torch
 
 
 @pytest.mark.parametrize("turns", [1, 3, 15])
@@ -21,3 +25,16 @@ def test_the_warp_wait_checks_its_arguments(gf):
     with pytest.raises(gf.GfError) as e:
         gf.gf_selftest_warp_wait(None, 1000, 0)
     assert e.value.status == gf.GF_ERR_NULL
+
+
+@pytest.mark.parametrize("how", ["deepcopy", "pickle"])
+def test_a_copied_optimizer_has_its_workspaces(gf, how):
+    """torch's base class copies settings, state and groups only; step() needs the rest too."""
+    opt = gf.Muon([torch.nn.Parameter(torch.zeros(4, 6))], lr=0.5)
+    again = copy.deepcopy(opt) if how == "deepcopy" else pickle.loads(pickle.dumps(opt))
+    assert again._workspaces == {} and again._workspaces is not opt._workspaces
+    assert again.param_groups[0]["lr"] == 0.5
+    p = again.param_groups[0]["params"][0]
+    p.grad = torch.zeros_like(p)
+    with pytest.raises(RuntimeError, match="no CPU path"):      # as far as a step gets here
+        again.step()
