@@ -74,6 +74,21 @@ class Muon(torch.optim.Optimizer):
         super().__setstate__(state)
         self.__dict__.setdefault("_workspaces", {})
 
+    def load_state_dict(self, state_dict):
+        # torch casts a state to the dtype of its parameter; the momentum is kept in 32 bits whatever that is, and so it is
+        # taken from the state as it was given (after the hooks that may change it)
+        given = {}
+        last = self.register_load_state_dict_pre_hook(lambda _, d: given.update(d))
+        try:
+            super().load_state_dict(state_dict)
+        finally:
+            last.remove()
+        ids = [i for group in given["param_groups"] for i in group["params"]]
+        for i, p in zip(ids, [p for group in self.param_groups for p in group["params"]]):
+            momentum = given["state"].get(i, {}).get("momentum")
+            if momentum is not None:
+                self.state[p]["momentum"] = momentum.to(device=p.device, dtype=torch.float32, copy=True)
+
     def _workspace(self, device, nbytes: int) -> torch.Tensor:
         # one per device and stream: calls on one stream follow one another
         key = device, torch.cuda.current_stream(device).cuda_stream
@@ -111,7 +126,7 @@ class Muon(torch.optim.Optimizer):
                     if m.shape != (rows, cols):
                         raise ValueError(f"a momentum of shape {(rows, cols)} expected, got {tuple(m.shape)}: was it kept with another "
                                          "setting of filtered_taps?")
-                    if m.dtype != torch.float32 or not m.is_contiguous():      # loading a state casts it to the parameter's dtype
+                    if m.dtype != torch.float32 or not m.is_contiguous():      # put there by someone else
                         m = state["momentum"] = m.to(torch.float32).contiguous()
                     momenta.append(m)
                 precision = group["precision"] or ("f32" if wdt == torch.float32 else "f16")

@@ -12,3 +12,24 @@ def test_the_lanes_of_a_warp_give_up_together(gf):
     gf.gf_selftest_warp_wait(result, 1_000_000)
     torch.cuda.synchronize()
     assert bool((result == 0).all()), result.tolist()
+
+
+def test_a_resumed_optimizer_goes_on_as_the_uninterrupted_one(gf):
+    """16-bit weights, 32-bit momentum: saving and loading between two steps changes no bit of the weights."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    start = torch.randn(40, 24, generator=g, device="cuda").bfloat16()
+    grads = [torch.randn(40, 24, generator=g, device="cuda").bfloat16() for _ in range(3)]
+    p = torch.nn.Parameter(start.clone())
+    opt = gf.Muon([p], lr=0.1)
+    for k, grad in enumerate(grads):
+        if k == 2:      # a second optimiser takes over here
+            q = torch.nn.Parameter(p.detach().clone())
+            other = gf.Muon([q], lr=0.1)
+            other.load_state_dict(opt.state_dict())
+            q.grad = grad.clone()
+            other.step()
+        p.grad = grad.clone()
+        opt.step()
+    assert torch.equal(p, q) and torch.equal(opt.state[p]["momentum"], other.state[q]["momentum"])
+    assert not torch.equal(p, start)

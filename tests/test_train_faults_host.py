@@ -38,3 +38,31 @@ def test_a_copied_optimizer_has_its_workspaces(gf, how):
     p.grad = torch.zeros_like(p)
     with pytest.raises(RuntimeError, match="no CPU path"):      # as far as a step gets here
         again.step()
+
+
+def test_a_loaded_momentum_keeps_its_32_bits(gf):
+    """Also with 16-bit parameters, to whose dtype torch casts a state; the saved tensors stay the saver's own, and a hook that
+    changes the state on its way in is heard."""
+    params = [torch.nn.Parameter(torch.zeros(4, 6, dtype=dt)) for dt in (torch.bfloat16, torch.float32, torch.bfloat16)]
+    opt = gf.Muon([{"params": params[:2]}, {"params": params[2:], "lr": 0.25}])
+    g = torch.Generator()
+    g.manual_seed(1)
+    for p in params[:2]:      # the third has not been updated yet
+        opt.state[p]["momentum"] = torch.randn(4, 6, generator=g)
+    saved = opt.state_dict()
+    fresh = [torch.nn.Parameter(p.detach().clone()) for p in params]
+    again = gf.Muon([{"params": fresh[:2]}, {"params": fresh[2:]}])
+    again.load_state_dict(saved)
+    for p, q in zip(params[:2], fresh):
+        m = again.state[q]["momentum"]
+        assert m.dtype == torch.float32 and torch.equal(m, opt.state[p]["momentum"])
+        m.zero_()
+        assert bool(opt.state[p]["momentum"].any())
+    assert "momentum" not in again.state.get(fresh[2], {}) and again.param_groups[1]["lr"] == 0.25
+
+    def doubled(_, d):
+        return {**d, "state": {k: {"momentum": 2 * v["momentum"]} for k, v in d["state"].items()}}
+
+    again.register_load_state_dict_pre_hook(doubled)
+    again.load_state_dict(saved)
+    assert torch.equal(again.state[fresh[0]]["momentum"], 2 * opt.state[params[0]]["momentum"])
