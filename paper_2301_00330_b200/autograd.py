@@ -90,6 +90,17 @@ class FilteredConv2d(torch.nn.Module):
         torch.nn.init.kaiming_normal_(self.weight)
         self.bias = torch.nn.Parameter(torch.zeros(out_channels, device=device, dtype=dtype)) if bias else None
 
+    # copying a parameter drops its attributes: a copy of the layer takes them along
+    def __getstate__(self):
+        return {**self.__dict__, "_weight_filtered_taps": getattr(self.weight, "filtered_taps", False)}
+
+    def __setstate__(self, state):
+        state = dict(state)
+        taps = state.pop("_weight_filtered_taps", None)
+        super().__setstate__(state)
+        if taps is not None:
+            self.weight.filtered_taps = taps
+
     def forward(self, x):
         y = filtered_conv2d(x, self.weight, self.r, self.groups, self.stride)
         return y if self.bias is None else y + self.bias.view(1, -1, 1, 1)

@@ -66,3 +66,19 @@ def test_a_loaded_momentum_keeps_its_32_bits(gf):
     again.register_load_state_dict_pre_hook(doubled)
     again.load_state_dict(saved)
     assert torch.equal(again.state[fresh[0]]["momentum"], 2 * opt.state[params[0]]["momentum"])
+
+
+@pytest.mark.parametrize("how", ["deepcopy", "copy", "pickle", "inside"])
+def test_a_copied_layer_keeps_what_its_weight_says_of_the_gradient(gf, how):
+    for r in (1, 2):
+        conv = gf.FilteredConv2d(4, 6, 3, r=r)
+        if how == "pickle":
+            again = pickle.loads(pickle.dumps(conv))
+        elif how == "inside":      # a layer of a model, copied with its optimiser
+            model, opt = copy.deepcopy((torch.nn.Sequential(conv), gf.Muon([conv.weight])))
+            again = model[0]
+            assert opt.param_groups[0]["params"][0] is again.weight
+        else:
+            again = getattr(copy, how)(conv)
+        assert again.weight.filtered_taps is (r == 2)
+        assert torch.equal(again.weight, conv.weight) and again.r == r and "_weight_filtered_taps" not in again.__dict__
