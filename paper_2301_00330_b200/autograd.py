@@ -73,7 +73,13 @@ class _FilteredConv2dFn(torch.autograd.Function):
 def filtered_conv2d(x: torch.Tensor, weight: torch.Tensor, r: int = 2, groups: int = 1, stride: int = 1) -> torch.Tensor:
     """conv2d(x, weight) with padding (k-1)/2 and the given stride whose gradients are the
     filtered ones with patch size r (r = 1: the exact gradients).  The bias, if any, is added
-    by the caller (its gradient is not affected by the method)."""
+    by the caller (its gradient is not affected by the method).
+
+    A weight marked `filtered_taps` (its gradients have one value for all taps of a kernel, which Muon makes use of)
+    loses the mark in a call with r = 1 that tracks gradients: from then on its gradients, and a momentum
+    that holds them, differ from tap to tap."""
+    if r < 2 and torch.is_grad_enabled() and weight.requires_grad and getattr(weight, "filtered_taps", False):
+        weight.filtered_taps = False
     return _FilteredConv2dFn.apply(x, weight, int(r), int(groups), int(stride))
 
 

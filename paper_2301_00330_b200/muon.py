@@ -52,7 +52,8 @@ class Muon(torch.optim.Optimizer):
     kernel -- the weights of FilteredConv2d with r >= 2 -- and its update then costs the products of
     [C_out, C_in / groups] alone; the result is the same.  This reads each gradient at its first tap: whatever
     else is added to such a gradient (an L2 term in the loss, another use of the weight) has to have one value
-    for all taps too, or the parameter's attribute, or `filtered_taps` here, is set to False.  Parameters of one
+    for all taps too, or the parameter's attribute, or `filtered_taps` here, is set to False.  Using the weight
+    with r = 1 does that by itself, for good; the momentum is spread over the taps then.  Parameters of one
     shape and kind go through one call of the library."""
 
     def __init__(self, params, lr: float = 1e-3, momentum: float = 0.95, nesterov: bool = True, weight_decay: float = 0.0,
@@ -123,6 +124,10 @@ class Muon(torch.optim.Optimizer):
                     if "momentum" not in state:
                         state["momentum"] = torch.zeros((rows, cols), dtype=torch.float32, device=device)
                     m = state["momentum"]
+                    all_taps = math.prod(p.shape[2:])
+                    if group["filtered_taps"] and taps == 1 and all_taps > 1 and m.shape == (rows, cols // all_taps):
+                        # kept while the gradients had one value for all taps, which they no longer have
+                        m = state["momentum"] = m.repeat_interleave(all_taps, 1)
                     if m.shape != (rows, cols):
                         raise ValueError(f"a momentum of shape {(rows, cols)} expected, got {tuple(m.shape)}: was it kept with another "
                                          "setting of filtered_taps?")

@@ -33,3 +33,25 @@ def test_a_resumed_optimizer_goes_on_as_the_uninterrupted_one(gf):
         opt.step()
     assert torch.equal(p, q) and torch.equal(opt.state[p]["momentum"], other.state[q]["momentum"])
     assert not torch.equal(p, start)
+
+
+def test_switching_a_layer_to_exact_gradients_reaches_its_update(gf):
+    """Two steps with filtered gradients, two with exact ones after conv.r = 1, one with filtered ones again: the updates are those
+    of an optimiser that never counted on equal taps.  Bound as where equal taps are compared with flattened kernels; with
+    one tap read for all the weights would be off by the size of a step, about 1e-2 of them."""
+    torch.manual_seed(5)
+    conv = gf.FilteredConv2d(12, 20, 3, r=2, bias=False, device="cuda")
+    twin = torch.nn.Parameter(conv.weight.detach().clone())
+    opt, other = gf.Muon([conv.weight], lr=1e-2, weight_decay=0.1), gf.Muon([twin], lr=1e-2, weight_decay=0.1, filtered_taps=False)
+    for r in (2, 2, 1, 1, 2):
+        conv.r = r
+        x = torch.randn(2, 12, 16, 16, device="cuda")
+        conv.weight.grad = None
+        conv(x).square().mean().backward()
+        taps = conv.weight.grad.flatten(2)
+        assert bool((taps == taps[..., :1]).all()) == (r == 2)
+        twin.grad = conv.weight.grad.clone()
+        opt.step()
+        other.step()
+        assert float((conv.weight - twin).detach().norm() / twin.detach().norm()) <= 1e-5, r
+    assert opt.state[conv.weight]["momentum"].shape == (20, 108)

@@ -82,3 +82,26 @@ def test_a_copied_layer_keeps_what_its_weight_says_of_the_gradient(gf, how):
             again = getattr(copy, how)(conv)
         assert again.weight.filtered_taps is (r == 2)
         assert torch.equal(again.weight, conv.weight) and again.r == r and "_weight_filtered_taps" not in again.__dict__
+
+
+def test_exact_gradients_take_the_mark_of_equal_taps_off(gf, monkeypatch):
+    """r is read at every call: once a call with r = 1 can put exact gradients into a weight, Muon must not read one tap for
+    all of them any more, whatever r is set to later."""
+    from paper_2301_00330_b200 import autograd
+    monkeypatch.setattr(autograd._FilteredConv2dFn, "apply", lambda x, *_: x)
+    x = torch.zeros(1, 4, 6, 6)
+    conv = gf.FilteredConv2d(4, 6, 3, r=2, bias=False)
+    conv(x)
+    assert conv.weight.filtered_taps
+    conv.r = 1
+    with torch.no_grad():
+        conv(x)
+    assert conv.weight.filtered_taps            # nothing was tracked
+    conv(x)
+    assert not conv.weight.filtered_taps
+    conv.r = 2
+    conv(x)
+    assert not conv.weight.filtered_taps        # the momentum holds exact gradients
+    conv = gf.FilteredConv2d(4, 6, 3, r=2, bias=False)
+    gf.filtered_conv2d(x, conv.weight, r=1)
+    assert not conv.weight.filtered_taps
