@@ -59,17 +59,25 @@ class Muon(torch.optim.Optimizer):
     def __init__(self, params, lr: float = 1e-3, momentum: float = 0.95, nesterov: bool = True, weight_decay: float = 0.0,
                  steps: int = 5, eps: float = 1e-7, precision: str | None = None,
                  filtered_taps: bool = True):
-        if lr < 0 or not 0 <= momentum < 1 or weight_decay < 0:
-            raise ValueError("lr >= 0, 0 <= momentum < 1 and weight_decay >= 0 expected")
-        if precision is not None and precision not in _PRECISION:
-            raise ValueError("precision is 'f16', 'f32' or None")
         super().__init__(params, dict(lr=lr, momentum=momentum, nesterov=nesterov, weight_decay=weight_decay, steps=steps, eps=eps,
                                       precision=precision, filtered_taps=filtered_taps))
-        for group in self.param_groups:
-            for p in group["params"]:
-                if p.dim() not in (2, 4):
-                    raise ValueError(f"Muon takes matrices and convolution kernels, got a parameter of shape {tuple(p.shape)}")
         self._workspaces = {}
+
+    def add_param_group(self, param_group):
+        """As torch's; settings and parameters are checked for every group, those of the constructor among them."""
+        if not isinstance(param_group["params"], torch.Tensor):
+            param_group["params"] = list(param_group["params"])      # (a generator can be read once)
+        params = param_group["params"]
+        for p in [params] if isinstance(params, torch.Tensor) else params:
+            p = p[1] if isinstance(p, tuple) else p                  # named parameters
+            if isinstance(p, torch.Tensor) and p.dim() not in (2, 4):
+                raise ValueError(f"Muon takes matrices and convolution kernels, got a parameter of shape {tuple(p.shape)}")
+        given = {**self.defaults, **param_group}
+        if given["lr"] < 0 or not 0 <= given["momentum"] < 1 or given["weight_decay"] < 0:
+            raise ValueError("lr >= 0, 0 <= momentum < 1 and weight_decay >= 0 expected")
+        if given["precision"] is not None and given["precision"] not in _PRECISION:
+            raise ValueError("precision is 'f16', 'f32' or None")
+        super().add_param_group(param_group)
 
     def __setstate__(self, state):      # of a copy, or of one that was pickled: a base class without the workspaces
         super().__setstate__(state)

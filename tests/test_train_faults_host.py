@@ -105,3 +105,22 @@ def test_exact_gradients_take_the_mark_of_equal_taps_off(gf, monkeypatch):
     conv = gf.FilteredConv2d(4, 6, 3, r=2, bias=False)
     gf.filtered_conv2d(x, conv.weight, r=1)
     assert not conv.weight.filtered_taps
+
+
+def test_every_parameter_group_is_checked(gf):
+    """Groups that are added later, and settings of a group of its own."""
+    matrix = lambda: torch.nn.Parameter(torch.zeros(8, 4))  # noqa: E731
+    opt = gf.Muon([matrix()])
+    with pytest.raises(ValueError, match="matrices"):
+        opt.add_param_group({"params": [torch.nn.Parameter(torch.zeros(8))]})
+    for bad in ({"lr": -1.0}, {"momentum": 1.0}, {"weight_decay": -0.1}, {"precision": "tf32"}):
+        with pytest.raises(ValueError):
+            opt.add_param_group({"params": [matrix()], **bad})
+        with pytest.raises(ValueError):
+            gf.Muon([{"params": [matrix()], **bad}])
+    assert len(opt.param_groups) == 1
+    opt.add_param_group({"params": (matrix() for _ in range(2)), "lr": 0.5})
+    opt.add_param_group({"params": matrix()})
+    assert [len(g["params"]) for g in opt.param_groups] == [1, 2, 1] and opt.param_groups[1]["lr"] == 0.5
+    named = gf.Muon(torch.nn.Linear(4, 8, bias=False).named_parameters())
+    assert len(named.param_groups[0]["params"]) == 1
