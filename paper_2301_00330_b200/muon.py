@@ -106,12 +106,24 @@ class Muon(torch.optim.Optimizer):
             ws = self._workspaces[key] = torch.empty(nbytes, dtype=torch.uint8, device=device)
         return ws
 
+    def _momentum(self, p, rows: int, cols: int) -> torch.Tensor:
+        state = self.state[p]
+        m = state.get("momentum")
+        if m is None:
+            m = torch.zeros((rows, cols), dtype=torch.float32, device=p.device)
+        elif m.shape != (rows, cols):      # kept while the gradients had one value for all taps, which they no longer have
+            m = m.repeat_interleave(cols // m.shape[1], 1)
+        state["momentum"] = m = m.to(torch.float32).contiguous()      # (itself, unless someone else put it there)
+        return m
+
     @torch.no_grad()
     def step(self, closure=None):
         loss = None
         if closure is not None:
             with torch.enable_grad():
                 loss = closure()
+        # what one call takes is gathered and checked first, for all groups: a step that is refused has changed nothing
+        calls = []
         for group in self.param_groups:
             alike = {}
             for p in group["params"]:
@@ -121,34 +133,29 @@ class Muon(torch.optim.Optimizer):
                     raise RuntimeError("Muon needs CUDA parameters: there is no CPU path")
                 if not p.is_contiguous():
                     raise ValueError("Muon updates parameters in place: they have to be contiguous")
+                if p.grad.layout != torch.strided:
+                    raise TypeError("Muon takes dense gradients")
                 rows, taps = p.shape[0], math.prod(p.shape[2:])
                 uniform = taps if group["filtered_taps"] and getattr(p, "filtered_taps", False) else 1
                 cols = p.numel() // rows // uniform
+                m = self.state[p].get("momentum") if p in self.state else None
+                if m is not None and m.shape != (rows, cols) and not (
+                        group["filtered_taps"] and uniform == 1 and taps > 1 and m.shape == (rows, cols // taps)):
+                    raise ValueError(f"a momentum of shape {(rows, cols)} expected, got {tuple(m.shape)}: was it kept with another "
+                                     "setting of filtered_taps?")
                 alike.setdefault((p.device, rows, cols, uniform, p.grad.dtype, p.dtype), []).append(p)
             for (device, rows, cols, taps, gdt, wdt), ps in alike.items():
-                momenta = []
-                for p in ps:
-                    state = self.state[p]
-                    if "momentum" not in state:
-                        state["momentum"] = torch.zeros((rows, cols), dtype=torch.float32, device=device)
-                    m = state["momentum"]
-                    all_taps = math.prod(p.shape[2:])
-                    if group["filtered_taps"] and taps == 1 and all_taps > 1 and m.shape == (rows, cols // all_taps):
-                        # kept while the gradients had one value for all taps, which they no longer have
-                        m = state["momentum"] = m.repeat_interleave(all_taps, 1)
-                    if m.shape != (rows, cols):
-                        raise ValueError(f"a momentum of shape {(rows, cols)} expected, got {tuple(m.shape)}: was it kept with another "
-                                         "setting of filtered_taps?")
-                    if m.dtype != torch.float32 or not m.is_contiguous():      # put there by someone else
-                        m = state["momentum"] = m.to(torch.float32).contiguous()
-                    momenta.append(m)
                 precision = group["precision"] or ("f32" if wdt == torch.float32 else "f16")
                 desc = B.make_muon_desc(len(ps), rows, cols, taps, grad_dtype=gdt, weight_dtype=wdt, precision=_PRECISION[precision],
                                         steps=group["steps"], nesterov=group["nesterov"], eps=group["eps"],
                                         momentum=group["momentum"], lr=group["lr"], weight_decay=group["weight_decay"],
                                         scale=0.2 * math.sqrt(max(rows, cols * taps)))
                 with torch.cuda.device(device):
-                    grads = [p.grad.contiguous() for p in ps]
-                    B.gf_muon_step(desc, grads, momenta, ps, momenta, ps, self._workspace(device, B.gf_muon_workspace_bytes(desc)),
-                                   None, None, torch.cuda.current_stream(device))
+                    calls.append((device, desc, ps, B.gf_muon_workspace_bytes(desc)))
+        for device, desc, ps, nbytes in calls:
+            momenta = [self._momentum(p, desc.rows, desc.cols) for p in ps]
+            with torch.cuda.device(device):
+                grads = [p.grad.contiguous() for p in ps]
+                B.gf_muon_step(desc, grads, momenta, ps, momenta, ps, self._workspace(device, nbytes), None, None,
+                               torch.cuda.current_stream(device))
         return loss

@@ -55,3 +55,23 @@ def test_switching_a_layer_to_exact_gradients_reaches_its_update(gf):
         other.step()
         assert float((conv.weight - twin).detach().norm() / twin.detach().norm()) <= 1e-5, r
     assert opt.state[conv.weight]["momentum"].shape == (20, 108)
+
+
+@pytest.mark.parametrize("bad", ["transposed", "too wide", "16-bit float", "sparse", "momentum", "on the CPU"])
+def test_a_step_that_is_refused_changes_nothing(gf, bad):
+    """A parameter that Muon cannot take, behind others that it can: their weights and their state stay as they were."""
+    good = torch.nn.Parameter(torch.ones(8, 6, device="cuda"))
+    other = torch.nn.Parameter({"transposed": lambda: torch.ones(6, 4, device="cuda").t(),
+                                "too wide": lambda: torch.ones(2, 16385, device="cuda"),
+                                "16-bit float": lambda: torch.ones(4, 6, device="cuda", dtype=torch.float16),
+                                "on the CPU": lambda: torch.ones(4, 6)}.get(bad, lambda: torch.ones(4, 6, device="cuda"))())
+    opt = gf.Muon([{"params": [good]}, {"params": [other]}])
+    good.grad = torch.ones_like(good)
+    other.grad = torch.ones_like(other).to_sparse() if bad == "sparse" else torch.ones_like(other)
+    if bad == "momentum":
+        opt.state[other]["momentum"] = torch.zeros(3, 3, device="cuda")
+    before = gf.gf_kernel_launch_count()
+    with pytest.raises((ValueError, TypeError, RuntimeError)):      # GfError is a RuntimeError
+        opt.step()
+    torch.cuda.synchronize()
+    assert bool((good == 1).all()) and "momentum" not in opt.state.get(good, {}) and gf.gf_kernel_launch_count() == before
