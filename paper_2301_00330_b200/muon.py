@@ -158,4 +158,6 @@ class Muon(torch.optim.Optimizer):
                 grads = [p.grad.contiguous() for p in ps]
                 B.gf_muon_step(desc, grads, momenta, ps, momenta, ps, self._workspace(device, nbytes), None, None,
                                torch.cuda.current_stream(device))
+            # the library writes through addresses, which autograd does not see: a graph that saved a weight before has to know
+            torch.autograd.graph.increment_version(ps)
         return loss

@@ -75,3 +75,18 @@ def test_a_step_that_is_refused_changes_nothing(gf, bad):
         opt.step()
     torch.cuda.synchronize()
     assert bool((good == 1).all()) and "momentum" not in opt.state.get(good, {}) and gf.gf_kernel_launch_count() == before
+
+
+def test_autograd_sees_that_a_step_has_changed_the_weights(gf):
+    """backward() through a graph that saved a weight before the step is refused, as with torch's optimisers, instead of
+    giving gradients of a mixture of old activations and new weights."""
+    p = torch.nn.Parameter(torch.randn(6, 5, device="cuda"))
+    x = torch.randn(3, 5, device="cuda", requires_grad=True)
+    opt = gf.Muon([p])
+    y = x @ p.t()
+    p.grad = torch.ones_like(p)
+    version = p._version
+    opt.step()
+    assert p._version > version
+    with pytest.raises(RuntimeError, match="inplace"):
+        y.sum().backward()
