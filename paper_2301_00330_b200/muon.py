@@ -127,7 +127,7 @@ class Muon(torch.optim.Optimizer):
         for group in self.param_groups:
             alike = {}
             for p in group["params"]:
-                if p.grad is None:
+                if p.grad is None or p.numel() == 0:
                     continue
                 if not p.is_cuda:
                     raise RuntimeError("Muon needs CUDA parameters: there is no CPU path")

@@ -124,3 +124,12 @@ def test_every_parameter_group_is_checked(gf):
     assert [len(g["params"]) for g in opt.param_groups] == [1, 2, 1] and opt.param_groups[1]["lr"] == 0.5
     named = gf.Muon(torch.nn.Linear(4, 8, bias=False).named_parameters())
     assert len(named.param_groups[0]["params"]) == 1
+
+
+@pytest.mark.parametrize("shape", [(0, 4), (4, 0), (6, 0, 3, 3)])
+def test_a_parameter_without_elements_is_left_alone(gf, shape):
+    p = torch.nn.Parameter(torch.zeros(shape))
+    opt = gf.Muon([p])
+    p.grad = torch.zeros(shape)
+    opt.step()
+    assert not opt.state
