@@ -25,6 +25,8 @@ class _LayerNormFn(torch.autograd.Function):
             raise RuntimeError("layer_norm needs CUDA tensors: there is no CPU path")
         C = x.shape[channel_dim]
         for p in (weight, bias):
+            if p is not None and p.device != x.device:
+                raise ValueError(f"weight and bias lie on the device of x, {x.device}, got {p.device}")
             if p is not None and p.shape != (C,):
                 raise ValueError(f"weight and bias have the shape ({C},), got {tuple(p.shape)}")
         if weight is not None and bias is not None and weight.dtype != bias.dtype:

@@ -133,3 +133,14 @@ def test_a_parameter_without_elements_is_left_alone(gf, shape):
     p.grad = torch.zeros(shape)
     opt.step()
     assert not opt.state
+
+
+def test_layer_norm_refuses_parameters_of_another_device(gf):
+    """A weight of another GPU would reach the kernel as an address.  (Tensors without memory stand in for those of two GPUs.)"""
+    from torch._subclasses.fake_tensor import FakeTensorMode
+    with FakeTensorMode():
+        x, near, far = (torch.empty(n, device=f"cuda:{d}") for n, d in (((4, 8), 0), ((8,), 0), ((8,), 1)))
+        assert x.is_cuda and far.device.index == 1
+        for weight, bias in ((far, None), (None, far), (near, far), (far, near)):
+            with pytest.raises(ValueError, match="device"):
+                gf.layer_norm(x, weight, bias)
