@@ -23,7 +23,7 @@ int g_prof_used = 0;             // event pairs recorded since the last read
 int g_prof_slot_kid[kProfPairs];
 const char* const kKernelNames[K_COUNT] = {
     "stash_pool", "ksum", "gy_pool", "gx_mix", "gw_partial", "gw_finish", "dw_fused", "exact_gx", "exact_gw", "gx_tc", "gw_tc", "split_f32", "gyx_fused", "gw_tiled",
-    "norm_fwd", "norm_bwd", "norm_sums", "ns_prepare", "ns_product"};
+    "norm_fwd", "norm_bwd", "norm_sums", "ns_prepare", "ns_product", "ns_finish"};
 }  // namespace
 
 ProfScope::ProfScope(int kernel_id, cudaStream_t s) : slot(-1), stream(s) {

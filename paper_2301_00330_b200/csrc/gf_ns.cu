@@ -1544,7 +1544,11 @@ gf_status ns_iterate(const NsPlan& p, char* base, int steps, const float* coeffs
     return p.split == 2 ? launch_iterate<2, false>(a, units, s) : launch_iterate<1, false>(a, units, s);
 }
 
-dim3 finish_grid(const NsPlan& p, int count) { return dim3((p.cols + kCast - 1) / kCast, (p.rows + kFinRows - 1) / kFinRows, count); }
+template <bool MUON> gf_status launch_finish(const NsPlan& p, const FinishArgs& f, int count, cudaStream_t s) {
+    ProfScope prof(K_NS_FINISH, s);
+    const dim3 grid((p.cols + kCast - 1) / kCast, (p.rows + kFinRows - 1) / kFinRows, count);
+    return launch_pdl(ns_finish_kernel<MUON>, grid, dim3(256), 0, s, f);
+}
 FinishArgs finish_args(const NsPlan& p, char* base, int steps, int first) {
     FinishArgs f = {};
     f.x = reinterpret_cast<const __half*>(base + p.off_x[steps & 1]) + 8LL * first * p.x_pieces * p.m;
@@ -1641,7 +1645,7 @@ gf_status gf_newton_schulz(const gf_ns_desc* d, const void* G, void* O, void* wo
     if (gf_status st = ns_iterate(p, base, d->steps, h_coeffs, s); st != GF_OK) return st;
     FinishArgs f = finish_args(p, base, d->steps, 0);
     f.out = O; f.bf16 = d->out_dtype == GF_BF16;
-    return launch_pdl(ns_finish_kernel<false>, finish_grid(p, d->batch), dim3(256), 0, s, f);
+    return launch_finish<false>(p, f, d->batch, s);
 }
 
 gf_status gf_muon_workspace_bytes(const gf_muon_desc* d, size_t* bytes) {
@@ -1710,7 +1714,7 @@ gf_status gf_muon_step(const gf_muon_desc* d, const void* const* h_grad, const f
         f.taps = d->taps; f.div_taps = FastDiv((uint32_t)d->taps); f.bf16 = d->weight_dtype == GF_BF16;
         f.keep = 1.f - d->lr * d->weight_decay;
         f.f = d->lr * d->scale / root;
-        if (gf_status st = launch_pdl(ns_finish_kernel<true>, finish_grid(p, n), dim3(256), 0, s, f); st != GF_OK) return st;
+        if (gf_status st = launch_finish<true>(p, f, n, s); st != GF_OK) return st;
     }
     return GF_OK;
 }

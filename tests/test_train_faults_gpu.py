@@ -90,3 +90,23 @@ def test_autograd_sees_that_a_step_has_changed_the_weights(gf):
     assert p._version > version
     with pytest.raises(RuntimeError, match="inplace"):
         y.sum().backward()
+
+
+def test_the_timing_of_a_step_covers_all_its_kernels(gf):
+    """Sums of squares, products and the kernel that writes the results: each launch lies between events of its own kind."""
+    rows, cols = 200, 160
+    G = torch.randn(1, rows, cols, device="cuda")
+    O, desc = torch.empty_like(G), gf.make_ns_desc(1, rows, cols)
+    muon = gf.make_muon_desc(1, rows, cols)
+    ws = torch.empty(max(gf.gf_newton_schulz_workspace_bytes(desc), gf.gf_muon_workspace_bytes(muon)), dtype=torch.uint8, device="cuda")
+    m, w = torch.zeros(rows, cols, device="cuda"), torch.zeros(rows, cols, device="cuda")
+    gf.gf_profile_read()
+    gf.gf_profile_configure(2)
+    try:
+        gf.gf_newton_schulz(desc, G, O, ws)
+        gf.gf_muon_step(muon, [G], [m], [w], [m], [w], ws)
+        got = gf.gf_profile_read()
+    finally:
+        gf.gf_profile_configure(0)
+    assert {name: n for name, (n, _) in got.items()} == {"ns_prepare": 2, "ns_product": 2, "ns_finish": 2}
+    assert all(ms > 0 for _, ms in got.values())
