@@ -66,8 +66,11 @@ gf_status gf_layer_norm_backward(const gf_norm_desc* desc, const void* g_y, cons
  *   precision GF_NS_F16: the products' operands are rounded to fp16 under a fixed scale (11
  *     significant bits), sums are fp32 -- for updates that are applied in 16 bits or that are
  *     small beside the weights.
- *   precision GF_NS_F32: operands are carried as pairs of fp16 (22 significant bits), three
- *     products each -- results as from fp32 arithmetic.
+ *   precision GF_NS_F32: operands are carried as pairs of fp16, an entry v to within
+ *     max(2^-22 |v|, 2^-35), three products each -- results of matrices in the range of real
+ *     updates as from fp32 arithmetic (off by 2e-6 to 8e-6 of their norm).  The second bound holds for
+ *     entries below 2^-13 of X, whose norm is 1 or, where eps is not small beside ||G||, less: a G
+ *     far below eps is orthogonalised to fewer bits.
  * The coefficients have to keep the entries of X, A and b A + c A A below 32 in magnitude (the
  * defaults keep the singular values below 1.3); beyond that the fp16 range ends and the result
  * is not finite.  A matrix of zeros gives zeros; one with a non-finite entry or whose squares

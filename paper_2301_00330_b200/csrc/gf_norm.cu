@@ -211,7 +211,8 @@ __global__ void __launch_bounds__(1024) ln_rows_fwd_kernel(const __grid_constant
     if (a.mean && g == 0) { a.mean[row] = mean; a.rstd[row] = rstd; }
 }
 
-// Rows longer than the registers of a block: the row is read again from L2 for each pass.
+// Rows longer than the registers of a block (16384): the row is read again from L2 for each pass, an element at a time.
+// 1024 x 20000 fp32: 80 us, a third of the copy bandwidth.
 template <typename T> __global__ void __launch_bounds__(1024) ln_rows_fwd_long_kernel(const __grid_constant__ NormArgs a) {
     __shared__ float red[2][32];
     const long long row = blockIdx.x;
@@ -333,8 +334,9 @@ __global__ void __launch_bounds__(WHOLE_BLOCK ? 512 : kRowThreads) ln_rows_bwd_k
     }
 }
 
-// Rows longer than the registers of a block: two passes over the row (the second from L2); the
-// column sums are kept in the block's line of the workspace, each by the thread that owns the column.
+// Rows longer than the registers of a block (8192): two passes over the row (the second from L2); the
+// column sums are kept in the block's line of the workspace, each by the thread that owns the column: read and written
+// for every row, which is most of the time (2048 x 12288 fp32: 222 us for 46 of bytes; 4096 x 8192, in registers: 77 for 61).
 template <typename T> __global__ void __launch_bounds__(1024) ln_rows_bwd_long_kernel(const __grid_constant__ NormArgs a) {
     __shared__ float red[4][32];
     float* part = a.part ? a.part + (size_t)blockIdx.x * 2 * a.C : nullptr;
@@ -372,7 +374,8 @@ template <typename T> __global__ void __launch_bounds__(1024) ln_rows_bwd_long_k
 // the sums and stores of the present one.  A batch is one contiguous piece of memory, copied from the 16-byte
 // boundary before it to the one after it.  The last bytes of a tensor whose size is no multiple of 16 are fetched with
 // plain loads.
-// Measured: 100352 x 576 fp32 forward 88 us, 5.2 TB/s (0.80 of the copy bandwidth); 8192 x 4096 bf16 backward 47 us and 4 us
+// Measured: 100352 x 576 fp32 forward 83 to 88 us, 5.3 to 5.6 TB/s (0.80 to 0.85 of the copy bandwidth), bf16 78 us
+// (0.45); 8192 x 4096 bf16 backward 47 us and 4 us
 // for the lines of sums, 4.3 TB/s: 8 warps per SM (the sums take their registers), about 7 us of it start and
 // end; two rows at once with one exchange measured the same, 16 elements per thread and 16 warps measured 56 us in all.
 //   SHIFT: rows whose length is no multiple of 16 bytes, one to a batch.  The number of teams is a multiple of the period (at most
@@ -664,7 +667,8 @@ __global__ void __launch_bounds__(BWD ? 256 : 512) ln_rows_ring_kernel(const __g
 }
 
 // ---- channels first --------------------------------------------------------------------------
-// For small planes of odd size, and more channels than the tiles below hold: a block takes 32 V consecutive pixels (lane = pixel, V
+// For small planes of odd size, and more channels than the tiles below hold (128 x 768 x 7 x 7 fp32: forward 48 us, backward 58,
+// for 6 and 9 us of bytes; bf16 128 x 768 x 14 x 14: 60 and 157 for 12 and 18): a block takes 32 V consecutive pixels (lane = pixel, V
 // per lane) and all channels; warp w of CG
 // has channels w, w + CG, ...  Pixels are numbered through all images, so that small planes fill
 // the lanes; V divides the plane, so that a vector stays in it.
@@ -949,7 +953,9 @@ __global__ void __launch_bounds__(512) ln_planes_bwd_long_kernel(const __grid_co
 // channels, so that the sums over channels (per pixel) are sums in registers and a few exchanges per tile,
 // and the sums over pixels (per channel) stay in a thread's registers for the whole kernel.  The tile is read
 // from shared memory once per pass over it (two backward, three forward).
-// Measured: 256 x 512 x 16 x 16 fp32 backward 77 us and 3 us for the lines of sums, 5.2 TB/s; 64 x 96 x 55 x 55 bf16 forward 35 us,
+// Measured: 256 x 512 x 16 x 16 fp32 backward 77 us and 3 us for the lines of sums, 5.2 TB/s; 128 x 576 x 28 x 28 fp32, whose rows
+// are 64 bytes long forward and 32 backward (longer ones of 576 channels do not fit three times), 129 and 177 us, 0.55 and 0.60 of the
+// copy bandwidth; 64 x 96 x 55 x 55 bf16 forward 35 us,
 // 2.2 TB/s: planes of odd size are read and written a pixel at a time, about 30 instructions per pixel and channel (tiles of
 // 128 pixels 37 us, of 8 warps 53).
 //   WHOLE: every row of a plane starts on a 16-byte boundary; tiles come as boxes of the copy engine, a lane has a

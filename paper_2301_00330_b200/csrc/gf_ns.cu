@@ -3,8 +3,8 @@
 // X [m, n] with m <= n (the input is transposed on its way in when it is tall).  All operands of the
 // products are fp16 times kScale = 2^10: X of a normalised matrix has entries of rms 1 / sqrt(m n) and
 // magnitude at most about 1.3, so that the scaled values use the middle of fp16's range.  With
-// GF_NS_F32 each operand is a pair hi + lo of fp16 and a product is hi hi + hi lo + lo hi (2^-22
-// relative is dropped).  X is carried as a pair in either case: a X is added to the product in fp32.
+// GF_NS_F32 each operand is a pair hi + lo of fp16, within max(2^-22 |v|, 2^-35) of its value v (below |v| = 2^-13 lo is
+// subnormal), and a product is hi hi + hi lo + lo hi (2^-22 relative is dropped).  X is carried as a pair in either case: a X is added to the product in fp32.
 // Accumulators are fp32 in tensor memory.
 //
 // Layout of X, A = X X^T and B = b A + c A A in the workspace: [part][matrix][column / 8][row][column % 8], 16
@@ -613,8 +613,9 @@ template <int SPLIT, bool PAIR> __device__ __forceinline__ PhaseView phase_view(
 // all meet between phases.  Each role has a loop over the phases of its own, so that its registers are its own.
 // The two issuing warps run as whole warps and elect the thread that issues: descriptors and addresses then stay in
 // uniform registers.  (With the loop under `lane == 0` every product took 110 clocks to issue, whatever its size.)
-// Measured, five steps: 4096 x 4096 in fp16 operands 1.3 ms with the kernels around it, a pair's chunk of 64 in 528 clocks where the
-// products alone take 512, under the power cap; 4 x 2048 x 512 with pairs of fp16 244 us, bound by operands from L2 (58
+// Measured, five steps: 4096 x 4096 in fp16 operands, with the kernels around it, 1.32 to 1.37 ms back to back under the power
+// cap (SM clock 1.43 to 1.53 GHz), 1.15 to 1.18 ms in runs of a few calls; a CTA pair's chunk of 64 in 528 clocks where the
+// products alone take 512, and 8 rounds of tiles for 7.1 rounds of work; 4 x 2048 x 512 with pairs of fp16 244 us, bound by operands from L2 (58
 // bytes per clock and SM), 3000 clocks per meeting and 2500 to 9000 per tile's results; 6 x 256 x 256 105 us, 12000 clocks per
 // phase of which the products take 3600.
 template <int SPLIT, bool PAIR> __global__ void __launch_bounds__(kThreads, 1) ns_iterate_kernel(const __grid_constant__ IterateArgs p) {

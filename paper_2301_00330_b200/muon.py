@@ -21,7 +21,8 @@ def newton_schulz(G: torch.Tensor, steps: int = 5, eps: float = 1e-7, precision:
     """Newton-Schulz iterates of G [..., rows, cols] (float32 or bfloat16), of G's dtype or `out_dtype`.
 
     precision: "f16" (products of fp16 operands, fp32 sums) or "f32" (operands as pairs); by default
-    "f32" for float32 results and "f16" for bfloat16 ones.  coeffs: (a, b, c) for each step."""
+    "f32" for float32 results and "f16" for bfloat16 ones.  coeffs: (a, b, c) for each step.  The result is not
+    connected to G for autograd."""
     if not G.is_cuda:
         raise RuntimeError("newton_schulz needs a CUDA tensor: there is no CPU path")
     if G.dim() < 2:
