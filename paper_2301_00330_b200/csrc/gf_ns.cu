@@ -613,7 +613,7 @@ template <int SPLIT, bool PAIR> __device__ __forceinline__ PhaseView phase_view(
 // all meet between phases.  Each role has a loop over the phases of its own, so that its registers are its own.
 // The two issuing warps run as whole warps and elect the thread that issues: descriptors and addresses then stay in
 // uniform registers.  (With the loop under `lane == 0` every product took 110 clocks to issue, whatever its size.)
-// Measured, five steps: 4096 x 4096 in fp16 operands, with the kernels around it, 1.32 to 1.37 ms back to back under the power
+// Measured, five steps: 4096 x 4096 in fp16 operands, with the kernels around it, 1.32 to 1.39 ms back to back under the power
 // cap (SM clock 1.43 to 1.53 GHz), 1.15 to 1.18 ms in runs of a few calls; a CTA pair's chunk of 64 in 528 clocks where the
 // products alone take 512, and 8 rounds of tiles for 7.1 rounds of work; 4 x 2048 x 512 with pairs of fp16 244 us, bound by operands from L2 (58
 // bytes per clock and SM), 3000 clocks per meeting and 2500 to 9000 per tile's results; 6 x 256 x 256 105 us, 12000 clocks per
