@@ -30,6 +30,8 @@ def newton_schulz(G: torch.Tensor, steps: int = 5, eps: float = 1e-7, precision:
     out_dtype = G.dtype if out_dtype is None else out_dtype
     if precision is None:
         precision = "f32" if out_dtype == torch.float32 else "f16"
+    if precision not in _PRECISION:
+        raise ValueError("precision is 'f16', 'f32' or None")
     rows, cols = G.shape[-2:]
     G = _dense(G.detach())
     O = torch.empty(G.shape, dtype=out_dtype, device=G.device)

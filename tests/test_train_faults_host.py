@@ -144,3 +144,12 @@ def test_layer_norm_refuses_parameters_of_another_device(gf):
         for weight, bias in ((far, None), (None, far), (near, far), (far, near)):
             with pytest.raises(ValueError, match="device"):
                 gf.layer_norm(x, weight, bias)
+
+
+def test_newton_schulz_refuses_an_unknown_precision(gf):
+    """As Muon does, and not as a missing key.  (Tensors without memory stand in for those of a GPU.)"""
+    from torch._subclasses.fake_tensor import FakeTensorMode
+    with FakeTensorMode():
+        G = torch.empty((4, 8), device="cuda:0")
+        with pytest.raises(ValueError, match="precision"):
+            gf.newton_schulz(G, precision="tf32")
