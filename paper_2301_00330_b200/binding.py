@@ -1,4 +1,4 @@
-"""ctypes binding over the C ABI declared in include/gf.h and include/gf_train.h.
+"""ctypes binding over the C ABI declared in include/gf.h, include/gf_train.h and include/gf_block.h.
 
 Argument marshalling only: every step of the method runs in the CUDA kernels
 of libgf_b200.so.  torch is used for device memory and streams.  There is no
@@ -34,6 +34,9 @@ EXPORTS = (
     "gf_layer_norm_forward", "gf_layer_norm_backward_workspace_bytes", "gf_layer_norm_backward",
     "gf_newton_schulz_workspace_bytes", "gf_newton_schulz", "gf_muon_workspace_bytes", "gf_muon_step",
     "gf_selftest_end_of_turn", "gf_selftest_warp_wait",
+    "gf_dropout_forward", "gf_dropout_backward", "gf_rms_norm_forward", "gf_rms_norm_forward_fp8",
+    "gf_rms_norm_backward_workspace_bytes", "gf_rms_norm_backward", "gf_fp8_quantize_rows", "gf_fp8_quantize_blocks",
+    "gf_fp8_matmul",
 )
 
 
@@ -56,6 +59,23 @@ class gf_muon_desc(ctypes.Structure):
     _fields_ = ([(n, ctypes.c_int32) for n in ("count", "rows", "cols", "taps", "grad_dtype", "weight_dtype", "precision",
                                                "steps", "nesterov")]
                 + [(n, ctypes.c_float) for n in ("eps", "momentum", "lr", "weight_decay", "scale")])
+
+
+class gf_dropout_desc(ctypes.Structure):
+    _fields_ = [("count", ctypes.c_int64), ("dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32), ("p", ctypes.c_float)]
+
+
+class gf_rms_desc(ctypes.Structure):
+    _fields_ = ([("rows", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in ("cols", "dtype", "residual_dtype", "param_dtype")]
+                + [("eps", ctypes.c_float), ("p", ctypes.c_float)])
+
+
+class gf_fp8_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rows", "cols", "dtype")]
+
+
+class gf_fp8_matmul_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("M", "N", "K", "transposed", "out_dtype", "bias_dtype")]
 
 
 class gf_kernel_time(ctypes.Structure):
@@ -135,6 +155,20 @@ def lib() -> ctypes.CDLL:
         L.gf_muon_step.argtypes = [md, vp, vp, vp, vp, vp, vp, sz, vp, vp]
         for name in ("gf_layer_norm_forward", "gf_layer_norm_backward_workspace_bytes", "gf_layer_norm_backward",
                      "gf_newton_schulz_workspace_bytes", "gf_newton_schulz", "gf_muon_workspace_bytes", "gf_muon_step"):
+            getattr(L, name).restype = ctypes.c_int
+        od, rd, qd, pd = (ctypes.POINTER(c) for c in (gf_dropout_desc, gf_rms_desc, gf_fp8_desc, gf_fp8_matmul_desc))
+        L.gf_dropout_forward.argtypes = [od, vp, vp, vp, vp, vp]
+        L.gf_dropout_backward.argtypes = [od, vp, vp, vp, vp]
+        L.gf_rms_norm_forward.argtypes = [rd, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.gf_rms_norm_forward_fp8.argtypes = [rd, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.gf_rms_norm_backward_workspace_bytes.argtypes = [rd, ctypes.POINTER(sz)]
+        L.gf_rms_norm_backward.argtypes = [rd, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.gf_fp8_quantize_rows.argtypes = [qd, vp, vp, vp, vp]
+        L.gf_fp8_quantize_blocks.argtypes = [qd, vp, vp, vp, vp]
+        L.gf_fp8_matmul.argtypes = [pd, vp, vp, vp, vp, vp, vp, vp]
+        for name in ("gf_dropout_forward", "gf_dropout_backward", "gf_rms_norm_forward", "gf_rms_norm_forward_fp8",
+                     "gf_rms_norm_backward_workspace_bytes", "gf_rms_norm_backward", "gf_fp8_quantize_rows",
+                     "gf_fp8_quantize_blocks", "gf_fp8_matmul"):
             getattr(L, name).restype = ctypes.c_int
         L.gf_selftest_bounded_wait.argtypes = [vp, ctypes.c_int64, vp]
         L.gf_selftest_bounded_wait.restype = ctypes.c_int
@@ -424,6 +458,88 @@ def gf_muon_step(desc: gf_muon_desc, grads, momenta, weights, momenta_out, weigh
     _check(lib().gf_muon_step(ctypes.byref(desc), _ptrs(grads, n), _ptrs(momenta, n), _ptrs(weights, n), _ptrs(momenta_out, n),
                               _ptrs(weights_out, n), _addr(workspace), workspace_bytes, _coeffs(coeffs, desc.steps),
                               _raw_stream(stream)), "gf_muon_step")
+
+
+# ---- operators of a residual block with frozen layers (gf_block.h) ---------------------------------
+
+def make_dropout_desc(count, *, dtype=GF_F32, out_dtype=None, p) -> gf_dropout_desc:
+    return gf_dropout_desc(count, _dt(dtype), _dt(dtype if out_dtype is None else out_dtype), p)
+
+
+def make_rms_desc(rows, cols, *, dtype=GF_F32, residual_dtype=None, param_dtype=GF_F32, eps=1e-5, p=0.0) -> gf_rms_desc:
+    return gf_rms_desc(rows, cols, _dt(dtype), _dt(dtype if residual_dtype is None else residual_dtype), _dt(param_dtype), eps, p)
+
+
+def make_fp8_desc(rows, cols, *, dtype=GF_F32) -> gf_fp8_desc:
+    return gf_fp8_desc(rows, cols, _dt(dtype))
+
+
+def make_fp8_matmul_desc(M, N, K, *, transposed=False, out_dtype=GF_BF16, bias_dtype=GF_F32) -> gf_fp8_matmul_desc:
+    return gf_fp8_matmul_desc(M, N, K, int(transposed), _dt(out_dtype), _dt(bias_dtype))
+
+
+def fp8_pitch(cols: int) -> int:
+    """Bytes between the rows of an 8-bit matrix."""
+    return (cols + 15) // 16 * 16
+
+
+def fp8_scale_pitch(rows: int) -> int:
+    """Places between the scales of one group of 128 columns and the next."""
+    return (rows + 3) // 4 * 4
+
+
+def gf_dropout_forward(desc: gf_dropout_desc, x, residual, seed, y, stream=None) -> None:
+    """y <- residual + dropout(x); the mask is a function of seed (two 64-bit words on the device) and the element's index."""
+    _check(lib().gf_dropout_forward(ctypes.byref(desc), _addr(x), _addr(residual), _addr(seed), _addr(y), _raw_stream(stream)),
+           "gf_dropout_forward")
+
+
+def gf_dropout_backward(desc: gf_dropout_desc, g_y, seed, g_x, stream=None) -> None:
+    _check(lib().gf_dropout_backward(ctypes.byref(desc), _addr(g_y), _addr(seed), _addr(g_x), _raw_stream(stream)),
+           "gf_dropout_backward")
+
+
+def gf_rms_norm_forward(desc: gf_rms_desc, x, residual, seed, gamma, h, y, rstd=None, stream=None) -> None:
+    """h <- residual + dropout(x), y <- h rstd gamma (h None: no residual and nothing dropped, h is x)."""
+    _check(lib().gf_rms_norm_forward(ctypes.byref(desc), _addr(x), _addr(residual), _addr(seed), _addr(gamma), _addr(h), _addr(y),
+                                     _addr(rstd), _raw_stream(stream)), "gf_rms_norm_forward")
+
+
+def gf_rms_norm_forward_fp8(desc: gf_rms_desc, x, residual, seed, gamma, h, codes, scales, rstd=None, stream=None) -> None:
+    """As gf_rms_norm_forward, with y as codes [rows, fp8_pitch(cols)] and scales [ceil(cols / 128), fp8_scale_pitch(rows)]."""
+    _check(lib().gf_rms_norm_forward_fp8(ctypes.byref(desc), _addr(x), _addr(residual), _addr(seed), _addr(gamma), _addr(h),
+                                         _addr(codes), _addr(scales), _addr(rstd), _raw_stream(stream)), "gf_rms_norm_forward_fp8")
+
+
+def gf_rms_norm_backward_workspace_bytes(desc: gf_rms_desc) -> int:
+    return _size(lib().gf_rms_norm_backward_workspace_bytes, desc, "gf_rms_norm_backward_workspace_bytes")
+
+
+def gf_rms_norm_backward(desc: gf_rms_desc, g_y, g_h, h, rstd, gamma, seed, g_residual, g_x, g_gamma, workspace,
+                         workspace_bytes=None, stream=None) -> None:
+    if workspace_bytes is None:
+        workspace_bytes = _nbytes(workspace)
+    _check(lib().gf_rms_norm_backward(ctypes.byref(desc), _addr(g_y), _addr(g_h), _addr(h), _addr(rstd), _addr(gamma), _addr(seed),
+                                      _addr(g_residual), _addr(g_x), _addr(g_gamma), _addr(workspace), workspace_bytes,
+                                      _raw_stream(stream)), "gf_rms_norm_backward")
+
+
+def gf_fp8_quantize_rows(desc: gf_fp8_desc, x, codes, scales, stream=None) -> None:
+    """codes [rows, fp8_pitch(cols)], scales [ceil(cols / 128), fp8_scale_pitch(rows)] <- x [rows, cols]."""
+    _check(lib().gf_fp8_quantize_rows(ctypes.byref(desc), _addr(x), _addr(codes), _addr(scales), _raw_stream(stream)),
+           "gf_fp8_quantize_rows")
+
+
+def gf_fp8_quantize_blocks(desc: gf_fp8_desc, w, codes, scales, stream=None) -> None:
+    """codes [rows, fp8_pitch(cols)], scales [ceil(rows / 128), ceil(cols / 128)] <- w [rows, cols]."""
+    _check(lib().gf_fp8_quantize_blocks(ctypes.byref(desc), _addr(w), _addr(codes), _addr(scales), _raw_stream(stream)),
+           "gf_fp8_quantize_blocks")
+
+
+def gf_fp8_matmul(desc: gf_fp8_matmul_desc, a, a_scales, w, w_scales, bias, out, stream=None) -> None:
+    """out [M, N] <- A W^T + bias, or with desc.transposed out [M, K] <- A W + bias."""
+    _check(lib().gf_fp8_matmul(ctypes.byref(desc), _addr(a), _addr(a_scales), _addr(w), _addr(w_scales), _addr(bias), _addr(out),
+                               _raw_stream(stream)), "gf_fp8_matmul")
 
 
 def gf_selftest_bounded_wait(workspace, limit_cycles: int, stream=None) -> None:

@@ -16,7 +16,8 @@ void count_launch(int n = 1);
 enum KernelId {
     K_STASH_POOL = 0, K_KSUM, K_GY_POOL, K_GX_MIX, K_GW_PARTIAL, K_GW_FINISH, K_DW_FUSED,
     K_EXACT_GX, K_EXACT_GW, K_GX_TC, K_GW_TC, K_SPLIT, K_GYX_FUSED, K_GW_TILED,
-    K_NORM_FWD, K_NORM_BWD, K_NORM_SUMS, K_NS_PREPARE, K_NS_PRODUCT, K_NS_FINISH, K_COUNT
+    K_NORM_FWD, K_NORM_BWD, K_NORM_SUMS, K_NS_PREPARE, K_NS_PRODUCT, K_NS_FINISH,
+    K_DROPOUT, K_RMS_FWD, K_RMS_BWD, K_FP8_QUANTIZE, K_FP8_PRODUCT, K_COUNT
 };
 
 // Brackets the launches made during its lifetime with a pair of events when

@@ -1,0 +1,107 @@
+// Dropout from a counter, with the residual's addition (gf_block.h).
+//
+// Bound by memory: x (and the residual) read once, y written once.  An octet is the unit: its 128 random bits are one Philox
+// block, about 90 instructions, which the memory's time covers (16 bits per element; 32 would take twice the blocks).
+#include "gf_block.h"
+#include "gf_octet.cuh"
+
+namespace gf {
+
+Drop make_drop(float p, const uint64_t* seed) {
+    Drop d;
+    d.threshold = (uint32_t)__builtin_rint((double)p * 65536.0);
+    d.scale = d.threshold < 65536u ? (float)(65536.0 / (65536.0 - d.threshold)) : 0.f;
+    d.seed = seed;
+    return d;
+}
+
+namespace {
+
+constexpr int kThreads = 256;
+
+template <typename TX, typename TY, bool RESIDUAL>
+__global__ void __launch_bounds__(kThreads) dropout_kernel(const TX* x, const TY* residual, TY* y, long long count, Drop d) {
+    pdl_launch_dependents();
+    const long long octets = (count + 7) / 8, step = (long long)gridDim.x * kThreads;
+    pdl_wait();
+    uint64_t key = 0, offset = 0;
+    if (d.threshold) { key = __ldg(d.seed); offset = __ldg(d.seed + 1); }
+    for (long long f = (long long)blockIdx.x * kThreads + threadIdx.x; f < octets; f += step) {
+        Octet<TX> a;
+        Octet<TY> r;
+        load_octet(a, x, f, count);
+        if constexpr (RESIDUAL) load_octet(r, residual, f, count);
+        float v[8];
+        a.get(v);
+        if (d.threshold) drop_octet(v, (uint64_t)f, key, offset, d.threshold, d.scale);
+        if constexpr (RESIDUAL) {
+            float w[8];
+            r.get(w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += w[i];
+        }
+        if (f * 8 + 8 <= count) {
+            r.set(v);
+            r.store(y + f * 8);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 7; ++i)
+                if (f * 8 + i < count) y[f * 8 + i] = from_f32<TY>(v[i]);
+        }
+    }
+}
+
+template <typename TX, typename TY> gf_status launch(const void* x, const void* residual, void* y, long long count, const Drop& d, cudaStream_t s) {
+    const long long octets = (count + 7) / 8, want = cdiv64(octets, kThreads), most = (long long)sm_count() * 8;
+    const dim3 grid((unsigned)(want < most ? want : most));
+    ProfScope prof(K_DROPOUT, s);
+    if (residual)
+        return launch_pdl(dropout_kernel<TX, TY, true>, grid, dim3(kThreads), 0, s, static_cast<const TX*>(x), static_cast<const TY*>(residual),
+                          static_cast<TY*>(y), count, d);
+    return launch_pdl(dropout_kernel<TX, TY, false>, grid, dim3(kThreads), 0, s, static_cast<const TX*>(x), static_cast<const TY*>(residual),
+                      static_cast<TY*>(y), count, d);
+}
+
+bool off16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
+bool is_dtype(int d) { return d == GF_F32 || d == GF_BF16; }
+
+gf_status run(const gf_dropout_desc* desc, const void* x, int x_dtype, const void* residual, const uint64_t* seed, void* y, int y_dtype,
+              cudaStream_t s) {
+    if (desc->count == 0) return GF_OK;
+    const Drop d = make_drop(desc->p, seed);
+    if (!x || !y || (d.threshold && !seed)) return GF_ERR_NULL;
+    if (off16(x) || off16(y) || off16(residual) || (reinterpret_cast<uintptr_t>(seed) & 7u) != 0) return GF_ERR_ALIGN;
+    if (x_dtype == GF_F32) {
+        if (y_dtype == GF_F32) return launch<float, float>(x, residual, y, desc->count, d, s);
+        return launch<float, __nv_bfloat16>(x, residual, y, desc->count, d, s);
+    }
+    if (y_dtype == GF_F32) return launch<__nv_bfloat16, float>(x, residual, y, desc->count, d, s);
+    return launch<__nv_bfloat16, __nv_bfloat16>(x, residual, y, desc->count, d, s);
+}
+
+gf_status validate(const gf_dropout_desc* d) {
+    if (!d) return GF_ERR_NULL;
+    if (d->count < 0 || !valid_p(d->p) || !is_dtype(d->dtype) || !is_dtype(d->out_dtype)) return GF_ERR_BAD_DESC;
+    return d->count > (int64_t)1 << 60 ? GF_ERR_UNSUPPORTED : GF_OK;
+}
+
+}  // namespace
+}  // namespace gf
+
+using namespace gf;
+
+extern "C" {
+
+gf_status gf_dropout_forward(const gf_dropout_desc* desc, const void* x, const void* residual, const uint64_t* seed, void* y, void* stream) {
+    const gf_status st = validate(desc);
+    if (st != GF_OK) return st;
+    return run(desc, x, desc->dtype, residual, seed, y, desc->out_dtype, static_cast<cudaStream_t>(stream));
+}
+
+gf_status gf_dropout_backward(const gf_dropout_desc* desc, const void* g_y, const uint64_t* seed, void* g_x, void* stream) {
+    const gf_status st = validate(desc);
+    if (st != GF_OK) return st;
+    return run(desc, g_y, desc->out_dtype, nullptr, seed, g_x, desc->dtype, static_cast<cudaStream_t>(stream));
+}
+
+}  // extern "C"

@@ -1,0 +1,184 @@
+// Rows taken as octets: eight consecutive elements, as the elementwise operators and row norms of gf_block.h read, compute and
+// write them, with the counter-based random bits of an octet and its rounding to 8 bits.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <stdint.h>
+
+#include "gf_common.cuh"
+
+namespace gf {
+
+// ---- eight elements as they lie in memory ------------------------------------------------------------------
+template <typename T> struct Octet {
+    static constexpr int kWords = 2 * (int)sizeof(T);      // 32-bit words
+    uint32_t w[kWords];
+
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) w[i] = 0u;
+    }
+    __device__ __forceinline__ void get(float (&v)[8]) const {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+        }
+    }
+    __device__ __forceinline__ void set(const float (&v)[8]) {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(v[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+                w[i] = *reinterpret_cast<const uint32_t*>(&b);
+            }
+        }
+    }
+    // p: 16-byte aligned
+    __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+        for (int i = 0; i < kWords; i += 4) {
+            const uint4 a = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint32_t*>(p) + i);
+            w[i] = a.x; w[i + 1] = a.y; w[i + 2] = a.z; w[i + 3] = a.w;
+        }
+    }
+    __device__ __forceinline__ void store(T* p) const {
+#pragma unroll
+        for (int i = 0; i < kWords; i += 4)
+            *reinterpret_cast<uint4*>(reinterpret_cast<uint32_t*>(p) + i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+    }
+    // element i from memory (i is a constant where this is called)
+    __device__ __forceinline__ void put(int i, T v) {
+        if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(v);
+        else {
+            const uint32_t b = __bfloat16_as_ushort(v);
+            w[i >> 1] = i & 1 ? (w[i >> 1] & 0xffffu) | (b << 16) : (w[i >> 1] & 0xffff0000u) | b;
+        }
+    }
+};
+
+// The aligned octet number f of a tensor of `total` elements; what lies past its end reads as zeros.
+template <typename T> __device__ __forceinline__ void load_octet(Octet<T>& o, const T* base, long long f, long long total) {
+    const long long e = f * 8;
+    if (e + 8 <= total) { o.load(base + e); return; }
+    o.clear();
+#pragma unroll
+    for (int i = 0; i < 7; ++i)
+        if (e + i < total) o.put(i, base[e + i]);
+}
+
+// Eight elements from element e on, wherever that lies; those past the tensor's end read as zeros.  Two aligned octets, shifted.
+template <typename T> __device__ __forceinline__ void load_anywhere(Octet<T>& o, const T* base, long long e, long long total) {
+    const int shift = (int)(e & 7);
+    Octet<T> a, b;
+    load_octet(a, base, e >> 3, total);
+    if (shift == 0) { o = a; return; }
+    b.clear();
+    if ((e >> 3) * 8 + 8 < total) load_octet(b, base, (e >> 3) + 1, total);
+    constexpr int n = Octet<T>::kWords;
+    uint32_t w[2 * n];
+#pragma unroll
+    for (int i = 0; i < n; ++i) { w[i] = a.w[i]; w[n + i] = b.w[i]; }
+    constexpr int four = n / 2, two = n / 4;
+    if (shift & 4) {
+#pragma unroll
+        for (int i = 0; i + four < 2 * n; ++i) w[i] = w[i + four];
+    }
+    if (shift & 2) {
+#pragma unroll
+        for (int i = 0; i + two < 2 * n; ++i) w[i] = w[i + two];
+    }
+    if (shift & 1) {
+#pragma unroll
+        for (int i = 0; i < n; ++i) w[i] = sizeof(T) == 4 ? w[i + 1] : __funnelshift_r(w[i], w[i + 1], 16);
+    }
+#pragma unroll
+    for (int i = 0; i < n; ++i) o.w[i] = w[i];
+}
+
+// ---- random bits of an octet ------------------------------------------------------------------------------------
+// Philox4x32 with ten rounds (Salmon, Moraes, Dror, Shaw: "Parallel random numbers: as easy as 1, 2, 3", SC 2011).
+__device__ __forceinline__ uint4 philox(uint64_t block, uint64_t offset, uint64_t key) {
+    uint32_t c0 = (uint32_t)block, c1 = (uint32_t)(block >> 32), c2 = (uint32_t)offset, c3 = (uint32_t)(offset >> 32);
+    uint32_t k0 = (uint32_t)key, k1 = (uint32_t)(key >> 32);
+#pragma unroll
+    for (int r = 0; r < 10; ++r) {
+        const uint64_t p0 = (uint64_t)0xD2511F53u * c0, p1 = (uint64_t)0xCD9E8D57u * c2;
+        c0 = (uint32_t)(p1 >> 32) ^ c1 ^ k0;
+        c1 = (uint32_t)p1;
+        c2 = (uint32_t)(p0 >> 32) ^ c3 ^ k1;
+        c3 = (uint32_t)p0;
+        k0 += 0x9E3779B9u;
+        k1 += 0xBB67AE85u;
+    }
+    return make_uint4(c0, c1, c2, c3);
+}
+
+// Dropout as the kernels take it.  threshold 0: nothing is dropped.
+struct Drop {
+    const uint64_t* seed;
+    uint32_t threshold;        // of 65536
+    float scale;               // 65536 / (65536 - threshold); 0 when all is dropped
+};
+Drop make_drop(float p, const uint64_t* seed);
+static inline bool valid_p(float p) { return p >= 0.f && p <= 1.f; }
+
+// v[i] <- kept ? v[i] scale : 0 for the elements of octet number f
+__device__ __forceinline__ void drop_octet(float (&v)[8], uint64_t f, uint64_t key, uint64_t offset, uint32_t threshold, float scale) {
+    const uint4 r = philox(f, offset, key);
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = (w[i] & 0xffffu) >= threshold ? v[2 * i] * scale : 0.f;
+        v[2 * i + 1] = (w[i] >> 16) >= threshold ? v[2 * i + 1] * scale : 0.f;
+    }
+}
+
+// ---- 8 bits ---------------------------------------------------------------------------------------------------------
+constexpr float kFp8Top = 448.f, kFp8Tiny = 1.17549435e-38f;
+
+// Largest magnitude as bits: ordered like unsigned numbers, NaN above all.
+__device__ __forceinline__ uint32_t magnitude(const float (&v)[8]) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+    return m;
+}
+__device__ __forceinline__ float scale_of(uint32_t magnitude_bits) {
+    return magnitude_bits >= 0x7f800000u ? __uint_as_float(magnitude_bits) : fmaxf(__uint_as_float(magnitude_bits) * (1.f / kFp8Top), kFp8Tiny);
+}
+// Two values to codes, the first in the low byte; values of magnitude above 448 give 448, NaN gives NaN.
+__device__ __forceinline__ uint32_t codes2(float a, float b) {
+    uint16_t r;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(b), "f"(a));
+    return r;
+}
+// Codes of eight values, of which `valid` are the row's (the others get 0), under `scale`, inv its rounded reciprocal.  The quotient is inv v with one correction by the remainder
+// (Markstein 1990: the correctly rounded quotient), so that codes are those of a division.  A scale that is not
+// finite leaves NaN.
+__device__ __forceinline__ uint2 codes8(const float (&v)[8], float scale, float inv, int valid) {
+    uint32_t c[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float q[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const float x = v[2 * i + k], y = x * inv;
+            q[k] = copysignf(__fmaf_rn(__fmaf_rn(-y, scale, x), inv, y), x);      // (the correction makes +0 of -0)
+        }
+        c[i] = codes2(q[0], q[1]);
+    }
+    uint2 r = make_uint2(c[0] | (c[1] << 16), c[2] | (c[3] << 16));
+    if (valid < 8) {
+        r.x = valid >= 4 ? r.x : valid <= 0 ? 0u : r.x & (0xffffffffu >> (32 - 8 * valid));
+        r.y = valid <= 4 ? 0u : r.y & (0xffffffffu >> (64 - 8 * valid));
+    }
+    return r;
+}
+
+}  // namespace gf

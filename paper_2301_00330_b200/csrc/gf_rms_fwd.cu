@@ -1,0 +1,350 @@
+// Root-mean-square norm of a residual sum, forward (gf_block.h), with results in 16, 32 or 8 bits.
+//
+// Bound by memory: x and residual are read and h and y (or codes) written once; a row stays in the registers of its team between
+// the sum and the results, and the team's next row is on its way meanwhile.
+#include "gf_rms.cuh"
+
+namespace gf {
+
+gf_status rms_validate(const gf_rms_desc* d) {
+    if (!d) return GF_ERR_NULL;
+    auto known = [](int t) { return t == GF_F32 || t == GF_BF16; };
+    if (d->rows < 0 || d->cols < 1 || !known(d->dtype) || !known(d->residual_dtype) || !known(d->param_dtype) || !(d->eps >= 0.f) || !valid_p(d->p))
+        return GF_ERR_BAD_DESC;
+    if (d->dtype == GF_F32 && d->residual_dtype == GF_BF16) return GF_ERR_UNSUPPORTED;
+    if (d->cols > 1 << 24 || d->rows > ((int64_t)1 << 60) / d->cols) return GF_ERR_UNSUPPORTED;
+    return GF_OK;
+}
+
+namespace {
+
+// A value's place in a row of floats in shared memory: threads that write (or read) elements 8 apart meet 32 different banks.
+__device__ __forceinline__ int skewed(int c) { return c + (c >> 5); }
+
+// ALIGNED: rows are whole octets.  OUT8: codes and scales in y's place; 16 threads that follow one another have the 128
+// columns of a scale.  Rows that are not whole octets change places for that through shared memory.
+template <typename TX, typename TR, int NO, bool WARP, bool ALIGNED, bool OUT8>
+__global__ void __launch_bounds__(WARP ? kRmsThreads : kRmsMostThreads) rms_fwd_kernel(const __grid_constant__ RmsArgs a) {
+    __shared__ __align__(16) float red[2][32];
+    extern __shared__ float rows_smem[];
+    pdl_launch_dependents();
+    const int tpr = WARP ? 1 << a.log_tpr : (int)blockDim.x;
+    const int g = WARP ? (int)threadIdx.x & (tpr - 1) : (int)threadIdx.x;
+    const int teams_pb = WARP ? kRmsThreads >> a.log_tpr : 1, team = WARP ? (int)threadIdx.x >> a.log_tpr : 0;
+    const int first_of_warp = WARP ? ((int)threadIdx.x & ~31) >> a.log_tpr : 0;
+    const long long step = (long long)gridDim.x * teams_pb;
+    long long row = (long long)blockIdx.x * teams_pb + team;
+    const int phase = ALIGNED ? 0 : (int)((row * a.cols) & 7);
+    float* const line = rows_smem + (size_t)team * skewed(a.cols + 7);
+    if (!WARP && threadIdx.x < 64) (&red[0][0])[threadIdx.x] = 0.f;
+    pdl_wait();
+    if (!WARP) __syncthreads();
+
+    const TX* const x = static_cast<const TX*>(a.x);
+    const TR* const res = static_cast<const TR*>(a.residual);
+    // octet k of this thread: columns c0[k] .. c0[k] + 7, of which lo .. hi - 1 are the row's
+    auto c0 = [&](int k) { return 8 * (k * tpr + g) - phase; };
+    float gam[NO][8];
+#pragma unroll
+    for (int k = 0; k < NO; ++k)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int c = c0(k) + i;
+            gam[k][i] = c >= 0 && c < a.cols ? rms_gamma(a, c) : 0.f;
+        }
+    uint64_t key = 0, offset = 0;
+    if (a.drop.threshold) { key = a.drop.seed[0]; offset = a.drop.seed[1]; }
+
+    Octet<TX> nx[NO];
+    Octet<TR> nr[NO];
+    auto fetch = [&](long long r) {
+        const long long base = r * a.cols >> 3;
+#pragma unroll
+        for (int k = 0; k < NO; ++k) {
+            nx[k].clear();
+            nr[k].clear();
+            if (r < a.rows && c0(k) < a.cols) {
+                const long long f = base + k * tpr + g;
+                if (ALIGNED) {
+                    nx[k].load(x + f * 8);
+                    if (res) nr[k].load(res + f * 8);
+                } else {
+                    load_octet(nx[k], x, f, a.total);
+                    if (res) load_octet(nr[k], res, f, a.total);
+                }
+            }
+        }
+    };
+    fetch(row);
+    int turn = 0;
+    // (the lanes of a warp go round together, as long as any of its rows is left)
+    for (long long warp_row = (long long)blockIdx.x * teams_pb + first_of_warp; warp_row < a.rows; warp_row += step, row += step, turn ^= 1) {
+        const bool live = row < a.rows;
+        const long long base = row * a.cols >> 3;
+        float v[NO][8];
+        float s = 0.f;
+#pragma unroll
+        for (int k = 0; k < NO; ++k) {
+            nx[k].get(v[k]);
+            if (a.drop.threshold && live && c0(k) < a.cols)
+                drop_octet(v[k], (uint64_t)(base + k * tpr + g), key, offset, a.drop.threshold, a.drop.scale);
+            if (res) {
+                float w[8];
+                nr[k].get(w);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[k][i] += w[i];
+            }
+        }
+        fetch(row + step);
+#pragma unroll
+        for (int k = 0; k < NO; ++k) {
+            const int c = c0(k);
+            if (a.h && live && c < a.cols) {
+                TR* const h = static_cast<TR*>(a.h) + (base + k * tpr + g) * 8;
+                Octet<TR> o;
+                o.set(v[k]);
+                o.get(v[k]);                             // the norm is that of h as it is kept
+                if (ALIGNED || (c >= 0 && c + 8 <= a.cols)) o.store(h);
+                else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (c + i >= 0 && c + i < a.cols) h[i] = from_f32<TR>(v[k][i]);
+                }
+            }
+            if (!ALIGNED) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (c + i < 0 || c + i >= a.cols) v[k][i] = 0.f;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s = fmaf(v[k][i], v[k][i], s);
+        }
+        s = rms_sum<WARP>(s, a.log_tpr, red[turn]);
+        const float rstd = __frcp_rn(__fsqrt_rn(fmaf(s, a.inv_c, a.eps)));
+        if (a.rstd && live && g == 0) a.rstd[row] = rstd;
+#pragma unroll
+        for (int k = 0; k < NO; ++k)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[k][i] = v[k][i] * rstd * gam[k][i];
+        if constexpr (!OUT8) {
+#pragma unroll
+            for (int k = 0; k < NO; ++k) {
+                const int c = c0(k);
+                if (!live || c >= a.cols) continue;
+                TX* const y = static_cast<TX*>(a.y) + (base + k * tpr + g) * 8;
+                if (ALIGNED || (c >= 0 && c + 8 <= a.cols)) {
+                    Octet<TX> o;
+                    o.set(v[k]);
+                    o.store(y);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (c + i >= 0 && c + i < a.cols) y[i] = from_f32<TX>(v[k][i]);
+                }
+            }
+        } else {
+            if constexpr (!ALIGNED) {                    // from the tensor's octets to the row's own
+#pragma unroll
+                for (int k = 0; k < NO; ++k)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int c = c0(k) + i;
+                        if (c >= 0 && c < a.cols) line[skewed(c)] = v[k][i];
+                    }
+                if (WARP) __syncwarp();
+                else __syncthreads();
+#pragma unroll
+                for (int k = 0; k < NO; ++k)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int c = 8 * (k * tpr + g) + i;
+                        v[k][i] = c < a.cols ? line[skewed(c)] : 0.f;
+                    }
+                if (WARP) __syncwarp();
+            }
+#pragma unroll
+            for (int k = 0; k < NO; ++k) {
+                const int c = 8 * (k * tpr + g);
+                uint32_t m = magnitude(v[k]);
+#pragma unroll
+                for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+                const float scale = scale_of(m);
+                if (live && c < a.pitch) {
+                    *reinterpret_cast<uint2*>(a.codes + row * a.pitch + c) = codes8(v[k], scale, __frcp_rn(scale), a.cols - c);
+                    if ((g & 15) == 0 && c < a.cols) a.scales[(long long)(c >> 7) * a.scale_pitch + row] = scale;
+                }
+            }
+        }
+    }
+}
+
+// Rows longer than the registers of a block: h is written on the way to the sum and read again (from L2) for the results.
+constexpr int kLongThreads = 1024;
+template <typename TX, typename TR, bool OUT8> __global__ void __launch_bounds__(kLongThreads) rms_fwd_long_kernel(const __grid_constant__ RmsArgs a) {
+    __shared__ __align__(16) float red[2][32];
+    pdl_launch_dependents();
+    pdl_wait();
+    const TX* const x = static_cast<const TX*>(a.x);
+    const TR* const res = static_cast<const TR*>(a.residual);
+    TR* const h = static_cast<TR*>(a.h);
+    uint64_t key = 0, offset = 0;
+    if (a.drop.threshold) { key = a.drop.seed[0]; offset = a.drop.seed[1]; }
+    int turn = 0;
+    for (long long row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
+        const long long e0 = row * a.cols, e1 = e0 + a.cols;
+        float s = 0.f;
+        for (long long f = (e0 >> 3) + threadIdx.x; f * 8 < e1; f += kLongThreads) {
+            Octet<TX> ox;
+            load_octet(ox, x, f, a.total);
+            float v[8];
+            ox.get(v);
+            if (a.drop.threshold) drop_octet(v, (uint64_t)f, key, offset, a.drop.threshold, a.drop.scale);
+            if (res) {
+                Octet<TR> r;
+                load_octet(r, res, f, a.total);
+                float w[8];
+                r.get(w);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] += w[i];
+            }
+            if (h) {
+                Octet<TR> o;
+                o.set(v);
+                o.get(v);
+                if (f * 8 >= e0 && f * 8 + 8 <= e1) o.store(h + f * 8);
+                else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (f * 8 + i >= e0 && f * 8 + i < e1) h[f * 8 + i] = from_f32<TR>(v[i]);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (f * 8 + i >= e0 && f * 8 + i < e1) s = fmaf(v[i], v[i], s);
+        }
+        s = rms_sum<false>(s, 0, red[turn]);              // (also: h of the whole row is visible to the block)
+        const float rstd = __frcp_rn(__fsqrt_rn(fmaf(s, a.inv_c, a.eps)));
+        if (a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
+        const TR* const from = h ? h : reinterpret_cast<const TR*>(a.x);      // without h: x, of the same type
+        if constexpr (OUT8) {
+            for (int c = 8 * (int)threadIdx.x; c < (a.pitch + 127) / 128 * 128; c += 8 * kLongThreads) {
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = c + i < a.cols ? to_f32(from[e0 + c + i]) * rstd * rms_gamma(a, c + i) : 0.f;
+                uint32_t m = magnitude(v);
+                const uint32_t half = 0xffffu << ((threadIdx.x & 16));
+#pragma unroll
+                for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(half, m, o));
+                const float scale = scale_of(m);
+                if (c < a.pitch) {
+                    *reinterpret_cast<uint2*>(a.codes + row * a.pitch + c) = codes8(v, scale, __frcp_rn(scale), a.cols - c);
+                    if ((threadIdx.x & 15) == 0 && c < a.cols) a.scales[(long long)(c >> 7) * a.scale_pitch + row] = scale;
+                }
+            }
+        } else {
+            TX* const y = static_cast<TX*>(a.y);
+            for (long long f = (e0 >> 3) + threadIdx.x; f * 8 < e1; f += kLongThreads) {
+                const int c = (int)(f * 8 - e0);
+                if (c >= 0 && c + 8 <= a.cols) {
+                    Octet<TR> o;
+                    o.load(from + f * 8);
+                    float v[8];
+                    o.get(v);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] = v[i] * rstd * rms_gamma(a, c + i);
+                    Octet<TX> t;
+                    t.set(v);
+                    t.store(y + f * 8);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (c + i >= 0 && c + i < a.cols) y[f * 8 + i] = from_f32<TX>(to_f32(from[f * 8 + i]) * rstd * rms_gamma(a, c + i));
+                }
+            }
+        }
+    }
+}
+
+template <typename TX, typename TR, int NO, bool WARP, bool ALIGNED, bool OUT8> gf_status launch(const RmsArgs& a, const RmsShape& sh, cudaStream_t s) {
+    auto kernel = rms_fwd_kernel<TX, TR, NO, WARP, ALIGNED, OUT8>;
+    const int teams = WARP ? kRmsThreads >> sh.log_tpr : 1;
+    const int width = a.cols + 7;
+    const size_t smem = OUT8 && !ALIGNED ? (size_t)teams * (width + (width >> 5)) * 4 : 0;
+    static int cached[WARP ? 6 : kRmsMostThreads / 32 + 1][kMaxDevices] = {};
+    const int resident = rms_resident(kernel, sh.threads, smem, cached[WARP ? sh.log_tpr : sh.threads / 32]);
+    const long long want = cdiv64(a.rows, teams), most = (long long)sm_count() * resident / 8 * 8;
+    long long grid = want < most ? want : most;
+    if (!ALIGNED) grid = cdiv64(grid, 8) * 8;             // steps of a multiple of eight rows
+    return launch_pdl(kernel, dim3((unsigned)grid), dim3(sh.threads), smem, s, a);
+}
+
+template <typename TX, typename TR, bool ALIGNED, bool OUT8> gf_status dispatch(const RmsArgs& a, cudaStream_t s) {
+    int n = rms_octets(a.cols);
+    if (OUT8 && a.pitch / 8 > n) n = a.pitch / 8;
+    if (n > 2 * kRmsMostThreads) {
+        const long long most = sm_count() * 2;
+        return launch_pdl(rms_fwd_long_kernel<TX, TR, OUT8>, dim3((unsigned)(a.rows < most ? a.rows : most)), dim3(kLongThreads), 0, s, a);
+    }
+    const RmsShape sh = rms_shape(n, 3, OUT8 ? 4 : 1);
+    RmsArgs b = a;
+    b.log_tpr = sh.log_tpr;
+    if (sh.warp) {
+        if (sh.per_thread == 1) return launch<TX, TR, 1, true, ALIGNED, OUT8>(b, sh, s);
+        if (sh.per_thread == 2) return launch<TX, TR, 2, true, ALIGNED, OUT8>(b, sh, s);
+        return launch<TX, TR, 3, true, ALIGNED, OUT8>(b, sh, s);
+    }
+    if (sh.per_thread == 1) return launch<TX, TR, 1, false, ALIGNED, OUT8>(b, sh, s);
+    return launch<TX, TR, 2, false, ALIGNED, OUT8>(b, sh, s);
+}
+
+template <bool OUT8> gf_status run(const gf_rms_desc* d, const void* x, const void* residual, const uint64_t* seed, const void* gamma, void* h, void* y,
+                                   void* codes, float* scales, float* rstd, void* stream) {
+    const gf_status st = rms_validate(d);
+    if (st != GF_OK) return st;
+    RmsArgs a = {};
+    a.drop = make_drop(d->p, seed);
+    const bool h_is_x = !residual && a.drop.threshold == 0;
+    if (h_is_x && (h || d->dtype != d->residual_dtype)) return GF_ERR_BAD_DESC;
+    if (d->rows == 0) return GF_OK;
+    if (!x || (OUT8 ? !codes || !scales : !y) || (a.drop.threshold && !seed) || (!h && !h_is_x)) return GF_ERR_NULL;
+    if (rms_off16(x) || rms_off16(residual) || rms_off16(gamma) || rms_off16(h) || rms_off16(y) || rms_off16(codes) || rms_off16(scales) ||
+        rms_off16(rstd) || (reinterpret_cast<uintptr_t>(seed) & 7u) != 0)
+        return GF_ERR_ALIGN;
+    a.x = x; a.residual = residual; a.gamma = gamma; a.gamma_bf16 = d->param_dtype == GF_BF16;
+    a.h = h;
+    a.y = y; a.codes = static_cast<uint8_t*>(codes); a.scales = scales; a.rstd = rstd;
+    a.rows = d->rows; a.cols = d->cols; a.total = d->rows * d->cols;
+    a.pitch = GF_FP8_PITCH(d->cols); a.scale_pitch = GF_FP8_SCALE_PITCH(d->rows);
+    a.eps = d->eps; a.inv_c = 1.f / (float)d->cols;
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    ProfScope prof(K_RMS_FWD, s);
+    const bool aligned = d->cols % 8 == 0;
+    auto go = [&](auto tx, auto tr) {
+        using TX = decltype(tx);
+        using TR = decltype(tr);
+        return aligned ? dispatch<TX, TR, true, OUT8>(a, s) : dispatch<TX, TR, false, OUT8>(a, s);
+    };
+    if (d->dtype == GF_F32) return go(float(), float());
+    if (d->residual_dtype == GF_F32) return go(__nv_bfloat16(), float());
+    return go(__nv_bfloat16(), __nv_bfloat16());
+}
+
+}  // namespace
+}  // namespace gf
+
+using namespace gf;
+
+extern "C" {
+
+gf_status gf_rms_norm_forward(const gf_rms_desc* desc, const void* x, const void* residual, const uint64_t* seed, const void* gamma, void* h,
+                              void* y, float* rstd, void* stream) {
+    return run<false>(desc, x, residual, seed, gamma, h, y, nullptr, nullptr, rstd, stream);
+}
+
+gf_status gf_rms_norm_forward_fp8(const gf_rms_desc* desc, const void* x, const void* residual, const uint64_t* seed, const void* gamma, void* h,
+                                  void* codes, float* scales, float* rstd, void* stream) {
+    if (desc && desc->rows > 0x7fffffffLL) return GF_ERR_UNSUPPORTED;
+    return run<true>(desc, x, residual, seed, gamma, h, nullptr, codes, scales, rstd, stream);
+}
+
+}  // extern "C"
