@@ -108,7 +108,7 @@ template <typename T> __global__ void __launch_bounds__(kQuantThreads) quantize_
 // W' = W^T (the layer) or W (the gradient of its input).  The tensor cores add a chunk into one of two accumulators in tensor
 // memory; warps that wait for it scale it and add it to fp32 registers while the next chunk is multiplied into the other.
 struct ProductArgs {
-    CUtensorMap tm_w, tm_a;
+    CUtensorMap tm_w, tm_a, tm_out;
     const float *sa, *sw;
     const void* bias;
     void* out;
@@ -116,6 +116,8 @@ struct ProductArgs {
     long long sa_pitch, sw_j, sw_q;      // strides of the scales: rows of sa; blocks of columns and chunks of sw
     int M, J, chunks, per, split;        // per: chunks of a CTA of a cluster of `split`
     int tiles_m, bias_bf16;
+    int bn;                              // wide: columns of a tile
+    int out_map;                         // wide: results leave by the copy engine (their rows are whole 16-byte pieces)
     int mn_major;                        // W is read with the contracted index as its rows
 };
 
@@ -136,9 +138,12 @@ __device__ __forceinline__ bool elect_one() {
     return r != 0;
 }
 __device__ __forceinline__ void cluster_meet() { asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory"); }
-__device__ __forceinline__ float peer_load(uint32_t addr, int rank) {
-    float v;
-    asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %1, %2;\n\tld.shared::cluster.f32 %0, [a];\n\t}" : "=f"(v) : "r"(addr), "r"(rank) : "memory");
+__device__ __forceinline__ float4 peer_load4(uint32_t addr, int rank) {
+    float4 v;
+    asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %4, %5;\n\tld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [a];\n\t}"
+                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+                 : "r"(addr), "r"(rank)
+                 : "memory");
     return v;
 }
 __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
@@ -149,9 +154,32 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
         : "r"(taddr)
         : "memory");
 }
+// Waits for the loads before, and says so of their registers: nothing that uses them comes earlier.
+__device__ __forceinline__ void tmem_ld_wait_for(uint32_t (&r)[16]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]),
+                   "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])::"memory");
+}
 __device__ __forceinline__ float bias_at(const ProductArgs& p, int j) {
     if (!p.bias) return 0.f;
     return p.bias_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p.bias)[j]) : static_cast<const float*>(p.bias)[j];
+}
+
+// Pairs of fp32: two operations per instruction, each half rounded as the scalar one is.
+__device__ __forceinline__ uint64_t pair_of(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float2 unpair(uint64_t v) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
 }
 
 // A tile is 128 columns of the result (rows of the accumulator) by T of its rows, so that the weight is the operand of
@@ -164,7 +192,7 @@ constexpr int kFewThreads = 192;
 __host__ __device__ constexpr int few_stages(int T) { return T <= 32 ? 4 : 3; }
 constexpr size_t few_smem(int T) { return (size_t)few_stages(T) * (16384 + T * 128) + 1024; }
 static_assert(227 * 1024 / few_smem(16) * 32 <= 512 && 227 * 1024 / few_smem(32) * 64 <= 512 && 227 * 1024 / few_smem(64) * 128 <= 512 &&
-                  227 * 1024 / few_smem(128) * 256 <= 512 && 227 * 1024 / few_smem(64) <= 3,
+                  227 * 1024 / few_smem(64) <= 3,
               "tensor memory of the blocks of an SM");
 
 template <int T, typename TO> __global__ void __launch_bounds__(kFewThreads) fp8_few_kernel(const __grid_constant__ ProductArgs p) {
@@ -175,7 +203,7 @@ template <int T, typename TO> __global__ void __launch_bounds__(kFewThreads) fp8
     __shared__ uint32_t tmem_base;
     __shared__ __align__(16) float scale[2][T];
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
-    const int rank = (int)blockIdx.x % p.split, tile = (int)blockIdx.x / p.split;
+    const int rank = (int)(blockIdx.x % (unsigned)p.split), tile = (int)(blockIdx.x / (unsigned)p.split);
     const int m0 = tile % p.tiles_m * T, j0 = tile / p.tiles_m * 128;
     const int q0 = rank * p.per, n = min(p.per, p.chunks - q0);
     if (threadIdx.x == 0) {
@@ -233,9 +261,9 @@ template <int T, typename TO> __global__ void __launch_bounds__(kFewThreads) fp8
         const float* const sw = p.sw + (long long)(j0 >> 7) * p.sw_j;
         const bool has = t < T && m0 + t < p.M;
         auto scale_at = [&](int q) { return has ? sa[(long long)(q0 + q) * p.sa_pitch] * sw[(long long)(q0 + q) * p.sw_q] : 0.f; };
-        float acc[T];
+        uint64_t acc[T / 2];
 #pragma unroll
-        for (int i = 0; i < T; ++i) acc[i] = 0.f;
+        for (int i = 0; i < T / 2; ++i) acc[i] = 0;
         if (t < T) scale[0][t] = scale_at(0);
         asm volatile("bar.sync 1, 128;" ::: "memory");
         for (int q = 0; q < n; ++q) {
@@ -248,9 +276,14 @@ template <int T, typename TO> __global__ void __launch_bounds__(kFewThreads) fp8
             for (int c = 0; c < T; c += 16) {
                 uint32_t raw[16];
                 tmem_ld16(lanes + (uint32_t)(buf * T + c), raw);
-                tmem_ld_wait();
+                tmem_ld_wait_for(raw);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) acc[c + i] = fmaf(__uint_as_float(raw[i]), scale[buf][c + i], acc[c + i]);
+                for (int i = 0; i < 16; i += 4) {
+                    const ulonglong2 s = *reinterpret_cast<const ulonglong2*>(&scale[buf][c + i]);
+                    uint64_t* const a = acc + (c + i) / 2;
+                    a[0] = fma_pair(pair_of(__uint_as_float(raw[i]), __uint_as_float(raw[i + 1])), s.x, a[0]);
+                    a[1] = fma_pair(pair_of(__uint_as_float(raw[i + 2]), __uint_as_float(raw[i + 3])), s.y, a[1]);
+                }
             }
             tc_fence_before_sync();
             __syncwarp();
@@ -259,17 +292,23 @@ template <int T, typename TO> __global__ void __launch_bounds__(kFewThreads) fp8
             asm volatile("bar.sync 1, 128;" ::: "memory");
         }
         const int r = quarter * 32 + lane, j = j0 + r;
-        TO* const out = static_cast<TO*>(p.out) + (long long)m0 * p.J + j;
         if (p.split == 1) {
+            TO* const out = static_cast<TO*>(p.out) + (long long)m0 * p.J + j;
             const float b = j < p.J ? bias_at(p, j) : 0.f;
 #pragma unroll
-            for (int i = 0; i < T; ++i)
-                if (j < p.J && m0 + i < p.M) out[(long long)i * p.J] = from_f32<TO>(acc[i] + b);
+            for (int i = 0; i < T; ++i) {
+                const float2 f = unpair(acc[i / 2]);
+                if (j < p.J && m0 + i < p.M) out[(long long)i * p.J] = from_f32<TO>((i & 1 ? f.y : f.x) + b);
+            }
         } else {
             float* const part = reinterpret_cast<float*>(dyn) + r;      // every copy and product of this CTA is done with the ring
             if (ok) {
 #pragma unroll
-                for (int i = 0; i < T; ++i) part[i * 128] = acc[i];
+                for (int i = 0; i < T; i += 2) {
+                    const float2 f = unpair(acc[i / 2]);
+                    part[i * 128] = f.x;
+                    part[i * 128 + 128] = f.y;
+                }
             }
         }
     }
@@ -278,21 +317,49 @@ template <int T, typename TO> __global__ void __launch_bounds__(kFewThreads) fp8
         let_settle();
     }
     if (p.split > 1) {
+        // A CTA adds its share of the tile's rows, four columns a thread, with the loads of all parts on their way at once.
+        constexpr int kCells = T * 32 / 128;                            // of a thread, for the whole tile
         cluster_meet();
+        const int i0 = (int)threadIdx.x - 64, first = T * rank / p.split, cells = (T * (rank + 1) / p.split - first) * 32;
+        float4 sum[kCells / 2];                                         // (split >= 2)
         if (warp >= 2) {
-            const int r = (warp & 3) * 32 + lane, j = j0 + r;
-            const int first = T * rank / p.split, end = T * (rank + 1) / p.split;
-            const uint32_t part = smem_u32(dyn) + (uint32_t)r * 4u;
-            const float b = j < p.J ? bias_at(p, j) : 0.f;
-            TO* const out = static_cast<TO*>(p.out) + (long long)m0 * p.J + j;
-            for (int i = first; i < end; ++i) {
-                if (m0 + i >= p.M) break;
-                float v = 0.f;
-                for (int k = 0; k < p.split; ++k) v += peer_load(part + (uint32_t)i * 512u, k);
-                if (j < p.J) out[(long long)i * p.J] = from_f32<TO>(v + b);
+#pragma unroll
+            for (int c = 0; c < kCells / 2; ++c) {
+                const int cell = i0 + c * 128;
+                if (cell < cells) {
+                    const uint32_t at = smem_u32(dyn) + (uint32_t)((first + (cell >> 5)) * 512 + (cell & 31) * 16);
+                    float4 v[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) v[k] = k < p.split ? peer_load4(at, k) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                    for (int k = 1; k < 8; ++k) { v[0].x += v[k].x; v[0].y += v[k].y; v[0].z += v[k].z; v[0].w += v[k].w; }
+                    sum[c] = v[0];
+                }
             }
         }
-        cluster_meet();                                  // nothing of another CTA is read any more
+        asm volatile("barrier.cluster.arrive.release;" ::: "memory");   // what this CTA needs of the others is read
+        if (warp >= 2) {
+#pragma unroll
+            for (int c = 0; c < kCells / 2; ++c) {
+                const int cell = i0 + c * 128, m = m0 + first + (cell >> 5), j = j0 + (cell & 31) * 4;
+                if (cell < cells && m < p.M && j < p.J) {
+                    const float v[4] = {sum[c].x, sum[c].y, sum[c].z, sum[c].w};
+                    TO* const out = static_cast<TO*>(p.out) + (long long)m * p.J + j;
+                    __align__(16) TO o[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[i] = from_f32<TO>(v[i] + (j + i < p.J ? bias_at(p, j + i) : 0.f));
+                    if ((p.J & 3) == 0) {
+                        if constexpr (sizeof(TO) == 4) *reinterpret_cast<uint4*>(out) = *reinterpret_cast<const uint4*>(o);
+                        else *reinterpret_cast<uint2*>(out) = *reinterpret_cast<const uint2*>(o);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (j + i < p.J) out[i] = o[i];
+                    }
+                }
+            }
+        }
+        asm volatile("barrier.cluster.wait.acquire;" ::: "memory");      // nothing of another CTA is read any more
     }
     tc_fence_before_sync();
     __syncthreads();
@@ -300,17 +367,25 @@ template <int T, typename TO> __global__ void __launch_bounds__(kFewThreads) fp8
     if (warp == 1) tmem_dealloc(tmem, kCols);
 }
 
-template <int T, typename TO> gf_status launch_few(ProductArgs& a, const void* codes, int L, long long a_pitch, cudaStream_t s) {
+// CTAs that share the chunks of a tile: up to two per SM in all.  Powers of two: clusters of 3 took up to twice the time.
+int few_split(long long tiles, int chunks) {
+    int split = 1;
+    while (split < 8 && 2 * split <= chunks && 2 * split * tiles <= 2LL * sm_count()) split *= 2;
+    return split;
+}
+
+template <int T, typename TO>
+gf_status launch_few(ProductArgs& a, const void* w, const void* codes, int N, int K, int L, long long a_pitch, cudaStream_t s) {
     static size_t configured[kMaxDevices] = {};
     auto kernel = fp8_few_kernel<T, TO>;
     const gf_status st = ensure_dyn_smem(kernel, few_smem(T), configured);
     if (st != GF_OK) return st;
+    // (in either form a box is 128 bytes of 128 rows of W)
+    if (!make_tmap_u8_2d(&a.tm_w, w, (uint64_t)K, (uint64_t)N, (uint64_t)GF_FP8_PITCH(K), 128)) return GF_ERR_CUDA;
     if (!make_tmap_u8_2d(&a.tm_a, codes, (uint64_t)L, (uint64_t)a.M, (uint64_t)a_pitch, T)) return GF_ERR_CUDA;
     a.tiles_m = (a.M + T - 1) / T;
     const long long tiles = (long long)a.tiles_m * ((a.J + 127) / 128);
-    int split = (int)(2LL * sm_count() / tiles);
-    split = split < 1 ? 1 : split > 8 ? 8 : split;
-    if (split > a.chunks) split = a.chunks;
+    const int split = few_split(tiles, a.chunks);
     a.per = (a.chunks + split - 1) / split;
     a.split = (a.chunks + a.per - 1) / a.per;
     if (tiles * a.split > 0x7fffffffLL) return GF_ERR_UNSUPPORTED;
@@ -327,11 +402,404 @@ template <int T, typename TO> gf_status launch_few(ProductArgs& a, const void* c
     return e == cudaSuccess ? GF_OK : GF_ERR_CUDA;
 }
 
-template <typename TO> gf_status product(ProductArgs& a, const void* codes, int L, long long a_pitch, cudaStream_t s) {
-    if (a.M <= 16) return launch_few<16, TO>(a, codes, L, a_pitch, s);
-    if (a.M <= 32) return launch_few<32, TO>(a, codes, L, a_pitch, s);
-    if (a.M <= 64) return launch_few<64, TO>(a, codes, L, a_pitch, s);
-    return launch_few<128, TO>(a, codes, L, a_pitch, s);
+// Many rows: pairs of CTAs walk over tiles of 256 rows by 128 or 256 columns.  Each CTA of a pair has 128 rows of the result, and
+// brings its 128 rows of A and half of the tile's columns of W; the products of a pair (cta_group::2) read both halves, so that a
+// chunk of 128 terms costs each SM 32 KB from L2 for 512 clocks of products.
+//   warp 0: copies; warp 1 (of the first CTA): products; warps 4 to 19: scaling, a quarter of the rows by a quarter of
+//   the columns each, in registers (which the first four warps give up for them); warp 3: takes the results to memory by the
+//   copy engine, while the next tile is on its way (starting a copy takes about 900 clocks: left to the scaling warps that
+//   was a fifth of the time of a 512-term tile).
+// What bounds it is the accumulators' way out of tensor memory, once for every 128 terms, which the scales ask for: with
+// the reads left out the products run at 2.97 PFLOP/s, with them and no arithmetic at 2.1, with all of it at 1.85 (4096 x 8192
+// x 4096; 1.6 under the power cap).  With 8 scaling warps of 128 columns 1.75.
+constexpr int kWideThreads = 640, kWideStages = 5, kWideStage = 32768, kWidePiece = 32 * 128;
+constexpr int kWideWarps = 16;                     // that scale
+constexpr size_t kWideSmem = (size_t)kWideStages * kWideStage + kWideWarps * kWidePiece + 1024;
+static_assert(kWideSmem + 256 <= 232448, "shared memory of a block");
+static_assert(128 * 32 + 512 * 112 <= kWideThreads * 96, "registers of the launch");
+constexpr uint32_t kLeaderMask = 0xFEFFFFFFu;      // a shared address of either CTA -> the same place in the first one
+
+__device__ __forceinline__ void load_box_pair(void* dst, const CUtensorMap* m, int x, int y, uint64_t* bar) {
+    // the bytes land here, their arrival is counted on the first CTA's barrier
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(y), "r"(smem_u32(bar) & kLeaderMask)
+        : "memory");
+}
+// As umma_smem_desc, for tiles of 64-byte rows under the 64-byte swizzle
+__device__ __forceinline__ uint64_t umma_smem_desc64(uint32_t saddr, uint32_t lbo_bytes, uint32_t sbo_bytes) {
+    return (umma_smem_desc(saddr, lbo_bytes, sbo_bytes) & ~((uint64_t)7 << 61)) | ((uint64_t)4 << 61);
+}
+__device__ __forceinline__ void umma_fp8_pair(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void commit_pair(uint64_t* bar) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_u32(bar)),
+                 "h"((uint16_t)3)
+                 : "memory");
+}
+// (What the arrival orders are reads of tensor memory, for which the fence of tcgen05 stands.  Releasing ordinary memory to the cluster
+// as well took about 1500 clocks an arrival: 3.0 -> 1.2 PFLOP/s of products.)
+__device__ __forceinline__ void arrive_leader(uint64_t* bar) {
+    asm volatile(
+        "{\n\t.reg .b32 a;\n\t"
+        "mapa.shared::cluster.u32 a, %0, 0;\n\t"
+        "mbarrier.arrive.shared::cluster.b64 _, [a];\n\t}" ::"r"(smem_u32(bar))
+        : "memory");
+}
+__device__ __forceinline__ void tmem_ld_wait_for(uint32_t (&r)[32]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]),
+                   "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]),
+                   "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]),
+                   "+r"(r[31])::"memory");
+}
+
+// NC columns of a warp's 32 rows into `buf`: a thread has a row, whose 16-byte pieces lie as the copy engine's
+// swizzle has them (rows of 128 or 64 bytes), so that neither these writes nor the copy's reads meet in a bank.
+template <typename TO, int NC> __device__ __forceinline__ void stage_piece(unsigned char* buf, const uint64_t* acc, int lane) {
+    constexpr int kVec = 16 / (int)sizeof(TO), kBytes = NC * (int)sizeof(TO);
+    static_assert(kBytes == 128 || kBytes == 64, "rows of a swizzle's width");
+    const int flip = kBytes == 128 ? lane & 7 : (lane >> 1) & 3;
+#pragma unroll
+    for (int c = 0; c < NC; c += kVec) {
+        float v[kVec];
+#pragma unroll
+        for (int i = 0; i < kVec; i += 2) {
+            const float2 f = unpair(acc[(c + i) / 2]);
+            v[i] = f.x; v[i + 1] = f.y;
+        }
+        uint4 w;
+        if constexpr (sizeof(TO) == 4) w = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+        else {
+            uint32_t* const q = &w.x;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+                q[i] = *reinterpret_cast<const uint32_t*>(&b);
+            }
+        }
+        *reinterpret_cast<uint4*>(buf + lane * kBytes + ((c / kVec) ^ flip) * 16) = w;
+    }
+}
+// The same piece to memory by the warp itself, where the result's rows are not whole 16-byte pieces: a row at a time, words of
+// 4 bytes (two bf16 values from the row's first even place on, and the odd ones at its ends).
+// (A call of its own, so that its registers are not taken from the loop that scales.)
+template <typename TO, int NC> __device__ __noinline__ void store_piece(TO* out, long long pitch, const unsigned char* buf, int rows, int live, int lane) {
+    constexpr int kVec = 16 / (int)sizeof(TO), kBytes = NC * (int)sizeof(TO), kEach = 4 / (int)sizeof(TO);
+    static_assert(NC <= 32 * kEach, "a word a lane");
+    auto at = [&](int r, int c) {
+        const int turn = kBytes == 128 ? r & 7 : (r >> 1) & 3;
+        return *reinterpret_cast<const TO*>(buf + r * kBytes + ((c / kVec) ^ turn) * 16 + c % kVec * (int)sizeof(TO));
+    };
+    __syncwarp();
+#pragma unroll 1
+    for (int r0 = 0; r0 < rows; r0 += 8) {
+        TO v[8][kEach], first[8];
+        int odd[8];                                      // places of a row's elements before its first whole word
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            odd[k] = sizeof(TO) == 4 ? 0 : (int)((reinterpret_cast<uintptr_t>(out + k * pitch) >> 1) & 1);
+            first[k] = at(r0 + k, 0);
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) v[k][i] = at(r0 + k, min(kEach * lane + odd[k] + i, NC - 1));
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            TO* const row = out + k * pitch;
+            const int c = kEach * lane + odd[k];
+            if (r0 + k < rows) {
+                if constexpr (sizeof(TO) == 4) {
+                    if (c < live) row[c] = v[k][0];
+                } else {
+                    if (c + 1 < live) {
+                        __nv_bfloat162 w;
+                        w.x = v[k][0];
+                        w.y = v[k][1];
+                        *reinterpret_cast<__nv_bfloat162*>(row + c) = w;
+                    } else if (c < live) row[c] = v[k][0];
+                    if (odd[k] && lane == 0) row[0] = first[k];
+                }
+            }
+        }
+        out += 8 * pitch;
+    }
+    __syncwarp();
+}
+
+// Adds the bias of a warp's columns, one (and for 64 columns another) of which each lane brings, by way of `buf`.
+__device__ __forceinline__ void add_bias(uint64_t (&acc)[32], float* buf, float b0, float b1, int cols, int lane) {
+    buf[lane] = b0;
+    buf[32 + lane] = b1;
+    __syncwarp();
+#pragma unroll
+    for (int c = 0; c < 64; c += 4) {
+        if (c < cols) {
+            const float4 v = *reinterpret_cast<const float4*>(buf + c);
+            const float2 x = unpair(acc[c / 2]), y = unpair(acc[c / 2 + 1]);
+            acc[c / 2] = pair_of(x.x + v.x, x.y + v.y);
+            acc[c / 2 + 1] = pair_of(y.x + v.z, y.y + v.w);
+        }
+    }
+    __syncwarp();
+}
+
+template <typename TO> __global__ void __launch_bounds__(kWideThreads, 1) fp8_wide_kernel(const __grid_constant__ ProductArgs p) {
+    extern __shared__ unsigned char dyn_raw[];
+    unsigned char* const dyn = align1024(dyn_raw);
+    __shared__ uint64_t full[kWideStages], empty[kWideStages], done[4], drained[4];
+    __shared__ uint32_t tmem_base;
+    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+    const int rank = (int)blockIdx.x & 1, unit = (int)blockIdx.x >> 1, units = (int)gridDim.x >> 1;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kWideStages; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
+        for (int s = 0; s < 4; ++s) { mbar_init(&done[s], 1); mbar_init(&drained[s], 2 * kWideWarps); }
+        mbar_fence_init();
+    }
+    pdl_wait();
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    cluster_meet();                                      // the other CTA's barriers are ready
+    tc_fence_after_sync();
+    pdl_launch_dependents();
+    const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_base, 0);
+    const int share = p.bn / 2;                          // columns whose W a CTA brings
+    const int tiles_j = (p.J + p.bn - 1) / p.bn;
+    const int tiles = p.tiles_m * tiles_j;
+    const uint32_t shift = p.bn == 256 ? 1u : 2u, buffers = 1u << shift;      // accumulators in tensor memory
+    // tiles unit, unit + units, ..: rows and columns of tiles are counted on, not divided
+    const int step_m = units / tiles_j, step_j = units % tiles_j;
+    auto advance = [&](int& tm, int& tj) {
+        tm += step_m;
+        tj += step_j;
+        if (tj >= tiles_j) { tj -= tiles_j; ++tm; }
+    };
+    unsigned char* const pieces = dyn + kWideStages * kWideStage;
+    constexpr int kPieceCols = sizeof(TO) == 2 ? 64 : 32;                      // columns that are staged at once, at most
+    bool ok = true;
+
+    if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
+    if (warp == 0) {
+        uint32_t ring = 0;                               // one bit per stage: the parity of its next use
+        int s = 0;
+        const uint32_t bytes = 16384u + (uint32_t)share * 128u;
+        int tm = unit / tiles_j, tj = unit % tiles_j;
+        for (int t = unit; t < tiles && ok; t += units, advance(tm, tj)) {
+            const int m = tm * 256 + rank * 128, j = tj * p.bn + rank * share;
+            for (int q = 0; q < p.chunks; ++q) {
+                ok = mbar_wait_warp(&empty[s], ((ring >> s) & 1u) ^ 1u);
+                if (!ok) break;
+                if (elect_one()) {
+                    unsigned char* const st = dyn + (size_t)s * kWideStage;
+                    if (rank == 0) mbar_expect_tx(&full[s], 2u * bytes);
+                    load_box_pair(st, &p.tm_a, q * 128, m, &full[s]);
+                    if (p.mn_major) load_box_pair(st + 16384, &p.tm_w, j, q * 128, &full[s]);
+                    else load_box_pair(st + 16384, &p.tm_w, q * 128, j, &full[s]);
+                }
+                __syncwarp();
+                ring ^= 1u << s;
+                if (++s == kWideStages) s = 0;
+            }
+        }
+    } else if (warp == 1) {
+        if (rank == 0) {
+            const uint32_t idesc = fp8_idesc(256, p.bn, 0u, p.mn_major ? 1u : 0u);
+            // W: rows of 128 terms, or 128 rows of a CTA's 128 or 64 columns
+            const uint64_t a_form = umma_smem_desc(0, 16, 1024);
+            const uint64_t b_form = p.mn_major && share == 64 ? umma_smem_desc64(0, 8192, 512) : umma_smem_desc(0, 16384, 1024);
+            const uint32_t b_step = p.mn_major ? (uint32_t)share * 2u : 2u;  // 32 terms further, in 16 bytes
+            const uint32_t ring0 = smem_u32(dyn) >> 4;
+            uint32_t ring = 0, use = 0;
+            int s = 0;
+            for (int t = unit; t < tiles && ok; t += units) {
+                for (int q = 0; q < p.chunks; ++q, ++use) {
+                    const uint32_t buf = use & (buffers - 1u);
+                    ok = mbar_wait_warp(&full[s], (ring >> s) & 1u);         // (long there: the accumulator is what is waited for)
+                    if (ok && use >= buffers) ok = mbar_wait_warp(&drained[buf], ((use >> shift) - 1u) & 1u);
+                    if (!ok) break;
+                    tc_fence_after_sync();
+                    if (elect_one()) {
+                        const uint32_t at = ring0 + (uint32_t)s * (kWideStage >> 4);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            umma_fp8_pair(tmem + buf * (uint32_t)p.bn, a_form + at + k * 2, b_form + at + 1024u + k * b_step, idesc, k > 0);
+                        commit_pair(&done[buf]);
+                        commit_pair(&empty[s]);
+                    }
+                    __syncwarp();
+                    ring ^= 1u << s;
+                    if (++s == kWideStages) s = 0;
+                }
+            }
+        }
+    }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 112;");
+        const int quarter = warp & 3, cols = p.bn / 4, col = ((warp - 4) >> 2) * cols;      // this warp's columns: 32 or 64, and where
+        const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)col;
+        unsigned char* const piece = pieces + (warp - 4) * kWidePiece;
+        // The scales of the next chunk, this tile's or the next one's, are fetched while one is added.
+        uint32_t n = 0;                                  // chunks so far
+        int ft = unit, fm = unit / tiles_j, fj = unit % tiles_j, fq = 0;
+        int tm = fm, tj = fj;
+        const float *fa = nullptr, *fw = nullptr;
+        auto fetch_from = [&] {
+            fa = p.sa + min((long long)fm * 256 + rank * 128 + quarter * 32 + lane, (long long)p.M - 1);
+            fw = p.sw + (long long)min((fj * p.bn + col) >> 7, (p.J - 1) >> 7) * p.sw_j;
+        };
+        fetch_from();
+        float a_next = __ldg(fa), w_next = __ldg(fw);
+        auto fetch = [&] {
+            if (++fq == p.chunks) {
+                fq = 0;
+                ft += units;
+                advance(fm, fj);
+                if (ft < tiles) fetch_from();            // (else: once more what is there)
+            } else {
+                fa += p.sa_pitch;
+                fw += p.sw_q;
+            }
+            a_next = __ldg(fa);
+            w_next = __ldg(fw);
+        };
+        for (int t = unit; t < tiles && ok; t += units, advance(tm, tj)) {
+            const long long row0 = (long long)tm * 256 + rank * 128 + quarter * 32;
+            const int j0 = tj * p.bn + col;
+            uint64_t acc[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) acc[i] = 0;
+            float bias0 = 0.f, bias1 = 0.f;              // of this lane's columns; on their way while the tile is computed
+            if (p.bias) {
+                if (j0 + lane < p.J) bias0 = bias_at(p, j0 + lane);
+                if (cols == 64 && j0 + 32 + lane < p.J) bias1 = bias_at(p, j0 + 32 + lane);
+            }
+            for (int q = 0; q < p.chunks && ok; ++q, ++n) {
+                const uint32_t buf = n & (buffers - 1u);
+                const float now = a_next * w_next;
+                const uint64_t scale = pair_of(now, now);
+                fetch();
+                ok = mbar_wait_warp(&done[buf], (n >> shift) & 1u);
+                if (!ok) break;
+                tc_fence_after_sync();
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    if (c * 32 < cols) {
+                        uint32_t raw[32];
+                        tmem_ld32(lanes + buf * (uint32_t)p.bn + (uint32_t)(c * 32), raw);
+                        tmem_ld_wait_for(raw);
+                        if ((c + 1) * 32 >= cols) {      // the accumulator is read
+                            tc_fence_before_sync();
+                            __syncwarp();
+                            if (lane == 0) arrive_leader(&drained[buf]);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            acc[c * 16 + i] = fma_pair(pair_of(__uint_as_float(raw[2 * i]), __uint_as_float(raw[2 * i + 1])), scale, acc[c * 16 + i]);
+                    }
+                }
+            }
+            if (!ok) break;
+            if (row0 >= p.M || j0 >= p.J) continue;
+            for (int c = 0; c < cols && j0 + c < p.J; c += kPieceCols) {
+                bulk_wait_read<0>();                     // the copy before has read the buffer (for the thread that started it)
+                __syncwarp();
+                if (c == 0 && p.bias) add_bias(acc, reinterpret_cast<float*>(piece), bias0, bias1, cols, lane);
+                if (cols >= kPieceCols) {
+                    if (c == 0) stage_piece<TO, kPieceCols>(piece, acc, lane);
+                    else stage_piece<TO, kPieceCols>(piece, acc + kPieceCols / 2 % 32, lane);
+                } else stage_piece<TO, 32>(piece, acc, lane);
+                if (p.out_map) {
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) {
+                        asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(reinterpret_cast<uint64_t>(&p.tm_out)),
+                                     "r"(j0 + c), "r"((int)row0), "r"(smem_u32(piece))
+                                     : "memory");
+                        bulk_commit();
+                    }
+                } else {
+                    TO* const out = static_cast<TO*>(p.out) + row0 * p.J + j0 + c;
+                    const int rows = (int)min(32LL, p.M - row0), live = min(p.J - j0 - c, min(cols, kPieceCols));
+                    if (cols >= kPieceCols) store_piece<TO, kPieceCols>(out, p.J, piece, rows, live, lane);
+                    else store_piece<TO, 32>(out, p.J, piece, rows, live, lane);
+                }
+            }
+        }
+        bulk_wait_all();
+    }
+    if (!ok) {
+        atomicOr(p.err_word, 8192u);
+        let_settle();
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    cluster_meet();                                      // nothing of the other CTA refers to this one any more
+    tc_fence_after_sync();
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+}
+
+int wide_columns(int J) { return J <= 128 ? 128 : 256; }
+
+template <typename TO> gf_status launch_wide(ProductArgs& a, const void* w, const void* codes, int N, int K, int L, long long a_pitch, cudaStream_t s) {
+    static size_t configured[kMaxDevices] = {};
+    auto kernel = fp8_wide_kernel<TO>;
+    const gf_status st = ensure_dyn_smem(kernel, kWideSmem, configured);
+    if (st != GF_OK) return st;
+    a.tiles_m = (a.M + 255) / 256;
+    a.bn = wide_columns(a.J);
+    if (!make_tmap_u8_2d(&a.tm_a, codes, (uint64_t)L, (uint64_t)a.M, (uint64_t)a_pitch, 128)) return GF_ERR_CUDA;
+    if (a.mn_major ? !make_tmap_u8_2d(&a.tm_w, w, (uint64_t)K, (uint64_t)N, (uint64_t)GF_FP8_PITCH(K), 128, (uint32_t)a.bn / 2)
+                   : !make_tmap_u8_2d(&a.tm_w, w, (uint64_t)K, (uint64_t)N, (uint64_t)GF_FP8_PITCH(K), (uint32_t)a.bn / 2))
+        return GF_ERR_CUDA;
+    // (a tile's last columns and rows are cut off by the map)
+    a.out_map = (long long)a.J * sizeof(TO) % 16 == 0;
+    if (a.out_map && !make_tmap_swizzled(&a.tm_out, a.out, (int)sizeof(TO), (uint64_t)a.J, (uint64_t)a.M, sizeof(TO) == 2 && a.bn == 256 ? 64u : 32u, 32u)) return GF_ERR_CUDA;
+    const long long tiles = (long long)a.tiles_m * ((a.J + a.bn - 1) / a.bn);
+    if (tiles > 0x7fffffffLL) return GF_ERR_UNSUPPORTED;
+    const long long pairs = sm_count() / 2;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(2 * (tiles < pairs ? tiles : pairs))); cfg.blockDim = dim3(kWideThreads); cfg.dynamicSmemBytes = kWideSmem; cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 2; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = 2;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, a);
+    count_launch();
+    return e == cudaSuccess ? GF_OK : GF_ERR_CUDA;
+}
+
+// Which kernel: estimates in microseconds, fitted to both on 1 to 2048 rows by 96 to 8192 columns and terms.  Wide: a chunk of a
+// tile of 256 columns takes 0.55 (128: 0.3), results 1.3, and 5 more where 16-bit rows start at odd places.  Few: 0.6 a chunk, or
+// 0.46 of an SM's time where there are more tiles than SMs, 0.7 to join parts.  (300 x 4096 x 4096: 20.3 wide, 25.2 few; 200 rows: 19.9, 17.4;
+// 2048 x 512 x 4096: 20.0, 17.5; 1024 x 2048 x 2048: 13.8, 15.8.)
+template <typename TO> bool wide_is_faster(const ProductArgs& a) {
+    if (a.M <= 32) return false;
+    const int bn = wide_columns(a.J), odd = (long long)a.J * sizeof(TO) % 4 != 0;
+    const double tiles = (double)((a.M + 255) / 256) * ((a.J + bn - 1) / bn), rounds = (double)(long long)((tiles + sm_count() / 2 - 1) / (sm_count() / 2));
+    const double wide = 3.2 + rounds * ((bn == 256 ? 0.55 : 0.3) * a.chunks + 1.3 + 5 * odd);
+    const long long few_tiles = (long long)((a.M + 63) / 64) * ((a.J + 127) / 128);
+    const int split = few_split(few_tiles, a.chunks);
+    const double alone = 0.6 * ((a.chunks + split - 1) / split), all = 0.46 * (double)few_tiles * a.chunks / sm_count();
+    return wide < 3.5 + (alone > all ? alone : all) + (split > 1 ? 0.7 : 0.0);
+}
+
+template <typename TO> gf_status product(ProductArgs& a, const void* w, const void* codes, int N, int K, int L, long long a_pitch, cudaStream_t s) {
+    if (wide_is_faster<TO>(a)) return launch_wide<TO>(a, w, codes, N, K, L, a_pitch, s);
+    if (a.M <= 16) return launch_few<16, TO>(a, w, codes, N, K, L, a_pitch, s);
+    if (a.M <= 32) return launch_few<32, TO>(a, w, codes, N, K, L, a_pitch, s);
+    return launch_few<64, TO>(a, w, codes, N, K, L, a_pitch, s);
 }
 
 constexpr int kMostDim = 1 << 24;
@@ -410,12 +878,10 @@ gf_status gf_fp8_matmul(const gf_fp8_matmul_desc* desc, const void* a, const flo
     p.mn_major = d.transposed;
     p.err_word = global_err_word();
     if (!p.err_word) return GF_ERR_CUDA;
-    // (in either form a box is 128 bytes of 128 rows of W)
-    if (!make_tmap_u8_2d(&p.tm_w, w, (uint64_t)d.K, (uint64_t)d.N, (uint64_t)GF_FP8_PITCH(d.K), 128)) return GF_ERR_CUDA;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     ProfScope prof(K_FP8_PRODUCT, s);
     const long long a_pitch = GF_FP8_PITCH((long long)L);
-    return d.out_dtype == GF_F32 ? product<float>(p, a, L, a_pitch, s) : product<__nv_bfloat16>(p, a, L, a_pitch, s);
+    return d.out_dtype == GF_F32 ? product<float>(p, w, a, d.N, d.K, L, a_pitch, s) : product<__nv_bfloat16>(p, w, a, d.N, d.K, L, a_pitch, s);
 }
 
 }  // extern "C"

@@ -44,17 +44,33 @@ bool make_tmap_bf16(CUtensorMap* out, const void* base, int rank, uint64_t d0, u
     return r == CUDA_SUCCESS;
 }
 
-bool make_tmap_u8_2d(CUtensorMap* out, const void* base, uint64_t width, uint64_t rows, uint64_t pitch, uint32_t box_rows) {
+bool make_tmap_u8_2d(CUtensorMap* out, const void* base, uint64_t width, uint64_t rows, uint64_t pitch, uint32_t box_rows,
+                     uint32_t box_bytes) {
     PFN_cuTensorMapEncodeTiled enc = encoder();
-    if (!enc) return false;
+    if (!enc || (box_bytes != 128 && box_bytes != 64)) return false;
     if ((reinterpret_cast<uintptr_t>(base) & 15u) != 0 || pitch % 16 != 0 || box_rows < 1 || box_rows > 256) return false;
     cuuint64_t dims[2] = {width, rows};
     cuuint64_t strides[1] = {pitch};
-    cuuint32_t box[2] = {128, box_rows};
+    cuuint32_t box[2] = {box_bytes, box_rows};
     cuuint32_t estr[2] = {1, 1};
     const CUresult r = enc(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
-                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                           CU_TENSOR_MAP_INTERLEAVE_NONE, box_bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS;
+}
+
+bool make_tmap_swizzled(CUtensorMap* out, const void* base, int elem_bytes, uint64_t d0, uint64_t d1, uint32_t box0, uint32_t box1) {
+    PFN_cuTensorMapEncodeTiled enc = encoder();
+    const uint32_t row = box0 * (uint32_t)elem_bytes;
+    if (!enc || (elem_bytes != 2 && elem_bytes != 4) || (row != 128 && row != 64)) return false;
+    if ((reinterpret_cast<uintptr_t>(base) & 15u) != 0 || d0 * elem_bytes % 16 != 0 || box1 < 1 || box1 > 256) return false;
+    cuuint64_t dims[2] = {d0, d1};
+    cuuint64_t strides[1] = {d0 * elem_bytes};
+    cuuint32_t box[2] = {box0, box1};
+    cuuint32_t estr[2] = {1, 1};
+    const CUresult r = enc(out, elem_bytes == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims,
+                           strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, row == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                           CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS;
 }
 

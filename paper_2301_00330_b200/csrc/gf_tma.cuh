@@ -34,9 +34,13 @@ bool make_tmap_bf16(CUtensorMap* out, const void* base, int rank, uint64_t d0, u
 bool make_tmap_plain(CUtensorMap* out, const void* base, int elem_bytes, uint64_t d0, uint64_t d1, uint64_t d2,
                      uint64_t stride1, uint64_t stride2, uint32_t box0, uint32_t box1, uint32_t box2);
 
-// Byte matrix [rows][pitch] (int8 operands), rows of `width` valid bytes, box = {128 bytes, box_rows},
-// 128-byte swizzle: a box lands as a K-major tile of 128-byte rows.  pitch is a multiple of 16.
-bool make_tmap_u8_2d(CUtensorMap* out, const void* base, uint64_t width, uint64_t rows, uint64_t pitch, uint32_t box_rows);
+// Byte matrix [rows][pitch] (8-bit operands), rows of `width` valid bytes, box = {box_bytes, box_rows}, box_bytes 128 or 64
+// under the swizzle of that width: a box lands as a tile of such rows.  pitch is a multiple of 16.
+bool make_tmap_u8_2d(CUtensorMap* out, const void* base, uint64_t width, uint64_t rows, uint64_t pitch, uint32_t box_rows, uint32_t box_bytes = 128);
+
+// Dense matrix [d1][d0] of 2-byte (bf16) or 4-byte (fp32) elements, box = {box0, box1} with rows of 128 or 64 bytes, under the
+// swizzle of that width: for results on their way out.
+bool make_tmap_swizzled(CUtensorMap* out, const void* base, int elem_bytes, uint64_t d0, uint64_t d1, uint32_t box0, uint32_t box1);
 
 // Plain map of a dense array [d2][d1][d0] of 8-byte units, strides in units, box = {box0, box1, 1}; an even box0 <= 256.
 bool make_tmap_u64(CUtensorMap* out, const void* base, uint64_t d0, uint64_t d1, uint64_t d2, uint64_t stride1, uint64_t stride2,
