@@ -17,32 +17,41 @@ Drop make_drop(float p, const uint64_t* seed) {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kEach = 2;
 
+// kEach octets a thread, the loads of all on their way before the first is computed
 template <typename TX, typename TY, bool RESIDUAL>
-__global__ void __launch_bounds__(kThreads) dropout_kernel(const TX* x, const TY* residual, TY* y, long long count, Drop d) {
+__global__ void __launch_bounds__(kThreads) dropout_kernel(const TX* x, const TY* residual, TY* y, long long count, const __grid_constant__ Drop d) {
     pdl_launch_dependents();
-    const long long octets = (count + 7) / 8, step = (long long)gridDim.x * kThreads;
+    const long long octets = (count + 7) / 8, first = (long long)blockIdx.x * (kThreads * kEach) + threadIdx.x;
     pdl_wait();
-    uint64_t key = 0, offset = 0;
-    if (d.threshold) { key = __ldg(d.seed); offset = __ldg(d.seed + 1); }
-    for (long long f = (long long)blockIdx.x * kThreads + threadIdx.x; f < octets; f += step) {
-        Octet<TX> a;
-        Octet<TY> r;
-        load_octet(a, x, f, count);
-        if constexpr (RESIDUAL) load_octet(r, residual, f, count);
-        float v[8];
-        a.get(v);
-        if (d.threshold) drop_octet(v, (uint64_t)f, key, offset, d.threshold, d.scale);
-        if constexpr (RESIDUAL) {
-            float w[8];
-            r.get(w);
+    uint64_t key, offset;
+    load_seed(d, key, offset);
+    Octet<TX> a[kEach];
+    Octet<TY> r[kEach];
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+        const long long f = first + k * kThreads;
+        if (f < octets) {
+            load_octet(a[k], x, f, count);
+            if constexpr (RESIDUAL) load_octet(r[k], residual, f, count);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+        const long long f = first + k * kThreads;
+        if (f >= octets) break;
+        float v[8], w[8];
+        a[k].get(v);
+        if constexpr (RESIDUAL) r[k].get(w);
+        if (d.threshold) drop_octet<RESIDUAL>(v, w, (uint64_t)f, key, offset, d);
+        else if constexpr (RESIDUAL) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] += w[i];
         }
         if (f * 8 + 8 <= count) {
-            r.set(v);
-            r.store(y + f * 8);
+            r[k].set(v);
+            r[k].store(y + f * 8);
         } else {
 #pragma unroll
             for (int i = 0; i < 7; ++i)
@@ -52,8 +61,8 @@ __global__ void __launch_bounds__(kThreads) dropout_kernel(const TX* x, const TY
 }
 
 template <typename TX, typename TY> gf_status launch(const void* x, const void* residual, void* y, long long count, const Drop& d, cudaStream_t s) {
-    const long long octets = (count + 7) / 8, want = cdiv64(octets, kThreads), most = (long long)sm_count() * 8;
-    const dim3 grid((unsigned)(want < most ? want : most));
+    const long long blocks = cdiv64((count + 7) / 8, kThreads * kEach);
+    const dim3 grid((unsigned)blocks);
     ProfScope prof(K_DROPOUT, s);
     if (residual)
         return launch_pdl(dropout_kernel<TX, TY, true>, grid, dim3(kThreads), 0, s, static_cast<const TX*>(x), static_cast<const TY*>(residual),
@@ -82,7 +91,7 @@ gf_status run(const gf_dropout_desc* desc, const void* x, int x_dtype, const voi
 gf_status validate(const gf_dropout_desc* d) {
     if (!d) return GF_ERR_NULL;
     if (d->count < 0 || !valid_p(d->p) || !is_dtype(d->dtype) || !is_dtype(d->out_dtype)) return GF_ERR_BAD_DESC;
-    return d->count > (int64_t)1 << 60 ? GF_ERR_UNSUPPORTED : GF_OK;
+    return d->count > (int64_t)1 << 43 ? GF_ERR_UNSUPPORTED : GF_OK;      // (blocks are counted in 31 bits)
 }
 
 }  // namespace

@@ -165,23 +165,6 @@ __device__ __forceinline__ float bias_at(const ProductArgs& p, int j) {
     return p.bias_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p.bias)[j]) : static_cast<const float*>(p.bias)[j];
 }
 
-// Pairs of fp32: two operations per instruction, each half rounded as the scalar one is.
-__device__ __forceinline__ uint64_t pair_of(float a, float b) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-    return r;
-}
-__device__ __forceinline__ float2 unpair(uint64_t v) {
-    float2 r;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
-    return r;
-}
-__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c) {
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-
 // A tile is 128 columns of the result (rows of the accumulator) by T of its rows, so that the weight is the operand of
 // 128 and few rows of A cost no more than they are.  The chunks of a tile are split over a cluster of CTAs where there
 // are few tiles, and the parts are added through distributed shared memory, in the order of the CTAs.

@@ -9,6 +9,51 @@
 
 namespace gf {
 
+// ---- pairs of fp32 ---------------------------------------------------------------------------------------
+// Two operations per instruction, each half rounded as the scalar one is: the loops over rows are bound by instructions.
+__device__ __forceinline__ uint64_t pair_of(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float2 unpair(uint64_t v) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ float sum_of(uint64_t v) {
+    const float2 f = unpair(v);
+    return f.x + f.y;
+}
+// Eight values as four pairs
+typedef uint64_t Eight[4];
+__device__ __forceinline__ void to_eight(const float (&v)[8], Eight& p) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = pair_of(v[2 * i], v[2 * i + 1]);
+}
+__device__ __forceinline__ void from_eight(const Eight& p, float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = unpair(p[i]);
+        v[2 * i] = f.x; v[2 * i + 1] = f.y;
+    }
+}
+
 // ---- eight elements as they lie in memory ------------------------------------------------------------------
 template <typename T> struct Octet {
     static constexpr int kWords = 2 * (int)sizeof(T);      // 32-bit words
@@ -38,6 +83,16 @@ template <typename T> struct Octet {
                 w[i] = *reinterpret_cast<const uint32_t*>(&b);
             }
         }
+    }
+    __device__ __forceinline__ void get(Eight& p) const {
+        float v[8];
+        get(v);
+        to_eight(v, p);
+    }
+    __device__ __forceinline__ void set(const Eight& p) {
+        float v[8];
+        from_eight(p, v);
+        set(v);
     }
     // p: 16-byte aligned
     __device__ __forceinline__ void load(const T* p) {
@@ -128,15 +183,36 @@ struct Drop {
 Drop make_drop(float p, const uint64_t* seed);
 static inline bool valid_p(float p) { return p >= 0.f && p <= 1.f; }
 
-// v[i] <- kept ? v[i] scale : 0 for the elements of octet number f
-__device__ __forceinline__ void drop_octet(float (&v)[8], uint64_t f, uint64_t key, uint64_t offset, uint32_t threshold, float scale) {
-    const uint4 r = philox(f, offset, key);
-    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        v[2 * i] = (w[i] & 0xffffu) >= threshold ? v[2 * i] * scale : 0.f;
-        v[2 * i + 1] = (w[i] >> 16) >= threshold ? v[2 * i + 1] * scale : 0.f;
+// The two words of a seed, the same in all threads: said in a way that lets the compiler keep them, and the keys of the ten rounds, in
+// uniform registers (integer additions of 20 to 160 clocks a block of bits otherwise).  Called by whole warps.
+__device__ __forceinline__ void load_seed(const Drop& d, uint64_t& key, uint64_t& offset) {
+    key = offset = 0;
+    if (d.threshold) {
+        key = __shfl_sync(0xffffffffu, d.seed[0], 0);
+        offset = __shfl_sync(0xffffffffu, d.seed[1], 0);
     }
+}
+
+// v[i] <- kept ? v[i] scale + add[i] : add[i] for the elements of octet number f.  A 16-bit half is compared at the top of a word:
+// (w >> 16) >= t is w >= t << 16, and for all to be dropped (t = 65536) no word passes.
+template <bool ADD> __device__ __forceinline__ void drop_octet(float (&v)[8], const float (&add)[8], uint64_t f, uint64_t key, uint64_t offset, const Drop& d) {
+    const uint4 r = philox(f, offset, key);
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w}, top = d.threshold << 16;
+    const bool none = d.threshold == 65536u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t bits = i & 1 ? w[i >> 1] : w[i >> 1] << 16;      // (what lies below the half does not matter)
+        const float kept = ADD ? fmaf(v[i], d.scale, add[i]) : v[i] * d.scale;
+        v[i] = bits >= top && !none ? kept : ADD ? add[i] : 0.f;
+    }
+}
+
+template <bool ADD> __device__ __forceinline__ void drop_octet(Eight& v, const Eight& add, uint64_t f, uint64_t key, uint64_t offset, const Drop& d) {
+    float x[8], w[8];
+    from_eight(v, x);
+    if (ADD) from_eight(add, w);
+    drop_octet<ADD>(x, w, f, key, offset, d);
+    to_eight(x, v);
 }
 
 // ---- 8 bits ---------------------------------------------------------------------------------------------------------
@@ -144,10 +220,10 @@ constexpr float kFp8Top = 448.f, kFp8Tiny = 1.17549435e-38f;
 
 // Largest magnitude as bits: ordered like unsigned numbers, NaN above all.
 __device__ __forceinline__ uint32_t magnitude(const float (&v)[8]) {
-    uint32_t m = 0;
+    float m = fabsf(v[0]);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
-    return m;
+    for (int i = 1; i < 8; ++i) asm("max.NaN.f32 %0, %0, %1;" : "+f"(m) : "f"(fabsf(v[i])));
+    return __float_as_uint(m) & 0x7fffffffu;
 }
 __device__ __forceinline__ float scale_of(uint32_t magnitude_bits) {
     return magnitude_bits >= 0x7f800000u ? __uint_as_float(magnitude_bits) : fmaxf(__uint_as_float(magnitude_bits) * (1.f / kFp8Top), kFp8Tiny);
@@ -163,15 +239,12 @@ __device__ __forceinline__ uint32_t codes2(float a, float b) {
 // finite leaves NaN.
 __device__ __forceinline__ uint2 codes8(const float (&v)[8], float scale, float inv, int valid) {
     uint32_t c[4];
+    const uint64_t inv2 = pair_of(inv, inv), minus = pair_of(-scale, -scale);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        float q[2];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const float x = v[2 * i + k], y = x * inv;
-            q[k] = copysignf(__fmaf_rn(__fmaf_rn(-y, scale, x), inv, y), x);      // (the correction makes +0 of -0)
-        }
-        c[i] = codes2(q[0], q[1]);
+        const uint64_t x = pair_of(v[2 * i], v[2 * i + 1]), y = mul_pair(x, inv2);
+        const float2 q = unpair(fma_pair(fma_pair(y, minus, x), inv2, y));
+        c[i] = codes2(copysignf(q.x, v[2 * i]), copysignf(q.y, v[2 * i + 1]));      // (the correction makes +0 of -0)
     }
     uint2 r = make_uint2(c[0] | (c[1] << 16), c[2] | (c[3] << 16));
     if (valid < 8) {

@@ -4,7 +4,7 @@
 // whole 16-byte vector wherever a row starts; the first and last octet of a row may hold neighbours' elements, which are masked.
 // A team of threads (part of a warp, or a block) has a row; thread g of T has octets g, g + T, ..  Teams walk over the
 // rows in steps of a multiple of eight rows, so that all rows of a team start at the same place of an octet: a
-// thread has the same columns in all of them, and keeps gamma (and, backwards, its sums) in registers.
+// thread has the same columns in all of them.
 #pragma once
 
 #include "gf_block.h"
@@ -34,6 +34,14 @@ __device__ __forceinline__ float rms_gamma(const RmsArgs& a, int c) {
     return a.gamma_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(a.gamma)[c]) : static_cast<const float*>(a.gamma)[c];
 }
 
+// gamma of the eight columns from c on; those outside the row get 0
+__device__ __forceinline__ void rms_gamma8(const RmsArgs& a, int c, Eight& p) {
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = c + i >= 0 && c + i < a.cols ? rms_gamma(a, c + i) : 0.f;
+    to_eight(v, p);
+}
+
 // The sum over a team; `red`: 32 floats that are not in use since the last sum but one.
 template <bool WARP> __device__ __forceinline__ float rms_sum(float v, int log_tpr, float* red) {
     if constexpr (WARP) {
@@ -59,15 +67,16 @@ gf_status rms_validate(const gf_rms_desc* d);
 // Octets of a row, wherever it starts
 static inline int rms_octets(int cols) { return cols % 8 == 0 ? cols / 8 : (cols + 14) / 8; }
 
-// Threads for rows of n octets, at most `most` octets per thread.  WARP: 1 << log_tpr threads per row.
+// Threads for rows of n octets.  WARP: 1 << log_tpr threads per row, of a whole warp up to `most` octets each; else a block, one or
+// two octets per thread.  In every form only a thread's last octet may lie past the row.
 struct RmsShape {
     bool warp;
     int log_tpr, threads, per_thread;
 };
 static inline RmsShape rms_shape(int n, int most, int least_log) {
     RmsShape s = {};
-    if (n <= 32 * most) {
-        s.warp = true;
+    s.warp = n <= 32 * most;
+    if (s.warp) {
         s.log_tpr = least_log;
         while (s.log_tpr < 5 && (1 << s.log_tpr) < n) ++s.log_tpr;
         s.per_thread = (n + (1 << s.log_tpr) - 1) >> s.log_tpr;
@@ -75,7 +84,6 @@ static inline RmsShape rms_shape(int n, int most, int least_log) {
     } else {
         s.per_thread = n > 128 ? 2 : 1;
         s.threads = ((n + s.per_thread - 1) / s.per_thread + 31) / 32 * 32;
-        s.log_tpr = 0;
     }
     return s;
 }

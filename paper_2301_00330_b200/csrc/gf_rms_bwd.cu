@@ -8,15 +8,19 @@ namespace gf {
 namespace {
 
 // Rows longer than the registers of a block come with their dots: the grid's second dimension then deals out column tiles.
+// With one or two octets a thread the team's next row is on its way while one is computed; with three there are no registers
+// for that, and more rows per block instead.
 template <typename TX, typename TR, int NO, bool WARP, bool ALIGNED, bool DOTS>
-__global__ void __launch_bounds__(WARP ? kRmsThreads : kRmsMostThreads) rms_bwd_kernel(const __grid_constant__ RmsArgs a) {
+__global__ void __launch_bounds__(WARP ? kRmsThreads : kRmsMostThreads, WARP && NO > 2 ? 2 : 1) rms_bwd_kernel(const __grid_constant__ RmsArgs a) {
     __shared__ __align__(16) float red[2][32];
     extern __shared__ float lines[];                     // WARP: [teams][cols] sums
     pdl_launch_dependents();
-    const int tpr = WARP ? 1 << a.log_tpr : (int)blockDim.x;
+    constexpr bool kAhead = NO <= 2;
+    const int tpr = !WARP ? (int)blockDim.x : NO > 1 ? 32 : 1 << a.log_tpr;
     const int g = WARP ? (int)threadIdx.x & (tpr - 1) : (int)threadIdx.x;
-    const int teams_pb = WARP ? kRmsThreads >> a.log_tpr : 1, team = WARP ? (int)threadIdx.x >> a.log_tpr : 0;
-    const int first_of_warp = WARP ? ((int)threadIdx.x & ~31) >> a.log_tpr : 0;
+    const int log_tpr = NO > 1 ? 5 : a.log_tpr;
+    const int teams_pb = WARP ? kRmsThreads >> log_tpr : 1, team = WARP ? (int)threadIdx.x >> log_tpr : 0;
+    const int first_of_warp = WARP ? ((int)threadIdx.x & ~31) >> log_tpr : 0;
     const long long step = (long long)gridDim.x * teams_pb;
     long long row = (long long)blockIdx.x * teams_pb + team;
     const int phase = ALIGNED ? 0 : (int)((row * a.cols) & 7);
@@ -25,116 +29,148 @@ __global__ void __launch_bounds__(WARP ? kRmsThreads : kRmsMostThreads) rms_bwd_
     pdl_wait();
     if (!WARP) __syncthreads();
 
-    // octet k of this thread: columns c0(k) .. c0(k) + 7; a tile's last octet belongs to the next tile unless it is the row's last
-    auto octet = [&](int k) { return tile0 + k * tpr + g; };
-    auto c0 = [&](int k) { return 8 * octet(k) - phase; };
-    auto mine = [&](int k) { return c0(k) < a.cols && (!DOTS || k * tpr + g < (a.col_tile >> 3)); };
-    float gam[NO][8], sum[NO][8];
+    // octet k of this thread: columns c0(k) .. c0(k) + 7; only its last may lie past the row
+    auto c0 = [&](int k) { return 8 * (tile0 + k * tpr + g) - phase; };
+    const bool last = c0(NO - 1) < a.cols;
+    auto there = [&](int k) { return k + 1 < NO || last; };
+    Eight gam[NO], sum[NO];
 #pragma unroll
-    for (int k = 0; k < NO; ++k)
+    for (int k = 0; k < NO; ++k) {
+        rms_gamma8(a, c0(k), gam[k]);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int c = c0(k) + i;
-            gam[k][i] = c >= 0 && c < a.cols ? rms_gamma(a, c) : 0.f;
-            sum[k][i] = 0.f;
-        }
-    uint64_t key = 0, offset = 0;
-    if (a.drop.threshold) { key = a.drop.seed[0]; offset = a.drop.seed[1]; }
+        for (int i = 0; i < 4; ++i) sum[k][i] = 0;
+    }
+    uint64_t key, offset;
+    load_seed(a.drop, key, offset);
 
+    const TX* const gy = static_cast<const TX*>(a.gy);
+    const TR* const h = static_cast<const TR*>(a.h);
+    const TR* const gh = a.gres || a.y ? static_cast<const TR*>(a.gh) : nullptr;
     Octet<TX> ngy[NO];
     Octet<TR> nh[NO], ngh[NO];
     float nrstd = 0.f, ndot = 0.f;
-    const TR* const gh = a.gres ? static_cast<const TR*>(a.gh) : a.y ? static_cast<const TR*>(a.gh) : nullptr;
-    auto fetch = [&](long long r) {
-        const long long base = r * a.cols >> 3;
-        if (r < a.rows) {
-            nrstd = a.rstd_in[r];
-            if (DOTS) ndot = a.dots[r];
+#pragma unroll
+    for (int k = 0; k < NO; ++k) {
+        ngy[k].clear();
+        nh[k].clear();
+        ngh[k].clear();
+    }
+    // e: the place of this thread's first octet in a row, in elements; e + 8 k tpr: of octet k
+    const long long e_step = step * a.cols;
+    long long e = ((row * a.cols >> 3) + tile0 + g) * 8;
+    auto fetch = [&](long long r, long long at) {
+        if (r >= a.rows) {                               // a row of zeros: it leaves the sums as they are
+            nrstd = 0.f;
+#pragma unroll
+            for (int k = 0; k < NO; ++k) {
+                ngy[k].clear();
+                nh[k].clear();
+            }
+            return;
         }
+        nrstd = a.rstd_in[r];
+        if (DOTS) ndot = a.dots[r];
 #pragma unroll
         for (int k = 0; k < NO; ++k) {
-            ngy[k].clear();
-            nh[k].clear();
-            ngh[k].clear();
-            if (r < a.rows && mine(k)) {
-                const long long f = base + octet(k);
+            if (there(k)) {
+                const long long p = at + 8 * k * tpr;
                 if (ALIGNED) {
-                    ngy[k].load(static_cast<const TX*>(a.gy) + f * 8);
-                    nh[k].load(static_cast<const TR*>(a.h) + f * 8);
-                    if (gh) ngh[k].load(gh + f * 8);
+                    ngy[k].load(gy + p);
+                    nh[k].load(h + p);
+                    if (gh) ngh[k].load(gh + p);
                 } else {
-                    load_octet(ngy[k], static_cast<const TX*>(a.gy), f, a.total);
-                    load_octet(nh[k], static_cast<const TR*>(a.h), f, a.total);
-                    if (gh) load_octet(ngh[k], gh, f, a.total);
+                    load_octet(ngy[k], gy, p >> 3, a.total);
+                    load_octet(nh[k], h, p >> 3, a.total);
+                    if (gh) load_octet(ngh[k], gh, p >> 3, a.total);
                 }
             }
         }
     };
-    fetch(row);
+    if (kAhead) fetch(row, e);
     int turn = 0;
-    for (long long warp_row = (long long)blockIdx.x * teams_pb + first_of_warp; warp_row < a.rows; warp_row += step, row += step, turn ^= 1) {
+    for (long long warp_row = (long long)blockIdx.x * teams_pb + first_of_warp; warp_row < a.rows; warp_row += step, row += step, e += e_step, turn ^= 1) {
+        if (!kAhead) fetch(row, e);
         const bool live = row < a.rows;
-        const long long base = row * a.cols >> 3;
-        const float rstd = live ? nrstd : 0.f;
-        float q[NO][8], xh[NO][8];
-        Octet<TR> add[NO];
-        float s = 0.f;
-        const float dot = ndot;
+        const float rstd = nrstd, dot = ndot;
+        const uint64_t rstd2 = pair_of(rstd, rstd);
+        // g_y and h rstd of octet k
+        auto take = [&](int k, Eight& q, Eight& xh) {
+            ngy[k].get(q);
+            nh[k].get(xh);
+            if (!ALIGNED) {
+                float f[8], x[8];
+                from_eight(q, f);
+                from_eight(xh, x);
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (c0(k) + i < 0 || c0(k) + i >= a.cols) f[i] = x[i] = 0.f;
+                to_eight(f, q);
+                to_eight(x, xh);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) xh[i] = mul_pair(xh[i], rstd2);
+        };
+        Eight q[kAhead ? NO : 1], xh[kAhead ? NO : 1];
+        Octet<TR> add[kAhead ? NO : 1];                  // g_h, which makes room for the next row's
+        uint64_t dots = 0;
 #pragma unroll
         for (int k = 0; k < NO; ++k) {
-            ngy[k].get(q[k]);
-            nh[k].get(xh[k]);
-            add[k] = ngh[k];
-        }
-        fetch(row + step);
+            const int s = kAhead ? k : 0;
+            take(k, q[s], xh[s]);
+            if (kAhead) add[s] = ngh[k];
 #pragma unroll
-        for (int k = 0; k < NO; ++k) {
-            const int c = c0(k);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (!ALIGNED && (c + i < 0 || c + i >= a.cols)) q[k][i] = xh[k][i] = 0.f;
-                xh[k][i] *= rstd;
-                sum[k][i] = fmaf(q[k][i], xh[k][i], sum[k][i]);
-                q[k][i] *= gam[k][i];
-                s = fmaf(q[k][i], xh[k][i], s);
+            for (int i = 0; i < 4; ++i) {
+                sum[k][i] = fma_pair(q[s][i], xh[s][i], sum[k][i]);
+                q[s][i] = mul_pair(q[s][i], gam[k][i]);
+                dots = fma_pair(q[s][i], xh[s][i], dots);
             }
         }
+        if (kAhead) fetch(row + step, e + e_step);
         if (!a.gres && !a.y) continue;
-        if (DOTS) s = dot;
-        else s = rms_sum<WARP>(s, a.log_tpr, red[turn]) * a.inv_c;
+        const float mean = DOTS ? dot : rms_sum<WARP>(sum_of(dots), log_tpr, red[turn]) * a.inv_c;
+        const uint64_t minus = pair_of(-mean, -mean);
 #pragma unroll
         for (int k = 0; k < NO; ++k) {
-            const int c = c0(k);
-            if (!live || !mine(k)) continue;
-            const long long e = (base + octet(k)) * 8;
-            float v[8];
-            add[k].get(v);
+            const int c = c0(k), s = kAhead ? k : 0;
+            if (!live || !there(k)) continue;
+            Eight v;
+            if (kAhead) add[s].get(v);
+            else {
+                ngh[k].get(v);
+                take(k, q[0], xh[0]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = fmaf(rstd, q[k][i] - xh[k][i] * s, v[i]);
+                for (int i = 0; i < 4; ++i) q[0][i] = mul_pair(q[0][i], gam[k][i]);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = fma_pair(rstd2, fma_pair(xh[s][i], minus, q[s][i]), v[i]);
             const bool whole = ALIGNED || (c >= 0 && c + 8 <= a.cols);
             if (a.gres) {
-                TR* const p = static_cast<TR*>(a.gres) + e;
+                TR* const p = static_cast<TR*>(a.gres) + e + 8 * k * tpr;
                 if (whole) {
                     Octet<TR> o;
                     o.set(v);
                     o.store(p);
                 } else {
+                    float f[8];
+                    from_eight(v, f);
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
-                        if (c + i >= 0 && c + i < a.cols) p[i] = from_f32<TR>(v[i]);
+                        if (c + i >= 0 && c + i < a.cols) p[i] = from_f32<TR>(f[i]);
                 }
             }
             if (a.y) {
-                if (a.drop.threshold) drop_octet(v, (uint64_t)(base + octet(k)), key, offset, a.drop.threshold, a.drop.scale);
-                TX* const p = static_cast<TX*>(a.y) + e;
+                if (a.drop.threshold) drop_octet<false>(v, v, (uint64_t)(e >> 3) + (uint64_t)(k * tpr), key, offset, a.drop);
+                TX* const p = static_cast<TX*>(a.y) + e + 8 * k * tpr;
                 if (whole) {
                     Octet<TX> o;
                     o.set(v);
                     o.store(p);
                 } else {
+                    float f[8];
+                    from_eight(v, f);
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
-                        if (c + i >= 0 && c + i < a.cols) p[i] = from_f32<TX>(v[i]);
+                        if (c + i >= 0 && c + i < a.cols) p[i] = from_f32<TX>(f[i]);
                 }
             }
         }
@@ -144,12 +180,15 @@ __global__ void __launch_bounds__(WARP ? kRmsThreads : kRmsMostThreads) rms_bwd_
     if constexpr (WARP) {
         float* const line = lines + (size_t)team * a.cols;
 #pragma unroll
-        for (int k = 0; k < NO; ++k)
+        for (int k = 0; k < NO; ++k) {
+            float f[8];
+            from_eight(sum[k], f);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int c = c0(k) + i;
-                if (c >= 0 && c < a.cols) line[c] = sum[k][i];
+                if (c >= 0 && c < a.cols) line[c] = f[i];
             }
+        }
         __syncthreads();
         for (int c = threadIdx.x; c < a.cols; c += kRmsThreads) {
             float t = lines[c];
@@ -159,11 +198,12 @@ __global__ void __launch_bounds__(WARP ? kRmsThreads : kRmsMostThreads) rms_bwd_
     } else {
 #pragma unroll
         for (int k = 0; k < NO; ++k) {
-            if (!mine(k)) continue;
+            float f[8];
+            from_eight(sum[k], f);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int c = c0(k) + i;
-                if (c >= 0 && c < a.cols) part[c] = sum[k][i];
+                if (c >= 0 && c < a.cols) part[c] = f[i];
             }
         }
     }
@@ -228,8 +268,10 @@ constexpr int kTileCols = 8 * kRmsMostThreads;
 BwdPlan plan(const gf_rms_desc* d) {
     BwdPlan p = {};
     const int n = rms_octets(d->cols);
+    // octets that a thread's registers hold of a row: of 32-bit rows, and of rows that start anywhere, fewer
+    const int each = d->cols % 8 != 0 || d->residual_dtype == GF_F32 ? 2 : 3;
     p.tiles = n > 2 * kRmsMostThreads;
-    p.shape = rms_shape(n, 2, 1);
+    p.shape = rms_shape(n, each, 1);
     if (p.tiles) p.shape = RmsShape{false, 0, kRmsMostThreads, 1};
     const int teams = p.shape.warp ? kRmsThreads >> p.shape.log_tpr : 1;
     const long long tiles = p.tiles ? cdiv64((long long)n * 8, kTileCols) : 1;
@@ -278,7 +320,11 @@ template <typename TX, typename TR, bool ALIGNED> gf_status dispatch(RmsArgs a, 
     }
     if (p.shape.warp) {
         if (p.shape.per_thread == 1) return launch<TX, TR, 1, true, ALIGNED, false>(a, p, g_gamma, s);
-        return launch<TX, TR, 2, true, ALIGNED, false>(a, p, g_gamma, s);
+        if (p.shape.per_thread == 2) return launch<TX, TR, 2, true, ALIGNED, false>(a, p, g_gamma, s);
+        if constexpr (ALIGNED) {
+            if constexpr (sizeof(TR) == 2) return launch<TX, TR, 3, true, ALIGNED, false>(a, p, g_gamma, s);
+        }
+        return GF_ERR_UNSUPPORTED;                        // (no plan asks for it)
     }
     if (p.shape.per_thread == 1) return launch<TX, TR, 1, false, ALIGNED, false>(a, p, g_gamma, s);
     return launch<TX, TR, 2, false, ALIGNED, false>(a, p, g_gamma, s);

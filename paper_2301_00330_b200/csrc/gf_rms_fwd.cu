@@ -28,10 +28,11 @@ __global__ void __launch_bounds__(WARP ? kRmsThreads : kRmsMostThreads) rms_fwd_
     __shared__ __align__(16) float red[2][32];
     extern __shared__ float rows_smem[];
     pdl_launch_dependents();
-    const int tpr = WARP ? 1 << a.log_tpr : (int)blockDim.x;
+    const int tpr = !WARP ? (int)blockDim.x : NO > 1 ? 32 : 1 << a.log_tpr;
     const int g = WARP ? (int)threadIdx.x & (tpr - 1) : (int)threadIdx.x;
-    const int teams_pb = WARP ? kRmsThreads >> a.log_tpr : 1, team = WARP ? (int)threadIdx.x >> a.log_tpr : 0;
-    const int first_of_warp = WARP ? ((int)threadIdx.x & ~31) >> a.log_tpr : 0;
+    const int log_tpr = NO > 1 ? 5 : a.log_tpr;
+    const int teams_pb = WARP ? kRmsThreads >> log_tpr : 1, team = WARP ? (int)threadIdx.x >> log_tpr : 0;
+    const int first_of_warp = WARP ? ((int)threadIdx.x & ~31) >> log_tpr : 0;
     const long long step = (long long)gridDim.x * teams_pb;
     long long row = (long long)blockIdx.x * teams_pb + team;
     const int phase = ALIGNED ? 0 : (int)((row * a.cols) & 7);
@@ -42,114 +43,126 @@ __global__ void __launch_bounds__(WARP ? kRmsThreads : kRmsMostThreads) rms_fwd_
 
     const TX* const x = static_cast<const TX*>(a.x);
     const TR* const res = static_cast<const TR*>(a.residual);
-    // octet k of this thread: columns c0[k] .. c0[k] + 7, of which lo .. hi - 1 are the row's
+    // octet k of this thread: columns c0(k) .. c0(k) + 7, of an ALIGNED row all of them or none
     auto c0 = [&](int k) { return 8 * (k * tpr + g) - phase; };
-    float gam[NO][8];
+    const bool last = c0(NO - 1) < a.cols;
+    auto there = [&](int k) { return k + 1 < NO || last; };
+    Eight gam[NO];
 #pragma unroll
-    for (int k = 0; k < NO; ++k)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int c = c0(k) + i;
-            gam[k][i] = c >= 0 && c < a.cols ? rms_gamma(a, c) : 0.f;
-        }
-    uint64_t key = 0, offset = 0;
-    if (a.drop.threshold) { key = a.drop.seed[0]; offset = a.drop.seed[1]; }
+    for (int k = 0; k < NO; ++k) rms_gamma8(a, c0(k), gam[k]);
+    uint64_t key, offset;
+    load_seed(a.drop, key, offset);
 
     Octet<TX> nx[NO];
     Octet<TR> nr[NO];
-    auto fetch = [&](long long r) {
-        const long long base = r * a.cols >> 3;
+#pragma unroll
+    for (int k = 0; k < NO; ++k) {
+        nx[k].clear();
+        nr[k].clear();
+    }
+    // e: the place of this thread's first octet in a row, in elements; e + 8 k tpr: of octet k
+    const long long e_step = step * a.cols;
+    long long e = ((row * a.cols >> 3) + g) * 8;
+    auto fetch = [&](long long at) {
 #pragma unroll
         for (int k = 0; k < NO; ++k) {
-            nx[k].clear();
-            nr[k].clear();
-            if (r < a.rows && c0(k) < a.cols) {
-                const long long f = base + k * tpr + g;
+            if (there(k)) {
                 if (ALIGNED) {
-                    nx[k].load(x + f * 8);
-                    if (res) nr[k].load(res + f * 8);
+                    nx[k].load(x + at + 8 * k * tpr);
+                    if (res) nr[k].load(res + at + 8 * k * tpr);
                 } else {
-                    load_octet(nx[k], x, f, a.total);
-                    if (res) load_octet(nr[k], res, f, a.total);
+                    load_octet(nx[k], x, (at >> 3) + k * tpr, a.total);
+                    if (res) load_octet(nr[k], res, (at >> 3) + k * tpr, a.total);
                 }
             }
         }
     };
-    fetch(row);
+    if (row < a.rows) fetch(e);
     int turn = 0;
     // (the lanes of a warp go round together, as long as any of its rows is left)
-    for (long long warp_row = (long long)blockIdx.x * teams_pb + first_of_warp; warp_row < a.rows; warp_row += step, row += step, turn ^= 1) {
+    for (long long warp_row = (long long)blockIdx.x * teams_pb + first_of_warp; warp_row < a.rows; warp_row += step, row += step, e += e_step, turn ^= 1) {
         const bool live = row < a.rows;
-        const long long base = row * a.cols >> 3;
-        float v[NO][8];
-        float s = 0.f;
+        Eight v[NO], w[NO];
 #pragma unroll
         for (int k = 0; k < NO; ++k) {
             nx[k].get(v[k]);
-            if (a.drop.threshold && live && c0(k) < a.cols)
-                drop_octet(v[k], (uint64_t)(base + k * tpr + g), key, offset, a.drop.threshold, a.drop.scale);
-            if (res) {
-                float w[8];
-                nr[k].get(w);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[k][i] += w[i];
-            }
+            nr[k].get(w[k]);                             // (zeros without a residual)
         }
-        fetch(row + step);
+        if (row + step < a.rows) fetch(e + e_step);
+        uint64_t squares = 0;
 #pragma unroll
         for (int k = 0; k < NO; ++k) {
             const int c = c0(k);
-            if (a.h && live && c < a.cols) {
-                TR* const h = static_cast<TR*>(a.h) + (base + k * tpr + g) * 8;
+            if (a.drop.threshold) drop_octet<true>(v[k], w[k], (uint64_t)(e >> 3) + (uint64_t)(k * tpr), key, offset, a.drop);
+            else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[k][i] = add_pair(v[k][i], w[k][i]);
+            }
+            if (a.h) {
                 Octet<TR> o;
                 o.set(v[k]);
                 o.get(v[k]);                             // the norm is that of h as it is kept
-                if (ALIGNED || (c >= 0 && c + 8 <= a.cols)) o.store(h);
-                else {
+                if (live && there(k)) {
+                    TR* const h = static_cast<TR*>(a.h) + e + 8 * k * tpr;
+                    if (ALIGNED || (c >= 0 && c + 8 <= a.cols)) o.store(h);
+                    else {
+                        float f[8];
+                        from_eight(v[k], f);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (c + i >= 0 && c + i < a.cols) h[i] = from_f32<TR>(v[k][i]);
+                        for (int i = 0; i < 8; ++i)
+                            if (c + i >= 0 && c + i < a.cols) h[i] = from_f32<TR>(f[i]);
+                    }
                 }
             }
-            if (!ALIGNED) {
+            if (!ALIGNED || (OUT8 && k + 1 == NO)) {     // what is not the row's counts as zero
+                float f[8];
+                from_eight(v[k], f);
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    if (c + i < 0 || c + i >= a.cols) v[k][i] = 0.f;
+                    if (c + i < 0 || c + i >= a.cols) f[i] = 0.f;
+                to_eight(f, v[k]);
             }
+            if (ALIGNED && k + 1 == NO && !last) continue;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s = fmaf(v[k][i], v[k][i], s);
+            for (int i = 0; i < 4; ++i) squares = fma_pair(v[k][i], v[k][i], squares);
         }
-        s = rms_sum<WARP>(s, a.log_tpr, red[turn]);
+        const float s = rms_sum<WARP>(sum_of(squares), log_tpr, red[turn]);
         const float rstd = __frcp_rn(__fsqrt_rn(fmaf(s, a.inv_c, a.eps)));
         if (a.rstd && live && g == 0) a.rstd[row] = rstd;
+        const uint64_t rstd2 = pair_of(rstd, rstd);
 #pragma unroll
         for (int k = 0; k < NO; ++k)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[k][i] = v[k][i] * rstd * gam[k][i];
+            for (int i = 0; i < 4; ++i) v[k][i] = mul_pair(mul_pair(v[k][i], rstd2), gam[k][i]);
         if constexpr (!OUT8) {
 #pragma unroll
             for (int k = 0; k < NO; ++k) {
                 const int c = c0(k);
-                if (!live || c >= a.cols) continue;
-                TX* const y = static_cast<TX*>(a.y) + (base + k * tpr + g) * 8;
+                if (!live || !there(k)) continue;
+                TX* const y = static_cast<TX*>(a.y) + e + 8 * k * tpr;
                 if (ALIGNED || (c >= 0 && c + 8 <= a.cols)) {
                     Octet<TX> o;
                     o.set(v[k]);
                     o.store(y);
                 } else {
+                    float f[8];
+                    from_eight(v[k], f);
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
-                        if (c + i >= 0 && c + i < a.cols) y[i] = from_f32<TX>(v[k][i]);
+                        if (c + i >= 0 && c + i < a.cols) y[i] = from_f32<TX>(f[i]);
                 }
             }
         } else {
+            float f[NO][8];
+#pragma unroll
+            for (int k = 0; k < NO; ++k) from_eight(v[k], f[k]);
             if constexpr (!ALIGNED) {                    // from the tensor's octets to the row's own
 #pragma unroll
                 for (int k = 0; k < NO; ++k)
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const int c = c0(k) + i;
-                        if (c >= 0 && c < a.cols) line[skewed(c)] = v[k][i];
+                        if (c >= 0 && c < a.cols) line[skewed(c)] = f[k][i];
                     }
                 if (WARP) __syncwarp();
                 else __syncthreads();
@@ -158,19 +171,19 @@ __global__ void __launch_bounds__(WARP ? kRmsThreads : kRmsMostThreads) rms_fwd_
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const int c = 8 * (k * tpr + g) + i;
-                        v[k][i] = c < a.cols ? line[skewed(c)] : 0.f;
+                        f[k][i] = c < a.cols ? line[skewed(c)] : 0.f;
                     }
                 if (WARP) __syncwarp();
             }
 #pragma unroll
             for (int k = 0; k < NO; ++k) {
                 const int c = 8 * (k * tpr + g);
-                uint32_t m = magnitude(v[k]);
+                uint32_t m = magnitude(f[k]);
 #pragma unroll
                 for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
                 const float scale = scale_of(m);
                 if (live && c < a.pitch) {
-                    *reinterpret_cast<uint2*>(a.codes + row * a.pitch + c) = codes8(v[k], scale, __frcp_rn(scale), a.cols - c);
+                    *reinterpret_cast<uint2*>(a.codes + row * a.pitch + c) = codes8(f[k], scale, __frcp_rn(scale), a.cols - c);
                     if ((g & 15) == 0 && c < a.cols) a.scales[(long long)(c >> 7) * a.scale_pitch + row] = scale;
                 }
             }
@@ -187,8 +200,8 @@ template <typename TX, typename TR, bool OUT8> __global__ void __launch_bounds__
     const TX* const x = static_cast<const TX*>(a.x);
     const TR* const res = static_cast<const TR*>(a.residual);
     TR* const h = static_cast<TR*>(a.h);
-    uint64_t key = 0, offset = 0;
-    if (a.drop.threshold) { key = a.drop.seed[0]; offset = a.drop.seed[1]; }
+    uint64_t key, offset;
+    load_seed(a.drop, key, offset);
     int turn = 0;
     for (long long row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
         const long long e0 = row * a.cols, e1 = e0 + a.cols;
@@ -196,14 +209,14 @@ template <typename TX, typename TR, bool OUT8> __global__ void __launch_bounds__
         for (long long f = (e0 >> 3) + threadIdx.x; f * 8 < e1; f += kLongThreads) {
             Octet<TX> ox;
             load_octet(ox, x, f, a.total);
-            float v[8];
+            Octet<TR> r;
+            r.clear();
+            if (res) load_octet(r, res, f, a.total);
+            float v[8], w[8];
             ox.get(v);
-            if (a.drop.threshold) drop_octet(v, (uint64_t)f, key, offset, a.drop.threshold, a.drop.scale);
-            if (res) {
-                Octet<TR> r;
-                load_octet(r, res, f, a.total);
-                float w[8];
-                r.get(w);
+            r.get(w);
+            if (a.drop.threshold) drop_octet<true>(v, w, (uint64_t)f, key, offset, a.drop);
+            else {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[i] += w[i];
             }
