@@ -38,6 +38,7 @@ __global__ void __launch_bounds__(kQuantThreads) quantize_rows_kernel(const T* x
 #pragma unroll
         for (int k = 0; k < kQuantGroups; ++k) {
             const int c = c0 + 128 * k;
+            if (c - part * 8 >= pitch) break;            // (the same for the block)
             float v[8];
             o[k].get(v);
             if (!ALIGNED) {
@@ -811,7 +812,7 @@ gf_status gf_fp8_quantize_rows(const gf_fp8_desc* desc, const void* x, void* cod
     const gf_status st = check(desc, x, codes, scales);
     if (st != GF_OK || desc->rows == 0) return st;
     const int chunks = (desc->cols + 128 * kQuantGroups - 1) / (128 * kQuantGroups);
-    const long long blocks = cdiv64(desc->rows, kQuantRows) * chunks, most = (long long)sm_count() * 8;
+    const long long blocks = cdiv64(desc->rows, kQuantRows) * chunks, most = 1 << 30;
     const dim3 grid((unsigned)(blocks < most ? blocks : most));
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     ProfScope prof(K_FP8_QUANTIZE, s);

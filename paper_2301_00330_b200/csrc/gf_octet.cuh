@@ -220,9 +220,10 @@ constexpr float kFp8Top = 448.f, kFp8Tiny = 1.17549435e-38f;
 
 // Largest magnitude as bits: ordered like unsigned numbers, NaN above all.
 __device__ __forceinline__ uint32_t magnitude(const float (&v)[8]) {
-    float m = fabsf(v[0]);
+    float m;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(v[0]), "f"(v[1]), "f"(v[2]));
 #pragma unroll
-    for (int i = 1; i < 8; ++i) asm("max.NaN.f32 %0, %0, %1;" : "+f"(m) : "f"(fabsf(v[i])));
+    for (int i = 3; i < 8; i += 2) asm("max.NaN.abs.f32 %0, %0, %1, %2;" : "+f"(m) : "f"(v[i]), "f"(v[i + 1 < 8 ? i + 1 : i]));
     return __float_as_uint(m) & 0x7fffffffu;
 }
 __device__ __forceinline__ float scale_of(uint32_t magnitude_bits) {
@@ -234,19 +235,20 @@ __device__ __forceinline__ uint32_t codes2(float a, float b) {
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(b), "f"(a));
     return r;
 }
-// Codes of eight values, of which `valid` are the row's (the others get 0), under `scale`, inv its rounded reciprocal.  The quotient is inv v with one correction by the remainder
-// (Markstein 1990: the correctly rounded quotient), so that codes are those of a division.  A scale that is not
-// finite leaves NaN.
+// Codes of eight values, of which `valid` are the row's (the others get 0), under `scale`, inv its rounded reciprocal.  The quotient
+// is the product with inv and one correction by the remainder (Markstein 1990: the correctly rounded quotient), so that codes
+// are those of a division.  It is formed of -v, and the codes' signs turned at the end: in that order of signs a remainder of
+// zero leaves the sign of a zero.  A scale that is not finite leaves NaN.
 __device__ __forceinline__ uint2 codes8(const float (&v)[8], float scale, float inv, int valid) {
     uint32_t c[4];
-    const uint64_t inv2 = pair_of(inv, inv), minus = pair_of(-scale, -scale);
+    const uint64_t minus_inv = pair_of(-inv, -inv), scale2 = pair_of(scale, scale);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const uint64_t x = pair_of(v[2 * i], v[2 * i + 1]), y = mul_pair(x, inv2);
-        const float2 q = unpair(fma_pair(fma_pair(y, minus, x), inv2, y));
-        c[i] = codes2(copysignf(q.x, v[2 * i]), copysignf(q.y, v[2 * i + 1]));      // (the correction makes +0 of -0)
+        const uint64_t x = pair_of(v[2 * i], v[2 * i + 1]), y = mul_pair(x, minus_inv);
+        const float2 q = unpair(fma_pair(fma_pair(y, scale2, x), minus_inv, y));
+        c[i] = codes2(q.x, q.y);
     }
-    uint2 r = make_uint2(c[0] | (c[1] << 16), c[2] | (c[3] << 16));
+    uint2 r = make_uint2((c[0] | (c[1] << 16)) ^ 0x80808080u, (c[2] | (c[3] << 16)) ^ 0x80808080u);
     if (valid < 8) {
         r.x = valid >= 4 ? r.x : valid <= 0 ? 0u : r.x & (0xffffffffu >> (32 - 8 * valid));
         r.y = valid <= 4 ? 0u : r.y & (0xffffffffu >> (64 - 8 * valid));

@@ -113,11 +113,18 @@ __global__ void __launch_bounds__(WARP ? kRmsThreads : kRmsMostThreads, WARP && 
         Eight q[kAhead ? NO : 1], xh[kAhead ? NO : 1];
         Octet<TR> add[kAhead ? NO : 1];                  // g_h, which makes room for the next row's
         uint64_t dots = 0;
+        if (kAhead) {
+#pragma unroll
+            for (int k = 0; k < NO; ++k) {
+                take(k, q[kAhead ? k : 0], xh[kAhead ? k : 0]);
+                add[kAhead ? k : 0] = ngh[k];
+            }
+            fetch(row + step, e + e_step);
+        }
 #pragma unroll
         for (int k = 0; k < NO; ++k) {
             const int s = kAhead ? k : 0;
-            take(k, q[s], xh[s]);
-            if (kAhead) add[s] = ngh[k];
+            if (!kAhead) take(k, q[0], xh[0]);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 sum[k][i] = fma_pair(q[s][i], xh[s][i], sum[k][i]);
@@ -125,7 +132,6 @@ __global__ void __launch_bounds__(WARP ? kRmsThreads : kRmsMostThreads, WARP && 
                 dots = fma_pair(q[s][i], xh[s][i], dots);
             }
         }
-        if (kAhead) fetch(row + step, e + e_step);
         if (!a.gres && !a.y) continue;
         const float mean = DOTS ? dot : rms_sum<WARP>(sum_of(dots), log_tpr, red[turn]) * a.inv_c;
         const uint64_t minus = pair_of(-mean, -mean);
