@@ -174,25 +174,27 @@ __device__ __forceinline__ float bias_at(const ProductArgs& p, int j) {
 // want more than its 512 columns, or two clusters could each hold what the other waits for.
 constexpr int kFewThreads = 192;
 __host__ __device__ constexpr int few_stages(int T) { return T <= 32 ? 4 : 3; }
+__host__ __device__ constexpr int few_buffers(int T) { return T <= 32 ? 4 : 2; }      // accumulators
+constexpr int kFewScales = 16;                                                        // chunks whose scales are held at once
 constexpr size_t few_smem(int T) { return (size_t)few_stages(T) * (16384 + T * 128) + 1024; }
-static_assert(227 * 1024 / few_smem(16) * 32 <= 512 && 227 * 1024 / few_smem(32) * 64 <= 512 && 227 * 1024 / few_smem(64) * 128 <= 512 &&
+static_assert(227 * 1024 / few_smem(16) * 64 <= 384 && 227 * 1024 / few_smem(32) * 128 <= 384 && 227 * 1024 / few_smem(64) * 128 <= 384 &&
                   227 * 1024 / few_smem(64) <= 3,
               "tensor memory of the blocks of an SM");
 
 template <int T, typename TO> __global__ void __launch_bounds__(kFewThreads) fp8_few_kernel(const __grid_constant__ ProductArgs p) {
     extern __shared__ unsigned char dyn_raw[];
     unsigned char* const dyn = align1024(dyn_raw);
-    constexpr int kStages = few_stages(T), kStageBytes = 16384 + T * 128, kCols = 2 * T;
-    __shared__ uint64_t full[kStages], empty[kStages], done[2], drained[2];
+    constexpr int kStages = few_stages(T), kStageBytes = 16384 + T * 128, kBuffers = few_buffers(T), kCols = kBuffers * T;
+    __shared__ uint64_t full[kStages], empty[kStages], done[kBuffers], drained[kBuffers];
     __shared__ uint32_t tmem_base;
-    __shared__ __align__(16) float scale[2][T];
+    __shared__ __align__(16) float scale[kFewScales][T];
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     const int rank = (int)(blockIdx.x % (unsigned)p.split), tile = (int)(blockIdx.x / (unsigned)p.split);
     const int m0 = tile % p.tiles_m * T, j0 = tile / p.tiles_m * 128;
     const int q0 = rank * p.per, n = min(p.per, p.chunks - q0);
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
-        for (int s = 0; s < 2; ++s) { mbar_init(&done[s], 1); mbar_init(&drained[s], 4); }
+        for (int s = 0; s < kBuffers; ++s) { mbar_init(&done[s], 1); mbar_init(&drained[s], 4); }
         mbar_fence_init();
     }
     pdl_wait();
@@ -223,8 +225,8 @@ template <int T, typename TO> __global__ void __launch_bounds__(kFewThreads) fp8
         const uint32_t idesc = fp8_idesc(128, T, p.mn_major ? 1u : 0u, 0u);
         const uint32_t a_step = p.mn_major ? 4096u : 32u;
         for (int q = 0; q < n; ++q) {
-            const int s = q % kStages, buf = q & 1;
-            if (q >= 2) ok = mbar_wait_warp(&drained[buf], ((uint32_t)(q >> 1) - 1u) & 1u);
+            const int s = q % kStages, buf = q % kBuffers;
+            if (q >= kBuffers) ok = mbar_wait_warp(&drained[buf], ((uint32_t)(q / kBuffers) - 1u) & 1u);
             if (ok) ok = mbar_wait_warp(&full[s], (uint32_t)(q / kStages) & 1u);
             if (!ok) break;
             tc_fence_after_sync();
@@ -241,20 +243,24 @@ template <int T, typename TO> __global__ void __launch_bounds__(kFewThreads) fp8
     } else {
         const int t = (int)threadIdx.x - 64, quarter = warp & 3;
         const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
-        const float* const sa = p.sa + m0 + t;
         const float* const sw = p.sw + (long long)(j0 >> 7) * p.sw_j;
-        const bool has = t < T && m0 + t < p.M;
-        auto scale_at = [&](int q) { return has ? sa[(long long)(q0 + q) * p.sa_pitch] * sw[(long long)(q0 + q) * p.sw_q] : 0.f; };
         uint64_t acc[T / 2];
 #pragma unroll
         for (int i = 0; i < T / 2; ++i) acc[i] = 0;
-        if (t < T) scale[0][t] = scale_at(0);
-        asm volatile("bar.sync 1, 128;" ::: "memory");
         for (int q = 0; q < n; ++q) {
-            const int buf = q & 1;
-            const float next = q + 1 < n ? scale_at(q + 1) : 0.f;
-            ok = mbar_wait_warp(&done[buf], (uint32_t)(q >> 1) & 1u);
-            if (bar_any(1, 128, !ok)) { ok = false; break; }
+            const int buf = q % kBuffers, held = q % kFewScales;
+            if (held == 0) {                             // the scales of the next chunks: by all four warps, for all
+                if (q > 0) asm volatile("bar.sync 1, 128;" ::: "memory");
+                for (int i = t; i < min(kFewScales, n - q) * T; i += 128) {
+                    const int m = m0 + i % T;
+                    const long long at = q0 + q + i / T;
+                    scale[i / T][i % T] = m < p.M ? p.sa[at * p.sa_pitch + m] * sw[at * p.sw_q] : 0.f;
+                }
+                asm volatile("bar.sync 1, 128;" ::: "memory");
+            }
+            // (after a wait that ran out a warp has part in the barriers above still, and in nothing else)
+            if (ok) ok = mbar_wait_warp(&done[buf], (uint32_t)(q / kBuffers) & 1u);
+            if (!ok) continue;
             tc_fence_after_sync();
 #pragma unroll
             for (int c = 0; c < T; c += 16) {
@@ -263,7 +269,7 @@ template <int T, typename TO> __global__ void __launch_bounds__(kFewThreads) fp8
                 tmem_ld_wait_for(raw);
 #pragma unroll
                 for (int i = 0; i < 16; i += 4) {
-                    const ulonglong2 s = *reinterpret_cast<const ulonglong2*>(&scale[buf][c + i]);
+                    const ulonglong2 s = *reinterpret_cast<const ulonglong2*>(&scale[held][c + i]);
                     uint64_t* const a = acc + (c + i) / 2;
                     a[0] = fma_pair(pair_of(__uint_as_float(raw[i]), __uint_as_float(raw[i + 1])), s.x, a[0]);
                     a[1] = fma_pair(pair_of(__uint_as_float(raw[i + 2]), __uint_as_float(raw[i + 3])), s.y, a[1]);
@@ -272,8 +278,6 @@ template <int T, typename TO> __global__ void __launch_bounds__(kFewThreads) fp8
             tc_fence_before_sync();
             __syncwarp();
             if (lane == 0) mbar_arrive(&drained[buf]);
-            if (t < T) scale[buf ^ 1][t] = next;
-            asm volatile("bar.sync 1, 128;" ::: "memory");
         }
         const int r = quarter * 32 + lane, j = j0 + r;
         if (p.split == 1) {
@@ -766,7 +770,7 @@ template <typename TO> gf_status launch_wide(ProductArgs& a, const void* w, cons
 
 // Which kernel: estimates in microseconds, fitted to both on 1 to 2048 rows by 96 to 8192 columns and terms.  Wide: a chunk of a
 // tile of 256 columns takes 0.55 (128: 0.3), results 1.3, and 5 more where 16-bit rows start at odd places.  Few: 0.6 a chunk, or
-// 0.46 of an SM's time where there are more tiles than SMs, 0.7 to join parts.  (300 x 4096 x 4096: 20.3 wide, 25.2 few; 200 rows: 19.9, 17.4;
+// of an SM's time, where there are more tiles than SMs, 0.46 a chunk and 1.5 a tile; 0.7 to join parts.  (300 x 4096 x 4096: 20.3 wide, 25.2 few; 200 rows: 19.9, 17.4;
 // 2048 x 512 x 4096: 20.0, 17.5; 1024 x 2048 x 2048: 13.8, 15.8.)
 template <typename TO> bool wide_is_faster(const ProductArgs& a) {
     if (a.M <= 32) return false;
@@ -775,7 +779,7 @@ template <typename TO> bool wide_is_faster(const ProductArgs& a) {
     const double wide = 3.2 + rounds * ((bn == 256 ? 0.55 : 0.3) * a.chunks + 1.3 + 5 * odd);
     const long long few_tiles = (long long)((a.M + 63) / 64) * ((a.J + 127) / 128);
     const int split = few_split(few_tiles, a.chunks);
-    const double alone = 0.6 * ((a.chunks + split - 1) / split), all = 0.46 * (double)few_tiles * a.chunks / sm_count();
+    const double alone = 0.6 * ((a.chunks + split - 1) / split), all = (0.46 * a.chunks + 1.5) * (double)few_tiles / sm_count();
     return wide < 3.5 + (alone > all ? alone : all) + (split > 1 ? 0.7 : 0.0);
 }
 
