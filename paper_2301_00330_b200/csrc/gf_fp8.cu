@@ -170,16 +170,11 @@ __device__ __forceinline__ float bias_at(const ProductArgs& p, int j) {
 // 128 and few rows of A cost no more than they are.  The chunks of a tile are split over a cluster of CTAs where there
 // are few tiles, and the parts are added through distributed shared memory, in the order of the CTAs.
 //   warp 0: copies; warp 1: products; warps 2 to 5: scaling, a quarter of the accumulator's rows each.
-// Blocks of a cluster wait for one another and hold tensor memory: the ring is sized so that the blocks an SM can hold never
-// want more than its 512 columns, or two clusters could each hold what the other waits for.
 constexpr int kFewThreads = 192;
 __host__ __device__ constexpr int few_stages(int T) { return T <= 32 ? 4 : 3; }
 __host__ __device__ constexpr int few_buffers(int T) { return T <= 32 ? 4 : 2; }      // accumulators
 constexpr int kFewScales = 16;                                                        // chunks whose scales are held at once
 constexpr size_t few_smem(int T) { return (size_t)few_stages(T) * (16384 + T * 128) + 1024; }
-static_assert(227 * 1024 / few_smem(16) * 64 <= 384 && 227 * 1024 / few_smem(32) * 128 <= 384 && 227 * 1024 / few_smem(64) * 128 <= 384 &&
-                  227 * 1024 / few_smem(64) <= 3,
-              "tensor memory of the blocks of an SM");
 
 template <int T, typename TO> __global__ void __launch_bounds__(kFewThreads) fp8_few_kernel(const __grid_constant__ ProductArgs p) {
     extern __shared__ unsigned char dyn_raw[];
@@ -304,6 +299,12 @@ template <int T, typename TO> __global__ void __launch_bounds__(kFewThreads) fp8
         atomicOr(p.err_word, 8192u);
         let_settle();
     }
+    // Tensor memory goes back before this CTA waits for the others of its cluster: a CTA that holds it waits for nothing but its own
+    // copies and products, so that no two clusters (of this or another kernel) can each hold what the other waits for.
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    if (warp == 1) tmem_dealloc(tmem, kCols);
     if (p.split > 1) {
         // A CTA adds its share of the tile's rows, four columns a thread, with the loads of all parts on their way at once.
         constexpr int kCells = T * 32 / 128;                            // of a thread, for the whole tile
@@ -349,10 +350,6 @@ template <int T, typename TO> __global__ void __launch_bounds__(kFewThreads) fp8
         }
         asm volatile("barrier.cluster.wait.acquire;" ::: "memory");      // nothing of another CTA is read any more
     }
-    tc_fence_before_sync();
-    __syncthreads();
-    tc_fence_after_sync();
-    if (warp == 1) tmem_dealloc(tmem, kCols);
 }
 
 // CTAs that share the chunks of a tile: up to two per SM in all.  Powers of two: clusters of 3 took up to twice the time.
@@ -371,7 +368,7 @@ gf_status launch_few(ProductArgs& a, const void* w, const void* codes, int N, in
     // (in either form a box is 128 bytes of 128 rows of W)
     if (!make_tmap_u8_2d(&a.tm_w, w, (uint64_t)K, (uint64_t)N, (uint64_t)GF_FP8_PITCH(K), 128)) return GF_ERR_CUDA;
     if (!make_tmap_u8_2d(&a.tm_a, codes, (uint64_t)L, (uint64_t)a.M, (uint64_t)a_pitch, T)) return GF_ERR_CUDA;
-    a.tiles_m = (a.M + T - 1) / T;
+    a.tiles_m = (int)cdiv64(a.M, T);
     const long long tiles = (long long)a.tiles_m * ((a.J + 127) / 128);
     const int split = few_split(tiles, a.chunks);
     a.per = (a.chunks + split - 1) / split;
@@ -743,7 +740,7 @@ template <typename TO> gf_status launch_wide(ProductArgs& a, const void* w, cons
     auto kernel = fp8_wide_kernel<TO>;
     const gf_status st = ensure_dyn_smem(kernel, kWideSmem, configured);
     if (st != GF_OK) return st;
-    a.tiles_m = (a.M + 255) / 256;
+    a.tiles_m = (int)cdiv64(a.M, 256);
     a.bn = wide_columns(a.J);
     if (!make_tmap_u8_2d(&a.tm_a, codes, (uint64_t)L, (uint64_t)a.M, (uint64_t)a_pitch, 128)) return GF_ERR_CUDA;
     if (a.mn_major ? !make_tmap_u8_2d(&a.tm_w, w, (uint64_t)K, (uint64_t)N, (uint64_t)GF_FP8_PITCH(K), 128, (uint32_t)a.bn / 2)
@@ -775,9 +772,9 @@ template <typename TO> gf_status launch_wide(ProductArgs& a, const void* w, cons
 template <typename TO> bool wide_is_faster(const ProductArgs& a) {
     if (a.M <= 32) return false;
     const int bn = wide_columns(a.J), odd = (long long)a.J * sizeof(TO) % 4 != 0;
-    const double tiles = (double)((a.M + 255) / 256) * ((a.J + bn - 1) / bn), rounds = (double)(long long)((tiles + sm_count() / 2 - 1) / (sm_count() / 2));
+    const double tiles = (double)cdiv64(a.M, 256) * ((a.J + bn - 1) / bn), rounds = (double)(long long)((tiles + sm_count() / 2 - 1) / (sm_count() / 2));
     const double wide = 3.2 + rounds * ((bn == 256 ? 0.55 : 0.3) * a.chunks + 1.3 + 5 * odd);
-    const long long few_tiles = (long long)((a.M + 63) / 64) * ((a.J + 127) / 128);
+    const long long few_tiles = cdiv64(a.M, 64) * ((a.J + 127) / 128);
     const int split = few_split(few_tiles, a.chunks);
     const double alone = 0.6 * ((a.chunks + split - 1) / split), all = (0.46 * a.chunks + 1.5) * (double)few_tiles / sm_count();
     return wide < 3.5 + (alone > all ? alone : all) + (split > 1 ? 0.7 : 0.0);
