@@ -12,47 +12,64 @@ bool off16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; 
 bool is_dtype(int d) { return d == GF_F32 || d == GF_BF16; }
 
 // ---- quantisers ------------------------------------------------------------------------------------------------------
-// Rows: sixteen threads have the 128 columns of a scale, a block 16 rows by 4 scales, so that the loads of four octets are on their
-// way at once and the scales of 16 rows make whole sectors.  Bound by memory.
-constexpr int kQuantThreads = 256, kQuantRows = 16, kQuantGroups = 4;
+// Rows: sixteen threads (eight, with two octets each, of 16-bit values) have the 128 columns of a scale; a block has 16 (32) rows by 4
+// scales, so that the loads of four octets and more are on their way at once and the scales of its rows make whole sectors.
+// Bound by memory and instructions alike.
+constexpr int kQuantThreads = 256, kQuantGroups = 4;
+template <typename T> constexpr int kQuantEach = sizeof(T) == 2 ? 2 : 1;
+template <typename T> constexpr int kQuantRows = kQuantThreads / (16 / kQuantEach<T>);
 
 template <typename T, bool ALIGNED>
 __global__ void __launch_bounds__(kQuantThreads) quantize_rows_kernel(const T* x, uint8_t* codes, float* scales, long long rows, int cols, int pitch,
                                                                       long long scale_pitch, int chunks, long long blocks) {
     pdl_launch_dependents();
     pdl_wait();
-    const int part = threadIdx.x & 15;
+    constexpr int E = kQuantEach<T>, kParts = 16 / E, G = kQuantGroups / E;      // loads at once: G groups
+    const int part = threadIdx.x % kParts;
     const long long total = rows * cols;
     for (long long b = blockIdx.x; b < blocks; b += gridDim.x) {
-        const long long row = b / chunks * kQuantRows + (threadIdx.x >> 4);
-        const int c0 = (int)(b % chunks) * (128 * kQuantGroups) + part * 8;
-        Octet<T> o[kQuantGroups];
+        const long long row = b / chunks * kQuantRows<T> + threadIdx.x / kParts;
+        const int first = (int)(b % chunks) * (128 * kQuantGroups), end = min(pitch, first + 128 * kQuantGroups);
+        for (int base = first; base < end; base += 128 * G) {                       // (the same for the block)
+            const int c0 = base + part * 8 * E;
+            Octet<T> o[G][E];
 #pragma unroll
-        for (int k = 0; k < kQuantGroups; ++k) {
-            const int c = c0 + 128 * k;
-            if (row < rows && c < cols) {
-                if (ALIGNED) o[k].load(x + row * cols + c);
-                else load_anywhere(o[k], x, row * cols + c, total);
-            } else o[k].clear();
-        }
+            for (int k = 0; k < G; ++k)
 #pragma unroll
-        for (int k = 0; k < kQuantGroups; ++k) {
-            const int c = c0 + 128 * k;
-            if (c - part * 8 >= pitch) break;            // (the same for the block)
-            float v[8];
-            o[k].get(v);
-            if (!ALIGNED) {
+                for (int e = 0; e < E; ++e) {
+                    const int c = c0 + 128 * k + 8 * e;
+                    if (row < rows && c < cols) {
+                        if (ALIGNED) o[k][e].load(x + row * cols + c);
+                        else load_anywhere(o[k][e], x, row * cols + c, total);
+                    } else o[k][e].clear();
+                }
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (c + i >= cols) v[i] = 0.f;
-            }
-            uint32_t m = magnitude(v);
+            for (int k = 0; k < G; ++k) {
+                const int c = c0 + 128 * k;
+                float v[E][8];
+                uint32_t m = 0;
 #pragma unroll
-            for (int s = 8; s > 0; s >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, s));
-            const float scale = scale_of(m);
-            if (row < rows && c < pitch) {
-                *reinterpret_cast<uint2*>(codes + row * pitch + c) = codes8(v, scale, __frcp_rn(scale), cols - c);
-                if (part == 0 && c < cols) scales[(long long)(c >> 7) * scale_pitch + row] = scale;
+                for (int e = 0; e < E; ++e) {
+                    o[k][e].get(v[e]);
+                    if (!ALIGNED) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            if (c + 8 * e + i >= cols) v[e][i] = 0.f;
+                    }
+                    m = max(m, magnitude(v[e]));
+                }
+#pragma unroll
+                for (int s = kParts / 2; s > 0; s >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, s));
+                const float scale = scale_of(m), inv = __frcp_rn(scale);
+                if (row < rows && c < pitch) {
+                    uint2 w[E];
+#pragma unroll
+                    for (int e = 0; e < E; ++e) w[e] = codes8(v[e], scale, inv, cols - c - 8 * e);
+                    uint8_t* const to = codes + row * pitch + c;
+                    if constexpr (E == 2) *reinterpret_cast<uint4*>(to) = make_uint4(w[0].x, w[0].y, w[1].x, w[1].y);      // (the pitch is one of 16)
+                    else *reinterpret_cast<uint2*>(to) = w[0];
+                    if (part == 0 && c < cols) scales[(long long)(c >> 7) * scale_pitch + row] = scale;
+                }
             }
         }
     }
@@ -813,7 +830,7 @@ gf_status gf_fp8_quantize_rows(const gf_fp8_desc* desc, const void* x, void* cod
     const gf_status st = check(desc, x, codes, scales);
     if (st != GF_OK || desc->rows == 0) return st;
     const int chunks = (desc->cols + 128 * kQuantGroups - 1) / (128 * kQuantGroups);
-    const long long blocks = cdiv64(desc->rows, kQuantRows) * chunks, most = 1 << 30;
+    const long long blocks = cdiv64(desc->rows, desc->dtype == GF_F32 ? kQuantRows<float> : kQuantRows<__nv_bfloat16>) * chunks, most = 1 << 30;
     const dim3 grid((unsigned)(blocks < most ? blocks : most));
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     ProfScope prof(K_FP8_QUANTIZE, s);

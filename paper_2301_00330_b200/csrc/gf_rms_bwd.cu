@@ -70,11 +70,12 @@ __global__ void __launch_bounds__(WARP ? kRmsThreads : kRmsMostThreads, WARP && 
         }
         nrstd = a.rstd_in[r];
         if (DOTS) ndot = a.dots[r];
+        const bool inside = at + 8 * (NO - 1) * tpr + 8 <= a.total;          // whole vectors (the tensor's last octet may not be one)
 #pragma unroll
         for (int k = 0; k < NO; ++k) {
             if (there(k)) {
                 const long long p = at + 8 * k * tpr;
-                if (ALIGNED) {
+                if (ALIGNED || inside) {
                     ngy[k].load(gy + p);
                     nh[k].load(h + p);
                     if (gh) ngh[k].load(gh + p);
@@ -89,7 +90,20 @@ __global__ void __launch_bounds__(WARP ? kRmsThreads : kRmsMostThreads, WARP && 
     if (kAhead) fetch(row, e);
     int turn = 0;
     for (long long warp_row = (long long)blockIdx.x * teams_pb + first_of_warp; warp_row < a.rows; warp_row += step, row += step, e += e_step, turn ^= 1) {
-        if (!kAhead) fetch(row, e);
+        if constexpr (!kAhead) {
+            fetch(row, e);
+            if (row + step < a.rows) {                   // the next row, from memory to L2 meanwhile
+#pragma unroll
+                for (int k = 0; k < NO; ++k) {
+                    if (there(k)) {
+                        const long long p = e + e_step + 8 * k * tpr;
+                        asm volatile("prefetch.global.L2 [%0];" ::"l"(gy + p));
+                        asm volatile("prefetch.global.L2 [%0];" ::"l"(h + p));
+                        if (gh) asm volatile("prefetch.global.L2 [%0];" ::"l"(gh + p));
+                    }
+                }
+            }
+        }
         const bool live = row < a.rows;
         const float rstd = nrstd, dot = ndot;
         const uint64_t rstd2 = pair_of(rstd, rstd);
@@ -97,7 +111,7 @@ __global__ void __launch_bounds__(WARP ? kRmsThreads : kRmsMostThreads, WARP && 
         auto take = [&](int k, Eight& q, Eight& xh) {
             ngy[k].get(q);
             nh[k].get(xh);
-            if (!ALIGNED) {
+            if (!ALIGNED && (c0(k) < 0 || c0(k) + 8 > a.cols)) {
                 float f[8], x[8];
                 from_eight(q, f);
                 from_eight(xh, x);

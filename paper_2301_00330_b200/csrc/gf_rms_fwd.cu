@@ -23,8 +23,10 @@ __device__ __forceinline__ int skewed(int c) { return c + (c >> 5); }
 
 // ALIGNED: rows are whole octets.  OUT8: codes and scales in y's place; 16 threads that follow one another have the 128
 // columns of a scale.  Rows that are not whole octets change places for that through shared memory.
+// (Registers: with a bound of one block per SM the compiler orders 32-bit rows of one octet a thread so that 65536 x 256 takes 43.5 us
+// instead of 51; the other forms are as fast or faster without: 100352 x 576 bf16 77, with it 100.)
 template <typename TX, typename TR, int NO, bool WARP, bool ALIGNED, bool OUT8>
-__global__ void __launch_bounds__(WARP ? kRmsThreads : kRmsMostThreads) rms_fwd_kernel(const __grid_constant__ RmsArgs a) {
+__global__ void __launch_bounds__(WARP ? kRmsThreads : kRmsMostThreads, WARP && NO == 1 && sizeof(TX) == 4 ? 1 : 0) rms_fwd_kernel(const __grid_constant__ RmsArgs a) {
     __shared__ __align__(16) float red[2][32];
     extern __shared__ float rows_smem[];
     pdl_launch_dependents();
@@ -64,10 +66,11 @@ __global__ void __launch_bounds__(WARP ? kRmsThreads : kRmsMostThreads) rms_fwd_
     const long long e_step = step * a.cols;
     long long e = ((row * a.cols >> 3) + g) * 8;
     auto fetch = [&](long long at) {
+        const bool inside = at + 8 * (NO - 1) * tpr + 8 <= a.total;          // whole vectors (the tensor's last octet may not be one)
 #pragma unroll
         for (int k = 0; k < NO; ++k) {
             if (there(k)) {
-                if (ALIGNED) {
+                if (ALIGNED || inside) {
                     nx[k].load(x + at + 8 * k * tpr);
                     if (res) nr[k].load(res + at + 8 * k * tpr);
                 } else {
@@ -114,7 +117,7 @@ __global__ void __launch_bounds__(WARP ? kRmsThreads : kRmsMostThreads) rms_fwd_
                     }
                 }
             }
-            if (!ALIGNED || (OUT8 && k + 1 == NO)) {     // what is not the row's counts as zero
+            if ((!ALIGNED && (c < 0 || c + 8 > a.cols)) || (OUT8 && k + 1 == NO && !last)) {     // what is not the row's counts as zero
                 float f[8];
                 from_eight(v[k], f);
 #pragma unroll
@@ -122,7 +125,6 @@ __global__ void __launch_bounds__(WARP ? kRmsThreads : kRmsMostThreads) rms_fwd_
                     if (c + i < 0 || c + i >= a.cols) f[i] = 0.f;
                 to_eight(f, v[k]);
             }
-            if (ALIGNED && k + 1 == NO && !last) continue;
 #pragma unroll
             for (int i = 0; i < 4; ++i) squares = fma_pair(v[k][i], v[k][i], squares);
         }
