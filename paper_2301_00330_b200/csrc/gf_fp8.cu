@@ -369,11 +369,14 @@ template <int T, typename TO> __global__ void __launch_bounds__(kFewThreads) fp8
     }
 }
 
-// CTAs that share the chunks of a tile: up to two per SM in all.  Powers of two: clusters of 3 took up to twice the time.
+// CTAs that share the chunks of a tile, up to two per SM in all, by what that takes in microseconds: 0.6 a chunk, 1.5 for the cluster
+// and its joining and 0.15 more for each of its CTAs.  Powers of two: clusters of 3 took up to twice the time.
+double few_time(int chunks, int split) { return 0.6 * ((chunks + split - 1) / split) + (split > 1 ? 1.5 + 0.15 * split : 0.0); }
 int few_split(long long tiles, int chunks) {
-    int split = 1;
-    while (split < 8 && 2 * split <= chunks && 2 * split * tiles <= 2LL * sm_count()) split *= 2;
-    return split;
+    int best = 1;
+    for (int split = 2; split <= 8 && split <= chunks && split * tiles <= 2LL * sm_count(); split *= 2)
+        if (few_time(chunks, split) < few_time(chunks, best)) best = split;
+    return best;
 }
 
 template <int T, typename TO>
@@ -782,19 +785,20 @@ template <typename TO> gf_status launch_wide(ProductArgs& a, const void* w, cons
     return e == cudaSuccess ? GF_OK : GF_ERR_CUDA;
 }
 
-// Which kernel: estimates in microseconds, fitted to both on 1 to 2048 rows by 96 to 8192 columns and terms.  Wide: a chunk of a
-// tile of 256 columns takes 0.55 (128: 0.3), results 1.3, and 5 more where 16-bit rows start at odd places.  Few: 0.6 a chunk, or
-// of an SM's time, where there are more tiles than SMs, 0.46 a chunk and 1.5 a tile; 0.7 to join parts.  (300 x 4096 x 4096: 20.3 wide, 25.2 few; 200 rows: 19.9, 17.4;
-// 2048 x 512 x 4096: 20.0, 17.5; 1024 x 2048 x 2048: 13.8, 15.8.)
+// Which kernel: estimates in microseconds, fitted to both on 1 to 10000 rows by 96 to 8192 columns and terms.  Wide: a chunk of a
+// tile of 256 columns takes 0.55 (128: 0.3), results 1.3, and 5 (32 bits: 2.5) more where rows are not whole
+// 16-byte pieces.  Few: as above, or of an SM's time, where there are more tiles than SMs, 0.46 a chunk and 1.8 a tile at least.  (300 x 4096 x 4096: 20.3 wide, 25.2 few; 200 rows:
+// 19.9, 17.4; 2048 x 512 x 4096: 20.0, 16.3; 1024 x 2048 x 2048: 13.8, 15.8; 2000 x 1000 x 576: 7.9, 6.7; 4099 rows: 8.2, 12.0.)
 template <typename TO> bool wide_is_faster(const ProductArgs& a) {
     if (a.M <= 32) return false;
-    const int bn = wide_columns(a.J), odd = (long long)a.J * sizeof(TO) % 4 != 0;
+    const int bn = wide_columns(a.J);
+    const double by_hand = (long long)a.J * sizeof(TO) % 16 == 0 ? 0.0 : sizeof(TO) == 4 ? 2.5 : 5.0;
     const double tiles = (double)cdiv64(a.M, 256) * ((a.J + bn - 1) / bn), rounds = (double)(long long)((tiles + sm_count() / 2 - 1) / (sm_count() / 2));
-    const double wide = 3.2 + rounds * ((bn == 256 ? 0.55 : 0.3) * a.chunks + 1.3 + 5 * odd);
+    const double wide = 3.2 + rounds * ((bn == 256 ? 0.55 : 0.3) * a.chunks + 1.3 + by_hand);
     const long long few_tiles = cdiv64(a.M, 64) * ((a.J + 127) / 128);
-    const int split = few_split(few_tiles, a.chunks);
-    const double alone = 0.6 * ((a.chunks + split - 1) / split), all = (0.46 * a.chunks + 1.5) * (double)few_tiles / sm_count();
-    return wide < 3.5 + (alone > all ? alone : all) + (split > 1 ? 0.7 : 0.0);
+    const double alone = few_time(a.chunks, few_split(few_tiles, a.chunks)), each = 0.46 * a.chunks;
+    const double all = (each > 1.8 ? each : 1.8) * (double)few_tiles / sm_count();
+    return wide < 3.5 + (alone > all ? alone : all);
 }
 
 template <typename TO> gf_status product(ProductArgs& a, const void* w, const void* codes, int N, int K, int L, long long a_pitch, cudaStream_t s) {
