@@ -7,7 +7,8 @@
  *
  * The conventions of gf.h hold: device pointers 16-byte aligned and dense, inputs read-only,
  * outputs overwritten, work enqueued on `stream` without synchronising, errors that the host can
- * detect returned before anything is launched.  A device-side wait that runs out (products only) is
+ * detect returned before anything is launched.  Make the first call of a kind on a device outside any
+ * stream capture (kernels are set up then).  A device-side wait that runs out (products only) is
  * reported to the library-wide word that gf_last_async_status reads with any zeroed workspace.  Results repeat bit for
  * bit.
  */

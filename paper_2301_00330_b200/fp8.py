@@ -31,8 +31,18 @@ class Fp8Matrix:
     cols: int
     blocks: bool
 
+    def check(self) -> None:
+        """The tensors have the sizes and types that the library reads."""
+        codes = (self.rows, B.fp8_pitch(self.cols))
+        scales = (-(-self.rows // 128), -(-self.cols // 128)) if self.blocks else (-(-self.cols // 128), B.fp8_scale_pitch(self.rows))
+        if tuple(self.codes.shape) != codes or self.codes.element_size() != 1:
+            raise ValueError(f"codes of one byte and shape {codes} expected, got {self.codes.dtype} {tuple(self.codes.shape)}")
+        if tuple(self.scales.shape) != scales or self.scales.dtype != torch.float32 or self.scales.device != self.codes.device:
+            raise ValueError(f"float32 scales of shape {scales} beside the codes expected, got {self.scales.dtype} {tuple(self.scales.shape)}")
+
     def dequantize(self) -> torch.Tensor:
         """The values as float32 [rows, cols]."""
+        self.check()
         v = self.codes.view(torch.float8_e4m3fn)[:, :self.cols].float()
         if self.blocks:
             s = self.scales.repeat_interleave(128, 0)[:self.rows]
@@ -88,6 +98,8 @@ def fp8_matmul(a: Fp8Matrix, w: Fp8Matrix, bias: torch.Tensor | None = None, tra
     inner, outer = (w.rows, w.cols) if transposed else (w.cols, w.rows)
     if a.cols != inner:
         raise ValueError(f"a has {a.cols} columns, the weight takes {inner}")
+    a.check()
+    w.check()
     if not a.codes.is_cuda or any(t is not None and t.device != a.codes.device for t in (w.codes, bias)):
         raise ValueError("a, w and bias lie on one CUDA device")
     if bias is not None and bias.shape != (outer,):

@@ -158,6 +158,12 @@ def test_fp8_wrappers_refuse_what_they_cannot_take(gf):
         gf.fp8_matmul(rows, blocks, transposed=True)
     with pytest.raises(ValueError, match="CUDA"):
         gf.fp8_matmul(rows, blocks)
+    for bad in (gf.Fp8Matrix(torch.zeros((4, 8), dtype=torch.uint8), rows.scales, 4, 8, False), gf.Fp8Matrix(rows.codes, torch.zeros(1, 3), 4, 8, False),
+                gf.Fp8Matrix(rows.codes.short(), rows.scales, 4, 8, False), gf.Fp8Matrix(rows.codes, rows.scales.double(), 4, 8, False)):
+        with pytest.raises(ValueError, match="expected"):
+            gf.fp8_matmul(bad, blocks)
+        with pytest.raises(ValueError, match="expected"):
+            bad.dequantize()
 
 
 def test_the_format_of_8_bit_values(gf):
