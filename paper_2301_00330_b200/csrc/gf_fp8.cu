@@ -492,48 +492,68 @@ template <typename TO, int NC> __device__ __forceinline__ void stage_piece(unsig
         *reinterpret_cast<uint4*>(buf + lane * kBytes + ((c / kVec) ^ flip) * 16) = w;
     }
 }
-// The same piece to memory by the warp itself, where the result's rows are not whole 16-byte pieces: a row at a time, words of
-// 4 bytes (two bf16 values from the row's first even place on, and the odd ones at its ends).
-// (A call of its own, so that its registers are not taken from the loop that scales.)
-template <typename TO, int NC> __device__ __noinline__ void store_piece(TO* out, long long pitch, const unsigned char* buf, int rows, int live, int lane) {
-    constexpr int kVec = 16 / (int)sizeof(TO), kBytes = NC * (int)sizeof(TO), kEach = 4 / (int)sizeof(TO);
-    static_assert(NC <= 32 * kEach, "a word a lane");
-    auto at = [&](int r, int c) {
-        const int turn = kBytes == 128 ? r & 7 : (r >> 1) & 3;
-        return *reinterpret_cast<const TO*>(buf + r * kBytes + ((c / kVec) ^ turn) * 16 + c % kVec * (int)sizeof(TO));
-    };
-    __syncwarp();
+// The same piece to memory by the warp itself, where the result's rows are not whole 16-byte pieces.
+// 32 bits: a row at a time, an element a lane.
+__device__ __forceinline__ void store_elements(float* out, int pitch, const unsigned char* buf, int rows, int live) {
+    const int lane = (int)threadIdx.x & 31;
 #pragma unroll 1
     for (int r0 = 0; r0 < rows; r0 += 8) {
-        TO v[8][kEach], first[8];
-        int odd[8];                                      // places of a row's elements before its first whole word
+        float w[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            odd[k] = sizeof(TO) == 4 ? 0 : (int)((reinterpret_cast<uintptr_t>(out + k * pitch) >> 1) & 1);
-            first[k] = at(r0 + k, 0);
+        for (int k = 0; k < 8; ++k) w[k] = *reinterpret_cast<const float*>(buf + (r0 + k) * 128 + (((lane >> 2) ^ k) & 7) * 16 + (lane & 3) * 4);
 #pragma unroll
-            for (int i = 0; i < kEach; ++i) v[k][i] = at(r0 + k, min(kEach * lane + odd[k] + i, NC - 1));
-        }
+        for (int k = 0; k < 8; ++k)
+            if (r0 + k < rows && lane < live) out[(long long)(r0 + k) * pitch + lane] = w[k];
+    }
+}
+// 16 bits: eight (four) lanes have a row and write what lies between its 16-byte boundaries in whole pieces, two of the buffer's
+// shifted, and the elements before and behind one by one (14672 x 4241 x 64: 97 us an element a lane, 59 so).
+template <int kBytes> __device__ __forceinline__ void store_shifted(__nv_bfloat16* out, int pitch, const unsigned char* buf, int rows, int live) {
+    using TO = __nv_bfloat16;
+    constexpr int kVec = 8, kLanes = kBytes / 16, kRows = 32 / kLanes;
+    const int lane = (int)threadIdx.x & 31, v = lane % kLanes;
+#pragma unroll 2
+    for (int r = lane / kLanes; r < 32; r += kRows) {
+        TO* const row = out + (long long)r * pitch;
+        const unsigned char* const from = buf + r * kBytes;
+        const int turn = kBytes == 128 ? r & 7 : (r >> 1) & 3;
+        const int head = (int)((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / 2;      // elements before the first boundary
+        const uint4 a = *reinterpret_cast<const uint4*>(from + (v ^ turn) * 16), b = *reinterpret_cast<const uint4*>(from + (min(v + 1, kLanes - 1) ^ turn) * 16);
+        if (r < rows) {
+            if (head + (v + 1) * kVec <= live) {
+                uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+                const int words = head / 2;                                                // 0 .. 3
+                if (words & 2) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            TO* const row = out + k * pitch;
-            const int c = kEach * lane + odd[k];
-            if (r0 + k < rows) {
-                if constexpr (sizeof(TO) == 4) {
-                    if (c < live) row[c] = v[k][0];
-                } else {
-                    if (c + 1 < live) {
-                        __nv_bfloat162 w;
-                        w.x = v[k][0];
-                        w.y = v[k][1];
-                        *reinterpret_cast<__nv_bfloat162*>(row + c) = w;
-                    } else if (c < live) row[c] = v[k][0];
-                    if (odd[k] && lane == 0) row[0] = first[k];
+                    for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
                 }
+                if (words & 1) {
+#pragma unroll
+                    for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+                }
+                if (head & 1) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+                }
+                *reinterpret_cast<uint4*>(row + head + v * kVec) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+            auto at = [&](int c) { return *reinterpret_cast<const TO*>(from + ((c / kVec) ^ turn) * 16 + c % kVec * 2); };
+            const int tail = live > head ? head + (live - head) / kVec * kVec : head;
+#pragma unroll
+            for (int e = v; e < kVec - 1; e += kLanes) {
+                if (e < min(head, live)) row[e] = at(e);
+                if (tail + e < live) row[tail + e] = at(tail + e);
             }
         }
-        out += 8 * pitch;
     }
+}
+// (A call of its own, so that its registers are not taken from the loop that scales: with them 64 bytes went to memory there, a
+// quarter of the time of 4096 x 8192 x 4096.)
+template <typename TO> __device__ __noinline__ void store_piece(TO* out, int pitch, const unsigned char* buf, int rows, int live, int bytes) {
+    __syncwarp();
+    if constexpr (sizeof(TO) == 4) store_elements(out, pitch, buf, rows, live);
+    else if (bytes == 128) store_shifted<128>(out, pitch, buf, rows, live);
+    else store_shifted<64>(out, pitch, buf, rows, live);
     __syncwarp();
 }
 
@@ -733,10 +753,8 @@ template <typename TO> __global__ void __launch_bounds__(kWideThreads, 1) fp8_wi
                         bulk_commit();
                     }
                 } else {
-                    TO* const out = static_cast<TO*>(p.out) + row0 * p.J + j0 + c;
-                    const int rows = (int)min(32LL, p.M - row0), live = min(p.J - j0 - c, min(cols, kPieceCols));
-                    if (cols >= kPieceCols) store_piece<TO, kPieceCols>(out, p.J, piece, rows, live, lane);
-                    else store_piece<TO, 32>(out, p.J, piece, rows, live, lane);
+                    store_piece(static_cast<TO*>(p.out) + row0 * p.J + j0 + c, p.J, piece, (int)min(32LL, p.M - row0), min(p.J - j0 - c, min(cols, kPieceCols)),
+                                min(cols, kPieceCols) * (int)sizeof(TO));
                 }
             }
         }
@@ -786,13 +804,13 @@ template <typename TO> gf_status launch_wide(ProductArgs& a, const void* w, cons
 }
 
 // Which kernel: estimates in microseconds, fitted to both on 1 to 10000 rows by 96 to 8192 columns and terms.  Wide: a chunk of a
-// tile of 256 columns takes 0.55 (128: 0.3), results 1.3, and 5 (32 bits: 2.5) more where rows are not whole
-// 16-byte pieces.  Few: as above, or of an SM's time, where there are more tiles than SMs, 0.46 a chunk and 1.8 a tile at least.  (300 x 4096 x 4096: 20.3 wide, 25.2 few; 200 rows:
+// tile of 256 columns takes 0.55 (128: 0.3), results 1.3, and 2.7 (32 bits: 3.5) more where rows are not
+// whole 16-byte pieces.  Few: as above, or of an SM's time, where there are more tiles than SMs, 0.46 a chunk and 1.8 a tile at least.  (300 x 4096 x 4096: 20.3 wide, 25.2 few; 200 rows:
 // 19.9, 17.4; 2048 x 512 x 4096: 20.0, 16.3; 1024 x 2048 x 2048: 13.8, 15.8; 2000 x 1000 x 576: 7.9, 6.7; 4099 rows: 8.2, 12.0.)
 template <typename TO> bool wide_is_faster(const ProductArgs& a) {
     if (a.M <= 32) return false;
     const int bn = wide_columns(a.J);
-    const double by_hand = (long long)a.J * sizeof(TO) % 16 == 0 ? 0.0 : sizeof(TO) == 4 ? 2.5 : 5.0;
+    const double by_hand = (long long)a.J * sizeof(TO) % 16 == 0 ? 0.0 : sizeof(TO) == 4 ? 3.5 : 2.7;
     const double tiles = (double)cdiv64(a.M, 256) * ((a.J + bn - 1) / bn), rounds = (double)(long long)((tiles + sm_count() / 2 - 1) / (sm_count() / 2));
     const double wide = 3.2 + rounds * ((bn == 256 ? 0.55 : 0.3) * a.chunks + 1.3 + by_hand);
     const long long few_tiles = cdiv64(a.M, 64) * ((a.J + 127) / 128);
