@@ -13,8 +13,9 @@ bool is_dtype(int d) { return d == GF_F32 || d == GF_BF16; }
 
 // ---- quantisers ------------------------------------------------------------------------------------------------------
 // Rows: sixteen threads (eight, with two octets each, of 16-bit values) have the 128 columns of a scale; a block has 16 (32) rows by 4
-// scales, so that the loads of four octets and more are on their way at once and the scales of its rows make whole sectors.
-// Bound by memory and instructions alike.
+// scales, so that the loads of four octets are on their way at once and the scales of its rows make whole sectors.
+// Bound by memory, for 16-bit values by instructions too (65536 x 512: 17.5 us, 0.88 of the copy bandwidth; 32 bits 26.6, 0.97; with one
+// octet a thread 16 bits took 20.7).  Rows that are not whole octets are put together from two vectors each: 20000 x 1001 bf16 25 us.
 constexpr int kQuantThreads = 256, kQuantGroups = 4;
 template <typename T> constexpr int kQuantEach = sizeof(T) == 2 ? 2 : 1;
 template <typename T> constexpr int kQuantRows = kQuantThreads / (16 / kQuantEach<T>);
@@ -187,6 +188,8 @@ __device__ __forceinline__ float bias_at(const ProductArgs& p, int j) {
 // 128 and few rows of A cost no more than they are.  The chunks of a tile are split over a cluster of CTAs where there
 // are few tiles, and the parts are added through distributed shared memory, in the order of the CTAs.
 //   warp 0: copies; warp 1: products; warps 2 to 5: scaling, a quarter of the accumulator's rows each.
+// Bound by latency: 8 x 4096 x 4096 6.2 us, of which its bytes take 2.6 (16.8 MB from memory; a launch, one round of copies, four chunks,
+// two meetings of the cluster); 8 x 768 x 768 3.4.
 constexpr int kFewThreads = 192;
 __host__ __device__ constexpr int few_stages(int T) { return T <= 32 ? 4 : 3; }
 __host__ __device__ constexpr int few_buffers(int T) { return T <= 32 ? 4 : 2; }      // accumulators
@@ -411,12 +414,15 @@ gf_status launch_few(ProductArgs& a, const void* w, const void* codes, int N, in
 // brings its 128 rows of A and half of the tile's columns of W; the products of a pair (cta_group::2) read both halves, so that a
 // chunk of 128 terms costs each SM 32 KB from L2 for 512 clocks of products.
 //   warp 0: copies; warp 1 (of the first CTA): products; warps 4 to 19: scaling, a quarter of the rows by a quarter of
-//   the columns each, in registers (which the first four warps give up for them); warp 3: takes the results to memory by the
-//   copy engine, while the next tile is on its way (starting a copy takes about 900 clocks: left to the scaling warps that
-//   was a fifth of the time of a 512-term tile).
-// What bounds it is the accumulators' way out of tensor memory, once for every 128 terms, which the scales ask for: with
-// the reads left out the products run at 2.97 PFLOP/s, with them and no arithmetic at 2.1, with all of it at 1.85 (4096 x 8192
-// x 4096; 1.6 under the power cap).  With 8 scaling warps of 128 columns 1.75.
+//   the columns each, in registers, which the first four warps give up for them; the next tile's first two chunks are
+//   multiplied while they write their results, by the copy engine where rows are whole 16-byte pieces (65536 x 2048 x 512: 99 us;
+//   stored by the warps 143).
+// What bounds it is the accumulators' way out of tensor memory, once for every 128 terms, which the scales ask for: reading one
+// takes the port that the products accumulate through for 260 clocks of a chunk's 512, and between a chunk's product and the next
+// product into its accumulator lie 1700 clocks of signals, reads and sums, with two accumulators: about 1100 clocks a chunk.  4096 x
+// 8192 x 4096 runs at 2.0 PFLOP/s (gradient of the input 1.95; 1.6 under the power cap, which runs of some milliseconds meet); with the
+// reads and sums left out the products take 2.97.  Measured and not taken: four accumulators of half the columns (A is read
+// twice: 159 us for 147), 8 scaling warps of 128 columns (157), scales through a ring in shared memory (147 for 140).
 constexpr int kWideThreads = 640, kWideStages = 5, kWideStage = 32768, kWidePiece = 32 * 128;
 constexpr int kWideWarps = 16;                     // that scale
 constexpr size_t kWideSmem = (size_t)kWideStages * kWideStage + kWideWarps * kWidePiece + 1024;
