@@ -183,13 +183,12 @@ struct Drop {
 Drop make_drop(float p, const uint64_t* seed);
 static inline bool valid_p(float p) { return p >= 0.f && p <= 1.f; }
 
-// The two words of a seed, the same in all threads: said in a way that lets the compiler keep them, and the keys of the ten rounds, in
-// uniform registers (integer additions of 20 to 160 clocks a block of bits otherwise).  Called by whole warps.
+// The two words of a seed.
 __device__ __forceinline__ void load_seed(const Drop& d, uint64_t& key, uint64_t& offset) {
     key = offset = 0;
     if (d.threshold) {
-        key = __shfl_sync(0xffffffffu, d.seed[0], 0);
-        offset = __shfl_sync(0xffffffffu, d.seed[1], 0);
+        key = d.seed[0];
+        offset = d.seed[1];
     }
 }
 

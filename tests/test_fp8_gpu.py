@@ -297,8 +297,8 @@ def test_frozen_layer_through_autograd(gf, form):
         # the bound of the products, with at most 200 terms of at most 4 deviations each under the sum of magnitudes
         assert float((rows(got.detach()).double() - want).abs().max()) <= (STEP[x.dtype] + 150 * U * 20) * float(want.abs().max())
     # and the layer is what it stands for: each operand is off by at most 2^-4 of its values, about 2.6 % of its norm
-    exact = rows(x).double() @ w.double().t() + layer.bias.double()
-    assert float((rows(y).double() - exact).norm() / exact.norm()) < 2.0 ** -4 * 2
+    exact = rows(x.detach()).double() @ w.double().t() + layer.bias.double()
+    assert float((rows(y.detach()).double() - exact).norm() / exact.norm()) < 2.0 ** -4 * 2
 
 
 @pytest.mark.parametrize("out", DTYPES, ids=["f32", "bf16"])
