@@ -114,17 +114,31 @@ def fp8_matmul(a: Fp8Matrix, w: Fp8Matrix, bias: torch.Tensor | None = None, tra
     return out
 
 
+def _keep(ctx, weights, *others) -> None:
+    """Saves the weights' tensors in the way that lets torch notice a change in place before the backward pass."""
+    ctx.sizes = [(w.rows, w.cols) for w in weights]
+    ctx.save_for_backward(*others, *(t for w in weights for t in (w.codes, w.scales)))
+
+
+def _kept(ctx):
+    """(others, weights) of _keep."""
+    saved, n = ctx.saved_tensors, 2 * len(ctx.sizes)
+    first = len(saved) - n
+    return saved[:first], [Fp8Matrix(saved[first + 2 * i], saved[first + 2 * i + 1], rows, cols, True) for i, (rows, cols) in enumerate(ctx.sizes)]
+
+
 class _Fp8LinearFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, layer):
-        ctx.layer, ctx.dtype = layer, x.dtype
+        ctx.dtype = x.dtype
         w = layer.matrix()
+        _keep(ctx, [w])
         return fp8_matmul(quantize_rows(x), w, layer.bias, out_dtype=x.dtype).view(*x.shape[:-1], w.rows)
 
     @staticmethod
     @once_differentiable
     def backward(ctx, g_y):
-        w = ctx.layer.matrix()
+        w, = _kept(ctx)[1]
         g_x = fp8_matmul(quantize_rows(g_y), w, transposed=True, out_dtype=ctx.dtype)
         return g_x.view(*g_y.shape[:-1], w.cols), None
 
@@ -200,20 +214,21 @@ class _RmsNormLinearFn(torch.autograd.Function):
         q = _empty_rows(desc.rows, desc.cols, x.device)
         with torch.cuda.device(x.device):
             B.gf_rms_norm_forward_fp8(desc, x, residual, seed, weight, h, q.codes, q.scales, rstd, torch.cuda.current_stream(x.device))
-        outs = [fp8_matmul(q, layer.matrix(), layer.bias, out_dtype=x.dtype).view(*x.shape[:-1], layer.out_features) for layer in layers]
-        ctx.desc, ctx.x_dtype, ctx.layers = desc, x.dtype, layers
-        ctx.save_for_backward(x if plain else h, rstd, weight, seed)
+        weights = [layer.matrix() for layer in layers]
+        outs = [fp8_matmul(q, w, layer.bias, out_dtype=x.dtype).view(*x.shape[:-1], w.rows) for w, layer in zip(weights, layers)]
+        ctx.desc, ctx.x_dtype = desc, x.dtype
+        _keep(ctx, weights, x if plain else h, rstd, weight, seed)
         return (h, *outs)
 
     @staticmethod
     @once_differentiable
     def backward(ctx, g_h, *g_outs):
-        h, rstd, weight, seed = ctx.saved_tensors
+        (h, rstd, weight, seed), weights = _kept(ctx)
         need_x, need_w, need_res = ctx.needs_input_grad[:3]
         g_y = None
-        for layer, g in zip(ctx.layers, g_outs):
-            if g is not None:
-                part = fp8_matmul(quantize_rows(g), layer.matrix(), transposed=True, out_dtype=ctx.x_dtype)
+        for w, g in zip(weights, g_outs):
+            if g is not None:            # parts are rounded to x's dtype and added in it, as torch adds the gradients of a shared input
+                part = fp8_matmul(quantize_rows(g), w, transposed=True, out_dtype=ctx.x_dtype)
                 g_y = part if g_y is None else g_y.add_(part)
         g_y = torch.zeros(h.shape, dtype=ctx.x_dtype, device=h.device) if g_y is None else g_y.view(h.shape)
         g_x, g_w, g_res = _norm_backward(ctx.desc, g_y, g_h, h, rstd, weight, seed, need_x, need_w, need_res, ctx.x_dtype)

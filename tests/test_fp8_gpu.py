@@ -308,3 +308,28 @@ def test_products_of_many_tiles(gf, M, N, K, out):
     some tiles only, results that leave by the copy engine and by hand."""
     for transposed in (False, True):
         _check_product(*_product(gf, M, N, K, transposed, out, torch.float32, seed=M + N), transposed)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("normed", [False, True], ids=["layer", "norm_and_layer"])
+def test_a_weight_changed_before_the_backward_pass_is_refused(gf, normed):
+    """The gradient is that of the weight that ran forward, or an error as for torch's layers: never another weight's."""
+    gen = torch.Generator().manual_seed(21)
+    w, other = (torch.randn(96, 160, generator=gen).cuda() for _ in range(2))
+
+    def forward(layer):
+        x = torch.randn(40, 160, generator=torch.Generator().manual_seed(22)).cuda().requires_grad_()
+        return x, gf.rms_norm_linear(x, None, layer) if normed else layer(x)
+
+    x, y = forward(gf.Fp8Linear(w))
+    y.sum().backward()
+    layer = gf.Fp8Linear(w)
+    x2, y2 = forward(layer)
+    layer.load_state_dict(gf.Fp8Linear(other).state_dict())
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y2.sum().backward()
+    layer = gf.Fp8Linear(w)
+    x3, y3 = forward(layer)
+    layer.codes, layer.scales = gf.Fp8Linear(other).codes, gf.Fp8Linear(other).scales      # put in their place, the old ones live on
+    y3.sum().backward()
+    assert torch.equal(x3.grad, x.grad)
