@@ -27,8 +27,8 @@ extern "C" {
  * Moraes, Dror, Shaw 2011) on the counter (i / 8, seed[1]) under the key seed[0] gives
  * 128 bits for eight elements, lowest 16 first.  The mask is a function of (seed, i): it is computed again
  * in the backward pass and never stored.  p is thereby rounded to a multiple of 2^-16, and the scale is
- * that of the rounded one, so that the mean is kept.  A dropped value counts as 0 whatever it is,
- * NaN included; t = 65536 drops all.
+ * that of the rounded one, so that the mean is kept.  The scaled value is rounded to fp32 before the
+ * residual is added.  A dropped value counts as 0 whatever it is, NaN included; t = 65536 drops all.
  * seed: DEVICE pointer to two 64-bit words, 8-byte aligned (NULL when t = 0); read when the kernel
  * runs, so that a captured graph takes a new mask from new words.
  * Backward: g_x[i] = keep[i] ? g_y[i] / (1 - t / 65536) : 0; the residual's gradient is g_y. */

@@ -46,8 +46,10 @@ __global__ void __launch_bounds__(kThreads) dropout_kernel(const TX* x, const TY
         float v[8], w[8];
         a[k].get(v);
         if constexpr (RESIDUAL) r[k].get(w);
-        if (d.threshold) drop_octet<RESIDUAL>(v, w, (uint64_t)f, key, offset, d);
-        else if constexpr (RESIDUAL) {
+        if (d.threshold) {
+            if constexpr (RESIDUAL) drop_octet(v, w, (uint64_t)f, key, offset, d);
+            else drop_octet(v, (uint64_t)f, key, offset, d);
+        } else if constexpr (RESIDUAL) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] += w[i];
         }

@@ -192,26 +192,56 @@ __device__ __forceinline__ void load_seed(const Drop& d, uint64_t& key, uint64_t
     }
 }
 
-// v[i] <- kept ? v[i] scale + add[i] : add[i] for the elements of octet number f.  A 16-bit half is compared at the top of a word:
-// (w >> 16) >= t is w >= t << 16, and for all to be dropped (t = 65536) no word passes.
-template <bool ADD> __device__ __forceinline__ void drop_octet(float (&v)[8], const float (&add)[8], uint64_t f, uint64_t key, uint64_t offset, const Drop& d) {
-    const uint4 r = philox(f, offset, key);
-    const uint32_t w[4] = {r.x, r.y, r.z, r.w}, top = d.threshold << 16;
-    const bool none = d.threshold == 65536u;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const uint32_t bits = i & 1 ? w[i >> 1] : w[i >> 1] << 16;      // (what lies below the half does not matter)
-        const float kept = ADD ? fmaf(v[i], d.scale, add[i]) : v[i] * d.scale;
-        v[i] = bits >= top && !none ? kept : ADD ? add[i] : 0.f;
-    }
+// The 16 bits of element i of an octet decide at the top of a word: (w >> 16) >= t is w >= t << 16, and for all to be dropped
+// (t = 65536) no word passes.
+__device__ __forceinline__ bool is_kept(const uint32_t (&w)[4], int i, const Drop& d) {
+    const uint32_t bits = i & 1 ? w[i >> 1] : w[i >> 1] << 16;          // (what lies below the half does not matter)
+    return bits >= d.threshold << 16 && d.threshold != 65536u;
 }
 
-template <bool ADD> __device__ __forceinline__ void drop_octet(Eight& v, const Eight& add, uint64_t f, uint64_t key, uint64_t offset, const Drop& d) {
-    float x[8], w[8];
+// v[i] <- kept ? v[i] scale : 0 for the elements of octet number f.
+__device__ __forceinline__ void drop_octet(float (&v)[8], uint64_t f, uint64_t key, uint64_t offset, const Drop& d) {
+    const uint4 r = philox(f, offset, key);
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = is_kept(w, i, d) ? v[i] * d.scale : 0.f;
+}
+
+__device__ __forceinline__ void drop_octet(Eight& v, uint64_t f, uint64_t key, uint64_t offset, const Drop& d) {
+    float x[8];
     from_eight(v, x);
-    if (ADD) from_eight(add, w);
-    drop_octet<ADD>(x, w, f, key, offset, d);
+    drop_octet(x, f, key, offset, d);
     to_eight(x, v);
+}
+
+// v[i] <- kept ? v[i] scale + add[i] : add[i].
+// The product is rounded before the sum, so that the sum is that of the dropped branch as it is without a residual.  Left unrounded
+// inside a fused operation it carries the scale's own error into sums that cancel: with 4/3 for p = 1/4 exact ties of a bf16 sum
+// went the wrong way, one element in 600.  (One value at a time: a product and a sum of pairs are fused by the compiler.)
+__device__ __forceinline__ void drop_octet(Eight& v, const Eight& add, uint64_t f, uint64_t key, uint64_t offset, const Drop& d) {
+    const uint4 r = philox(f, offset, key);
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+    float kept[8], dropped[8];
+    from_eight(v, kept);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) kept[i] = __fmul_rn(kept[i], d.scale);
+    Eight sum;
+    to_eight(kept, sum);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[i] = add_pair(sum[i], add[i]);
+    from_eight(sum, kept);
+    from_eight(add, dropped);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) kept[i] = is_kept(w, i, d) ? kept[i] : dropped[i];
+    to_eight(kept, v);
+}
+
+__device__ __forceinline__ void drop_octet(float (&v)[8], const float (&add)[8], uint64_t f, uint64_t key, uint64_t offset, const Drop& d) {
+    Eight x, w;
+    to_eight(v, x);
+    to_eight(add, w);
+    drop_octet(x, w, f, key, offset, d);
+    from_eight(x, v);
 }
 
 // ---- 8 bits ---------------------------------------------------------------------------------------------------------

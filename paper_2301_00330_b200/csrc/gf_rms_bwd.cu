@@ -182,7 +182,7 @@ __global__ void __launch_bounds__(WARP ? kRmsThreads : kRmsMostThreads, WARP && 
                 }
             }
             if (a.y) {
-                if (a.drop.threshold) drop_octet<false>(v, v, (uint64_t)(e >> 3) + (uint64_t)(k * tpr), key, offset, a.drop);
+                if (a.drop.threshold) drop_octet(v, (uint64_t)(e >> 3) + (uint64_t)(k * tpr), key, offset, a.drop);
                 TX* const p = static_cast<TX*>(a.y) + e + 8 * k * tpr;
                 if (whole) {
                     Octet<TX> o;

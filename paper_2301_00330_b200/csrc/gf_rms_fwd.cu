@@ -99,7 +99,7 @@ __global__ void __launch_bounds__(WARP ? kRmsThreads : kRmsMostThreads, WARP && 
 #pragma unroll
         for (int k = 0; k < NO; ++k) {
             const int c = c0(k);
-            if (a.drop.threshold) drop_octet<true>(v[k], w[k], (uint64_t)(e >> 3) + (uint64_t)(k * tpr), key, offset, a.drop);
+            if (a.drop.threshold) drop_octet(v[k], w[k], (uint64_t)(e >> 3) + (uint64_t)(k * tpr), key, offset, a.drop);
             else {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) v[k][i] = add_pair(v[k][i], w[k][i]);
@@ -220,7 +220,7 @@ template <typename TX, typename TR, bool OUT8> __global__ void __launch_bounds__
             float v[8], w[8];
             ox.get(v);
             r.get(w);
-            if (a.drop.threshold) drop_octet<true>(v, w, (uint64_t)f, key, offset, a.drop);
+            if (a.drop.threshold) drop_octet(v, w, (uint64_t)f, key, offset, a.drop);
             else {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[i] += w[i];

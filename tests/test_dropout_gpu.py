@@ -166,3 +166,21 @@ def test_seeds_follow_torchs_generator_and_a_graph_draws_anew(gf):
         assert torch.equal(y, g)                          # the same mask both ways
         seen.append(y.clone())
     assert not torch.equal(seen[0], seen[1]) and not torch.equal(seen[1], seen[2])
+
+
+@pytest.mark.parametrize("normed", [False, True], ids=["dropout", "norm"])
+@pytest.mark.parametrize("n", [4096, 4099])
+def test_ties_of_the_sum_are_those_of_the_exact_sum(gf, n, normed):
+    """p = 1/4 scales by 4/3, which fp32 holds only nearly.  For x = 3 k the scaled value is the integer 4 k, as the product rounded to
+    fp32 is too (4/3 is off by a third of a step, 2^-25 of it: less than half a step of any product), and its sum with an integer residual below 2^12 is exact in fp32: rounded to
+    bf16 (to even in ties, which fall on many of these sums) the result is that of 64 bits, to the bit."""
+    gen = torch.Generator().manual_seed(5)
+    x = 3.0 * torch.randint(-85, 86, (8, n), generator=gen)
+    residual = torch.randint(-256, 257, (8, n), generator=gen).double()      # (both exact in bf16: 8 bits)
+    seed = torch.tensor([11, 12], device="cuda")
+    xb, rb = x.cuda().bfloat16(), residual.cuda().bfloat16()
+    assert torch.equal(xb.double().cpu(), x.double()) and torch.equal(rb.double().cpu(), residual)
+    kept = gf.dropout(torch.ones(8, n, device="cuda"), 0.25, seed=seed) != 0
+    want = (residual + torch.where(kept.cpu(), x.double() / 3.0 * 4.0, 0.0)).cuda()
+    got = gf.rms_norm(xb, None, residual=rb, p=0.25, seed=seed)[1] if normed else gf.dropout(xb, 0.25, residual=rb, seed=seed)
+    assert torch.equal(got, want.bfloat16())
