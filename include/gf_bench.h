@@ -60,6 +60,13 @@ gf_status gf_selftest_warp_wait(uint32_t* result, int64_t limit_cycles, void* st
  * after the last turn. */
 int32_t gf_selftest_end_of_turn(int32_t turn, int32_t turns, int32_t ok, int32_t met);
 
+/* Which kernel gf_fp8_matmul (gf_block.h) launches for a product on the current device, so that tests can say
+ * which form they reach; found on the host, nothing is launched.  Few rows: 256 times the CTAs of a
+ * cluster.  Many rows: 1, plus 2 for tiles of 128 columns and 4 where the warps store the results
+ * (their rows are not whole 16-byte pieces).  -1: no rows, or a descriptor that is refused. */
+struct gf_fp8_matmul_desc;
+int32_t gf_selftest_fp8_form(const struct gf_fp8_matmul_desc* desc);
+
 /* Name of a kernel id (ids are 0 .. gf_kernel_id_count()-1), NULL if out of range. */
 const char* gf_kernel_name(int32_t kernel_id);
 int32_t gf_kernel_id_count(void);

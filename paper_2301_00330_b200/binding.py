@@ -36,7 +36,7 @@ EXPORTS = (
     "gf_selftest_end_of_turn", "gf_selftest_warp_wait",
     "gf_dropout_forward", "gf_dropout_backward", "gf_rms_norm_forward", "gf_rms_norm_forward_fp8",
     "gf_rms_norm_backward_workspace_bytes", "gf_rms_norm_backward", "gf_fp8_quantize_rows", "gf_fp8_quantize_blocks",
-    "gf_fp8_matmul",
+    "gf_fp8_matmul", "gf_selftest_fp8_form",
 )
 
 
@@ -170,6 +170,7 @@ def lib() -> ctypes.CDLL:
                      "gf_rms_norm_backward_workspace_bytes", "gf_rms_norm_backward", "gf_fp8_quantize_rows",
                      "gf_fp8_quantize_blocks", "gf_fp8_matmul"):
             getattr(L, name).restype = ctypes.c_int
+        L.gf_selftest_fp8_form.argtypes, L.gf_selftest_fp8_form.restype = [pd], i32
         L.gf_selftest_bounded_wait.argtypes = [vp, ctypes.c_int64, vp]
         L.gf_selftest_bounded_wait.restype = ctypes.c_int
         L.gf_selftest_warp_wait.argtypes = [vp, ctypes.c_int64, vp]
@@ -540,6 +541,11 @@ def gf_fp8_matmul(desc: gf_fp8_matmul_desc, a, a_scales, w, w_scales, bias, out,
     """out [M, N] <- A W^T + bias, or with desc.transposed out [M, K] <- A W + bias."""
     _check(lib().gf_fp8_matmul(ctypes.byref(desc), _addr(a), _addr(a_scales), _addr(w), _addr(w_scales), _addr(bias), _addr(out),
                                _raw_stream(stream)), "gf_fp8_matmul")
+
+
+def gf_selftest_fp8_form(desc: gf_fp8_matmul_desc) -> int:
+    """Which kernel gf_fp8_matmul launches (include/gf_bench.h)."""
+    return lib().gf_selftest_fp8_form(ctypes.byref(desc))
 
 
 def gf_selftest_bounded_wait(workspace, limit_cycles: int, stream=None) -> None:

@@ -1,4 +1,5 @@
 // Matrices in 8 bits with scales for groups of 128 (gf_block.h): quantisers, and the product of 8-bit rows with an 8-bit weight.
+#include "gf_bench.h"
 #include "gf_block.h"
 #include "gf_octet.cuh"
 #include "gf_pipe.cuh"
@@ -382,6 +383,15 @@ int few_split(long long tiles, int chunks) {
     return best;
 }
 
+// Rows of A of a tile
+int few_rows(int M) { return M <= 16 ? 16 : M <= 32 ? 32 : 64; }
+// The chunks of a CTA and the CTAs of a cluster
+int few_cluster(const ProductArgs& a, int rows, int& per) {
+    const int split = few_split(cdiv64(a.M, rows) * ((a.J + 127) / 128), a.chunks);
+    per = (a.chunks + split - 1) / split;
+    return (a.chunks + per - 1) / per;
+}
+
 template <int T, typename TO>
 gf_status launch_few(ProductArgs& a, const void* w, const void* codes, int N, int K, int L, long long a_pitch, cudaStream_t s) {
     static size_t configured[kMaxDevices] = {};
@@ -393,9 +403,7 @@ gf_status launch_few(ProductArgs& a, const void* w, const void* codes, int N, in
     if (!make_tmap_u8_2d(&a.tm_a, codes, (uint64_t)L, (uint64_t)a.M, (uint64_t)a_pitch, T)) return GF_ERR_CUDA;
     a.tiles_m = (int)cdiv64(a.M, T);
     const long long tiles = (long long)a.tiles_m * ((a.J + 127) / 128);
-    const int split = few_split(tiles, a.chunks);
-    a.per = (a.chunks + split - 1) / split;
-    a.split = (a.chunks + a.per - 1) / a.per;
+    a.split = few_cluster(a, T, a.per);
     if (tiles * a.split > 0x7fffffffLL) return GF_ERR_UNSUPPORTED;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(tiles * a.split)); cfg.blockDim = dim3(kFewThreads); cfg.dynamicSmemBytes = few_smem(T); cfg.stream = s;
@@ -778,6 +786,7 @@ template <typename TO> __global__ void __launch_bounds__(kWideThreads, 1) fp8_wi
 }
 
 int wide_columns(int J) { return J <= 128 ? 128 : 256; }
+template <typename TO> bool whole_pieces(int J) { return (long long)J * sizeof(TO) % 16 == 0; }
 
 template <typename TO> gf_status launch_wide(ProductArgs& a, const void* w, const void* codes, int N, int K, int L, long long a_pitch, cudaStream_t s) {
     static size_t configured[kMaxDevices] = {};
@@ -791,7 +800,7 @@ template <typename TO> gf_status launch_wide(ProductArgs& a, const void* w, cons
                    : !make_tmap_u8_2d(&a.tm_w, w, (uint64_t)K, (uint64_t)N, (uint64_t)GF_FP8_PITCH(K), (uint32_t)a.bn / 2))
         return GF_ERR_CUDA;
     // (a tile's last columns and rows are cut off by the map)
-    a.out_map = (long long)a.J * sizeof(TO) % 16 == 0;
+    a.out_map = whole_pieces<TO>(a.J);
     if (a.out_map && !make_tmap_swizzled(&a.tm_out, a.out, (int)sizeof(TO), (uint64_t)a.J, (uint64_t)a.M, sizeof(TO) == 2 && a.bn == 256 ? 64u : 32u, 32u)) return GF_ERR_CUDA;
     const long long tiles = (long long)a.tiles_m * ((a.J + a.bn - 1) / a.bn);
     if (tiles > 0x7fffffffLL) return GF_ERR_UNSUPPORTED;
@@ -816,7 +825,7 @@ template <typename TO> gf_status launch_wide(ProductArgs& a, const void* w, cons
 template <typename TO> bool wide_is_faster(const ProductArgs& a) {
     if (a.M <= 32) return false;
     const int bn = wide_columns(a.J);
-    const double by_hand = (long long)a.J * sizeof(TO) % 16 == 0 ? 0.0 : sizeof(TO) == 4 ? 3.5 : 2.7;
+    const double by_hand = whole_pieces<TO>(a.J) ? 0.0 : sizeof(TO) == 4 ? 3.5 : 2.7;
     const double tiles = (double)cdiv64(a.M, 256) * ((a.J + bn - 1) / bn), rounds = (double)(long long)((tiles + sm_count() / 2 - 1) / (sm_count() / 2));
     const double wide = 3.2 + rounds * ((bn == 256 ? 0.55 : 0.3) * a.chunks + 1.3 + by_hand);
     const long long few_tiles = cdiv64(a.M, 64) * ((a.J + 127) / 128);
@@ -827,9 +836,17 @@ template <typename TO> bool wide_is_faster(const ProductArgs& a) {
 
 template <typename TO> gf_status product(ProductArgs& a, const void* w, const void* codes, int N, int K, int L, long long a_pitch, cudaStream_t s) {
     if (wide_is_faster<TO>(a)) return launch_wide<TO>(a, w, codes, N, K, L, a_pitch, s);
-    if (a.M <= 16) return launch_few<16, TO>(a, w, codes, N, K, L, a_pitch, s);
-    if (a.M <= 32) return launch_few<32, TO>(a, w, codes, N, K, L, a_pitch, s);
-    return launch_few<64, TO>(a, w, codes, N, K, L, a_pitch, s);
+    switch (few_rows(a.M)) {
+        case 16: return launch_few<16, TO>(a, w, codes, N, K, L, a_pitch, s);
+        case 32: return launch_few<32, TO>(a, w, codes, N, K, L, a_pitch, s);
+        default: return launch_few<64, TO>(a, w, codes, N, K, L, a_pitch, s);
+    }
+}
+
+template <typename TO> int32_t form(const ProductArgs& a) {
+    if (wide_is_faster<TO>(a)) return 1 | (wide_columns(a.J) == 128 ? 2 : 0) | (whole_pieces<TO>(a.J) ? 0 : 4);
+    int per;
+    return few_cluster(a, few_rows(a.M), per) << 8;
 }
 
 constexpr int kMostDim = 1 << 24;
@@ -838,6 +855,15 @@ gf_status validate(const gf_fp8_desc* d) {
     if (!d) return GF_ERR_NULL;
     if (d->rows < 0 || d->cols < 1 || !is_dtype(d->dtype)) return GF_ERR_BAD_DESC;
     return d->cols > kMostDim ? GF_ERR_UNSUPPORTED : GF_OK;
+}
+
+gf_status validate(const gf_fp8_matmul_desc& d) {
+    if (d.M < 0 || d.N < 1 || d.K < 1 || d.transposed < 0 || d.transposed > 1 || !is_dtype(d.out_dtype) || !is_dtype(d.bias_dtype)) return GF_ERR_BAD_DESC;
+    return d.N > kMostDim || d.K > kMostDim ? GF_ERR_UNSUPPORTED : GF_OK;
+}
+
+void set_sizes(ProductArgs& p, const gf_fp8_matmul_desc& d) {
+    p.M = d.M; p.J = d.transposed ? d.K : d.N; p.chunks = ((d.transposed ? d.N : d.K) + 127) / 128;
 }
 
 gf_status check(const gf_fp8_desc* d, const void* x, const void* codes, const void* scales) {
@@ -892,16 +918,15 @@ gf_status gf_fp8_matmul(const gf_fp8_matmul_desc* desc, const void* a, const flo
                         void* out, void* stream) {
     if (!desc) return GF_ERR_NULL;
     const gf_fp8_matmul_desc& d = *desc;
-    if (d.M < 0 || d.N < 1 || d.K < 1 || d.transposed < 0 || d.transposed > 1 || !is_dtype(d.out_dtype) || !is_dtype(d.bias_dtype)) return GF_ERR_BAD_DESC;
-    if (d.N > kMostDim || d.K > kMostDim) return GF_ERR_UNSUPPORTED;
-    if (d.M == 0) return GF_OK;
+    const gf_status st = validate(d);
+    if (st != GF_OK || d.M == 0) return st;
     if (!a || !a_scales || !w || !w_scales || !out) return GF_ERR_NULL;
     if (off16(a) || off16(a_scales) || off16(w) || off16(w_scales) || off16(bias) || off16(out)) return GF_ERR_ALIGN;
     const int L = d.transposed ? d.N : d.K;                 // contracted
     const long long col_blocks = (d.K + 127) / 128;
     ProductArgs p = {};
     p.sa = a_scales; p.sw = w_scales; p.bias = bias; p.bias_bf16 = d.bias_dtype == GF_BF16; p.out = out;
-    p.M = d.M; p.J = d.transposed ? d.K : d.N; p.chunks = (L + 127) / 128;
+    set_sizes(p, d);
     p.sa_pitch = GF_FP8_SCALE_PITCH((long long)d.M);
     p.sw_j = d.transposed ? 1 : col_blocks;
     p.sw_q = d.transposed ? col_blocks : 1;
@@ -912,6 +937,13 @@ gf_status gf_fp8_matmul(const gf_fp8_matmul_desc* desc, const void* a, const flo
     ProfScope prof(K_FP8_PRODUCT, s);
     const long long a_pitch = GF_FP8_PITCH((long long)L);
     return d.out_dtype == GF_F32 ? product<float>(p, w, a, d.N, d.K, L, a_pitch, s) : product<__nv_bfloat16>(p, w, a, d.N, d.K, L, a_pitch, s);
+}
+
+int32_t gf_selftest_fp8_form(const gf_fp8_matmul_desc* desc) {
+    if (!desc || validate(*desc) != GF_OK || desc->M == 0) return -1;
+    ProductArgs p = {};
+    set_sizes(p, *desc);
+    return desc->out_dtype == GF_F32 ? form<float>(p) : form<__nv_bfloat16>(p);
 }
 
 }  // extern "C"
