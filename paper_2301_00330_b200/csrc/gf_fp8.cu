@@ -16,7 +16,7 @@ bool is_dtype(int d) { return d == GF_F32 || d == GF_BF16; }
 // Rows: sixteen threads (eight, with two octets each, of 16-bit values) have the 128 columns of a scale; a block has 16 (32) rows by 4
 // scales, so that the loads of four octets are on their way at once and the scales of its rows make whole sectors.
 // Bound by memory, for 16-bit values by instructions too (65536 x 512: 17.5 us, 0.88 of the copy bandwidth; 32 bits 26.6, 0.97; with one
-// octet a thread 16 bits took 20.7).  Rows that are not whole octets are put together from two vectors each: 20000 x 1001 bf16 25 us.
+// octet a thread 16 bits took 20.7).  Rows that are not whole octets are put together from two vectors each: 20000 x 1001 bf16 21 us.
 constexpr int kQuantThreads = 256, kQuantGroups = 4;
 template <typename T> constexpr int kQuantEach = sizeof(T) == 2 ? 2 : 1;
 template <typename T> constexpr int kQuantRows = kQuantThreads / (16 / kQuantEach<T>);
@@ -29,6 +29,7 @@ __global__ void __launch_bounds__(kQuantThreads) quantize_rows_kernel(const T* x
     constexpr int E = kQuantEach<T>, kParts = 16 / E, G = kQuantGroups / E;      // loads at once: G groups
     const int part = threadIdx.x % kParts;
     const long long total = rows * cols;
+    uint32_t least = 0xffffffffu;                    // of the scales' orders
     for (long long b = blockIdx.x; b < blocks; b += gridDim.x) {
         const long long row = b / chunks * kQuantRows<T> + threadIdx.x / kParts;
         const int first = (int)(b % chunks) * (128 * kQuantGroups), end = min(pitch, first + 128 * kQuantGroups);
@@ -63,6 +64,7 @@ __global__ void __launch_bounds__(kQuantThreads) quantize_rows_kernel(const T* x
 #pragma unroll
                 for (int s = kParts / 2; s > 0; s >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, s));
                 const float scale = scale_of(m), inv = __frcp_rn(scale);
+                least = min(least, scale_order(scale));
                 if (row < rows && c < pitch) {
                     uint2 w[E];
 #pragma unroll
@@ -74,6 +76,16 @@ __global__ void __launch_bounds__(kQuantThreads) quantize_rows_kernel(const T* x
                 }
             }
         }
+    }
+    if (!__any_sync(0xffffffffu, is_small_order(least))) return;
+    __syncwarp();
+    for (long long b = blockIdx.x; b < blocks; b += gridDim.x) {      // once more: scales and values lie in memory
+        const long long row = b / chunks * kQuantRows<T> + threadIdx.x / kParts;
+        const int first = (int)(b % chunks) * (128 * kQuantGroups), end = min(cols, first + 128 * kQuantGroups);
+        if (row < rows)
+            for (int c = first + part * 8 * E; c < end; c += 128)
+                divide_codes(codes + row * pitch + c, scales[(long long)(c >> 7) * scale_pitch + row], min(8 * E, cols - c),
+                             [&](int i) { return to_f32(x[row * cols + c + i]); });
     }
 }
 
@@ -116,8 +128,11 @@ template <typename T> __global__ void __launch_bounds__(kQuantThreads) quantize_
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 if (c + i >= cols) v[i] = 0.f;
-            if (row < rows && c < pitch)
-                *reinterpret_cast<uint2*>(codes + row * pitch + c) = codes8(v, scale, inv, cols - c);
+            if (row < rows && c < pitch) {
+                uint8_t* const to = codes + row * pitch + c;
+                *reinterpret_cast<uint2*>(to) = codes8(v, scale, inv, cols - c);
+                divide_codes(to, scale, min(8, cols - c), [&](int i) { return to_f32(x[row * cols + c + i]); });
+            }
         }
         if (threadIdx.x == 0) scales[b] = scale;
     }
