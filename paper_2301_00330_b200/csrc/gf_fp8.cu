@@ -6,6 +6,8 @@
 #include "gf_tc.cuh"
 #include "gf_tma.cuh"
 
+#include <type_traits>
+
 namespace gf {
 namespace {
 
@@ -200,6 +202,22 @@ __device__ __forceinline__ float bias_at(const ProductArgs& p, int j) {
     return p.bias_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p.bias)[j]) : static_cast<const float*>(p.bias)[j];
 }
 
+// A row's scale times a block's, where that product is no normal number of fp32 (rows of zeros have the smallest scale, 2^-126): the sum
+// of a chunk, zero or a multiple of 2^-18 below 2^25, is taken `first` times, which is exact, and then `then` times.  Asked for every
+// chunk before its accumulator is waited for, and the other way of adding stands apart, so that sums under normal products are not held up
+// (4096 x 8192 x 4096 151 -> 153 us; with a row of zeros in a hundred 150 -> 175, 65536 x 2048 x 512 110 -> 113).
+constexpr float kFirst = 0x1p100f;
+struct TwoFactors {
+    float first, then;
+};
+__device__ __forceinline__ bool is_normal(float s) { return fabsf(s) >= 0x1p-126f && fabsf(s) < INFINITY; }
+__device__ __forceinline__ TwoFactors two_factors(float a, float w) {
+    const float s = a * w, most = fmaxf(fabsf(a), fabsf(w)), least = fminf(fabsf(a), fabsf(w));
+    if (fabsf(s) < 0x1p-126f) return {1.f / kFirst, copysignf(least * kFirst * most, s)};       // (below 2^-226 nothing is left either way)
+    if (isinf(s) && most < INFINITY) return {kFirst, copysignf(fminf(most * (1.f / kFirst) * least, 0x1.fffffep127f), s)};      // finite: zero stays zero
+    return {1.f, s};
+}
+
 // A tile is 128 columns of the result (rows of the accumulator) by T of its rows, so that the weight is the operand of
 // 128 and few rows of A cost no more than they are.  The chunks of a tile are split over a cluster of CTAs where there
 // are few tiles, and the parts are added through distributed shared memory, in the order of the CTAs.
@@ -219,6 +237,8 @@ template <int T, typename TO> __global__ void __launch_bounds__(kFewThreads) fp8
     __shared__ uint64_t full[kStages], empty[kStages], done[kBuffers], drained[kBuffers];
     __shared__ uint32_t tmem_base;
     __shared__ __align__(16) float scale[kFewScales][T];
+    __shared__ __align__(16) __nv_bfloat16 first[kFewScales][T];      // and factors before them (two_factors), powers of two
+    __shared__ int any_first;                            // other than 1 so far; written and read on either side of the scales' barriers
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     const int rank = (int)(blockIdx.x % (unsigned)p.split), tile = (int)(blockIdx.x / (unsigned)p.split);
     const int m0 = tile % p.tiles_m * T, j0 = tile / p.tiles_m * 128;
@@ -226,6 +246,7 @@ template <int T, typename TO> __global__ void __launch_bounds__(kFewThreads) fp8
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
         for (int s = 0; s < kBuffers; ++s) { mbar_init(&done[s], 1); mbar_init(&drained[s], 4); }
+        any_first = 0;
         mbar_fence_init();
     }
     pdl_wait();
@@ -278,26 +299,24 @@ template <int T, typename TO> __global__ void __launch_bounds__(kFewThreads) fp8
         uint64_t acc[T / 2];
 #pragma unroll
         for (int i = 0; i < T / 2; ++i) acc[i] = 0;
-        for (int q = 0; q < n; ++q) {
-            const int buf = q % kBuffers, held = q % kFewScales;
-            if (held == 0) {                             // the scales of the next chunks: by all four warps, for all
-                if (q > 0) asm volatile("bar.sync 1, 128;" ::: "memory");
-                for (int i = t; i < min(kFewScales, n - q) * T; i += 128) {
-                    const int m = m0 + i % T;
-                    const long long at = q0 + q + i / T;
-                    scale[i / T][i % T] = m < p.M ? p.sa[at * p.sa_pitch + m] * sw[at * p.sw_q] : 0.f;
-                }
-                asm volatile("bar.sync 1, 128;" ::: "memory");
-            }
-            // (after a wait that ran out a warp has part in the barriers above still, and in nothing else)
-            if (ok) ok = mbar_wait_warp(&done[buf], (uint32_t)(q / kBuffers) & 1u);
-            if (!ok) continue;
-            tc_fence_after_sync();
+        // adds the accumulator of a chunk under its scales
+        auto add = [&](auto with_first, int buf, int held) {
 #pragma unroll
             for (int c = 0; c < T; c += 16) {
                 uint32_t raw[16];
                 tmem_ld16(lanes + (uint32_t)(buf * T + c), raw);
                 tmem_ld_wait_for(raw);
+                if constexpr (decltype(with_first)::value) {
+#pragma unroll
+                    for (int h = 0; h < 16; h += 8) {
+                        Octet<__nv_bfloat16> o;
+                        float f[8];
+                        o.load(&first[held][c + h]);
+                        o.get(f);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) raw[h + i] = __float_as_uint(__uint_as_float(raw[h + i]) * f[i]);
+                    }
+                }
 #pragma unroll
                 for (int i = 0; i < 16; i += 4) {
                     const ulonglong2 s = *reinterpret_cast<const ulonglong2*>(&scale[held][c + i]);
@@ -306,6 +325,36 @@ template <int T, typename TO> __global__ void __launch_bounds__(kFewThreads) fp8
                     a[1] = fma_pair(pair_of(__uint_as_float(raw[i + 2]), __uint_as_float(raw[i + 3])), s.y, a[1]);
                 }
             }
+        };
+        for (int q = 0; q < n; ++q) {
+            const int buf = q % kBuffers, held = q % kFewScales;
+            if (held == 0) {                             // the scales of the next chunks: by all four warps, for all
+                if (q > 0) asm volatile("bar.sync 1, 128;" ::: "memory");
+                for (int i = t; i < min(kFewScales, n - q) * T; i += 128) {
+                    const int m = m0 + i % T;
+                    const long long at = q0 + q + i / T;
+                    float s = 0.f, before = 1.f;
+                    if (m < p.M) {
+                        const float a = p.sa[at * p.sa_pitch + m], w = sw[at * p.sw_q];
+                        s = a * w;
+                        if (!is_normal(s)) {
+                            const TwoFactors f = two_factors(a, w);
+                            s = f.then;
+                            before = f.first;
+                            any_first = 1;
+                        }
+                    }
+                    scale[i / T][i % T] = s;
+                    first[i / T][i % T] = __float2bfloat16_rn(before);
+                }
+                asm volatile("bar.sync 1, 128;" ::: "memory");
+            }
+            // (after a wait that ran out a warp has part in the barriers above still, and in nothing else)
+            if (ok) ok = mbar_wait_warp(&done[buf], (uint32_t)(q / kBuffers) & 1u);
+            if (!ok) continue;
+            tc_fence_after_sync();
+            if (any_first) add(std::true_type(), buf, held);
+            else add(std::false_type(), buf, held);
             tc_fence_before_sync();
             __syncwarp();
             if (lane == 0) mbar_arrive(&drained[buf]);
@@ -737,13 +786,11 @@ template <typename TO> __global__ void __launch_bounds__(kWideThreads, 1) fp8_wi
                 if (j0 + lane < p.J) bias0 = bias_at(p, j0 + lane);
                 if (cols == 64 && j0 + 32 + lane < p.J) bias1 = bias_at(p, j0 + 32 + lane);
             }
-            for (int q = 0; q < p.chunks && ok; ++q, ++n) {
-                const uint32_t buf = n & (buffers - 1u);
-                const float now = a_next * w_next;
-                const uint64_t scale = pair_of(now, now);
-                fetch();
+            // waits for a chunk's accumulator and adds it (twice in the code, so that nothing is asked between the wait and the sums)
+            auto add = [&](auto with_first, uint32_t buf, TwoFactors f) {
+                const uint64_t scale = pair_of(f.then, f.then);
                 ok = mbar_wait_warp(&done[buf], (n >> shift) & 1u);
-                if (!ok) break;
+                if (!ok) return;
                 tc_fence_after_sync();
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
@@ -757,10 +804,22 @@ template <typename TO> __global__ void __launch_bounds__(kWideThreads, 1) fp8_wi
                             if (lane == 0) arrive_leader(&drained[buf]);
                         }
 #pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            acc[c * 16 + i] = fma_pair(pair_of(__uint_as_float(raw[2 * i]), __uint_as_float(raw[2 * i + 1])), scale, acc[c * 16 + i]);
+                        for (int i = 0; i < 16; ++i) {
+                            uint64_t v = pair_of(__uint_as_float(raw[2 * i]), __uint_as_float(raw[2 * i + 1]));
+                            if constexpr (decltype(with_first)::value) v = mul_pair(v, pair_of(f.first, f.first));
+                            acc[c * 16 + i] = fma_pair(v, scale, acc[c * 16 + i]);
+                        }
                     }
                 }
+            };
+            for (int q = 0; q < p.chunks && ok; ++q, ++n) {
+                const uint32_t buf = n & (buffers - 1u);
+                const float a_now = a_next, w_now = w_next, now = a_now * w_now;
+                const bool normal = __all_sync(0xffffffffu, is_normal(now));
+                fetch();
+                if (normal) add(std::false_type(), buf, TwoFactors{1.f, now});
+                else add(std::true_type(), buf, two_factors(a_now, w_now));
+                if (!ok) break;
             }
             if (!ok) break;
             if (row0 >= p.M || j0 >= p.J) continue;
