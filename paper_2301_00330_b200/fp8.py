@@ -14,6 +14,7 @@ import torch
 from torch.autograd.function import once_differentiable
 
 from . import binding as B
+from .autograd import FilteredConv2d
 from .dropout import _check_p, _seed_for
 from .norm import _dense
 from .rms import _check_args, _norm_backward, _norm_desc
@@ -166,12 +167,16 @@ class Fp8Linear(torch.nn.Module):
 
     @classmethod
     def from_layer(cls, layer: torch.nn.Module) -> "Fp8Linear":
-        """From a torch.nn.Linear, or a 1 x 1 convolution (torch's or FilteredConv2d) of stride 1 without groups."""
-        w = layer.weight
-        if w.dim() == 2:
-            return cls(w, layer.bias)
-        stride, padding = getattr(layer, "stride", 1), getattr(layer, "padding", 0)
-        if w.dim() != 4 or w.shape[2:] != (1, 1) or layer.groups != 1 or stride not in (1, (1, 1)) or padding not in (0, (0, 0), "same", "valid"):
+        """From a torch.nn.Linear, or a 1 x 1 convolution (torch.nn.Conv2d or FilteredConv2d) of stride 1 without groups.
+
+        Other layers are refused, whatever their weight's shape: some keep it the other way round (torch.nn.ConvTranspose2d).  The gradient
+        of a FilteredConv2d's input is a filtered one; that of the layer made from it is not, and is off only by the 8 bits."""
+        if isinstance(layer, torch.nn.Linear):
+            return cls(layer.weight, layer.bias)
+        if not isinstance(layer, (torch.nn.Conv2d, FilteredConv2d)):
+            raise ValueError(f"a linear layer or a 1 x 1 convolution expected, got {type(layer).__name__}")
+        w, stride, padding = layer.weight, layer.stride, getattr(layer, "padding", 0)      # (a FilteredConv2d of 1 x 1 has none)
+        if w.shape[2:] != (1, 1) or layer.groups != 1 or stride not in (1, (1, 1)) or padding not in (0, (0, 0), "same", "valid"):
             raise ValueError("a linear layer, or a 1 x 1 convolution of stride 1 without groups or padding, expected")
         return cls(w, layer.bias, channel_dim=1)
 

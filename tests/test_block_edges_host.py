@@ -1,4 +1,6 @@
 """Calls of the residual-block operators (include/gf_block.h) at the ends of what they take, as far as the host decides."""
+import pytest
+import torch
 
 
 def test_which_product_kernel(gf):
@@ -11,3 +13,19 @@ def test_which_product_kernel(gf):
         for M in (1, 16, 17, 32):
             form = f(mk(M, 4096, 4096, transposed=t))
             assert form & 255 == 0 and 1 <= form >> 8 <= 8
+
+
+def test_frozen_layers_are_made_of_layers_whose_weight_is_known(gf):
+    """A weight of the right shape is not enough: a transposed convolution keeps it as [in, out, 1, 1], others as [in, out]."""
+    class Other(torch.nn.Module):
+        def __init__(self):
+            super().__init__()
+            self.weight, self.bias = torch.nn.Parameter(torch.zeros(8, 8)), None
+
+    for layer in (torch.nn.ConvTranspose2d(8, 8, 1), torch.nn.ConvTranspose2d(8, 12, 1, bias=False), Other(), torch.nn.Embedding(8, 8),
+                  torch.nn.Conv1d(8, 8, 1), torch.nn.Conv2d(8, 8, 1, stride=2), torch.nn.LayerNorm(8)):
+        with pytest.raises(ValueError):
+            gf.Fp8Linear.from_layer(layer)
+    for layer in (torch.nn.Linear(8, 12), torch.nn.Conv2d(8, 12, 1), gf.FilteredConv2d(8, 12, 1)):      # on to the quantiser
+        with pytest.raises(RuntimeError, match="no CPU path"):
+            gf.Fp8Linear.from_layer(layer)
