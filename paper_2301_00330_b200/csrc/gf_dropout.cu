@@ -20,6 +20,7 @@ Drop make_drop(float p, const uint64_t* seed) {
 namespace {
 
 constexpr int kThreads = 256, kEach = 2;
+constexpr int64_t kMostCount = 0x7fffffffLL * (kThreads * kEach * 8);      // blocks of a grid
 
 // kEach octets a thread, the loads of all on their way before the first is computed
 template <typename TX, typename TY, bool RESIDUAL>
@@ -95,7 +96,7 @@ gf_status run(const gf_dropout_desc* desc, const void* x, int x_dtype, const voi
 gf_status validate(const gf_dropout_desc* d) {
     if (!d) return GF_ERR_NULL;
     if (d->count < 0 || !valid_p(d->p) || !is_dtype(d->dtype) || !is_dtype(d->out_dtype)) return GF_ERR_BAD_DESC;
-    return d->count > (int64_t)1 << 43 ? GF_ERR_UNSUPPORTED : GF_OK;      // (blocks are counted in 31 bits)
+    return d->count > kMostCount ? GF_ERR_UNSUPPORTED : GF_OK;
 }
 
 }  // namespace

@@ -1,4 +1,6 @@
 """Calls of the residual-block operators (include/gf_block.h) at the ends of what they take, as far as the host decides."""
+import ctypes
+
 import pytest
 import torch
 
@@ -29,3 +31,13 @@ def test_frozen_layers_are_made_of_layers_whose_weight_is_known(gf):
     for layer in (torch.nn.Linear(8, 12), torch.nn.Conv2d(8, 12, 1), gf.FilteredConv2d(8, 12, 1)):      # on to the quantiser
         with pytest.raises(RuntimeError, match="no CPU path"):
             gf.Fp8Linear.from_layer(layer)
+
+
+def test_counts_that_no_grid_holds_are_refused(gf):
+    """A block has 4096 elements and a grid 2^31 - 1 blocks; the refusal comes before anything is launched."""
+    a = ctypes.c_void_p(0x1000)                          # never dereferenced
+    most = ((1 << 31) - 1) * 4096
+    for count in (most + 1, most + 2, 1 << 43, (1 << 43) + 1, (1 << 63) - 1):
+        d = gf.make_dropout_desc(count, p=0.5)
+        assert gf.lib().gf_dropout_forward(ctypes.byref(d), a, a, a, a, None) == gf.GF_ERR_UNSUPPORTED
+        assert gf.lib().gf_dropout_backward(ctypes.byref(d), a, a, a, None) == gf.GF_ERR_UNSUPPORTED
