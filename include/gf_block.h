@@ -39,10 +39,11 @@ typedef struct gf_dropout_desc {
     float p;                /* 0 .. 1 */
 } gf_dropout_desc;
 
-/* residual NULL: none.  y may be x or residual (in place) where the dtypes are the same. */
+/* residual NULL: none.  y may be residual (in place), or x where the dtypes are the same; else, as everywhere here
+ * where an output would lie over an input of another type, GF_ERR_UNSUPPORTED. */
 gf_status gf_dropout_forward(const gf_dropout_desc* desc, const void* x, const void* residual,
                              const uint64_t* seed, void* y, void* stream);
-/* g_x may be g_y. */
+/* g_x may be g_y where the dtypes are the same. */
 gf_status gf_dropout_backward(const gf_dropout_desc* desc, const void* g_y, const uint64_t* seed,
                               void* g_x, void* stream);
 
@@ -68,7 +69,7 @@ typedef struct gf_rms_desc {
 } gf_rms_desc;
 
 /* gamma NULL: ones.  residual NULL: h = dropout(x).  h: required but where it is x, then NULL; it
- * may be residual, or x, and y may be x (in place).  rstd NULL: not wanted. */
+ * may be residual, or x where the dtypes are the same, and y may be x (in place).  rstd NULL: not wanted. */
 gf_status gf_rms_norm_forward(const gf_rms_desc* desc, const void* x, const void* residual,
                               const uint64_t* seed, const void* gamma, void* h, void* y, float* rstd,
                               void* stream);
@@ -80,8 +81,8 @@ gf_status gf_rms_norm_forward_fp8(const gf_rms_desc* desc, const void* x, const 
 
 /* h (or x, where h is x) and rstd from the forward pass; gamma NULL: ones; g_h NULL: zeros.
  * g_residual, g_x and g_gamma may each be NULL and are then skipped; with p = 0 and one dtype g_x and
- * g_residual are the same values.  g_residual may be g_h or g_y, g_x may be g_y (in place).  The workspace
- * may be NULL where its size is 0. */
+ * g_residual are the same values.  g_residual may be g_h, or g_y where the dtypes are the same, and g_x may be g_y
+ * (in place).  The workspace may be NULL where its size is 0. */
 gf_status gf_rms_norm_backward_workspace_bytes(const gf_rms_desc* desc, size_t* bytes);
 gf_status gf_rms_norm_backward(const gf_rms_desc* desc, const void* g_y, const void* g_h, const void* h,
                                const float* rstd, const void* gamma, const uint64_t* seed, void* g_residual,

@@ -85,6 +85,7 @@ gf_status run(const gf_dropout_desc* desc, const void* x, int x_dtype, const voi
     const Drop d = make_drop(desc->p, seed);
     if (!x || !y || (d.threshold && !seed)) return GF_ERR_NULL;
     if (off16(x) || off16(y) || off16(residual) || (reinterpret_cast<uintptr_t>(seed) & 7u) != 0) return GF_ERR_ALIGN;
+    if (x_dtype != y_dtype && y == x) return GF_ERR_UNSUPPORTED;          // an element's place is not its result's
     if (x_dtype == GF_F32) {
         if (y_dtype == GF_F32) return launch<float, float>(x, residual, y, desc->count, d, s);
         return launch<float, __nv_bfloat16>(x, residual, y, desc->count, d, s);

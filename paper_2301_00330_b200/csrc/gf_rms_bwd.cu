@@ -385,6 +385,7 @@ gf_status gf_rms_norm_backward(const gf_rms_desc* desc, const void* g_y, const v
     if (rms_off16(g_y) || rms_off16(g_h) || rms_off16(h) || rms_off16(rstd) || rms_off16(gamma) || rms_off16(g_residual) || rms_off16(g_x) ||
         rms_off16(workspace) || (reinterpret_cast<uintptr_t>(seed) & 7u) != 0)
         return GF_ERR_ALIGN;
+    if (desc->dtype != desc->residual_dtype && g_residual == g_y) return GF_ERR_UNSUPPORTED;      // an element's place is not its gradient's
     if ((g_gamma || p.tiles) && workspace_bytes < p.bytes) return GF_ERR_WORKSPACE;
     a.gy = g_y; a.gh = g_h; a.h = const_cast<void*>(h); a.rstd_in = rstd; a.gamma = gamma; a.gamma_bf16 = desc->param_dtype == GF_BF16;
     a.gres = g_residual; a.y = g_x;

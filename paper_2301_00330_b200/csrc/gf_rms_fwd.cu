@@ -344,6 +344,7 @@ template <bool OUT8> gf_status run(const gf_rms_desc* d, const void* x, const vo
     if (rms_off16(x) || rms_off16(residual) || rms_off16(gamma) || rms_off16(h) || rms_off16(y) || rms_off16(codes) || rms_off16(scales) ||
         rms_off16(rstd) || (reinterpret_cast<uintptr_t>(seed) & 7u) != 0)
         return GF_ERR_ALIGN;
+    if (d->dtype != d->residual_dtype && h == x) return GF_ERR_UNSUPPORTED;       // an element's place is not its sum's
     a.x = x; a.residual = residual; a.gamma = gamma; a.gamma_bf16 = d->param_dtype == GF_BF16;
     a.h = h;
     a.y = y; a.codes = static_cast<uint8_t*>(codes); a.scales = scales; a.rstd = rstd;

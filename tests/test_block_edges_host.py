@@ -41,3 +41,21 @@ def test_counts_that_no_grid_holds_are_refused(gf):
         d = gf.make_dropout_desc(count, p=0.5)
         assert gf.lib().gf_dropout_forward(ctypes.byref(d), a, a, a, a, None) == gf.GF_ERR_UNSUPPORTED
         assert gf.lib().gf_dropout_backward(ctypes.byref(d), a, a, a, None) == gf.GF_ERR_UNSUPPORTED
+
+
+def test_no_output_over_an_input_of_another_type(gf):
+    """In place, an element's result would lie where another element is still to be read."""
+    L, vp = gf.lib(), ctypes.c_void_p
+    a, b, c, d = (vp(0x1000 * k) for k in (1, 2, 3, 4))      # never dereferenced: all calls fail on the host
+    for xt, yt in ((gf.GF_F32, gf.GF_BF16), (gf.GF_BF16, gf.GF_F32)):
+        desc = ctypes.byref(gf.make_dropout_desc(64, dtype=xt, out_dtype=yt, p=0.5))
+        assert L.gf_dropout_forward(desc, a, b, c, a, None) == gf.GF_ERR_UNSUPPORTED
+        assert L.gf_dropout_forward(desc, a, None, c, a, None) == gf.GF_ERR_UNSUPPORTED
+        assert L.gf_dropout_backward(desc, a, c, a, None) == gf.GF_ERR_UNSUPPORTED
+    for cols in (8, 1001, 9000):
+        rms = gf.make_rms_desc(4, cols, dtype=gf.GF_BF16, residual_dtype=gf.GF_F32)
+        need = gf.gf_rms_norm_backward_workspace_bytes(rms)
+        desc = ctypes.byref(rms)
+        assert L.gf_rms_norm_forward(desc, a, b, None, None, a, c, None, None) == gf.GF_ERR_UNSUPPORTED
+        assert L.gf_rms_norm_forward_fp8(desc, a, b, None, None, a, c, d, None, None) == gf.GF_ERR_UNSUPPORTED
+        assert L.gf_rms_norm_backward(desc, a, None, b, c, None, None, a, None, None, d, need, None) == gf.GF_ERR_UNSUPPORTED
