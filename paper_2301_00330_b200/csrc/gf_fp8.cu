@@ -151,7 +151,8 @@ struct ProductArgs {
     void* out;
     uint32_t* err_word;
     long long sa_pitch, sw_j, sw_q;      // strides of the scales: rows of sa; blocks of columns and chunks of sw
-    int M, J, chunks, per, split;        // per: chunks of a CTA of a cluster of `split`
+    int M, J, chunks, split;
+    int share, longer;                   // few: of the `split` CTAs of a cluster the first `longer` have share + 1 chunks, the others share
     int tiles_m, bias_bf16;
     int bn;                              // wide: columns of a tile
     int out_map;                         // wide: results leave by the copy engine (their rows are whole 16-byte pieces)
@@ -242,7 +243,7 @@ template <int T, typename TO> __global__ void __launch_bounds__(kFewThreads) fp8
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     const int rank = (int)(blockIdx.x % (unsigned)p.split), tile = (int)(blockIdx.x / (unsigned)p.split);
     const int m0 = tile % p.tiles_m * T, j0 = tile / p.tiles_m * 128;
-    const int q0 = rank * p.per, n = min(p.per, p.chunks - q0);
+    const int q0 = rank * p.share + min(rank, p.longer), n = p.share + (rank < p.longer);
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
         for (int s = 0; s < kBuffers; ++s) { mbar_init(&done[s], 1); mbar_init(&drained[s], 4); }
@@ -438,23 +439,26 @@ template <int T, typename TO> __global__ void __launch_bounds__(kFewThreads) fp8
 }
 
 // CTAs that share the chunks of a tile, up to two per SM in all, by what that takes in microseconds: 0.6 a chunk, 1.5 for the cluster
-// and its joining and 0.15 more for each of its CTAs.  Powers of two: clusters of 3 took up to twice the time.
-double few_time(int chunks, int split) { return 0.6 * ((chunks + split - 1) / split) + (split > 1 ? 1.5 + 0.15 * split : 0.0); }
-int few_split(long long tiles, int chunks) {
+// and its joining and 0.15 more for each of its CTAs.  Halves, quarters and eighths are considered, each with as many CTAs as it has
+// shares: 6 of 3 chunks for 17 and 18 (8 x 2304 x 2304 4.9 us; dealt to 8 it takes 5.4).  Only 3 are 4 instead (8 x 768 x 768 3.4 us for 3.7,
+// 100 x 768 x 768 5.2 for 5.7).
+int few_ctas(int chunks, int split) {
+    const int share = (chunks + split - 1) / split, ctas = (chunks + share - 1) / share;
+    return ctas == 3 ? 4 : ctas;
+}
+double few_time(int chunks, int ctas) { return 0.6 * ((chunks + ctas - 1) / ctas) + (ctas > 1 ? 1.5 + 0.15 * ctas : 0.0); }
+int few_cluster(long long tiles, int chunks) {
     int best = 1;
-    for (int split = 2; split <= 8 && split <= chunks && split * tiles <= 2LL * sm_count(); split *= 2)
-        if (few_time(chunks, split) < few_time(chunks, best)) best = split;
+    for (int split = 2; split <= 8 && split <= chunks && split * tiles <= 2LL * sm_count(); split *= 2) {
+        const int ctas = few_ctas(chunks, split);
+        if (few_time(chunks, ctas) < few_time(chunks, best)) best = ctas;
+    }
     return best;
 }
 
 // Rows of A of a tile
 int few_rows(int M) { return M <= 16 ? 16 : M <= 32 ? 32 : 64; }
-// The chunks of a CTA and the CTAs of a cluster
-int few_cluster(const ProductArgs& a, int rows, int& per) {
-    const int split = few_split(cdiv64(a.M, rows) * ((a.J + 127) / 128), a.chunks);
-    per = (a.chunks + split - 1) / split;
-    return (a.chunks + per - 1) / per;
-}
+int few_cluster(const ProductArgs& a, int rows) { return few_cluster(cdiv64(a.M, rows) * ((a.J + 127) / 128), a.chunks); }
 
 template <int T, typename TO>
 gf_status launch_few(ProductArgs& a, const void* w, const void* codes, int N, int K, int L, long long a_pitch, cudaStream_t s) {
@@ -467,7 +471,9 @@ gf_status launch_few(ProductArgs& a, const void* w, const void* codes, int N, in
     if (!make_tmap_u8_2d(&a.tm_a, codes, (uint64_t)L, (uint64_t)a.M, (uint64_t)a_pitch, T)) return GF_ERR_CUDA;
     a.tiles_m = (int)cdiv64(a.M, T);
     const long long tiles = (long long)a.tiles_m * ((a.J + 127) / 128);
-    a.split = few_cluster(a, T, a.per);
+    a.split = few_cluster(a, T);
+    a.share = a.chunks / a.split;
+    a.longer = a.chunks % a.split;
     if (tiles * a.split > 0x7fffffffLL) return GF_ERR_UNSUPPORTED;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(tiles * a.split)); cfg.blockDim = dim3(kFewThreads); cfg.dynamicSmemBytes = few_smem(T); cfg.stream = s;
@@ -903,7 +909,7 @@ template <typename TO> bool wide_is_faster(const ProductArgs& a) {
     const double tiles = (double)cdiv64(a.M, 256) * ((a.J + bn - 1) / bn), rounds = (double)(long long)((tiles + sm_count() / 2 - 1) / (sm_count() / 2));
     const double wide = 3.2 + rounds * ((bn == 256 ? 0.55 : 0.3) * a.chunks + 1.3 + by_hand);
     const long long few_tiles = cdiv64(a.M, 64) * ((a.J + 127) / 128);
-    const double alone = few_time(a.chunks, few_split(few_tiles, a.chunks)), each = 0.46 * a.chunks;
+    const double alone = few_time(a.chunks, few_cluster(a, 64)), each = 0.46 * a.chunks;
     const double all = (each > 1.8 ? each : 1.8) * (double)few_tiles / sm_count();
     return wide < 3.5 + (alone > all ? alone : all);
 }
@@ -919,8 +925,7 @@ template <typename TO> gf_status product(ProductArgs& a, const void* w, const vo
 
 template <typename TO> int32_t form(const ProductArgs& a) {
     if (wide_is_faster<TO>(a)) return 1 | (wide_columns(a.J) == 128 ? 2 : 0) | (whole_pieces<TO>(a.J) ? 0 : 4);
-    int per;
-    return few_cluster(a, few_rows(a.M), per) << 8;
+    return few_cluster(a, few_rows(a.M)) << 8;
 }
 
 constexpr int kMostDim = 1 << 24;

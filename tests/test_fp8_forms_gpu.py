@@ -55,3 +55,15 @@ def test_every_number_of_chunks_of_few_rows(gf, M, chunks, transposed):
     out = DTYPES[chunks % 2]
     assert not gf.gf_selftest_fp8_form(gf.make_fp8_matmul_desc(M, N, K, transposed=transposed, out_dtype=out)) & WIDE
     _check_product(*_product(gf, M, N, K, transposed, out, F32, seed=M + chunks), transposed)
+
+
+def test_clusters_have_no_idle_cta(gf):
+    """As many CTAs as there are shares of a half, quarter or eighth of the chunks, rounded up; not 3."""
+    seen = set()
+    for chunks in range(1, 200):
+        for M, N in ((4, 640), (40, 640), (120, 640), (4, 10240)):       # (80 tiles: clusters of 2 at most)
+            ctas = gf.gf_selftest_fp8_form(gf.make_fp8_matmul_desc(M, N, 128 * chunks, out_dtype=BF16)) >> 8
+            if ctas:
+                assert 1 <= ctas <= min(8, chunks) and ctas != 3
+                seen.add(ctas)
+    assert seen >= {1, 2, 4, 5, 6, 7, 8}
