@@ -204,9 +204,10 @@ __device__ __forceinline__ float bias_at(const ProductArgs& p, int j) {
 }
 
 // A row's scale times a block's, where that product is no normal number of fp32 (rows of zeros have the smallest scale, 2^-126): the sum
-// of a chunk, zero or a multiple of 2^-18 below 2^25, is taken `first` times, which is exact, and then `then` times.  Asked for every
-// chunk before its accumulator is waited for, and the other way of adding stands apart, so that sums under normal products are not held up
-// (4096 x 8192 x 4096 151 -> 153 us; with a row of zeros in a hundred 150 -> 175, 65536 x 2048 x 512 110 -> 113).
+// of a chunk, zero or a multiple of 2^-18 below 2^25, is taken `first` times, which is exact, and then `then` times.  That way of adding
+// stands apart, so that sums under normal products are not held up (for many rows the warp that has waited asks with the vote that ends
+// its wait: the gradient of 4096 x 8192 x 4096 takes 155.6 us, 154.3 without the question, with a row of zeros in a hundred 183.8 and 150.8;
+// 65536 x 2048 x 512 112.6 and 112.4, 115.3 and 112.1).
 constexpr float kFirst = 0x1p100f;
 struct TwoFactors {
     float first, then;
@@ -792,11 +793,9 @@ template <typename TO> __global__ void __launch_bounds__(kWideThreads, 1) fp8_wi
                 if (j0 + lane < p.J) bias0 = bias_at(p, j0 + lane);
                 if (cols == 64 && j0 + 32 + lane < p.J) bias1 = bias_at(p, j0 + 32 + lane);
             }
-            // waits for a chunk's accumulator and adds it (twice in the code, so that nothing is asked between the wait and the sums)
+            // adds a chunk's accumulator
             auto add = [&](auto with_first, uint32_t buf, TwoFactors f) {
                 const uint64_t scale = pair_of(f.then, f.then);
-                ok = mbar_wait_warp(&done[buf], (n >> shift) & 1u);
-                if (!ok) return;
                 tc_fence_after_sync();
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
@@ -821,11 +820,14 @@ template <typename TO> __global__ void __launch_bounds__(kWideThreads, 1) fp8_wi
             for (int q = 0; q < p.chunks && ok; ++q, ++n) {
                 const uint32_t buf = n & (buffers - 1u);
                 const float a_now = a_next, w_now = w_next, now = a_now * w_now;
-                const bool normal = __all_sync(0xffffffffu, is_normal(now));
                 fetch();
-                if (normal) add(std::false_type(), buf, TwoFactors{1.f, now});
-                else add(std::true_type(), buf, two_factors(a_now, w_now));
-                if (!ok) break;
+                const bool normal = is_normal(now), there = mbar_wait_bounded(&done[buf], (n >> shift) & 1u);
+                if (__all_sync(0xffffffffu, there && normal)) add(std::false_type(), buf, TwoFactors{1.f, now});
+                else {
+                    ok = __all_sync(0xffffffffu, there);
+                    if (!ok) break;
+                    add(std::true_type(), buf, two_factors(a_now, w_now));
+                }
             }
             if (!ok) break;
             if (row0 >= p.M || j0 >= p.J) continue;
