@@ -224,8 +224,8 @@ __device__ __forceinline__ TwoFactors two_factors(float a, float w) {
 // 128 and few rows of A cost no more than they are.  The chunks of a tile are split over a cluster of CTAs where there
 // are few tiles, and the parts are added through distributed shared memory, in the order of the CTAs.
 //   warp 0: copies; warp 1: products; warps 2 to 5: scaling, a quarter of the accumulator's rows each.
-// Bound by latency: 8 x 4096 x 4096 6.2 us, of which its bytes take 2.6 (16.8 MB from memory; a launch, one round of copies, four chunks,
-// two meetings of the cluster); 8 x 768 x 768 3.4.
+// Bound by latency: 8 x 4096 x 4096 6.2 to 6.9 us, of which its bytes take 2.6 (16.8 MB from memory; a launch, one round of copies, four chunks,
+// two meetings of the cluster); 8 x 768 x 768 3.4 to 3.8.
 constexpr int kFewThreads = 192;
 __host__ __device__ constexpr int few_stages(int T) { return T <= 32 ? 4 : 3; }
 __host__ __device__ constexpr int few_buffers(int T) { return T <= 32 ? 4 : 2; }      // accumulators
@@ -301,65 +301,71 @@ template <int T, typename TO> __global__ void __launch_bounds__(kFewThreads) fp8
         uint64_t acc[T / 2];
 #pragma unroll
         for (int i = 0; i < T / 2; ++i) acc[i] = 0;
-        // adds the accumulator of a chunk under its scales
-        auto add = [&](auto with_first, int buf, int held) {
+        // adds the accumulators of chunks from .. to - 1, whose scales are held
+        auto add = [&](auto with_first, int from, int to) {
+            for (int q = from; q < to && ok; ++q) {
+                const int buf = q % kBuffers, held = q % kFewScales;
+                ok = mbar_wait_warp(&done[buf], (uint32_t)(q / kBuffers) & 1u);
+                if (!ok) break;
+                tc_fence_after_sync();
 #pragma unroll
-            for (int c = 0; c < T; c += 16) {
-                uint32_t raw[16];
-                tmem_ld16(lanes + (uint32_t)(buf * T + c), raw);
-                tmem_ld_wait_for(raw);
-                if constexpr (decltype(with_first)::value) {
+                for (int c = 0; c < T; c += 16) {
+                    uint32_t raw[16];
+                    tmem_ld16(lanes + (uint32_t)(buf * T + c), raw);
+                    tmem_ld_wait_for(raw);
+                    if constexpr (decltype(with_first)::value) {
 #pragma unroll
-                    for (int h = 0; h < 16; h += 8) {
-                        Octet<__nv_bfloat16> o;
-                        float f[8];
-                        o.load(&first[held][c + h]);
-                        o.get(f);
+                        for (int h = 0; h < 16; h += 8) {
+                            Octet<__nv_bfloat16> o;
+                            float f[8];
+                            o.load(&first[held][c + h]);
+                            o.get(f);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) raw[h + i] = __float_as_uint(__uint_as_float(raw[h + i]) * f[i]);
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < 16; i += 4) {
-                    const ulonglong2 s = *reinterpret_cast<const ulonglong2*>(&scale[held][c + i]);
-                    uint64_t* const a = acc + (c + i) / 2;
-                    a[0] = fma_pair(pair_of(__uint_as_float(raw[i]), __uint_as_float(raw[i + 1])), s.x, a[0]);
-                    a[1] = fma_pair(pair_of(__uint_as_float(raw[i + 2]), __uint_as_float(raw[i + 3])), s.y, a[1]);
-                }
-            }
-        };
-        for (int q = 0; q < n; ++q) {
-            const int buf = q % kBuffers, held = q % kFewScales;
-            if (held == 0) {                             // the scales of the next chunks: by all four warps, for all
-                if (q > 0) asm volatile("bar.sync 1, 128;" ::: "memory");
-                for (int i = t; i < min(kFewScales, n - q) * T; i += 128) {
-                    const int m = m0 + i % T;
-                    const long long at = q0 + q + i / T;
-                    float s = 0.f, before = 1.f;
-                    if (m < p.M) {
-                        const float a = p.sa[at * p.sa_pitch + m], w = sw[at * p.sw_q];
-                        s = a * w;
-                        if (!is_normal(s)) {
-                            const TwoFactors f = two_factors(a, w);
-                            s = f.then;
-                            before = f.first;
-                            any_first = 1;
+                            for (int i = 0; i < 8; ++i) raw[h + i] = __float_as_uint(__uint_as_float(raw[h + i]) * f[i]);
                         }
                     }
-                    scale[i / T][i % T] = s;
-                    first[i / T][i % T] = __float2bfloat16_rn(before);
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4) {
+                        const ulonglong2 s = *reinterpret_cast<const ulonglong2*>(&scale[held][c + i]);
+                        uint64_t* const a = acc + (c + i) / 2;
+                        a[0] = fma_pair(pair_of(__uint_as_float(raw[i]), __uint_as_float(raw[i + 1])), s.x, a[0]);
+                        a[1] = fma_pair(pair_of(__uint_as_float(raw[i + 2]), __uint_as_float(raw[i + 3])), s.y, a[1]);
+                    }
                 }
-                asm volatile("bar.sync 1, 128;" ::: "memory");
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&drained[buf]);
             }
-            // (after a wait that ran out a warp has part in the barriers above still, and in nothing else)
-            if (ok) ok = mbar_wait_warp(&done[buf], (uint32_t)(q / kBuffers) & 1u);
-            if (!ok) continue;
-            tc_fence_after_sync();
-            if (any_first) add(std::true_type(), buf, held);
-            else add(std::false_type(), buf, held);
-            tc_fence_before_sync();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&drained[buf]);
+        };
+        // (after a wait that ran out a warp has part in the barriers still, and in nothing else)
+        for (int q = 0; q < n; q += kFewScales) {
+            if (q > 0) asm volatile("bar.sync 1, 128;" ::: "memory");
+            const int end = min(n, q + kFewScales);      // the scales of the chunks up to there: by all four warps, for all
+            bool odd = false;
+            for (int i = t; i < (end - q) * T; i += 128) {
+                const int m = m0 + i % T;
+                const long long at = q0 + q + i / T;
+                const float s = m < p.M ? p.sa[at * p.sa_pitch + m] * sw[at * p.sw_q] : 0.f;
+                scale[i / T][i % T] = s;
+                first[i / T][i % T] = __float2bfloat16_rn(1.f);
+                odd |= m < p.M && !is_normal(s);
+            }
+            if (odd) {
+                any_first = 1;
+#pragma unroll 1
+                for (int i = t; i < (end - q) * T; i += 128) {
+                    const int m = m0 + i % T;
+                    const long long at = q0 + q + i / T;
+                    if (m < p.M) {
+                        const TwoFactors f = two_factors(p.sa[at * p.sa_pitch + m], sw[at * p.sw_q]);
+                        scale[i / T][i % T] = f.then;
+                        first[i / T][i % T] = __float2bfloat16_rn(f.first);
+                    }
+                }
+            }
+            asm volatile("bar.sync 1, 128;" ::: "memory");
+            if (any_first) add(std::true_type(), q, end);
+            else add(std::false_type(), q, end);
         }
         const int r = quarter * 32 + lane, j = j0 + r;
         if (p.split == 1) {
@@ -494,13 +500,13 @@ gf_status launch_few(ProductArgs& a, const void* w, const void* codes, int N, in
 // chunk of 128 terms costs each SM 32 KB from L2 for 512 clocks of products.
 //   warp 0: copies; warp 1 (of the first CTA): products; warps 4 to 19: scaling, a quarter of the rows by a quarter of
 //   the columns each, in registers, which the first four warps give up for them; the next tile's first two chunks are
-//   multiplied while they write their results, by the copy engine where rows are whole 16-byte pieces (65536 x 2048 x 512: 99 us;
-//   stored by the warps 143).
+//   multiplied while they write their results, by the copy engine where rows are whole 16-byte pieces (65536 x 2048 x 512: 97 to 113 us;
+//   stored by the warps 143; 14672 x 4241 x 64, whose rows are not, 59 in bf16 and 102 in fp32, 4240 columns 24 and 47).
 // What bounds it is the accumulators' way out of tensor memory, once for every 128 terms, which the scales ask for: reading one
 // takes the port that the products accumulate through for 260 clocks of a chunk's 512, and between a chunk's product and the next
 // product into its accumulator lie 1700 clocks of signals, reads and sums, with two accumulators: about 1100 clocks a chunk.  4096 x
-// 8192 x 4096 runs at 2.0 PFLOP/s (gradient of the input 1.95; 1.6 under the power cap, which runs of some milliseconds meet); with the
-// reads and sums left out the products take 2.97.  Measured and not taken: four accumulators of half the columns (A is read
+// 8192 x 4096 runs at 1.75 to 1.9 PFLOP/s either way (the power that its data take decides; 1.6 under the power cap, which runs of some
+// milliseconds meet); with the reads and sums left out the products take 2.97.  Measured and not taken: four accumulators of half the columns (A is read
 // twice: 159 us for 147), 8 scaling warps of 128 columns (157), scales through a ring in shared memory (147 for 140).
 constexpr int kWideThreads = 640, kWideStages = 5, kWideStage = 32768, kWidePiece = 32 * 128;
 constexpr int kWideWarps = 16;                     // that scale
