@@ -2,8 +2,9 @@
 //
 // Bound by memory: x (and the residual) read once, y written once.  An octet is the unit: its 128 random bits are one Philox
 // block of some 80 integer instructions, with the choices 120, which the memory's time covers (16 bits per element; 32 would take twice
-// the blocks).  Two octets a thread and a block for every 512: 100352 x 576 bf16 with a residual 50 us, the copy bandwidth (one
-// octet a thread in blocks that stay: 68).
+// the blocks).  Two octets a thread and a block for every 512: 100352 x 576 bf16 with a residual 50 us in a captured run of
+// calls, 53 from a cold cache, 57 as a program calls it (its bytes ask for 53; a quarter of those it writes are still in L2 when it ends).
+// One octet a thread in blocks that stay: 68.
 #include "gf_block.h"
 #include "gf_octet.cuh"
 

@@ -88,7 +88,8 @@ static inline RmsShape rms_shape(int n, int most, int least_log) {
     return s;
 }
 
-// Blocks of `kernel` that an SM holds; the query is made once per kernel and device.
+// Blocks of `kernel` that an SM holds; the query is made once per kernel, number of threads and device.  (The shared memory of some forms
+// grows with the columns, but never so far that it, and not the registers, decides.)
 template <typename Kern> static inline int rms_resident(Kern kernel, int threads, size_t smem, int (&cached)[kMaxDevices]) {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return 1;

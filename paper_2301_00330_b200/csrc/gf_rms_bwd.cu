@@ -4,7 +4,7 @@
 // its columns in registers over all rows of its team; each block leaves a line of sums, which a second kernel adds in a fixed order.
 // Measured: 65536 x 256 fp32 44 us (0.92 of the copy bandwidth), 16384 x 2048 bf16 with an fp32 residual 92 (0.89), 8192 x 4096 bf16 51
 // (0.79: 28 rows per block, of which the first and the lines of sums take 6 us), 100352 x 576 bf16 with dropout 114 (0.77; without the
-// next row brought to L2 136), 4099 x 1001 fp32 20 (0.63: 7 rows per block).
+// next row brought to L2 136), 4099 x 1001 fp32 19 to 20 (0.63: 7 rows per block), in tiles of columns 2000 x 16384 bf16 112 (0.36), fp32 150 (0.53).
 #include "gf_rms.cuh"
 
 namespace gf {

@@ -2,9 +2,10 @@
 //
 // Bound by memory: x and residual are read and h and y (or codes) written once; a row stays in the registers of its team between
 // the sum and the results, and the team's next row is on its way meanwhile.  Rows of three octets a thread are bound by instructions
-// as well: 106 a thread and octet, with dropout's random bits 228, with rounding to 8 bits 175.
-// Measured: 16384 x 2048 bf16 with an fp32 residual to 8 bits 59 us (0.95 of the copy bandwidth), 100352 x 576 bf16 77 us (0.91), with
-// dropout 92, to 8 bits 74 to 82, 65536 x 256 fp32 44 (0.93).
+// as well: 106 a thread and octet, with dropout's random bits 228, with rounding to 8 bits 184 (of 96 octets that the lanes have for
+// 576 columns' 72).
+// Measured: 16384 x 2048 bf16 with an fp32 residual to 8 bits 59 to 64 us (0.88 to 0.95 of the copy bandwidth), 100352 x 576 bf16 75 to 77 (0.91
+// to 0.94), with dropout 92 to 98, to 8 bits 76 to 82, 65536 x 256 fp32 43 (0.95); rows in parts, 2000 x 16384 bf16 88 (0.45), fp32 120 (0.67).
 #include "gf_rms.cuh"
 
 namespace gf {
