@@ -57,8 +57,8 @@ gf_status gf_dropout_backward(const gf_dropout_desc* desc, const void* g_y, cons
  * Without a residual and with p = 0, h is x itself: it is not written, and residual_dtype = dtype.
  * x, y, g_y, g_x have the descriptor's dtype; residual, h, g_h, g_residual its residual_dtype (bf16
  * x with an fp32 residual is possible, the opposite GF_ERR_UNSUPPORTED); rstd (rows values) and
- * g_gamma are fp32.  Arithmetic is fp32.  A non-finite value spoils its own row, and the sums of the
- * columns it reaches. */
+ * g_gamma are fp32.  Arithmetic is fp32: where a row's sum of squares passes its range rstd is 0, as for an
+ * infinite value.  A non-finite value spoils its own row, and the sums of the columns it reaches. */
 typedef struct gf_rms_desc {
     int64_t rows;           /* >= 0 */
     int32_t cols;           /* >= 1 */
@@ -117,7 +117,7 @@ gf_status gf_fp8_quantize_blocks(const gf_fp8_desc* desc, const void* w, void* c
  *   transposed 0 (the layer):                 out[M, N] = A[M, K] W^T + bias[N]
  *   transposed 1 (the gradient of its input): out[M, K] = A[M, N] W   + bias[K]
  * Each 128 terms of a sum are added by the tensor cores, the scaled sums of 128 in fp32; the result is
- * rounded once to out_dtype. */
+ * rounded once to out_dtype.  The product of a row's scale and a block's need not be a normal number of fp32. */
 typedef struct gf_fp8_matmul_desc {
     int32_t M;              /* >= 0 */
     int32_t N, K;           /* >= 1 */
